@@ -30,7 +30,13 @@
  *   festina_dispatch_requests -- one operating point per GPU (its current frequency),
  *       the 2% stability tie-break, the F_max fallback and scale-out (Sec. 3.3).
  *   festina_dispatch_waves    -- the same over arrival waves, each wave's placements
- *       committed to the GPUs' batch, memory and frequency before the next wave.
+ *       committed to the GPUs' batch, memory and frequency before the next wave;
+ * and, on the GPU that a request was placed on, the serving step whose memory and latency
+ * the calls above reckon with:
+ *   festina_extend_blocks     -- cache blocks and slots for the requests' new tokens;
+ *   festina_release_blocks    -- finished requests' blocks back into the pool;
+ *   festina_store_kv          -- new keys and values into the cache, in 8 bits;
+ *   festina_attend            -- attention of the new tokens over the cache.
  *
  * Conventions shared by every entry point
  *  - All array pointers inside the structs are DEVICE pointers (HIP global memory
@@ -506,6 +512,145 @@ typedef struct festina_moves {
 festina_status festina_request_moves(const festina_lut *lut, const festina_transfer *transfer,
                                      const festina_plan *plan, const festina_inflight *req,
                                      festina_moves *out, void *stream);
+
+/* ---- The serving step on one GPU: cache blocks, an 8-bit key/value cache, attention over it ----
+ *
+ * The memory that a placement reckons with (Req_mem = KV bytes per token x tokens, Sec. 3.3) is
+ * a pool of n_blocks cache blocks of block_tokens tokens each.  A request's tokens lie in the
+ * blocks of its row of the block table, token p at slot
+ * block_table[r][p / block_tokens] * block_tokens + p % block_tokens.  Blocks, slots and tables
+ * are shared by all layers; each layer has its own festina_kv_cache. */
+
+/* One step's requests on the GPU.  Sizes: block_tokens is 16, 32, 64, 128 or 256;
+ * n_blocks * block_tokens and max_blocks * block_tokens are below 2^31; n_requests is at most
+ * 2^20.  n_free is a count in device memory (taken as 0 or n_blocks where it lies outside). */
+typedef struct festina_kv_requests {
+  int32_t n_requests;                /* R >= 0 */
+  int32_t max_blocks;                /* MB >= 1 columns of the block table */
+  int32_t block_tokens;              /* BT */
+  int32_t n_blocks;                  /* NB >= 1 blocks of the pool */
+  const int32_t *held;               /* [R] tokens already in the cache */
+  const int32_t *add;                /* [R] new tokens of this step, 0 = none */
+  int32_t *block_table;              /* [R][MB] block ids, in and out */
+  int32_t *free_ids;                 /* [NB] the pool's free blocks, a stack: the last is taken first */
+  const int32_t *n_free;             /* [1] entries of free_ids */
+} festina_kv_requests;
+
+/* Results (device memory, written by the call; length may be held's own array and n_free_out
+ * n_free's own, which are then updated in place):
+ *   served[r] = 1 when the request gets its tokens.  Requests are served in index order, and
+ *     from the first whose blocks or tokens no longer fit (the pool; max_tokens), none is.  A
+ *     request with held < 0, add < 0 or held + add > MB * BT is not served and takes nothing;
+ *   first[r]  = first of the request's new tokens in the step's token list, first[R] = their
+ *     total; request r has tokens first[r] .. first[r+1]-1 (none unless served);
+ *   slot[t]   = cache slot of token t; -1 for t >= first[R] and where the id in the table or in
+ *     free_ids lies outside [0, NB);
+ *   length[r] = tokens held afterwards;  n_free_out = free blocks left.
+ * New columns of the served requests' rows are filled with the blocks taken.  length and served are
+ * also what a serving loop needs to carry on. */
+typedef struct festina_kv_step {
+  int32_t max_tokens;                /* entries of slot, >= 0: the step's token budget */
+  int32_t *first;                    /* [R + 1] */
+  int32_t *slot;                     /* [max_tokens] */
+  int32_t *length;                   /* [R] */
+  uint8_t *served;                   /* [R] */
+  int32_t *n_free_out;               /* [1] */
+} festina_kv_step;
+
+/* Bytes of device workspace of festina_extend_blocks and festina_release_blocks (0 for invalid
+ * sizes; never less for more requests or more tokens). */
+size_t festina_blocks_workspace_bytes(int32_t n_requests, int32_t max_tokens);
+
+/* Blocks and slots for the step's new tokens.  Workspace 256-byte aligned, clobbered; one kernel
+ * launch on `stream` for a small step, three otherwise. */
+festina_status festina_extend_blocks(const festina_kv_requests *req, festina_kv_step *out, void *workspace,
+                                     size_t workspace_bytes, void *stream);
+
+/* The blocks of every request with done[r] != 0 go onto free_ids, request by request and column by
+ * column (ceil(held / BT) each), and its length becomes 0; other lengths are held's.  n_free_out
+ * is the new count (at most NB; ids that would lie past free_ids are dropped).  A request with
+ * held < 0 or held > MB * BT gives nothing.  add is not read (NULL is allowed); of `out` only
+ * length and n_free_out are used.  Workspace as above. */
+festina_status festina_release_blocks(const festina_kv_requests *req, const uint8_t *done, festina_kv_step *out,
+                                      void *workspace, size_t workspace_bytes, void *stream);
+
+/* Element types of keys, values, queries and outputs. */
+#define FESTINA_BF16 0
+#define FESTINA_F16 1
+#define FESTINA_F32 2
+
+/* One layer's cache in 8 bits: codes of the e4m3 format (4 exponent bits, 3 fraction bits, largest value
+ * 448, no infinities, NaN = 0x7F and 0xFF) and one scale for each block and key head; an element is
+ * its code's value times the scale.  Values are held with their tokens running fastest, so
+ * that attention reads both operands of its matrix products as they lie.  head_dim is 64, 96,
+ * 128 or 256.  k and v are 16-byte aligned. */
+typedef struct festina_kv_cache {
+  int32_t n_blocks;                  /* NB >= 1 */
+  int32_t block_tokens;              /* BT, as in festina_kv_requests */
+  int32_t n_kv_heads;                /* H >= 1 */
+  int32_t head_dim;                  /* D */
+  uint8_t *k;                        /* [NB][H][BT][D] */
+  uint8_t *v;                        /* [NB][H][D][BT] */
+  float *k_scale;                    /* [NB][H] */
+  float *v_scale;                    /* [NB][H] */
+} festina_kv_cache;
+
+/* New keys and values of a step, [T][H][D] with the last axis contiguous and any strides (in
+ * elements, >= 0) of the others, e.g. slices of one projection's output. */
+typedef struct festina_kv_tokens {
+  int32_t n_tokens;                  /* T >= 0 */
+  int32_t dtype;                     /* FESTINA_BF16, FESTINA_F16 or FESTINA_F32 */
+  const void *k, *v;
+  int64_t k_token_stride, k_head_stride, v_token_stride, v_head_stride;
+  const int32_t *slot;               /* [T] e.g. festina_extend_blocks' slots; outside [0, NB * BT): not stored */
+} festina_kv_tokens;
+
+/* Store a step's keys and values.  A run is a stretch of consecutive tokens whose slots are consecutive
+ * and in one block (what festina_extend_blocks makes); no two runs of a call may be in one block
+ * (what they leave in that block is undefined otherwise, no other block is touched).  For each run and head:
+ *   scale: s = the least power of two with |x| <= 448 s for the run's finite elements, within
+ *     [2^-32, 2^32]; a run at the block's first slot begins the block anew with s, any other takes
+ *     max(block's scale, s), and where that is larger than before, the codes of the slots before the run
+ *     are rounded anew, code' = e4m3(code * old / new) (exact unless a code becomes subnormal);
+ *   code = x / scale rounded to the nearest e4m3 value, ties to even; finite values beyond the
+ *     format saturate at 448, others are held as NaN.
+ * Slots behind the run are left as they are.  No workspace; one kernel launch on `stream`. */
+festina_status festina_store_kv(const festina_kv_cache *cache, const festina_kv_tokens *tokens, void *stream);
+
+/* Attention of a step's new tokens over the cache.  Query token first[r] + i of request r, i in
+ * 0 .. n-1 with n = first[r+1] - first[r], stands at position p = length[r] - n + i and sees the
+ * keys j <= p, with window > 0 only those with j > p - window.  Query head h reads key head
+ * h / (n_heads / H).  With x_j = scale * <q, k_j> over those keys:
+ *   out = sum_j softmax(x)_j v_j,    lse = log sum_j exp(x_j).
+ * A row that sees no key (p < 0) has out = 0 and lse = -inf.  Keys whose table entry lies
+ * outside [0, NB) are not seen.  What is not seen (slots behind the last token, later tokens)
+ * may hold anything, NaN included.  Rows of tokens that no request has are not written.
+ * v_scale is taken within [2^-32, 2^32] (where festina_store_kv keeps it). */
+typedef struct festina_attention {
+  int32_t n_requests;                /* R >= 0 */
+  int32_t max_blocks;                /* MB >= 1 columns of the block table */
+  int32_t n_tokens;                  /* T >= 0 rows of q */
+  int32_t n_heads;                   /* query heads, a multiple of H */
+  int32_t max_new;                   /* an upper bound of n over the requests, >= 1 (chooses the kernels) */
+  int32_t dtype;                     /* FESTINA_BF16 or FESTINA_F16: q and out */
+  int32_t window;                    /* 0: none */
+  float scale;                       /* of the logits, e.g. 1 / sqrt(D) */
+  const int32_t *block_table;        /* [R][MB] */
+  const int32_t *length;             /* [R] tokens in the cache, the new ones included (at most MB * BT) */
+  const int32_t *first;              /* [R + 1] non-decreasing, as from festina_extend_blocks */
+  const void *q;                     /* [T][n_heads][D], last axis contiguous, 16-byte aligned rows */
+  int64_t q_token_stride, q_head_stride;       /* in elements, multiples of 8 */
+  void *out;                         /* [T][n_heads][D], as q */
+  int64_t out_token_stride, out_head_stride;
+  float *lse;                        /* [T][n_heads] or NULL */
+} festina_attention;
+
+/* Bytes of device workspace of festina_attend (reads only sizes; 0 for invalid ones). */
+size_t festina_attend_workspace_bytes(const festina_kv_cache *cache, const festina_attention *att);
+
+/* Workspace 256-byte aligned, clobbered.  One to five kernel launches on `stream`. */
+festina_status festina_attend(const festina_kv_cache *cache, const festina_attention *att, void *workspace,
+                              size_t workspace_bytes, void *stream);
 
 /* Static, NUL-terminated description of a status code. */
 const char *festina_status_string(festina_status status);

@@ -9,12 +9,15 @@ from __future__ import annotations
 import hashlib
 import os
 import subprocess
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SRCS = [os.path.join(HERE, "csrc", n) for n in ("festina.hip", "fronts.hip", "sweep.hip", "preferred.hip",
-                                                       "dispatch.hip", "transfer.hip")]
-HDRS = [os.path.join(HERE, "csrc", "fronts.h")]
+                                                       "dispatch.hip", "transfer.hip", "blocks.hip", "cache.hip",
+                                                       "attend.hip")]
+HDRS = [os.path.join(HERE, "csrc", n) for n in ("fronts.h", "kv.h")]
 LIB = os.path.join(HERE, "libfestina.so")
 HASH_FILE = LIB + ".sources"
 HEADER = os.path.join(ROOT, "include", "festina.h")
@@ -35,14 +38,23 @@ def source_hash() -> str:
     return h.hexdigest()
 
 
-def build_hip(verbose: bool = False) -> str:
-    cmd = ["hipcc", *HIPCC_FLAGS, "-o", LIB + ".tmp", *SRCS]
+def _run(cmd) -> str:
     proc = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)
     out = proc.stdout.decode()
-    noise = "packed-fp32-ops"
-    msgs = "\n".join(l for l in out.splitlines() if noise not in l and l.strip())
     if proc.returncode != 0:
         raise RuntimeError(f"hipcc failed ({proc.returncode}):\n{out}")
+    return out
+
+
+def build_hip(verbose: bool = False) -> str:
+    flags = [f for f in HIPCC_FLAGS if f != "-shared"]
+    with tempfile.TemporaryDirectory() as tmp, ThreadPoolExecutor(4) as pool:   # a compiler a source, four at a time
+        objs = [os.path.join(tmp, os.path.basename(s) + ".o") for s in SRCS]
+        parts = list(pool.map(lambda so: _run(["hipcc", *flags, "-c", so[0], "-o", so[1]]), zip(SRCS, objs)))
+        parts.append(_run(["hipcc", *HIPCC_FLAGS, "-o", LIB + ".tmp", *objs]))
+    out = "".join(parts)
+    noise = "packed-fp32-ops"
+    msgs = "\n".join(l for l in out.splitlines() if noise not in l and l.strip())
     if verbose and msgs:
         print(msgs)
     os.replace(LIB + ".tmp", LIB)

@@ -1,0 +1,1054 @@
+// attend.hip -- MI355X (gfx950) kernels and C-ABI host dispatch of attention over the 8-bit key/value cache.
+//
+// With codes kc, vc and scales ks, vs of a key's block, the logit in base 2 is
+//   x_j = (scale log2 e) ks <q, kc_j>,
+// and one pass over the keys keeps, for each query row, the running maximum m of y_j = x_j + log2 vs_j, the sum
+// l = sum 2^(y_j - m) / vs_j and the vector o = sum 2^(y_j - m) vc_j; then out = o / l and
+// lse = (m + log2 l) ln 2.  Folding vs into the exponent costs nothing (the scaling of the logit
+// is a fused multiply-add either way), leaves weights of at most 1 for the second product, and lets the codes
+// be its other operand as they are.
+//
+// Both products run on the matrix cores, keys (and values' dims) as rows and queries as columns: S' = K Q' and
+// O' = V' P'.  A column then stays in the same lanes through both, so P goes from the first product's
+// result straight into the second's operand: the keys of a tile are dealt to the first product's rows in the
+// order in which the second wants them, and no value crosses lanes but the maximum and the sum.  Codes are
+// converted exactly (e4m3 fits bfloat16 and half); q keeps its own type, the weights (at most 1) and the value
+// codes are taken in half precision, whose 11 bits leave less error than the outputs' rounding; sums are
+// float32.
+//
+// k_rows    up to 64 query rows a request and key head (single tokens, short runs): 16 NT rows against 64 keys
+//   per wave and step, operands loaded from the cache into the lanes that use them.  Bound by the cache's bytes.
+//   All requests' keys form one line of 64-key units, cut into equal pieces, one a workgroup, so that
+//   ragged lengths leave no workgroup behind; a request that a cut falls into is joined by k_rows_join.
+// k_tiles   prompts: 128 query rows a workgroup, tiles of 64 keys converted once into LDS (two buffers, the next
+//   tile's loads in flight meanwhile) and read by four waves of 32 rows.  Bound by the matrix cores and the exponentials.
+//   Few tiles over a long cache are split over the keys and joined by k_tiles_join.
+// k_plan    running sums of the requests' units and tiles, for many requests.
+#include <hip/hip_runtime.h>
+
+#include <climits>
+#include <cstddef>
+#include <cstdint>
+
+#include "festina.h"
+#include "kv.h"
+
+namespace {
+
+using namespace festina_kv;
+
+typedef __bf16 bf16;
+typedef _Float16 f16;
+typedef bf16 bf2 __attribute__((ext_vector_type(2)));
+typedef bf16 bf8 __attribute__((ext_vector_type(8)));
+typedef f16 h2 __attribute__((ext_vector_type(2)));
+typedef f16 h8 __attribute__((ext_vector_type(8)));
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef float f16v __attribute__((ext_vector_type(16)));
+typedef unsigned u4 __attribute__((ext_vector_type(4)));
+typedef unsigned u2 __attribute__((ext_vector_type(2)));
+
+constexpr int kUnit = 64;            // keys of a step
+constexpr int kWaves = 4;
+constexpr int kBlock = 64 * kWaves;
+constexpr int kWorkers = 512;        // pieces that k_rows cuts the keys into: two workgroups a compute unit
+constexpr int kListed = 512;         // requests whose running sums a workgroup forms by itself
+constexpr int kTileRows = 128;
+constexpr int kMaxRequests = 1 << 20;
+constexpr float kLn2 = 0.6931471805599453f;
+
+template <typename T> struct Vec8;
+template <> struct Vec8<bf16> { typedef bf8 type; };
+template <> struct Vec8<f16> { typedef h8 type; };
+
+struct AttArgs {
+  int32_t R, MB, T, Hq, H, G, shift, NB, window;
+  int32_t rows_max;                  // requests of at most so many rows are k_rows' (the others k_tiles')
+  int32_t tiles_each;                // k_rows without cuts: row tiles a request
+  int32_t workers, splits;
+  float scale;                       // times log2 e
+  const int32_t *table, *length, *first;
+  const void *q;
+  int64_t q_token, q_head;
+  void *out;
+  int64_t out_token, out_head;
+  float *lse;
+  const uint8_t *k, *v;
+  const float *ks, *vs;
+  const long long *plan;             // [2][R + 1] running sums of units and of tiles, or NULL
+  float *part_o, *part_ml;           // pieces: unnormalised rows; (m, l)
+};
+
+struct Request {
+  int first, n, length;
+};
+
+__device__ __forceinline__ Request request(const AttArgs &a, int r) {
+  Request q;
+  q.first = min(max(a.first[r], 0), a.T);
+  q.n = min(max(a.first[r + 1], q.first), a.T) - q.first;
+  q.length = min(max(a.length[r], 0), a.MB << a.shift);
+  return q;
+}
+
+__device__ __forceinline__ int cdiv(int x, int y) { return (x + y - 1) / y; }
+
+// First 64-key unit that any of the request's rows sees, and how many from there on (at least one, so that rows
+// without keys are written too).
+__device__ __forceinline__ int first_unit(const AttArgs &a, const Request &q) {
+  return a.window > 0 ? max(q.length - q.n - a.window + 1, 0) / kUnit : 0;
+}
+__device__ __forceinline__ int units(const AttArgs &a, const Request &q) {
+  return max(cdiv(q.length, kUnit) - first_unit(a, q), 1);
+}
+
+template <int ROWS>
+__device__ __forceinline__ long long units_of(const AttArgs &a, int r) {
+  const Request q = request(a, r);
+  const int rows = q.n * a.G;
+  return rows > 0 && rows <= a.rows_max ? (long long)units(a, q) * cdiv(rows, ROWS) * a.H : 0;
+}
+
+__device__ __forceinline__ long long tiles_of(const AttArgs &a, int r) {
+  const int rows = request(a, r).n * a.G;
+  return rows > a.rows_max ? cdiv(rows, kTileRows) : 0;
+}
+
+// Running sums over a workgroup of N threads: returns the exclusive sum and the whole.
+template <int N>
+__device__ __forceinline__ long long scan(long long x, long long *lds, long long *whole) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  long long s = x;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const long long y = __shfl_up(s, d);
+    if (lane >= d) s += y;
+  }
+  if (lane == 63) lds[wave] = s;
+  __syncthreads();
+  long long before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < N / 64; ++w) {
+    const long long y = lds[w];
+    before += w < wave ? y : 0;
+    all += y;
+  }
+  __syncthreads();
+  *whole = all;
+  return s - x + before;
+}
+
+// list[0 .. R]: running sums of f(r) over the requests, R <= kListed.
+template <typename F>
+__device__ __forceinline__ void list_sums(const AttArgs &a, F f, long long *list, long long *lds) {
+  const int r = threadIdx.x * 2;
+  const long long x = r < a.R ? f(r) : 0, y = r + 1 < a.R ? f(r + 1) : 0;
+  long long whole;
+  const long long before = scan<kBlock>(x + y, lds, &whole);
+  if (r <= a.R) list[r] = before;
+  if (r + 1 <= a.R) list[r + 1] = before + x;
+  if (threadIdx.x == 0) list[a.R] = whole;
+  __syncthreads();
+}
+
+// The r with list[r] <= u < list[r + 1].
+__device__ __forceinline__ int find(const long long *list, int R, long long u) {
+  int lo = 0, hi = R;
+  while (hi - lo > 1) {
+    const int m = (lo + hi) >> 1;
+    if (list[m] <= u) lo = m; else hi = m;
+  }
+  return lo;
+}
+
+template <int ROWS>
+__global__ void __launch_bounds__(1024) k_plan(AttArgs a, long long *plan) {
+  __shared__ long long lds[16];
+  long long u0 = 0, t0 = 0, whole;
+  for (int r0 = 0; r0 < a.R; r0 += 1024) {
+    const int r = r0 + threadIdx.x;
+    const long long u = scan<1024>(r < a.R ? units_of<ROWS>(a, r) : 0, lds, &whole) + u0;
+    u0 += whole;
+    const long long t = scan<1024>(r < a.R ? tiles_of(a, r) : 0, lds, &whole) + t0;
+    t0 += whole;
+    if (r < a.R) {
+      plan[r] = u;
+      plan[a.R + 1 + r] = t;
+    }
+  }
+  if (threadIdx.x == 0) {
+    plan[a.R] = u0;
+    plan[2 * a.R + 1] = t0;
+  }
+}
+
+// ------------------------------------------------------------------ operands
+
+__device__ __forceinline__ void decode4(unsigned c, bf16 *x) {
+  *reinterpret_cast<bf2 *>(x) = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)c, 1.f, false);
+  *reinterpret_cast<bf2 *>(x + 2) = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)c, 1.f, true);
+}
+__device__ __forceinline__ void decode4(unsigned c, f16 *x) {
+  *reinterpret_cast<h2 *>(x) = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)c, 1.f, false);
+  *reinterpret_cast<h2 *>(x + 2) = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)c, 1.f, true);
+}
+template <typename T>
+__device__ __forceinline__ typename Vec8<T>::type decode8(unsigned c0, unsigned c1) {
+  union { T x[8]; typename Vec8<T>::type v; } u;
+  decode4(c0, u.x);
+  decode4(c1, u.x + 4);
+  return u.v;
+}
+
+__device__ __forceinline__ f4 mfma16(bf8 a, bf8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f4 mfma16(h8 a, h8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f16v mfma32(bf8 a, bf8 b, f16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f16v mfma32(h8 a, h8 b, f16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float log2_(float x) { return __builtin_amdgcn_logf(x); }
+__device__ __forceinline__ float kNegInf() { return -__builtin_inff(); }
+
+// Which bytes of a word of four codes are NaN, as 0xff each.
+__device__ __forceinline__ unsigned nan_bytes(unsigned c) {
+  const unsigned h = ((c & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+  return (h >> 7) * 0xffu;
+}
+constexpr unsigned kOnes = 0x38383838u;     // four codes of 1.0
+
+// Bytes of the word of codes 4w .. 4w + 3 that lie below n.
+__device__ __forceinline__ unsigned below(int n, int w) {
+  const int k = n - 4 * w;
+  return k >= 4 ? ~0u : k <= 0 ? 0u : (1u << (8 * k)) - 1;
+}
+
+// Weight of a piece with maximum m in a row whose maximum is M.
+__device__ __forceinline__ float weight(float m, float M) { return m == kNegInf() ? 0.f : exp2_(m - M); }
+
+template <typename T>
+__device__ __forceinline__ void put4(T *p, const float *x) {
+  union { T t[4]; u2 w; } u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) u.t[i] = (T)x[i];
+  *reinterpret_cast<u2 *>(p) = u.w;
+}
+
+// ------------------------------------------------------------------ k_rows
+
+// What one wave keeps of the cache for a step: the raw codes of 64 keys and values.
+template <int D>
+struct RowsStep {
+  u4 k[4][D / 64];
+  u2 kr[4][D % 64 ? 1 : 1];
+  u4 v[D / 16];
+  float ks, vs;
+  bool ok;
+};
+
+template <typename T, int D, int NT>
+struct Rows {
+  static constexpr int kRows = 16 * NT, kSteps = D / 32, kPitch = D + 4;
+  // One step in flight beside the one at work where registers allow
+  static constexpr bool kAhead = D <= 128 && NT == 1;
+
+  struct Shared {
+    float o[kWaves][16][kPitch];
+    float m[kWaves][kRows], l[kWaves][kRows];
+  };
+
+  static __device__ __forceinline__ void load(const AttArgs &a, const int32_t *table, int h, int base, RowsStep<D> &s) {
+    const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4, bt = 1 << a.shift;
+    // row m of the first product's tile u is key 16 (m / 4) + 4 u + m % 4 of the step; a lane holds the values of
+    // keys 16 g .. 16 g + 15
+    const int key_k = base + (m >> 2) * 16, key_v = base + g * 16;
+    int id_k = table[min(key_k >> a.shift, a.MB - 1)], id_v = table[min(key_v >> a.shift, a.MB - 1)];
+    s.ok = (unsigned)id_v < (unsigned)a.NB;
+    id_k = (unsigned)id_k < (unsigned)a.NB ? id_k : 0;
+    id_v = s.ok ? id_v : 0;
+    const size_t bh_k = (size_t)id_k * a.H + h, bh_v = (size_t)id_v * a.H + h;
+    const uint8_t *k = a.k + (bh_k * bt + (key_k & (bt - 1)) + (m & 3)) * D;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+#pragma unroll
+      for (int j = 0; j < D / 64; ++j) s.k[u][j] = *reinterpret_cast<const u4 *>(k + u * 4 * D + j * 64 + g * 16);
+      if constexpr (D % 64 != 0) s.kr[u][0] = *reinterpret_cast<const u2 *>(k + u * 4 * D + D / 64 * 64 + g * 8);
+    }
+    s.ks = a.ks[bh_v];
+    s.vs = a.vs[bh_v];
+    const uint8_t *v = a.v + (bh_v * D + m) * bt + (key_v & (bt - 1));
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) s.v[t] = *reinterpret_cast<const u4 *>(v + (size_t)t * 16 * bt);
+  }
+
+  struct State {
+    typename Vec8<T>::type q[NT][kSteps];
+    f4 o[NT][D / 16];
+    float m[NT], l[NT];
+    int pos[NT];
+  };
+
+  static __device__ __forceinline__ void step(const AttArgs &a, const Request &rq, int base, int pos_min, int pos_max,
+                                              RowsStep<D> &s, State &st) {
+    const int g = (threadIdx.x & 63) >> 4;
+    f4 x[NT][4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) x[nt][u] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) {
+        typename Vec8<T>::type kf;
+        if (i < D / 64 * 2) kf = decode8<T>(s.k[u][i / 2][(i & 1) * 2], s.k[u][i / 2][(i & 1) * 2 + 1]);
+        else kf = decode8<T>(s.kr[u][0][0], s.kr[u][0][1]);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) x[nt][u] = mfma16(kf, st.q[nt][i], x[nt][u]);
+      }
+    }
+    const float c = a.scale * s.ks, vs = fminf(fmaxf(s.vs, kScaleMin), kScaleMax);
+    const float lv = log2_(vs), iv = 1.f / vs;
+    const bool masked = base + kUnit - 1 > pos_min || (a.window > 0 && base <= pos_max - a.window) || __any(!s.ok);
+    h8 w[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[nt][u][i] = fmaf(x[nt][u][i], c, lv);
+      if (masked) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int key = base + 16 * g + 4 * u + i;
+            const bool sees = s.ok && key <= st.pos[nt] && (a.window <= 0 || key > st.pos[nt] - a.window);
+            x[nt][u][i] = sees ? x[nt][u][i] : kNegInf();
+          }
+      }
+      float top = x[nt][0][0];
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, x[nt][u][i]);
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float was = st.m[nt];
+      if (__any(top > was)) {
+        const float now = fmaxf(was, top), f = weight(was, now);
+        st.m[nt] = now;
+        st.l[nt] *= f;
+#pragma unroll
+        for (int t = 0; t < D / 16; ++t) st.o[nt][t] *= f;
+      }
+      const float m = st.m[nt] == kNegInf() ? 0.f : st.m[nt];
+      float sum = 0.f;
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float p = exp2_(x[nt][u][i] - m);
+          sum += p;
+          w[nt][u >> 1][(u & 1) * 4 + i] = (f16)p;
+        }
+      st.l[nt] = fmaf(sum, iv, st.l[nt]);
+    }
+    bool nans = false;
+    if (masked) {
+      // what lies behind the last token may be anything: no product with it
+      const int n = s.ok ? min(max(rq.length - (base + 16 * g), 0), 16) : 0;
+#pragma unroll
+      for (int t = 0; t < D / 16; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s.v[t][i] &= below(n, i);
+      unsigned any = 0;
+#pragma unroll
+      for (int t = 0; t < D / 16; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) any |= nan_bytes(s.v[t][i]);
+      nans = __any(any != 0);
+    }
+    if (nans) {
+      // a NaN that some rows see and others do not: it is left out of the product and put into the rows that see it
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        h8 sees[2];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int key = base + 16 * g + i;
+          const bool y = s.ok && key <= st.pos[nt] && (a.window <= 0 || key > st.pos[nt] - a.window);
+          sees[i >> 3][i & 7] = y ? (f16)1.f : (f16)0.f;
+        }
+#pragma unroll
+        for (int t = 0; t < D / 16; ++t) {
+          f4 hits = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const unsigned n0 = nan_bytes(s.v[t][2 * i]), n1 = nan_bytes(s.v[t][2 * i + 1]);
+            hits = mfma16(decode8<f16>(n0 & kOnes, n1 & kOnes), sees[i], hits);
+            st.o[nt][t] = mfma16(decode8<f16>(s.v[t][2 * i] & ~n0, s.v[t][2 * i + 1] & ~n1), w[nt][i], st.o[nt][t]);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (hits[i] > 0.f) st.o[nt][t][i] = __builtin_nanf("");
+        }
+      }
+      return;
+    }
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const h8 vf = decode8<f16>(s.v[t][2 * i], s.v[t][2 * i + 1]);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) st.o[nt][t] = mfma16(vf, w[nt][i], st.o[nt][t]);
+      }
+  }
+
+  // Rows `tile` of request r and key head h over its units k0 .. k1 - 1; `part` < 0: all of them, else the place
+  // where the piece's result goes.
+  static __device__ __forceinline__ void piece(const AttArgs &a, int r, const Request &rq, int h, int tile, int k0, int k1,
+                                               int part, Shared &sh) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
+    const int rows = rq.n * a.G, row0 = tile * kRows, before = rq.length - rq.n;
+    const int pos_min = before + row0 / a.G, pos_max = before + (min(row0 + kRows, rows) - 1) / a.G;
+    State st;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int i = row0 + nt * 16 + c, t = i / a.G;
+      const bool in = i < rows;
+      st.pos[nt] = in ? before + t : -1;
+      st.m[nt] = kNegInf();
+      st.l[nt] = 0.f;
+#pragma unroll
+      for (int d = 0; d < D / 16; ++d) st.o[nt][d] = f4{0.f, 0.f, 0.f, 0.f};
+      const T *q = static_cast<const T *>(a.q) + (int64_t)(rq.first + (in ? t : 0)) * a.q_token +
+                   (int64_t)(h * a.G + (in ? i - t * a.G : 0)) * a.q_head;
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        const int d = s < D / 64 * 2 ? (s >> 1) * 64 + g * 16 + (s & 1) * 8 : D / 64 * 64 + g * 8;
+        u4 raw = *reinterpret_cast<const u4 *>(q + d);
+        if (!in) raw = u4{0u, 0u, 0u, 0u};
+        st.q[nt][s] = __builtin_bit_cast(typename Vec8<T>::type, raw);
+      }
+    }
+    const int32_t *table = a.table + (size_t)r * a.MB;
+    const int u0 = first_unit(a, rq);
+    int u = k0 + wave;
+    if constexpr (kAhead) {
+      RowsStep<D> s, next;
+      if (u < k1) load(a, table, h, (u0 + u) * kUnit, s);
+      while (u < k1) {
+        const int n = u + kWaves;
+        if (n < k1) load(a, table, h, (u0 + n) * kUnit, next);
+        step(a, rq, (u0 + u) * kUnit, pos_min, pos_max, s, st);
+        s = next;
+        u = n;
+      }
+    } else {
+      for (; u < k1; u += kWaves) {
+        RowsStep<D> s;
+        load(a, table, h, (u0 + u) * kUnit, s);
+        step(a, rq, (u0 + u) * kUnit, pos_min, pos_max, s, st);
+      }
+    }
+    // the four waves' parts of each row
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      st.l[nt] += __shfl_xor(st.l[nt], 16);
+      st.l[nt] += __shfl_xor(st.l[nt], 32);
+      if (g == 0) {
+        sh.m[wave][nt * 16 + c] = st.m[nt];
+        sh.l[wave][nt * 16 + c] = st.l[nt];
+      }
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int t = 0; t < D / 16; ++t) *reinterpret_cast<f4 *>(&sh.o[wave][c][t * 16 + g * 4]) = st.o[nt][t];
+      __syncthreads();
+      for (int e = threadIdx.x; e < 16 * (D / 4); e += kBlock) {
+        const int y = e / (D / 4), d = (e % (D / 4)) * 4, i = row0 + nt * 16 + y;
+        if (i >= rows) break;
+        float M = kNegInf(), L = 0.f;
+        f4 O = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) M = fmaxf(M, sh.m[w][nt * 16 + y]);
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+          const float f = weight(sh.m[w][nt * 16 + y], M);
+          L = fmaf(sh.l[w][nt * 16 + y], f, L);
+          O += *reinterpret_cast<const f4 *>(&sh.o[w][y][d]) * f;
+        }
+        if (part < 0) {
+          const int t = i / a.G, head = h * a.G + i - t * a.G;
+          finish(a, rq.first + t, head, d, M, L, O);
+        } else {
+          const size_t p = (size_t)part * kRows + nt * 16 + y;
+          *reinterpret_cast<f4 *>(a.part_o + p * D + d) = O;
+          if (d == 0) {
+            a.part_ml[p * 2] = M;
+            a.part_ml[p * 2 + 1] = L;
+          }
+        }
+      }
+      __syncthreads();
+    }
+  }
+
+  static __device__ __forceinline__ void finish(const AttArgs &a, int t, int head, int d, float M, float L, f4 O) {
+    const bool none = M == kNegInf();
+    const float f = none ? 0.f : 1.f / L;
+    float x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = none ? 0.f : O[i] * f;
+    put4(static_cast<T *>(a.out) + (int64_t)t * a.out_token + (int64_t)head * a.out_head + d, x);
+    if (d == 0 && a.lse) a.lse[(size_t)t * a.Hq + head] = none ? kNegInf() : (M + log2_(L)) * kLn2;
+  }
+};
+
+// Pieces of equal length, at least a step for each wave.
+__device__ __forceinline__ int pieces(const AttArgs &a, long long all) {
+  return (int)min((long long)a.workers, max((all + kWaves - 1) / kWaves, 1ll));
+}
+__device__ __forceinline__ long long piece_start(long long all, int w, int n) { return all * w / n; }
+
+template <typename T, int D, int NT, bool CUT>
+__global__ void __launch_bounds__(kBlock, (D <= 128 && NT <= 2) ? 2 : 1) k_rows(AttArgs a) {
+  typedef Rows<T, D, NT> K;
+  __shared__ typename K::Shared sh;
+  if constexpr (!CUT) {
+    // a workgroup for each row tile and key head
+    const int tile = blockIdx.x % a.tiles_each, rest = blockIdx.x / a.tiles_each, h = rest % a.H, r = rest / a.H;
+    const Request rq = request(a, r);
+    const int rows = rq.n * a.G;
+    if (rows > a.rows_max || tile * K::kRows >= rows) return;
+    K::piece(a, r, rq, h, tile, 0, units(a, rq), -1, sh);
+    return;
+  }
+  __shared__ long long list_[kListed + 2], lds[kWaves];
+  const long long *list = a.plan;
+  if (!list) {
+    list_sums(a, [&](int r) { return units_of<K::kRows>(a, r); }, list_, lds);
+    list = list_;
+  }
+  const long long all = list[a.R];
+  const int n = pieces(a, all), w = blockIdx.x;
+  if (w >= n) return;
+  long long u = piece_start(all, w, n);
+  const long long end = piece_start(all, w + 1, n);
+  for (int place = 2 * w; u < end; ++place) {
+    const int r = find(list, a.R, u);
+    const Request rq = request(a, r);
+    const int each = units(a, rq), at = (int)((u - list[r]) / each), tiles = cdiv(rq.n * a.G, K::kRows);
+    const int k0 = (int)(u - list[r] - (long long)at * each), k1 = (int)min((long long)each, k0 + (end - u));
+    const bool whole = k0 == 0 && k1 == each;
+    K::piece(a, r, rq, at / tiles, at % tiles, k0, k1, whole ? -1 : min(place, 2 * w + 1), sh);
+    u += k1 - k0;
+  }
+}
+
+// Joins one row's pieces `first_part`, then `next_part`, next_part + stride, ... : a wave, lanes over the row.
+template <typename T, int D>
+__device__ __forceinline__ void join_row(const AttArgs &a, size_t p0, size_t p1, size_t stride, int n, int t, int head) {
+  const int lane = threadIdx.x & 63;
+  const auto at = [&](int i) { return i == 0 ? p0 : p1 + (size_t)(i - 1) * stride; };
+  float M = kNegInf(), L = 0.f;
+  for (int i = lane; i < n; i += 64) M = fmaxf(M, a.part_ml[at(i) * 2]);
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor(M, d));
+  for (int i = lane; i < n; i += 64) L = fmaf(a.part_ml[at(i) * 2 + 1], weight(a.part_ml[at(i) * 2], M), L);
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) L += __shfl_xor(L, d);
+  if (lane * 4 < D) {
+    f4 O = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int i = 0; i < n; ++i)
+      O += *reinterpret_cast<const f4 *>(a.part_o + at(i) * D + lane * 4) * weight(a.part_ml[at(i) * 2], M);
+    Rows<T, D, 1>::finish(a, t, head, lane * 4, M, L, O);
+  }
+}
+
+// Workgroup (w - 1, y) joins rows 4 y .. 4 y + 3 of the row tile that the cut between pieces w - 1 and w falls into,
+// if it is the tile's first cut.
+template <typename T, int D, int NT>
+__global__ void __launch_bounds__(kBlock) k_rows_join(AttArgs a) {
+  constexpr int kRows = 16 * NT;
+  __shared__ long long list_[kListed + 2], lds[kWaves];
+  const long long *list = a.plan;
+  if (!list) {
+    list_sums(a, [&](int r) { return units_of<kRows>(a, r); }, list_, lds);
+    list = list_;
+  }
+  const long long all = list[a.R];
+  const int n = pieces(a, all), w = blockIdx.x + 1;
+  if (w >= n) return;
+  const long long u = piece_start(all, w, n);
+  const int r = find(list, a.R, u);
+  const Request rq = request(a, r);
+  const int each = units(a, rq), at = (int)((u - list[r]) / each), tiles = cdiv(rq.n * a.G, kRows);
+  const long long begin = list[r] + (long long)at * each, end = begin + each;
+  const long long prior = piece_start(all, w - 1, n);
+  if (begin == u || prior > begin) return;
+  const int row = blockIdx.y * kWaves + (threadIdx.x >> 6), i = (at % tiles) * kRows + row;
+  if (i >= rq.n * a.G) return;
+  const int last = (int)((end * n - 1) / all);                        // piece of the tile's last unit
+  const int t = i / a.G, head = (at / tiles) * a.G + i - t * a.G;
+  // a piece that begins in the tile or at its start holds it as its first part, one that began before as its second
+  const size_t p0 = (size_t)(2 * (w - 1) + (prior < begin ? 1 : 0)) * kRows + row, p1 = (size_t)(2 * w) * kRows + row;
+  join_row<T, D>(a, p0, p1, 2 * kRows, last - w + 2, rq.first + t, head);
+}
+
+// ------------------------------------------------------------------ k_tiles
+
+template <typename T, int D>
+struct Tiles {
+  static constexpr int kPitchK = D + 8, kPitchV = kUnit + 8;
+  static constexpr int kLoads = (kUnit * D / 16 + kBlock - 1) / kBlock, kItems = kUnit * D / 16;
+
+  struct Buffer {
+    T k[kUnit][kPitchK];
+    f16 v[D][kPitchV];
+    float c[4], lv[4], iv[4];
+    int nans[kWaves];
+  };
+
+  struct Raw {
+    u4 k[kLoads], v[kLoads];
+    float ks, vs;
+    bool ok;
+  };
+
+  static __device__ __forceinline__ int block_of(const AttArgs &a, const int32_t *table, int key) {
+    return table[min(key >> a.shift, a.MB - 1)];
+  }
+
+  static __device__ __forceinline__ void load(const AttArgs &a, const int32_t *table, int h, int length, int base, Raw &raw) {
+    const int bt = 1 << a.shift;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int e = threadIdx.x + i * kBlock;
+      raw.k[i] = raw.v[i] = u4{0u, 0u, 0u, 0u};
+      if (kItems % kBlock != 0 && e >= kItems) continue;
+      const int key = base + e / (D / 16);
+      int id = block_of(a, table, key);
+      if ((unsigned)id < (unsigned)a.NB)
+        raw.k[i] = *reinterpret_cast<const u4 *>(a.k + (((size_t)id * a.H + h) * bt + (key & (bt - 1))) * D + e % (D / 16) * 16);
+      const int from = base + (e & 3) * 16;
+      id = block_of(a, table, from);
+      if ((unsigned)id < (unsigned)a.NB) {
+        u4 v = *reinterpret_cast<const u4 *>(a.v + (((size_t)id * a.H + h) * D + (e >> 2)) * bt + (from & (bt - 1)));
+        const int n = length - from;                   // what lies behind the last token may be anything
+        if (n < 16) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[j] &= below(n, j);
+        }
+        raw.v[i] = v;
+      }
+    }
+    raw.ok = false;
+    raw.ks = raw.vs = 1.f;
+    if (threadIdx.x < 4) {
+      const int id = block_of(a, table, base + threadIdx.x * 16);
+      raw.ok = (unsigned)id < (unsigned)a.NB;
+      if (raw.ok) {
+        raw.ks = a.ks[(size_t)id * a.H + h];
+        raw.vs = a.vs[(size_t)id * a.H + h];
+      }
+    }
+  }
+
+  // `look`: some row of the workgroup does not see all of the tile.
+  static __device__ __forceinline__ void store(const AttArgs &a, const Raw &raw, bool look, Buffer &b) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int e = threadIdx.x + i * kBlock;
+      if (kItems % kBlock != 0 && e >= kItems) continue;
+      const int key = e / (D / 16), d = e % (D / 16) * 16, vd = e >> 2, from = (e & 3) * 16;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        *reinterpret_cast<typename Vec8<T>::type *>(&b.k[key][d + j * 8]) = decode8<T>(raw.k[i][2 * j], raw.k[i][2 * j + 1]);
+        *reinterpret_cast<h8 *>(&b.v[vd][from + j * 8]) = decode8<f16>(raw.v[i][2 * j], raw.v[i][2 * j + 1]);
+      }
+    }
+    if (threadIdx.x < 4) {
+      // a block that is not there: its codes are zeros and its logits -inf
+      const float vs = fminf(fmaxf(raw.vs, kScaleMin), kScaleMax);
+      b.c[threadIdx.x] = raw.ok ? a.scale * raw.ks : 0.f;
+      b.lv[threadIdx.x] = raw.ok ? log2_(vs) : kNegInf();
+      b.iv[threadIdx.x] = raw.ok ? 1.f / vs : 0.f;
+    }
+    unsigned any = 0;
+    if (look) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) any |= nan_bytes(raw.v[i][j]);
+    }
+    const bool nans = __any(any != 0);
+    if ((threadIdx.x & 63) == 0) b.nans[threadIdx.x >> 6] = nans;
+  }
+
+  struct State {
+    typename Vec8<T>::type q[D / 16];
+    f16v o[D / 32];
+    float m, l;
+    int pos;
+  };
+
+  static __device__ __forceinline__ void step(const AttArgs &a, int base, int pos_min, int pos_max, const Buffer &b,
+                                              State &st) {
+    const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5;
+    // row c of a first product is key 16 (c / 4 % 2) + 4 (c / 8) + c % 4 of its 32
+    const int key_row = ((c >> 2) & 1) * 16 + (c >> 3) * 4 + (c & 3);
+    f16v x[2];
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      f16v s;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i)
+        s = mfma32(*reinterpret_cast<const typename Vec8<T>::type *>(&b.k[g * 32 + key_row][i * 16 + h * 8]), st.q[i], s);
+      const float cc = b.c[g * 2 + h], lv = b.lv[g * 2 + h];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[g][i] = fmaf(s[i], cc, lv);
+    }
+    const bool masked = base + kUnit - 1 > pos_min || (a.window > 0 && base <= pos_max - a.window);
+    if (masked) {
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int key = base + g * 32 + h * 16 + i;
+          const bool sees = key <= st.pos && (a.window <= 0 || key > st.pos - a.window);
+          x[g][i] = sees ? x[g][i] : kNegInf();
+        }
+    }
+    float top = x[0][0];
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, x[g][i]);
+    top = fmaxf(top, __shfl_xor(top, 32));
+    if (__any(top > st.m)) {
+      const float now = fmaxf(st.m, top), f = weight(st.m, now);
+      st.m = now;
+      st.l *= f;
+#pragma unroll
+      for (int t = 0; t < D / 32; ++t) st.o[t] *= f;
+    }
+    const float m = st.m == kNegInf() ? 0.f : st.m;
+    h8 w[2][2];
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float p = exp2_(x[g][i] - m);
+        sum += p;
+        w[g][i >> 3][i & 7] = (f16)p;
+      }
+      st.l = fmaf(sum, b.iv[g * 2 + h], st.l);
+    }
+    const bool nans = masked && (b.nans[0] | b.nans[1] | b.nans[2] | b.nans[3]);
+    if (!nans) {
+#pragma unroll
+      for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+          for (int s = 0; s < 2; ++s)
+            st.o[t] = mfma32(*reinterpret_cast<const h8 *>(&b.v[t * 32 + c][g * 32 + h * 16 + s * 8]), w[g][s], st.o[t]);
+      return;
+    }
+    // a NaN that some rows see and others do not: it is left out of the product and put into the rows that see it
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t) {
+      f16v hits;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) hits[i] = 0.f;
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          h8 vf = *reinterpret_cast<const h8 *>(&b.v[t * 32 + c][g * 32 + h * 16 + s * 8]), isnan, sees;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const bool n = vf[i] != vf[i];
+            const int key = base + g * 32 + h * 16 + s * 8 + i;
+            const bool y = key <= st.pos && (a.window <= 0 || key > st.pos - a.window);
+            isnan[i] = n ? (f16)1.f : (f16)0.f;
+            sees[i] = y ? (f16)1.f : (f16)0.f;
+            vf[i] = n ? (f16)0.f : vf[i];
+          }
+          hits = mfma32(isnan, sees, hits);
+          st.o[t] = mfma32(vf, w[g][s], st.o[t]);
+        }
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (hits[i] > 0.f) st.o[t][i] = __builtin_nanf("");
+    }
+  }
+};
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kBlock, D <= 128 ? 2 : 1) k_tiles(AttArgs a) {
+  typedef Tiles<T, D> K;
+  __shared__ typename K::Buffer buf[2];
+  __shared__ long long list_[kListed + 2], lds[kWaves];
+  const long long *list = a.plan ? a.plan + a.R + 1 : nullptr;
+  if (!list) {
+    list_sums(a, [&](int r) { return tiles_of(a, r); }, list_, lds);
+    list = list_;
+  }
+  // neighbouring workgroups take different key heads, so that (for 8 heads) the workgroups of one XCD share one
+  // head's keys in its L2; a request's last rows, which see most keys, come first
+  const int h = blockIdx.x % a.H;
+  const long long at = min(list[a.R], (long long)(gridDim.x / a.H)) - 1 - blockIdx.x / a.H;
+  if (at < 0) return;
+  const int r = find(list, a.R, at);
+  const Request rq = request(a, r);
+  const int rows = rq.n * a.G, row0 = (int)(at - list[r]) * kTileRows, before = rq.length - rq.n;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 31, half = lane >> 5;
+  const int wave0 = row0 + wave * 32, i = wave0 + c, t = i / a.G;
+  const bool in = i < rows;
+  const int pos_lo = before + row0 / a.G, pos_hi = before + (min(row0 + kTileRows, rows) - 1) / a.G;
+  const int pos_min = before + wave0 / a.G, pos_max = before + (min(wave0 + 32, rows) - 1) / a.G;
+  int u = a.window > 0 ? max(pos_lo - a.window + 1, 0) / kUnit : 0;
+  int end = pos_hi < 0 ? u : max(cdiv(pos_hi + 1, kUnit), u);
+  if (a.splits > 1) {
+    const int n = end - u, s = blockIdx.y;
+    end = u + (int)((long long)n * (s + 1) / a.splits);
+    u += (int)((long long)n * s / a.splits);
+  }
+  typename K::State st;
+  st.pos = in ? before + t : -1;
+  st.m = kNegInf();
+  st.l = 0.f;
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+    for (int y = 0; y < 16; ++y) st.o[d][y] = 0.f;
+  const T *q = static_cast<const T *>(a.q) + (int64_t)(rq.first + (in ? t : 0)) * a.q_token +
+               (int64_t)(h * a.G + (in ? i - t * a.G : 0)) * a.q_head;
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) {
+    u4 raw = *reinterpret_cast<const u4 *>(q + s * 16 + half * 8);
+    if (!in) raw = u4{0u, 0u, 0u, 0u};
+    st.q[s] = __builtin_bit_cast(typename Vec8<T>::type, raw);
+  }
+  const int32_t *table = a.table + (size_t)r * a.MB;
+  const auto look = [&](int unit) {
+    return unit * kUnit + kUnit - 1 > pos_lo || (a.window > 0 && unit * kUnit <= pos_hi - a.window);
+  };
+  typename K::Raw raw;
+  if (u < end) {
+    K::load(a, table, h, rq.length, u * kUnit, raw);
+    K::store(a, raw, look(u), buf[u & 1]);
+  }
+  __syncthreads();
+  for (; u < end; ++u) {
+    if (u + 1 < end) K::load(a, table, h, rq.length, (u + 1) * kUnit, raw);
+    const int base = u * kUnit;
+    if (wave0 < rows && base <= pos_max && (a.window <= 0 || base + kUnit - 1 > pos_min - a.window))
+      K::step(a, base, pos_min, pos_max, buf[u & 1], st);
+    if (u + 1 < end) K::store(a, raw, look(u + 1), buf[(u + 1) & 1]);
+    __syncthreads();
+  }
+  if (!in) return;
+  st.l += __shfl_xor(st.l, 32);
+  if (a.splits > 1) {
+    const size_t p = (((size_t)at * a.H + h) * a.splits + blockIdx.y) * kTileRows + wave * 32 + c;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int y = 0; y < 4; ++y)
+        *reinterpret_cast<f4 *>(a.part_o + p * D + d * 32 + y * 8 + half * 4) =
+            f4{st.o[d][y * 4], st.o[d][y * 4 + 1], st.o[d][y * 4 + 2], st.o[d][y * 4 + 3]};
+    if (half == 0) {
+      a.part_ml[p * 2] = st.m;
+      a.part_ml[p * 2 + 1] = st.l;
+    }
+    return;
+  }
+  const int head = h * a.G + i - t * a.G;
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+    for (int y = 0; y < 4; ++y)
+      Rows<T, D, 1>::finish(a, rq.first + t, head, d * 32 + y * 8 + half * 4, st.m, st.l,
+                            f4{st.o[d][y * 4], st.o[d][y * 4 + 1], st.o[d][y * 4 + 2], st.o[d][y * 4 + 3]});
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kBlock) k_tiles_join(AttArgs a) {
+  __shared__ long long list_[kListed + 2], lds[kWaves];
+  const long long *list = a.plan ? a.plan + a.R + 1 : nullptr;
+  if (!list) {
+    list_sums(a, [&](int r) { return tiles_of(a, r); }, list_, lds);
+    list = list_;
+  }
+  const int h = blockIdx.x % a.H;
+  const long long at = min(list[a.R], (long long)(gridDim.x / a.H)) - 1 - blockIdx.x / a.H;
+  if (at < 0) return;
+  const int r = find(list, a.R, at);
+  const Request rq = request(a, r);
+  const int row = blockIdx.y * kWaves + (threadIdx.x >> 6), i = (int)(at - list[r]) * kTileRows + row, t = i / a.G;
+  if (i >= rq.n * a.G) return;
+  const size_t p = ((size_t)at * a.H + h) * a.splits * kTileRows + row;
+  join_row<T, D>(a, p, p + kTileRows, kTileRows, a.splits, rq.first + t, h * a.G + i - t * a.G);
+}
+
+// ------------------------------------------------------------------ host
+
+struct Shape {
+  int nt;                            // k_rows' row tiles of 16, 0: k_rows does not run
+  int rows_max;
+  bool cut, tiles;                   // k_rows with pieces; k_tiles runs
+  int tiles_each;
+  long long tile_groups;             // bound of the row tiles of all requests
+  int splits;
+  size_t plan, part_ml, part_o, bytes;
+};
+
+size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
+
+festina_status shape_of(const festina_kv_cache *c, const festina_attention *t, Shape *s) {
+  const festina_status bad = check_cache(c);
+  if (bad != FESTINA_OK) return bad;
+  if (!t || t->n_requests < 0 || t->max_blocks < 1 || t->n_tokens < 0 || t->n_heads < 1 || t->max_new < 1 || t->window < 0)
+    return FESTINA_ERR_INVALID;
+  if (t->n_heads % c->n_kv_heads) return FESTINA_ERR_INVALID;
+  if (t->dtype != FESTINA_BF16 && t->dtype != FESTINA_F16) return FESTINA_ERR_UNSUPPORTED;
+  if ((long long)t->max_blocks * c->block_tokens > INT_MAX / 2 || (long long)t->n_tokens * t->n_heads > INT_MAX / 2 ||
+      t->n_requests > kMaxRequests || t->n_heads > 65536)
+    return FESTINA_ERR_UNSUPPORTED;
+  const int G = t->n_heads / c->n_kv_heads, H = c->n_kv_heads, D = c->head_dim;
+  const long long most = (long long)t->max_new * G;                   // rows of one request and key head
+  *s = Shape{};
+  s->tiles = most > 64 && t->max_new > 1;
+  const long long rows = s->tiles ? G : most;                         // with prompts about: the single tokens' rows
+  s->nt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  if (s->tiles && G > 64) s->nt = 0;
+  s->rows_max = s->tiles ? 16 * s->nt : INT_MAX;
+  const long long keys = (long long)t->max_blocks * c->block_tokens;
+  s->tiles_each = (int)((rows + 16 * s->nt - 1) / max(16 * s->nt, 1));
+  s->cut = keys > 2 * kWaves * kUnit;
+  if (!s->cut && (long long)t->n_requests * H * max(s->tiles_each, 1) > INT_MAX) return FESTINA_ERR_UNSUPPORTED;
+  size_t parts = 0;
+  if (s->nt && s->cut) parts = (size_t)2 * kWorkers * 16 * s->nt;
+  if (s->tiles) {
+    s->tile_groups = ((long long)t->n_tokens * G + kTileRows - 1) / kTileRows + t->n_requests;
+    if (s->tile_groups * H > INT_MAX) return FESTINA_ERR_UNSUPPORTED;
+    // at least two workgroups a compute unit, of at least 16 steps each
+    const long long groups = max(((long long)t->n_tokens * G + kTileRows - 1) / kTileRows, 1ll) * H;
+    const long long wanted = (kWorkers + groups - 1) / groups;
+    s->splits = (int)max(min(wanted, keys / (16 * kUnit)), 1ll);
+    if (s->splits > 1) {
+      const size_t p = (size_t)s->tile_groups * H * s->splits * kTileRows;
+      parts = p > parts ? p : parts;
+    }
+  }
+  s->plan = 0;
+  s->part_ml = up((size_t)2 * (t->n_requests + 1) * 8);
+  s->part_o = s->part_ml + up(parts * 8);
+  s->bytes = s->part_o + up(parts * D * 4);
+  return FESTINA_OK;
+}
+
+template <typename T, int D, int NT>
+void run_rows(const AttArgs &a, const Shape &s, hipStream_t st) {
+  if (!s.cut) {
+    k_rows<T, D, NT, false><<<(unsigned)(a.R * a.H * s.tiles_each), kBlock, 0, st>>>(a);
+    return;
+  }
+  k_rows<T, D, NT, true><<<a.workers, kBlock, 0, st>>>(a);
+  k_rows_join<T, D, NT><<<dim3(a.workers - 1, 16 * NT / kWaves), kBlock, 0, st>>>(a);
+}
+
+template <typename T, int D>
+void run(AttArgs a, const Shape &s, long long *plan, hipStream_t st) {
+  if (a.R > kListed) {
+    if (s.nt == 1) k_plan<16><<<1, 1024, 0, st>>>(a, plan);
+    else if (s.nt == 2) k_plan<32><<<1, 1024, 0, st>>>(a, plan);
+    else k_plan<64><<<1, 1024, 0, st>>>(a, plan);
+    a.plan = plan;
+  }
+  if (s.nt == 1) run_rows<T, D, 1>(a, s, st);
+  else if (s.nt == 2) run_rows<T, D, 2>(a, s, st);
+  else if (s.nt == 4) run_rows<T, D, 4>(a, s, st);
+  if (s.tiles) {
+    k_tiles<T, D><<<dim3((unsigned)(s.tile_groups * a.H), s.splits), kBlock, 0, st>>>(a);
+    if (s.splits > 1)
+      k_tiles_join<T, D><<<dim3((unsigned)(s.tile_groups * a.H), kTileRows / kWaves), kBlock, 0, st>>>(a);
+  }
+}
+
+template <typename T>
+void run_dim(const AttArgs &a, const Shape &s, int D, long long *plan, hipStream_t st) {
+  switch (D) {
+    case 64: run<T, 64>(a, s, plan, st); break;
+    case 96: run<T, 96>(a, s, plan, st); break;
+    case 128: run<T, 128>(a, s, plan, st); break;
+    default: run<T, 256>(a, s, plan, st); break;
+  }
+}
+
+}  // namespace
+
+extern "C" size_t festina_attend_workspace_bytes(const festina_kv_cache *cache, const festina_attention *att) {
+  Shape s;
+  return shape_of(cache, att, &s) == FESTINA_OK ? s.bytes : 0;
+}
+
+extern "C" festina_status festina_attend(const festina_kv_cache *cache, const festina_attention *att, void *workspace,
+                                         size_t workspace_bytes, void *stream) {
+  Shape s;
+  const festina_status bad = shape_of(cache, att, &s);
+  if (bad != FESTINA_OK) return bad;
+  if (att->n_requests == 0 || att->n_tokens == 0) return FESTINA_OK;
+  if (!att->block_table || !att->length || !att->first || !att->q || !att->out) return FESTINA_ERR_INVALID;
+  if (att->q_token_stride < 0 || att->q_head_stride < 0 || att->out_token_stride < 0 || att->out_head_stride < 0 ||
+      !(att->scale == att->scale))
+    return FESTINA_ERR_INVALID;
+  if ((reinterpret_cast<uintptr_t>(att->q) | reinterpret_cast<uintptr_t>(att->out)) & 15) return FESTINA_ERR_INVALID;
+  if ((att->q_token_stride | att->q_head_stride | att->out_token_stride | att->out_head_stride) & 7)
+    return FESTINA_ERR_INVALID;
+  if (!workspace || workspace_bytes < s.bytes || (reinterpret_cast<uintptr_t>(workspace) & 255)) return FESTINA_ERR_INVALID;
+  char *w = static_cast<char *>(workspace);
+  AttArgs a{};
+  a.R = att->n_requests;
+  a.MB = att->max_blocks;
+  a.T = att->n_tokens;
+  a.Hq = att->n_heads;
+  a.H = cache->n_kv_heads;
+  a.G = a.Hq / a.H;
+  a.shift = __builtin_ctz((unsigned)cache->block_tokens);
+  a.NB = cache->n_blocks;
+  a.window = att->window;
+  a.rows_max = s.rows_max;
+  a.tiles_each = s.tiles_each;
+  a.workers = kWorkers;
+  a.splits = s.splits;
+  a.scale = att->scale * 1.44269504088896341f;
+  a.table = att->block_table;
+  a.length = att->length;
+  a.first = att->first;
+  a.q = att->q;
+  a.q_token = att->q_token_stride;
+  a.q_head = att->q_head_stride;
+  a.out = att->out;
+  a.out_token = att->out_token_stride;
+  a.out_head = att->out_head_stride;
+  a.lse = att->lse;
+  a.k = cache->k;
+  a.v = cache->v;
+  a.ks = cache->k_scale;
+  a.vs = cache->v_scale;
+  a.part_ml = reinterpret_cast<float *>(w + s.part_ml);
+  a.part_o = reinterpret_cast<float *>(w + s.part_o);
+  long long *plan = reinterpret_cast<long long *>(w + s.plan);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (att->dtype == FESTINA_BF16) run_dim<bf16>(a, s, cache->head_dim, plan, st);
+  else run_dim<f16>(a, s, cache->head_dim, plan, st);
+  return hipGetLastError() == hipSuccess ? FESTINA_OK : FESTINA_ERR_DEVICE;
+}

@@ -1,0 +1,271 @@
+// cache.hip -- MI355X (gfx950) kernel and C-ABI host dispatch of the write into the 8-bit key/value cache.
+//
+// k_store  a workgroup takes the runs (stretches of tokens in one block) that begin among its tokens, for one key
+//   head and either the keys or the values.  For each run: the largest finite magnitude over the run's
+//   elements, the block's scale from it, where that grew the older codes anew, then the new codes.
+//   Keys are stored as they come ([token][dim]); values pass through LDS, 64 slots at a time, and leave with
+//   their tokens running fastest, 16 tokens of a row in one 16-byte store.
+//
+// Scales are powers of two, so x / scale and the change from one scale to another are exact and each code
+// is one rounding of its element (v_cvt_pk_fp8_f32: to nearest, ties to even), in whatever portions
+// the tokens arrive; a block's scale grows a few times in its life rather than with every new maximum.
+// Bound by the bytes it moves on prompts and by latency on a step of single tokens.
+#include <hip/hip_runtime.h>
+
+#include <cstddef>
+#include <cstdint>
+
+#include "festina.h"
+#include "kv.h"
+
+namespace {
+
+using namespace festina_kv;
+
+constexpr int kThreads = 256;
+constexpr int kSlots = 64;           // slots of a block that the values' transpose takes at a time
+
+typedef float f2 __attribute__((ext_vector_type(2)));
+
+struct StoreArgs {
+  int32_t T, H, shift, slots;        // tokens, key heads, log2 of the block's tokens, NB * BT
+  int32_t span;                      // tokens a workgroup looks for runs in
+  const void *x[2];                  // keys, values
+  int64_t token_stride[2], head_stride[2];
+  bool vec[2];                       // rows of 8 elements are 16-byte aligned
+  const int32_t *slot;
+  uint8_t *codes[2];
+  float *scale[2];
+};
+
+template <int TYPE>
+__device__ __forceinline__ void load8(const void *base, int64_t at, bool vec, float (&x)[8]) {
+  if constexpr (TYPE == FESTINA_F32) {
+    const float *p = static_cast<const float *>(base) + at;
+    if (vec) {
+      const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
+      x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = p[i];
+    }
+  } else {
+    const uint16_t *p = static_cast<const uint16_t *>(base) + at;
+    uint16_t u[8];
+    if (vec) {
+      *reinterpret_cast<uint4 *>(u) = *reinterpret_cast<const uint4 *>(p);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) u[i] = p[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      x[i] = TYPE == FESTINA_BF16 ? __uint_as_float((unsigned)u[i] << 16) : (float)__builtin_bit_cast(_Float16, u[i]);
+  }
+}
+
+__device__ __forceinline__ bool finite(float x) { return __builtin_fabsf(x) < __builtin_inff(); }
+
+// Four codes; `inv` is the scale's reciprocal, a power of two.
+__device__ __forceinline__ unsigned encode4(const float *x, float inv) {
+  float y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    y[i] = finite(x[i]) ? fminf(fmaxf(x[i] * inv, -448.f), 448.f) : __builtin_nanf("");
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
+  return (unsigned)w;
+}
+
+// Four older codes under a scale that is 1 / ratio times larger (exact products, one rounding).
+__device__ __forceinline__ unsigned recode4(unsigned c, float ratio) {
+  const f2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, true);
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a.x * ratio, a.y * ratio, 0, false);
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(b.x * ratio, b.y * ratio, w, true);
+  return (unsigned)w;
+}
+
+// The least power of two s with amax <= 448 s = 1.75 * 2^8 s, from amax's bits: a fraction above 1.75 carries
+// into the exponent.
+__device__ __forceinline__ float scale_of(float amax) {
+  const int e = (int)((__float_as_uint(amax) + 0x1fffffu) >> 23) - 8;
+  return fminf(fmaxf(__uint_as_float((unsigned)max(e, 1) << 23), kScaleMin), kScaleMax);
+}
+
+template <int TYPE, int D>
+__device__ __forceinline__ void store_run(const StoreArgs &a, int which, int h, int t, int n, int slot, float *lds_max,
+                                          uint8_t *tile) {
+  constexpr int kVecs = D / 8, kPitch = D + 4;
+  const int bt = 1 << a.shift, off = slot & (bt - 1);
+  const size_t bh = (size_t)(slot >> a.shift) * a.H + h;
+  const int64_t ts = a.token_stride[which], row0 = (int64_t)h * a.head_stride[which] + (int64_t)t * ts;
+  const void *x = a.x[which];
+  const bool vec = a.vec[which];
+  uint8_t *codes = a.codes[which] + bh * D * bt;
+  const float old = a.scale[which][bh];
+  float v[8], amax = 0.f;
+  for (int i = threadIdx.x; i < n * kVecs; i += kThreads) {
+    load8<TYPE>(x, row0 + (int64_t)(i / kVecs) * ts + (i % kVecs) * 8, vec, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) amax = fmaxf(amax, finite(v[j]) ? __builtin_fabsf(v[j]) : 0.f);
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) amax = fmaxf(amax, __shfl_xor(amax, d));
+  if ((threadIdx.x & 63) == 0) lds_max[threadIdx.x >> 6] = amax;
+  __syncthreads();
+  amax = fmaxf(fmaxf(lds_max[0], lds_max[1]), fmaxf(lds_max[2], lds_max[3]));
+  float scale = scale_of(amax);
+  if (off > 0) scale = fmaxf(scale, old);
+  const float inv = 1.f / scale;                       // exact
+  if (threadIdx.x == 0) a.scale[which][bh] = scale;
+  if (off > 0 && scale > old) {
+    const float ratio = old / scale;
+    if (which == 0) {
+      uint4 *p = reinterpret_cast<uint4 *>(codes);
+      for (int i = threadIdx.x; i < off * D / 16; i += kThreads) {
+        uint4 c = p[i];
+        c.x = recode4(c.x, ratio), c.y = recode4(c.y, ratio), c.z = recode4(c.z, ratio), c.w = recode4(c.w, ratio);
+        p[i] = c;
+      }
+    } else {
+      const int words = (off + 3) / 4;
+      for (int i = threadIdx.x; i < D * words; i += kThreads) {
+        const int d = i / words, o = (i - d * words) * 4;
+        uint8_t *p = codes + (size_t)d * bt + o;
+        const unsigned c = recode4(*reinterpret_cast<const unsigned *>(p), ratio);
+        if (o + 4 <= off) {
+          *reinterpret_cast<unsigned *>(p) = c;
+        } else {                                       // the run's first slots share this word
+#pragma unroll
+          for (int j = 0; j < 3; ++j)
+            if (o + j < off) p[j] = (uint8_t)(c >> (8 * j));
+        }
+      }
+    }
+  }
+  if (which == 0) {
+    for (int i = threadIdx.x; i < n * kVecs; i += kThreads) {
+      const int k = i / kVecs, d = (i % kVecs) * 8;
+      load8<TYPE>(x, row0 + (int64_t)k * ts + d, vec, v);
+      *reinterpret_cast<uint2 *>(codes + (size_t)(off + k) * D + d) = make_uint2(encode4(v, inv), encode4(v + 4, inv));
+    }
+    __syncthreads();                                   // lds_max serves the next run
+    return;
+  }
+  for (int s0 = off & ~(kSlots - 1); s0 < off + n; s0 += kSlots) {     // slots s0 .. s0 + kSlots - 1 of the block
+    const int lo = max(off, s0), hi = min(off + n, s0 + kSlots);
+    for (int i = threadIdx.x; i < (hi - lo) * kVecs; i += kThreads) {
+      const int k = lo + i / kVecs, d = (i % kVecs) * 8;
+      load8<TYPE>(x, row0 + (int64_t)(k - off) * ts + d, vec, v);
+      unsigned *p = reinterpret_cast<unsigned *>(tile + (k - s0) * kPitch + d);
+      p[0] = encode4(v, inv);
+      p[1] = encode4(v + 4, inv);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < D; i += kThreads) {                  // D / 4 groups of rows x 4 groups of slots
+      const int g = i & 3, d = (i >> 2) * 4, s = s0 + g * 16;
+      if (s >= hi || s + 16 <= lo) continue;
+      unsigned w[4][4];                                                // [row][word of four slots]
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        unsigned c[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) c[q] = *reinterpret_cast<const unsigned *>(tile + (g * 16 + j * 4 + q) * kPitch + d);
+        const unsigned x0 = __builtin_amdgcn_perm(c[1], c[0], 0x05010400), x1 = __builtin_amdgcn_perm(c[1], c[0], 0x07030602);
+        const unsigned y0 = __builtin_amdgcn_perm(c[3], c[2], 0x05010400), y1 = __builtin_amdgcn_perm(c[3], c[2], 0x07030602);
+        w[0][j] = __builtin_amdgcn_perm(y0, x0, 0x05040100);
+        w[1][j] = __builtin_amdgcn_perm(y0, x0, 0x07060302);
+        w[2][j] = __builtin_amdgcn_perm(y1, x1, 0x05040100);
+        w[3][j] = __builtin_amdgcn_perm(y1, x1, 0x07060302);
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        uint8_t *p = codes + (size_t)(d + r) * bt + s;
+        if (s >= lo && s + 16 <= hi) {
+          *reinterpret_cast<uint4 *>(p) = make_uint4(w[r][0], w[r][1], w[r][2], w[r][3]);
+        } else {
+#pragma unroll
+          for (int o = 0; o < 16; ++o)
+            if (s + o >= lo && s + o < hi) p[o] = (uint8_t)(w[r][o >> 2] >> (8 * (o & 3)));
+        }
+      }
+    }
+    __syncthreads();
+  }
+}
+
+template <int TYPE, int D>
+__global__ void __launch_bounds__(kThreads) k_store(StoreArgs a) {
+  __shared__ float lds_max[kThreads / 64];
+  __shared__ __attribute__((aligned(16))) uint8_t tile[kSlots * (D + 4)];
+  const int h = blockIdx.y, which = blockIdx.z, bt = 1 << a.shift;
+  const int t0 = blockIdx.x * a.span, t1 = min(t0 + a.span, a.T);
+  for (int t = t0; t < t1; ++t) {                      // everything here is the same in all threads
+    const int slot = a.slot[t];
+    if ((unsigned)slot >= (unsigned)a.slots) continue;
+    if (t > 0 && (slot & (bt - 1)) != 0 && a.slot[t - 1] == slot - 1) continue;
+    const int most = min(bt - (slot & (bt - 1)), a.T - t);
+    int n = 1;
+    for (int i = 0; i < most; i += 64) {               // the run ends at the first slot that does not follow
+      const int k = i + (threadIdx.x & 63);
+      const unsigned long long follows = __ballot(k < most && a.slot[min(t + k, a.T - 1)] == slot + k);
+      n = i + (follows == ~0ull ? 64 : __builtin_ctzll(~follows));
+      if (follows != ~0ull) break;
+    }
+    store_run<TYPE, D>(a, which, h, t, n, slot, lds_max, tile);
+  }
+}
+
+template <int TYPE>
+void launch(const StoreArgs &a, int D, dim3 grid, hipStream_t st) {
+  switch (D) {
+    case 64: k_store<TYPE, 64><<<grid, kThreads, 0, st>>>(a); break;
+    case 96: k_store<TYPE, 96><<<grid, kThreads, 0, st>>>(a); break;
+    case 128: k_store<TYPE, 128><<<grid, kThreads, 0, st>>>(a); break;
+    default: k_store<TYPE, 256><<<grid, kThreads, 0, st>>>(a); break;
+  }
+}
+
+}  // namespace
+
+extern "C" festina_status festina_store_kv(const festina_kv_cache *cache, const festina_kv_tokens *tokens,
+                                           void *stream) {
+  const festina_status bad = check_cache(cache);
+  if (bad != FESTINA_OK) return bad;
+  if (!tokens || tokens->n_tokens < 0) return FESTINA_ERR_INVALID;
+  if (tokens->dtype != FESTINA_BF16 && tokens->dtype != FESTINA_F16 && tokens->dtype != FESTINA_F32)
+    return FESTINA_ERR_INVALID;
+  if (tokens->k_token_stride < 0 || tokens->k_head_stride < 0 || tokens->v_token_stride < 0 || tokens->v_head_stride < 0)
+    return FESTINA_ERR_INVALID;
+  if (tokens->n_tokens == 0) return FESTINA_OK;
+  if (!tokens->k || !tokens->v || !tokens->slot) return FESTINA_ERR_INVALID;
+  const int size = tokens->dtype == FESTINA_F32 ? 4 : 2;
+  if ((reinterpret_cast<uintptr_t>(tokens->k) | reinterpret_cast<uintptr_t>(tokens->v)) % size) return FESTINA_ERR_INVALID;
+  StoreArgs a;
+  a.T = tokens->n_tokens;
+  a.H = cache->n_kv_heads;
+  a.shift = __builtin_ctz((unsigned)cache->block_tokens);
+  a.slots = cache->n_blocks * cache->block_tokens;
+  a.x[0] = tokens->k;
+  a.x[1] = tokens->v;
+  a.token_stride[0] = tokens->k_token_stride;
+  a.token_stride[1] = tokens->v_token_stride;
+  a.head_stride[0] = tokens->k_head_stride;
+  a.head_stride[1] = tokens->v_head_stride;
+  for (int i = 0; i < 2; ++i)
+    a.vec[i] = ((reinterpret_cast<uintptr_t>(a.x[i]) | (uintptr_t)(a.token_stride[i] * size) |
+                 (uintptr_t)(a.head_stride[i] * size)) & 15) == 0;
+  a.slot = tokens->slot;
+  a.codes[0] = cache->k;
+  a.codes[1] = cache->v;
+  a.scale[0] = cache->k_scale;
+  a.scale[1] = cache->v_scale;
+  a.span = a.T <= 2048 ? 1 : 16;
+  const long long groups = ((long long)a.T + a.span - 1) / a.span;
+  const dim3 grid((unsigned)groups, a.H, 2);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (tokens->dtype == FESTINA_BF16) launch<FESTINA_BF16>(a, cache->head_dim, grid, st);
+  else if (tokens->dtype == FESTINA_F16) launch<FESTINA_F16>(a, cache->head_dim, grid, st);
+  else launch<FESTINA_F32>(a, cache->head_dim, grid, st);
+  return hipGetLastError() == hipSuccess ? FESTINA_OK : FESTINA_ERR_DEVICE;
+}

@@ -2,7 +2,8 @@
 
 Argument marshalling only: every step of the search runs in the HIP library
 (``libfestina.so`` built from ``csrc/festina.hip``, ``csrc/fronts.hip``, ``csrc/sweep.hip``,
-``csrc/preferred.hip``, ``csrc/dispatch.hip`` and ``csrc/transfer.hip``).  PyTorch provides device
+``csrc/preferred.hip``, ``csrc/dispatch.hip`` and ``csrc/transfer.hip``; the serving step's kernels
+from ``csrc/blocks.hip``, ``csrc/cache.hip`` and ``csrc/attend.hip``).  PyTorch provides device
 memory and streams.  There is no CPU fallback: if the library is missing this
 module raises.
 """
@@ -24,6 +25,9 @@ FESTINA_ERR_TOO_LARGE = 4
 FESTINA_NOALLOC_WORKSPACE_BYTES = 32 << 20
 FESTINA_STATIC_PER_TASK = 0      # sweep energy readings (festina_batches.static_power)
 FESTINA_STATIC_PER_BATCH = 1
+FESTINA_BF16 = 0                 # element types of keys, values, queries and outputs
+FESTINA_F16 = 1
+FESTINA_F32 = 2
 
 
 class FestinaError(RuntimeError):
@@ -132,13 +136,47 @@ class festina_moves(C.Structure):
     _fields_ = [("decision", C.c_void_p), ("remaining_ms", C.c_void_p), ("migrate_ms", C.c_void_p)]
 
 
+class festina_kv_requests(C.Structure):
+    _fields_ = [("n_requests", C.c_int32), ("max_blocks", C.c_int32), ("block_tokens", C.c_int32),
+                ("n_blocks", C.c_int32), ("held", C.c_void_p), ("add", C.c_void_p), ("block_table", C.c_void_p),
+                ("free_ids", C.c_void_p), ("n_free", C.c_void_p)]
+
+
+class festina_kv_step(C.Structure):
+    _fields_ = [("max_tokens", C.c_int32), ("first", C.c_void_p), ("slot", C.c_void_p), ("length", C.c_void_p),
+                ("served", C.c_void_p), ("n_free_out", C.c_void_p)]
+
+
+class festina_kv_cache(C.Structure):
+    _fields_ = [("n_blocks", C.c_int32), ("block_tokens", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p),
+                ("v_scale", C.c_void_p)]
+
+
+class festina_kv_tokens(C.Structure):
+    _fields_ = [("n_tokens", C.c_int32), ("dtype", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("k_token_stride", C.c_int64), ("k_head_stride", C.c_int64), ("v_token_stride", C.c_int64),
+                ("v_head_stride", C.c_int64), ("slot", C.c_void_p)]
+
+
+class festina_attention(C.Structure):
+    _fields_ = [("n_requests", C.c_int32), ("max_blocks", C.c_int32), ("n_tokens", C.c_int32),
+                ("n_heads", C.c_int32), ("max_new", C.c_int32), ("dtype", C.c_int32), ("window", C.c_int32),
+                ("scale", C.c_float), ("block_table", C.c_void_p), ("length", C.c_void_p), ("first", C.c_void_p),
+                ("q", C.c_void_p), ("q_token_stride", C.c_int64), ("q_head_stride", C.c_int64),
+                ("out", C.c_void_p), ("out_token_stride", C.c_int64), ("out_head_stride", C.c_int64),
+                ("lse", C.c_void_p)]
+
+
 EXPORTED = ("festina_abi_version", "festina_status_string", "festina_placements_workspace_bytes",
             "festina_score_placements", "festina_score_placements_noalloc", "festina_migrations_workspace_bytes",
             "festina_score_migrations",
             "festina_sweep_batches", "festina_preferred_configs", "festina_ewr_workspace_bytes",
             "festina_fleet_ewr", "festina_dispatch_workspace_bytes", "festina_dispatch_requests",
             "festina_transfer_costs", "festina_request_moves", "festina_score_placements_timed",
-            "festina_score_migrations_timed", "festina_dispatch_waves_workspace_bytes", "festina_dispatch_waves")
+            "festina_score_migrations_timed", "festina_dispatch_waves_workspace_bytes", "festina_dispatch_waves",
+            "festina_blocks_workspace_bytes", "festina_extend_blocks", "festina_release_blocks", "festina_store_kv",
+            "festina_attend_workspace_bytes", "festina_attend")
 
 _lib = None
 
@@ -213,6 +251,20 @@ def lib():
         L.festina_score_placements_timed.restype = C.c_int
         L.festina_score_migrations_timed.argtypes = L.festina_score_migrations.argtypes + [C.c_void_p, C.c_void_p]
         L.festina_score_migrations_timed.restype = C.c_int
+        L.festina_blocks_workspace_bytes.argtypes = [C.c_int32, C.c_int32]
+        L.festina_blocks_workspace_bytes.restype = C.c_size_t
+        L.festina_extend_blocks.argtypes = [P(festina_kv_requests), P(festina_kv_step), C.c_void_p, C.c_size_t,
+                                            C.c_void_p]
+        L.festina_extend_blocks.restype = C.c_int
+        L.festina_release_blocks.argtypes = [P(festina_kv_requests), C.c_void_p, P(festina_kv_step), C.c_void_p,
+                                             C.c_size_t, C.c_void_p]
+        L.festina_release_blocks.restype = C.c_int
+        L.festina_store_kv.argtypes = [P(festina_kv_cache), P(festina_kv_tokens), C.c_void_p]
+        L.festina_store_kv.restype = C.c_int
+        L.festina_attend_workspace_bytes.argtypes = [P(festina_kv_cache), P(festina_attention)]
+        L.festina_attend_workspace_bytes.restype = C.c_size_t
+        L.festina_attend.argtypes = [P(festina_kv_cache), P(festina_attention), C.c_void_p, C.c_size_t, C.c_void_p]
+        L.festina_attend.restype = C.c_int
         _lib = L
     return _lib
 
@@ -570,6 +622,171 @@ class DeviceTransfer:
                 self.migrate[:Q].cpu().numpy())
 
 
+def _check(t, name, dtypes, shape=None):
+    """A device tensor of one of these types (and of this shape, contiguous, if one is given)."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name}: a tensor in device memory is needed")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name}: dtype {t.dtype}, not {' or '.join(str(d) for d in dtypes)}")
+    if shape is not None and (tuple(t.shape) != tuple(shape) or not t.is_contiguous()):
+        raise ValueError(f"{name}: a contiguous tensor of shape {tuple(shape)} is needed, not {tuple(t.shape)}")
+
+
+def _on(stream, device):
+    """A context in which torch allocates for `stream` (None: the current one)."""
+    import contextlib
+    import torch
+    if stream is None:
+        return contextlib.nullcontext()
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device=device)
+    return torch.cuda.stream(stream)
+
+
+class _Workspaces:
+    """Device scratch, one for each stream that calls come on, so that they may overlap."""
+
+    def __init__(self):
+        self.by_stream = {}
+
+    def get(self, n, stream, device):
+        import torch
+        key = _stream_handle(stream).value
+        ws = self.by_stream.get(key)
+        if ws is None or ws.numel() < n:
+            with _on(stream, device):
+                ws = self.by_stream[key] = torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+        return ws
+
+
+class DeviceBlocks:
+    """The cache blocks of one GPU's requests: int32 device tensors held [R], add [R], table
+    [R][max_blocks], free_ids [n_blocks], n_free [1] (festina_kv_requests), used in place.
+
+    extend() gives every request blocks and slots for its add new tokens: table, and first [R+1],
+    slot [max_tokens], length [R], served [R], n_free_out [1].  release(done) returns the blocks of the
+    requests whose uint8 done is not 0: free_ids, length, n_free_out.  advance() makes length and n_free_out
+    the next step's held and n_free (no work on the device)."""
+
+    def __init__(self, held, add, table, free_ids, n_free, block_tokens: int, max_tokens: int):
+        import torch
+        if not isinstance(table, torch.Tensor) or table.dim() != 2:
+            raise ValueError("table: a tensor of two dimensions is needed")
+        R = int(table.shape[0])
+        for name, t, shape in (("held", held, (R,)), ("add", add, (R,)), ("table", table, table.shape),
+                               ("free_ids", free_ids, (free_ids.numel(),)), ("n_free", n_free, (1,))):
+            _check(t, name, (torch.int32,), shape)
+        device = table.device
+        self.held, self.add, self.table, self.free_ids, self.n_free = held, add, table, free_ids, n_free
+        self.block_tokens, self.max_tokens = int(block_tokens), int(max_tokens)
+        i32 = lambda n: torch.empty(n, dtype=torch.int32, device=device)
+        self.first, self.slot, self.length, self.n_free_out = i32(R + 1), i32(max(self.max_tokens, 0)), i32(R), i32(1)
+        self.served = torch.empty(R, dtype=torch.uint8, device=device)
+        self.ws_bytes = festina_blocks_workspace_bytes(R, self.max_tokens)
+        self._ws = _Workspaces()
+        self._structs()
+
+    def _structs(self):
+        self.req = festina_kv_requests(int(self.table.shape[0]), int(self.table.shape[1]), self.block_tokens,
+                                       int(self.free_ids.numel()), _ptr(self.held), _ptr(self.add), _ptr(self.table),
+                                       _ptr(self.free_ids), _ptr(self.n_free))
+        self.out = festina_kv_step(self.max_tokens, _ptr(self.first), _ptr(self.slot), _ptr(self.length),
+                                   _ptr(self.served), _ptr(self.n_free_out))
+
+    def extend(self, stream=None):
+        festina_extend_blocks(self.req, self.out, self._ws.get(self.ws_bytes, stream, self.table.device),
+                              self.ws_bytes, stream)
+
+    def release(self, done, stream=None):
+        import torch
+        _check(done, "done", (torch.uint8, torch.bool), self.held.shape)
+        festina_release_blocks(self.req, done, self.out, self._ws.get(self.ws_bytes, stream, self.table.device),
+                               self.ws_bytes, stream)
+
+    def advance(self):
+        self.held, self.length = self.length, self.held
+        self.n_free, self.n_free_out = self.n_free_out, self.n_free
+        self._structs()
+
+
+class DeviceCache:
+    """One layer's key/value cache in 8 bits (festina_kv_cache): uint8 codes k [n_blocks][kv heads][block tokens]
+    [dim], v [n_blocks][kv heads][dim][block tokens] and float32 scales k_scale, v_scale [n_blocks][kv heads],
+    device tensors used in place (``DeviceCache.empty`` makes them)."""
+
+    def __init__(self, k, v, k_scale, v_scale):
+        import torch
+        _check(k, "k", (torch.uint8,), k.shape)
+        if k.dim() != 4:
+            raise ValueError("k: [blocks][kv heads][block tokens][dim]")
+        n, h, bt, d = (int(x) for x in k.shape)
+        _check(v, "v", (torch.uint8,), (n, h, d, bt))
+        _check(k_scale, "k_scale", (torch.float32,), (n, h))
+        _check(v_scale, "v_scale", (torch.float32,), (n, h))
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.cache = festina_kv_cache(n, bt, h, d, _ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale))
+        self._ws = _Workspaces()
+
+    @classmethod
+    def empty(cls, n_blocks: int, block_tokens: int, n_kv_heads: int, head_dim: int, device="cuda"):
+        import torch
+        u8 = lambda *s: torch.empty(s, dtype=torch.uint8, device=device)
+        f32 = lambda: torch.zeros((n_blocks, n_kv_heads), dtype=torch.float32, device=device)
+        return cls(u8(n_blocks, n_kv_heads, block_tokens, head_dim), u8(n_blocks, n_kv_heads, head_dim, block_tokens),
+                   f32(), f32())
+
+    def store(self, k, v, slot, stream=None):
+        """Store keys and values [tokens][kv heads][dim] (bfloat16, half or float32; any strides but the last)
+        at the int32 slots [tokens]."""
+        import torch
+        types = {torch.bfloat16: FESTINA_BF16, torch.float16: FESTINA_F16, torch.float32: FESTINA_F32}
+        c = self.cache
+        for name, x in (("k", k), ("v", v)):
+            _check(x, name, tuple(types))
+            if tuple(x.shape[1:]) != (c.n_kv_heads, c.head_dim) or x.dim() != 3 or (x.numel() and x.stride(2) != 1):
+                raise ValueError(f"{name}: [tokens][{c.n_kv_heads}][{c.head_dim}] with its last axis contiguous")
+        if k.dtype != v.dtype or k.shape[0] != v.shape[0]:
+            raise ValueError("k and v: one type and number of tokens")
+        _check(slot, "slot", (torch.int32,), (k.shape[0],))
+        tokens = festina_kv_tokens(int(k.shape[0]), types[k.dtype], _ptr(k), _ptr(v), k.stride(0), k.stride(1),
+                                   v.stride(0), v.stride(1), _ptr(slot))
+        festina_store_kv(c, tokens, stream)
+
+    def attend(self, q, table, length, first, max_new: int, scale=None, window: int = 0, out=None, lse=None,
+               stream=None):
+        """Attention of the queries [tokens][heads][dim] (bfloat16 or half) over the cache: (out, lse).  table
+        [requests][columns], length [requests] (new tokens included) and first [requests+1] are a step's
+        (DeviceBlocks); max_new bounds the new tokens of one request.  out and lse are made where not given."""
+        import torch
+        types = {torch.bfloat16: FESTINA_BF16, torch.float16: FESTINA_F16}
+        c = self.cache
+        _check(q, "q", tuple(types))
+        if q.dim() != 3 or q.shape[2] != c.head_dim or (q.numel() and q.stride(2) != 1):
+            raise ValueError(f"q: [tokens][heads][{c.head_dim}] with its last axis contiguous")
+        _check(table, "table", (torch.int32,), table.shape)
+        if table.dim() != 2:
+            raise ValueError("table: a tensor of two dimensions is needed")
+        R = int(table.shape[0])
+        _check(length, "length", (torch.int32,), (R,))
+        _check(first, "first", (torch.int32,), (R + 1,))
+        if out is None or lse is None:
+            with _on(stream, q.device):
+                out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+                lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if lse is None else lse
+        _check(out, "out", (q.dtype,))
+        if out.shape != q.shape or (out.numel() and out.stride(2) != 1):
+            raise ValueError("out: q's shape with its last axis contiguous")
+        _check(lse, "lse", (torch.float32,), q.shape[:2])
+        att = festina_attention(R, int(table.shape[1]), int(q.shape[0]), int(q.shape[1]), int(max_new), types[q.dtype],
+                                int(window), float(c.head_dim ** -0.5 if scale is None else scale), _ptr(table),
+                                _ptr(length), _ptr(first), _ptr(q), q.stride(0), q.stride(1), _ptr(out), out.stride(0),
+                                out.stride(1), _ptr(lse))
+        n = festina_attend_workspace_bytes(c, att)
+        festina_attend(c, att, self._ws.get(n, stream, q.device), n, stream)
+        return out, lse
+
+
 # ------------------------------------------------------------------ the ABI calls
 def festina_placements_workspace_bytes(lut, gpus, req) -> int:
     return int(lib().festina_placements_workspace_bytes(C.byref(lut), C.byref(gpus), C.byref(req)))
@@ -680,3 +897,38 @@ def festina_request_moves(lut, transfer, plan, req, out, stream=None) -> None:
                                      _stream_handle(stream))
     if st != FESTINA_OK:
         raise FestinaError(st, "festina_request_moves")
+
+
+def festina_blocks_workspace_bytes(n_requests: int, max_tokens: int) -> int:
+    return int(lib().festina_blocks_workspace_bytes(int(n_requests), int(max_tokens)))
+
+
+def festina_extend_blocks(req, out, workspace, workspace_bytes, stream=None) -> None:
+    st = lib().festina_extend_blocks(C.byref(req), C.byref(out), _ptr(workspace), int(workspace_bytes),
+                                     _stream_handle(stream))
+    if st != FESTINA_OK:
+        raise FestinaError(st, "festina_extend_blocks")
+
+
+def festina_release_blocks(req, done, out, workspace, workspace_bytes, stream=None) -> None:
+    st = lib().festina_release_blocks(C.byref(req), _ptr(done), C.byref(out), _ptr(workspace), int(workspace_bytes),
+                                      _stream_handle(stream))
+    if st != FESTINA_OK:
+        raise FestinaError(st, "festina_release_blocks")
+
+
+def festina_store_kv(cache, tokens, stream=None) -> None:
+    st = lib().festina_store_kv(C.byref(cache), C.byref(tokens), _stream_handle(stream))
+    if st != FESTINA_OK:
+        raise FestinaError(st, "festina_store_kv")
+
+
+def festina_attend_workspace_bytes(cache, att) -> int:
+    return int(lib().festina_attend_workspace_bytes(C.byref(cache), C.byref(att)))
+
+
+def festina_attend(cache, att, workspace, workspace_bytes, stream=None) -> None:
+    st = lib().festina_attend(C.byref(cache), C.byref(att), _ptr(workspace), int(workspace_bytes),
+                              _stream_handle(stream))
+    if st != FESTINA_OK:
+        raise FestinaError(st, "festina_attend")

@@ -1,0 +1,387 @@
+"""GPU tests of attention over the 8-bit cache against the definition in 64 bits.  The bounds come from the arithmetic
+(kv_reference.attend_bounds): float32 logits and sums, weights in half precision, one rounding of the output."""
+import numpy as np
+import pytest
+
+import kv_reference as K
+
+torch = pytest.importorskip("torch")
+pytestmark = [pytest.mark.gpu,
+              pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a GPU")]
+
+# unit roundoff of 8 and 11 significant bits: half a unit in the last place just above a power of two
+TYPES = {"bf16": (torch.bfloat16, 2.0 ** -8), "f16": (torch.float16, 2.0 ** -11)}
+
+
+class Case:
+    """Requests of (length, new tokens) over a shuffled pool; what no request holds is NaN codes."""
+
+    def __init__(self, rng, requests, D=128, H=2, G=4, bt=32, dtype="bf16", spread=1.0, columns=None, powers=True):
+        self.D, self.H, self.G, self.bt, self.dtype = D, H, G, bt, dtype
+        self.length = np.array([x for x, _ in requests], np.int64)
+        self.new = np.array([x for _, x in requests], np.int64)
+        self.first = np.concatenate([[0], np.cumsum(self.new)])
+        cols = -(-self.length // bt)
+        MB = columns or int(max(1, cols.max(initial=1)))
+        n = int(cols.sum()) + 2
+        ids = rng.permutation(n)
+        self.table = np.full((len(requests), MB), -1, np.int64)
+        at = 0
+        for r, c in enumerate(cols):
+            self.table[r, :c] = ids[at:at + c]
+            at += c
+        self.k = K.encode(rng.normal(0, 112, (n, H, bt, D)).clip(-448, 448))
+        self.v = K.encode(rng.normal(0, 112, (n, H, D, bt)).clip(-448, 448))
+        self.ks = (2.0 ** rng.integers(-8, -5, (n, H)) * spread).astype(np.float32)
+        self.vs = (2.0 ** rng.integers(-10, -3, (n, H))).astype(np.float32)
+        if not powers:
+            self.ks *= rng.uniform(0.5, 1.5, (n, H)).astype(np.float32)
+            self.vs *= rng.uniform(0.5, 1.5, (n, H)).astype(np.float32)
+        for r, c in enumerate(cols):                        # behind the last token: NaN
+            o = int(self.length[r]) % bt
+            if o:
+                self.k[self.table[r, c - 1], :, o:] = 0xFF
+                self.v[self.table[r, c - 1], :, :, o:] = 0x7F
+        self.k[ids[at:]], self.v[ids[at:]] = 0x7F, 0x7F
+        self.ks[ids[at:]], self.vs[ids[at:]] = np.nan, np.nan
+        T = int(self.first[-1])
+        self.q = torch.from_numpy(rng.normal(0, 1, (T, H * G, D))).to(TYPES[dtype][0]).cuda()
+
+    def tensors(self):
+        up = lambda x, t: torch.from_numpy(np.ascontiguousarray(x, t)).cuda()
+        return (up(self.table, np.int32), up(self.length, np.int32), up(self.first, np.int32))
+
+    def cache(self):
+        from paper_2606_30391_amd import festina as F
+        up = lambda x: torch.from_numpy(x).cuda()
+        return F.DeviceCache(up(self.k), up(self.v), up(self.ks), up(self.vs))
+
+    def want(self, scale=None, window=0):
+        return K.attend(self.q.double().cpu().numpy(), self.k, self.v, self.ks, self.vs, self.table, self.length,
+                        self.first, np.float32(self.D ** -0.5 if scale is None else scale).astype(np.float64), window)
+
+    def compare(self, out, lse, want):
+        o, l, magnitude = want
+        tol_o, tol_l = K.attend_bounds(o, l, magnitude, self.D, TYPES[self.dtype][1])
+        got_o, got_l = out.double().cpu().numpy(), lse.double().cpu().numpy()
+        assert np.array_equal(np.isnan(got_o), np.isnan(o))
+        with np.errstate(invalid="ignore"):
+            bad = np.abs(got_o - o) > tol_o
+            assert not bad.any(), f"out: {np.nanmax(np.abs(got_o - o) / tol_o):.3g} of the bound at {np.argwhere(bad)[0]}"
+            assert np.array_equal(np.isneginf(got_l), np.isneginf(l))
+            fin = np.isfinite(l)
+            assert np.all(np.abs(got_l - l)[fin] <= tol_l[fin]), "lse"
+            assert np.array_equal(np.isnan(got_l), np.isnan(l))
+
+    def check(self, scale=None, window=0, max_new=None, label=""):
+        print(f"[gpu] attend D={self.D} H={self.H} G={self.G} bt={self.bt} {self.dtype} requests="
+              f"{list(zip(self.length.tolist(), self.new.tolist()))[:6]} window={window} {label}", flush=True)
+        out, lse = self.cache().attend(self.q, *self.tensors(), max_new=max_new or max(1, int(self.new.max(initial=1))),
+                                       scale=scale, window=window)
+        torch.cuda.synchronize()
+        self.compare(out, lse, self.want(scale, window))
+        return out, lse
+
+
+# single tokens: no token, one, block and step ends, ragged, short tables (one launch) and long ones (pieces)
+DECODE = [[(1, 1)], [(0, 1), (63, 1), (64, 1), (65, 1), (16, 1)], [(500, 1), (3, 1), (0, 0), (511, 1)],
+          [(513, 1), (1, 1), (2000, 1), (0, 0), (129, 1)], [(4099, 1)]]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("D", [64, 96, 128, 256])
+@pytest.mark.parametrize("requests", DECODE)
+def test_single_tokens(requests, D, dtype):
+    rng = np.random.default_rng(D + len(requests))
+    Case(rng, requests, D=D, dtype=dtype).check()
+
+
+@pytest.mark.parametrize("bt", [16, 64, 128, 256])
+@pytest.mark.parametrize("H,G", [(1, 1), (3, 7), (2, 16), (1, 24), (1, 64), (2, 33), (1, 130)])
+def test_head_layouts_and_blocks(bt, H, G):
+    rng = np.random.default_rng(bt * H * G)
+    Case(rng, [(700, 1), (17, 1), (bt, 1)], D=64, H=H, G=G, bt=bt).check()
+    Case(rng, [(90, 1)], D=128, H=H, G=G, bt=bt).check()
+
+
+@pytest.mark.parametrize("D", [64, 96, 128, 256])
+@pytest.mark.parametrize("new", [2, 3, 4, 8, 13, 16])
+def test_short_runs(new, D):
+    """Up to 64 rows a request, and the first sizes past that."""
+    rng = np.random.default_rng(new * D)
+    Case(rng, [(new, new), (700, new), (1, 1), (65, min(new, 5)), (0, 0)], D=D).check()
+
+
+# prompts: row tiles of 128, odd lengths, on top of a cache, tokens before the cache's start (rows without keys)
+PROMPTS = [[(33, 33)], [(128, 128), (1, 1), (300, 40)], [(1000, 77), (200, 200), (0, 0), (5, 5)], [(129, 129), (64, 17)]]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("D,G", [(64, 1), (96, 3), (128, 4), (256, 2)])
+@pytest.mark.parametrize("requests", PROMPTS)
+def test_prompts(requests, D, G, dtype):
+    rng = np.random.default_rng(D + len(requests))
+    Case(rng, requests, D=D, G=G, dtype=dtype).check(max_new=200)
+
+
+@pytest.mark.parametrize("requests,max_new", [([(5000, 40)], 40), ([(2500, 100), (4096, 1), (100, 100)], 100)])
+def test_prompts_over_a_long_cache(requests, max_new):
+    """Few row tiles: split over the keys and joined."""
+    rng = np.random.default_rng(max_new)
+    Case(rng, requests, D=64, H=1, G=4, bt=64).check(max_new=max_new)
+    Case(rng, requests, D=128, H=2, G=2, bt=16).check(max_new=max_new)
+
+
+@pytest.mark.parametrize("window", [1, 16, 63, 200, 10 ** 9])
+def test_windows(window):
+    rng = np.random.default_rng(window % 1000)
+    Case(rng, [(700, 1), (1, 1), (1500, 1), (64, 1)], D=64).check(window=window)
+    Case(rng, [(700, 5), (3, 3), (1500, 4)], D=64).check(window=window)
+    Case(rng, [(400, 150), (90, 90), (2500, 60)], D=64).check(window=window)
+
+
+@pytest.mark.parametrize("new", [1, 3, 40])
+def test_tokens_before_the_cache_see_nothing(new):
+    """A length below the number of new tokens leaves rows without keys: zeros and -inf."""
+    rng = np.random.default_rng(new)
+    c = Case(rng, [(new, new), (50, new), (600, new)], D=64)
+    c.length[0], c.length[1] = 0, new - 1
+    out, lse = c.check()
+    first = int(c.first[1])
+    assert not out[:new].any() and torch.isneginf(lse[:new]).all() and torch.isneginf(lse[first]).all()
+
+
+@pytest.mark.parametrize("new", [1, 4, 50])
+def test_blocks_that_are_not_there_are_not_seen(new):
+    rng = np.random.default_rng(new + 70)
+    c = Case(rng, [(300, new), (700, new), (64, new)], D=64, bt=16)
+    c.table[0, 3], c.table[1, 10], c.table[1, 20] = -1, 10 ** 6, -2 ** 31
+    c.table[2, :] = -7                                       # nothing at all
+    out, lse = c.check()
+    assert not out[2 * new:].any() and torch.isneginf(lse[2 * new:]).all()
+
+
+@pytest.mark.parametrize("new,window", [(4, 0), (40, 0), (4, 20), (40, 20), (1, 0), (1, 20)])
+def test_nan_in_values_reaches_only_the_rows_that_see_it(new, window):
+    rng = np.random.default_rng(new + 80)
+    c = Case(rng, [(200, new), (600, new)], D=64, bt=32)
+    for r, p in ((0, 200 - (new + 1) // 2), (1, 600 - new), (1, 300)):
+        b, o = c.table[r, p // 32], p % 32
+        c.v[b, 0, 5, o] = 0x7F
+        c.v[b, 1, 60, o] = 0xFF
+    c.check(window=window, label="NaN values")
+
+
+@pytest.mark.parametrize("new", [1, 4, 40])
+def test_nan_in_keys_reaches_only_the_rows_that_see_it(new):
+    rng = np.random.default_rng(new + 90)
+    c = Case(rng, [(200, new), (600, new)], D=64, bt=32)
+    p = 600 - (new + 1) // 2
+    c.k[c.table[1, p // 32], 1, p % 32, 3] = 0x7F
+    c.check(label="NaN keys")
+
+
+def test_large_logits_and_scales_that_are_no_powers_of_two():
+    rng = np.random.default_rng(21)
+    for new in (1, 3, 50):
+        Case(rng, [(700, new), (90, new)], D=64, powers=False).check()
+        Case(rng, [(700, new), (90, new)], D=128, spread=30.0).check()
+        Case(rng, [(700, new)], D=64).check(scale=-0.3)
+        Case(rng, [(700, new)], D=64).check(scale=0.0)
+
+
+def test_value_scales_far_apart():
+    """Blocks of zeros (the least scale) and of large values beside ordinary ones weigh as their keys say."""
+    rng = np.random.default_rng(22)
+    for new in (1, 40):
+        c = Case(rng, [(640, new)], D=64, bt=32)
+        for i, s in ((1, 2.0 ** -32), (4, 2.0 ** -32), (7, 2.0 ** 20), (9, 0.0), (11, 2.0 ** 32)):
+            c.vs[c.table[0, i]] = s
+            if s < 1:
+                c.v[c.table[0, i]] = 0
+        c.check()
+
+
+@pytest.mark.parametrize("R", [511, 512, 513, 1500])
+def test_many_requests(R):
+    """Around the number of requests from which running sums are formed by a launch of their own."""
+    rng = np.random.default_rng(R)
+    new = [(int(x), 1) for x in rng.integers(0, 40, R)]
+    new[7], new[R - 1] = (700, 1), (600, 1)
+    Case(rng, new, D=64, H=1, G=2, bt=16).check()
+    new[9] = (90, 70)
+    Case(rng, new, D=64, H=1, G=2, bt=16).check()
+
+
+def test_strides_of_queries_and_outputs():
+    rng = np.random.default_rng(31)
+    for requests in ([(300, 1), (20, 1)], [(300, 60)]):
+        c = Case(rng, requests, D=64, H=2, G=3)
+        T = c.q.shape[0]
+        wide = torch.randn((T, 10, 64), device="cuda").to(torch.bfloat16)
+        c.q = wide[:, 2:8]                                    # queries beside keys and values
+        out = torch.full((6, T, 72), 7.0, dtype=torch.bfloat16, device="cuda")
+        o = out.permute(1, 0, 2)[:, :, :64]
+        print("[gpu] attend strides", flush=True)
+        lse = torch.empty((T, 6), device="cuda")
+        got = c.cache().attend(c.q, *c.tensors(), max_new=60, out=o, lse=lse)
+        torch.cuda.synchronize()
+        assert got[0] is o and got[1] is lse
+        c.compare(o, lse, c.want())
+        assert bool((out[:, :, 64:] == 7.0).all())            # nothing behind the rows
+
+
+def test_rows_of_no_request_are_not_written():
+    rng = np.random.default_rng(32)
+    for requests in ([(300, 1), (20, 1)], [(300, 60)]):
+        c = Case(rng, requests, D=64, H=1, G=2)
+        T = int(c.first[-1])
+        c.q = torch.randn((T + 9, 2, 64), device="cuda").to(torch.bfloat16)
+        out = torch.full_like(c.q, 5.0)
+        lse = torch.full((T + 9, 2), 5.0, device="cuda")
+        print("[gpu] attend more rows than tokens", flush=True)
+        c.cache().attend(c.q, *c.tensors(), max_new=60, out=out, lse=lse)
+        torch.cuda.synchronize()
+        assert bool((out[T:] == 5.0).all()) and bool((lse[T:] == 5.0).all())
+        want = c.want()
+        c.q = c.q[:T]
+        c.compare(out[:T], lse[:T], tuple(x[:T] for x in want[:2]) + (tuple(x[:T] for x in want[2]),))
+
+
+def test_the_result_does_not_depend_on_the_workspace_or_the_bound():
+    """Outputs equal bit for bit whatever the workspace held; a bound above the longest run changes only kernels."""
+    rng = np.random.default_rng(33)
+    for requests in ([(3000, 1), (50, 1), (700, 1)], [(3000, 90), (50, 1)]):
+        c = Case(rng, requests, D=128)
+        cache = c.cache()
+        print("[gpu] attend workspace", flush=True)
+        a = cache.attend(c.q, *c.tensors(), max_new=90)
+        for ws in cache._ws.by_stream.values():
+            ws.fill_(255)
+        b = cache.attend(c.q, *c.tensors(), max_new=90)
+        torch.cuda.synchronize()
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+        want = c.want()
+        for bound in (90, 200, 3000):
+            out, lse = cache.attend(c.q, *c.tensors(), max_new=bound)
+            torch.cuda.synchronize()
+            c.compare(out, lse, want)
+
+
+def test_a_cache_past_32_bit_offsets():
+    """Blocks whose codes lie beyond 2^32 bytes."""
+    from paper_2606_30391_amd import festina as F
+    rng = np.random.default_rng(34)
+    H, G, D, bt, n = 4, 2, 256, 64, 70_000
+    for new in (1, 40):
+        c = Case(rng, [(600, new), (130, new)], D=D, H=H, G=G, bt=bt)
+        print(f"[gpu] attend past 32 bits, {new} new", flush=True)
+        cache = F.DeviceCache.empty(n, bt, H, D)
+        used = np.unique(c.table[c.table >= 0])
+        place = {int(b): n - 1 - 3 * i for i, b in enumerate(used)}
+        small, want = c.cache(), c.want()
+        to = torch.tensor([place[int(b)] for b in used], device="cuda")
+        src = torch.from_numpy(used).cuda()
+        for big, x in ((cache.k, small.k), (cache.v, small.v), (cache.k_scale, small.k_scale),
+                       (cache.v_scale, small.v_scale)):
+            big[to] = x[src]
+        c.table = np.vectorize(lambda b: place.get(int(b), -1))(c.table)
+        out, lse = cache.attend(c.q, *c.tensors(), max_new=new)
+        torch.cuda.synchronize()
+        c.compare(out, lse, want)
+        del cache
+
+
+def test_streams_and_graphs():
+    rng = np.random.default_rng(35)
+    for requests, new in (([(3000, 1), (50, 1), (700, 1)], 1), ([(3000, 60), (50, 1)], 60), ([(300, 1)], 1)):
+        c = Case(rng, requests, D=64)
+        cache, t = c.cache(), c.tensors()
+        print(f"[gpu] attend on a stream, in a graph {requests}", flush=True)
+        want = cache.attend(c.q, *t, max_new=new)
+        torch.cuda.synchronize()
+        s = torch.cuda.Stream()
+        out, lse = cache.attend(c.q, *t, max_new=new, stream=s)      # beside the current stream's workspace
+        raw, _ = cache.attend(c.q, *t, max_new=new, stream=s.cuda_stream)
+        s.synchronize()
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1]) and torch.equal(raw, want[0])
+        assert len(cache._ws.by_stream) == 2
+        g = torch.cuda.CUDAGraph()
+        out, lse = torch.empty_like(want[0]), torch.empty_like(want[1])
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            cache.attend(c.q, *t, max_new=new, out=out, lse=lse)
+        torch.cuda.current_stream().wait_stream(side)
+        torch.cuda.synchronize()
+        with torch.cuda.graph(g):
+            cache.attend(c.q, *t, max_new=new, out=out, lse=lse)
+        for _ in range(3):
+            out.fill_(float("nan"))
+            lse.fill_(float("nan"))
+            torch.cuda.synchronize()
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+
+
+def test_a_step_through_all_operators():
+    """Blocks, slots, store and attention of two steps (prompts, then a token each) against dense attention over
+    the keys and values themselves: the cache's 4-bit significands are all that separates them."""
+    from paper_2606_30391_amd import festina as F
+    rng = np.random.default_rng(36)
+    R, H, G, D, bt, MB = 5, 2, 4, 64, 32, 8
+    prompts = np.array([33, 1, 200, 64, 90])
+    i32 = lambda x: torch.from_numpy(np.ascontiguousarray(x, np.int32)).cuda()
+    blocks = F.DeviceBlocks(i32(np.zeros(R)), i32(prompts), i32(np.full((R, MB), -1)), i32(rng.permutation(40)),
+                            i32([40]), bt, int(prompts.sum()))
+    cache = F.DeviceCache.empty(40, bt, H, D)
+    kept = [(np.zeros((0, H, D)), np.zeros((0, H, D))) for _ in range(R)]
+    for add in (prompts, np.ones(R, int), np.ones(R, int)):
+        print(f"[gpu] a step of {int(add.sum())} tokens", flush=True)
+        blocks.add.copy_(i32(add))
+        blocks.extend()
+        T = int(add.sum())
+        k, v, q = (torch.from_numpy(rng.normal(0, 1, (T, n, D))).to(torch.bfloat16).cuda() for n in (H, H, H * G))
+        slot = blocks.slot[:T].contiguous()
+        cache.store(k, v, slot)
+        out, lse = cache.attend(q, blocks.table, blocks.length, blocks.first, max_new=int(add.max()))
+        torch.cuda.synchronize()
+        assert int(blocks.first[-1]) == T and bool((blocks.served == 1).all())
+        at = 0
+        for r in range(R):
+            n = int(add[r])
+            kept[r] = tuple(np.concatenate([old, x[at:at + n].double().cpu().numpy()]) for old, x in zip(kept[r], (k, v)))
+            K_, V_ = kept[r]
+            for i in range(n):
+                seen = len(K_) - n + i + 1
+                for h in range(H * G):
+                    x = K_[:seen, h // G] @ q[at + i, h].double().cpu().numpy() / 8.0
+                    w = np.exp(x - x.max())
+                    w /= w.sum()
+                    o = w @ V_[:seen, h // G]
+                    # codes are within 2^-4 of their elements: logits within 2^-4 sum |q k| / 8, values within 2^-4
+                    dx = 2.0 ** -4 * (np.abs(K_[:seen, h // G]) @ np.abs(q[at + i, h].double().cpu().numpy())).max() / 8.0
+                    assert np.all(np.abs(out[at + i, h].double().cpu().numpy() - o) <=
+                                  (np.exp(2 * dx) - 1 + 2.0 ** -4 * np.exp(2 * dx) + 0.01) * (w @ np.abs(V_[:seen, h // G])) + 0.01)
+            at += n
+        blocks.advance()
+
+
+def test_binding_checks_its_tensors():
+    rng = np.random.default_rng(37)
+    c = Case(rng, [(20, 2), (30, 1)], D=64)
+    cache, (table, length, first) = c.cache(), c.tensors()
+    ok = dict(q=c.q, table=table, length=length, first=first, max_new=2)
+    cache.attend(**ok)
+    for key, bad in [("q", c.q.float()), ("q", c.q[:, :, :32]), ("q", c.q.cpu()), ("table", table.long()),
+                     ("table", table[0]), ("length", length[:1]), ("first", first[:-1]), ("out", c.q.float()),
+                     ("lse", torch.zeros(3, device="cuda"))]:
+        with pytest.raises(ValueError):
+            cache.attend(**{**ok, key: bad})
+    from paper_2606_30391_amd import festina as F
+    for key, bad in [("max_new", 0), ("window", -1)]:
+        with pytest.raises(F.FestinaError):
+            cache.attend(**{**ok, key: bad})
+    with pytest.raises(F.FestinaError):
+        cache.attend(**{**ok, "q": c.q[:, :7]})               # no multiple of the key heads
