@@ -18,8 +18,9 @@
 //
 // k_rows    up to 64 query rows a request and key head (single tokens, short runs): 16 NT rows against 64 keys
 //   per wave and step, operands loaded from the cache into the lanes that use them.  Bound by the cache's bytes.
-//   All requests' keys form one line of 64-key units, cut into equal pieces, one a workgroup, so that
-//   ragged lengths leave no workgroup behind; a request that a cut falls into is joined by k_rows_join.
+//   All requests' keys form one line of 64-key units, cut into equal pieces, one a wave, so that
+//   ragged lengths leave no wave behind; a row tile that a cut falls into is joined by k_rows_join.
+// k_rows_whole   the same for short tables: a workgroup a row tile, joined in LDS, one launch.
 // k_tiles   prompts: 128 query rows a workgroup, tiles of 64 keys converted once into LDS (two buffers, the next
 //   tile's loads in flight meanwhile) and read by four waves of 32 rows.  Bound by the matrix cores and the exponentials.
 //   Few tiles over a long cache are split over the keys and joined by k_tiles_join.
@@ -51,7 +52,8 @@ typedef unsigned u2 __attribute__((ext_vector_type(2)));
 constexpr int kUnit = 64;            // keys of a step
 constexpr int kWaves = 4;
 constexpr int kBlock = 64 * kWaves;
-constexpr int kWorkers = 512;        // pieces that k_rows cuts the keys into: two workgroups a compute unit
+constexpr int kWorkers = 2048;       // pieces that k_rows cuts the keys into: two waves a SIMD
+constexpr int kGroups = 512;         // workgroups of k_tiles that fill the chip: two a compute unit
 constexpr int kListed = 512;         // requests whose running sums a workgroup forms by itself
 constexpr int kTileRows = 128;
 constexpr int kMaxRequests = 1 << 20;
@@ -77,6 +79,16 @@ struct AttArgs {
   const float *ks, *vs;
   const long long *plan;             // [2][R + 1] running sums of units and of tiles, or NULL
   float *part_o, *part_ml;           // pieces: unnormalised rows; (m, l)
+  struct Cut *cuts;                  // [workers]
+};
+
+// What k_rows_join needs of the row tile that begins a join at a piece's start; n = 0: none.
+struct Cut {
+  int32_t n;                         // pieces
+  int32_t second;                    // the first of them is its piece's second part
+  int32_t row0, rows;                // first row of the tile, rows of the request
+  int32_t first, head;               // the request's first token, the key head's first query head
+  int32_t unused[2];
 };
 
 struct Request {
@@ -100,6 +112,12 @@ __device__ __forceinline__ int first_unit(const AttArgs &a, const Request &q) {
 }
 __device__ __forceinline__ int units(const AttArgs &a, const Request &q) {
   return max(cdiv(q.length, kUnit) - first_unit(a, q), 1);
+}
+
+// A value that is the same in all lanes, kept once.
+__device__ __forceinline__ long long same(long long x) {
+  const unsigned lo = __builtin_amdgcn_readfirstlane((int)x), hi = __builtin_amdgcn_readfirstlane((int)(x >> 32));
+  return (long long)((unsigned long long)hi << 32 | lo);
 }
 
 template <int ROWS>
@@ -138,27 +156,41 @@ __device__ __forceinline__ long long scan(long long x, long long *lds, long long
   return s - x + before;
 }
 
-// list[0 .. R]: running sums of f(r) over the requests, R <= kListed.
+// list[0 .. R]: running sums of f(r) over the requests, R <= kListed; every wave of a workgroup forms and writes
+// all of them, so no wave waits for another.
 template <typename F>
-__device__ __forceinline__ void list_sums(const AttArgs &a, F f, long long *list, long long *lds) {
-  const int r = threadIdx.x * 2;
-  const long long x = r < a.R ? f(r) : 0, y = r + 1 < a.R ? f(r + 1) : 0;
-  long long whole;
-  const long long before = scan<kBlock>(x + y, lds, &whole);
-  if (r <= a.R) list[r] = before;
-  if (r + 1 <= a.R) list[r + 1] = before + x;
-  if (threadIdx.x == 0) list[a.R] = whole;
-  __syncthreads();
+__device__ __forceinline__ void list_sums(const AttArgs &a, F f, long long *list) {
+  const int lane = threadIdx.x & 63;
+  long long sum = 0;
+  for (int r0 = 0; r0 < a.R; r0 += 64) {
+    const int r = r0 + lane;
+    long long x = r < a.R ? f(r) : 0;
+    const long long own = x;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const long long y = __shfl_up(x, d);
+      if (lane >= d) x += y;
+    }
+    if (r < a.R) list[r] = sum + x - own;
+    sum += __shfl(x, 63);
+  }
+  if (lane == 0) list[a.R] = sum;
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
-// The r with list[r] <= u < list[r + 1].
+// The r with list[r] <= u < list[r + 1]: a wave compares 64 entries a time.
 __device__ __forceinline__ int find(const long long *list, int R, long long u) {
-  int lo = 0, hi = R;
-  while (hi - lo > 1) {
-    const int m = (lo + hi) >> 1;
-    if (list[m] <= u) lo = m; else hi = m;
+  const int lane = threadIdx.x & 63;
+  int lo = 0, n = R;
+  while (n > 1) {
+    const int s = (n + 63) >> 6, i = lo + lane * s;
+    const unsigned long long at = __ballot(lane * s < n && list[i < lo + n ? i : lo] <= u);
+    const int k = (__builtin_popcountll(at) - 1) * s;
+    lo += k;
+    n = min(s, n - k);
   }
-  return lo;
+  return __builtin_amdgcn_readfirstlane(lo);
 }
 
 template <int ROWS>
@@ -209,6 +241,32 @@ __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(
 __device__ __forceinline__ float log2_(float x) { return __builtin_amdgcn_logf(x); }
 __device__ __forceinline__ float kNegInf() { return -__builtin_inff(); }
 
+// Over the lanes that differ by 16 and 32, or by 32 alone.
+template <typename F>
+__device__ __forceinline__ float across32(float x, F f) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+template <typename F>
+__device__ __forceinline__ float across16(float x, F f) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float max_(float x, float y) { return fmaxf(x, y); }
+__device__ __forceinline__ float add_(float x, float y) { return x + y; }
+
+// The keys a row sees: `count` from `from` on.
+struct Span {
+  int from, count;
+  __device__ __forceinline__ bool has(int key) const { return (unsigned)(key - from) < (unsigned)count; }
+};
+__device__ __forceinline__ Span span(const AttArgs &a, int pos) {
+  const int from = a.window > 0 ? max(pos - a.window + 1, 0) : 0;
+  return Span{from, max(pos - from + 1, 0)};
+}
+// Keeps a rare branch a branch: without it the compiler computes the masks of every step.
+__device__ __forceinline__ void rarely() { asm volatile(""); }
+
 // Which bytes of a word of four codes are NaN, as 0xff each.
 __device__ __forceinline__ unsigned nan_bytes(unsigned c) {
   const unsigned h = ((c & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
@@ -248,8 +306,6 @@ struct RowsStep {
 template <typename T, int D, int NT>
 struct Rows {
   static constexpr int kRows = 16 * NT, kSteps = D / 32, kPitch = D + 4;
-  // One step in flight beside the one at work where registers allow
-  static constexpr bool kAhead = D <= 128 && NT == 1;
 
   struct Shared {
     float o[kWaves][16][kPitch];
@@ -284,7 +340,7 @@ struct Rows {
     typename Vec8<T>::type q[NT][kSteps];
     f4 o[NT][D / 16];
     float m[NT], l[NT];
-    int pos[NT];
+    Span sees[NT];
   };
 
   static __device__ __forceinline__ void step(const AttArgs &a, const Request &rq, int base, int pos_min, int pos_max,
@@ -315,22 +371,19 @@ struct Rows {
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[nt][u][i] = fmaf(x[nt][u][i], c, lv);
       if (masked) {
+        rarely();
+        const Span sees{st.sees[nt].from - base - 16 * g, s.ok ? st.sees[nt].count : 0};
 #pragma unroll
         for (int u = 0; u < 4; ++u)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int key = base + 16 * g + 4 * u + i;
-            const bool sees = s.ok && key <= st.pos[nt] && (a.window <= 0 || key > st.pos[nt] - a.window);
-            x[nt][u][i] = sees ? x[nt][u][i] : kNegInf();
-          }
+          for (int i = 0; i < 4; ++i) x[nt][u][i] = sees.has(4 * u + i) ? x[nt][u][i] : kNegInf();
       }
       float top = x[nt][0][0];
 #pragma unroll
       for (int u = 0; u < 4; ++u)
 #pragma unroll
         for (int i = 0; i < 4; ++i) top = fmaxf(top, x[nt][u][i]);
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
+      top = across32(across16(top, max_), max_);
       const float was = st.m[nt];
       if (__any(top > was)) {
         const float now = fmaxf(was, top), f = weight(was, now);
@@ -351,47 +404,46 @@ struct Rows {
         }
       st.l[nt] = fmaf(sum, iv, st.l[nt]);
     }
-    bool nans = false;
     if (masked) {
+      rarely();
       // what lies behind the last token may be anything: no product with it
       const int n = s.ok ? min(max(rq.length - (base + 16 * g), 0), 16) : 0;
-#pragma unroll
-      for (int t = 0; t < D / 16; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s.v[t][i] &= below(n, i);
       unsigned any = 0;
 #pragma unroll
       for (int t = 0; t < D / 16; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) any |= nan_bytes(s.v[t][i]);
-      nans = __any(any != 0);
-    }
-    if (nans) {
-      // a NaN that some rows see and others do not: it is left out of the product and put into the rows that see it
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        h8 sees[2];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int key = base + 16 * g + i;
-          const bool y = s.ok && key <= st.pos[nt] && (a.window <= 0 || key > st.pos[nt] - a.window);
-          sees[i >> 3][i & 7] = y ? (f16)1.f : (f16)0.f;
+        for (int i = 0; i < 4; ++i) {
+          s.v[t][i] &= below(n, i);
+          any |= nan_bytes(s.v[t][i]);
         }
+      if (__any(any != 0)) {
+        rarely();
+        // a NaN that some rows see and others do not is put into the rows that see it and left out of the product
 #pragma unroll
         for (int t = 0; t < D / 16; ++t) {
-          f4 hits = f4{0.f, 0.f, 0.f, 0.f};
+          unsigned nan[4];
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const unsigned n0 = nan_bytes(s.v[t][2 * i]), n1 = nan_bytes(s.v[t][2 * i + 1]);
-            hits = mfma16(decode8<f16>(n0 & kOnes, n1 & kOnes), sees[i], hits);
-            st.o[nt][t] = mfma16(decode8<f16>(s.v[t][2 * i] & ~n0, s.v[t][2 * i + 1] & ~n1), w[nt][i], st.o[nt][t]);
+          for (int i = 0; i < 4; ++i) {
+            nan[i] = nan_bytes(s.v[t][i]);
+            s.v[t][i] &= ~nan[i];
           }
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (hits[i] > 0.f) st.o[nt][t][i] = __builtin_nanf("");
+          for (int nt = 0; nt < NT; ++nt) {
+            f4 hits = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              h8 sees;
+#pragma unroll
+              for (int j = 0; j < 8; ++j)
+                sees[j] = s.ok && st.sees[nt].has(base + 16 * g + 8 * i + j) ? (f16)1.f : (f16)0.f;
+              hits = mfma16(decode8<f16>(nan[2 * i] & kOnes, nan[2 * i + 1] & kOnes), sees, hits);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) st.o[nt][t][i] = hits[i] > 0.f ? __builtin_nanf("") : st.o[nt][t][i];
+          }
+          __builtin_amdgcn_sched_barrier(0);           // one tile's operands at a time
         }
       }
-      return;
     }
 #pragma unroll
     for (int t = 0; t < D / 16; ++t)
@@ -403,19 +455,17 @@ struct Rows {
       }
   }
 
-  // Rows `tile` of request r and key head h over its units k0 .. k1 - 1; `part` < 0: all of them, else the place
-  // where the piece's result goes.
-  static __device__ __forceinline__ void piece(const AttArgs &a, int r, const Request &rq, int h, int tile, int k0, int k1,
-                                               int part, Shared &sh) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
+  // Rows `tile` of request r and key head h: every `stride`th of its units from k0 to k1.
+  static __device__ __forceinline__ void scan_keys(const AttArgs &a, int r, const Request &rq, int h, int tile, int k0,
+                                                   int k1, int stride, State &st) {
+    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
     const int rows = rq.n * a.G, row0 = tile * kRows, before = rq.length - rq.n;
     const int pos_min = before + row0 / a.G, pos_max = before + (min(row0 + kRows, rows) - 1) / a.G;
-    State st;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const int i = row0 + nt * 16 + c, t = i / a.G;
       const bool in = i < rows;
-      st.pos[nt] = in ? before + t : -1;
+      st.sees[nt] = span(a, in ? before + t : -1);
       st.m[nt] = kNegInf();
       st.l[nt] = 0.f;
 #pragma unroll
@@ -432,36 +482,53 @@ struct Rows {
     }
     const int32_t *table = a.table + (size_t)r * a.MB;
     const int u0 = first_unit(a, rq);
-    int u = k0 + wave;
-    if constexpr (kAhead) {
-      RowsStep<D> s, next;
-      if (u < k1) load(a, table, h, (u0 + u) * kUnit, s);
-      while (u < k1) {
-        const int n = u + kWaves;
-        if (n < k1) load(a, table, h, (u0 + n) * kUnit, next);
-        step(a, rq, (u0 + u) * kUnit, pos_min, pos_max, s, st);
-        s = next;
-        u = n;
-      }
-    } else {
-      for (; u < k1; u += kWaves) {
-        RowsStep<D> s;
-        load(a, table, h, (u0 + u) * kUnit, s);
-        step(a, rq, (u0 + u) * kUnit, pos_min, pos_max, s, st);
-      }
+    for (int u = k0; u < k1; u += stride) {
+      RowsStep<D> s;
+      load(a, table, h, (u0 + u) * kUnit, s);
+      step(a, rq, (u0 + u) * kUnit, pos_min, pos_max, s, st);
     }
-    // the four waves' parts of each row
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) st.l[nt] = across32(across16(st.l[nt], add_), add_);
+  }
+
+  // One wave's keys alone: the rows themselves (part < 0), or the piece's result at its place.
+  static __device__ __forceinline__ void piece(const AttArgs &a, int r, const Request &rq, int h, int tile, int k0, int k1,
+                                               int part) {
+    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+    State st;
+    scan_keys(a, r, rq, h, tile, k0, k1, 1, st);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      st.l[nt] += __shfl_xor(st.l[nt], 16);
-      st.l[nt] += __shfl_xor(st.l[nt], 32);
+      const int i = tile * kRows + nt * 16 + c;
+      if (i >= rq.n * a.G) continue;
+      if (part < 0) {
+        const int t = i / a.G;
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) finish(a, rq.first + t, h * a.G + i - t * a.G, d * 16 + g * 4, st.m[nt], st.l[nt], st.o[nt][d]);
+      } else {
+        const size_t p = (size_t)part * kRows + nt * 16 + c;
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) *reinterpret_cast<f4 *>(a.part_o + p * D + d * 16 + g * 4) = st.o[nt][d];
+        if (g == 0) {
+          a.part_ml[p * 2] = st.m[nt];
+          a.part_ml[p * 2 + 1] = st.l[nt];
+        }
+      }
+    }
+  }
+
+  // A workgroup's keys: its waves' parts of each row joined in LDS.
+  static __device__ __forceinline__ void whole(const AttArgs &a, int r, const Request &rq, int h, int tile, Shared &sh) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
+    const int rows = rq.n * a.G, row0 = tile * kRows;
+    State st;
+    scan_keys(a, r, rq, h, tile, wave, units(a, rq), kWaves, st);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
       if (g == 0) {
         sh.m[wave][nt * 16 + c] = st.m[nt];
         sh.l[wave][nt * 16 + c] = st.l[nt];
       }
-    }
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
       for (int t = 0; t < D / 16; ++t) *reinterpret_cast<f4 *>(&sh.o[wave][c][t * 16 + g * 4]) = st.o[nt][t];
       __syncthreads();
@@ -478,17 +545,8 @@ struct Rows {
           L = fmaf(sh.l[w][nt * 16 + y], f, L);
           O += *reinterpret_cast<const f4 *>(&sh.o[w][y][d]) * f;
         }
-        if (part < 0) {
-          const int t = i / a.G, head = h * a.G + i - t * a.G;
-          finish(a, rq.first + t, head, d, M, L, O);
-        } else {
-          const size_t p = (size_t)part * kRows + nt * 16 + y;
-          *reinterpret_cast<f4 *>(a.part_o + p * D + d) = O;
-          if (d == 0) {
-            a.part_ml[p * 2] = M;
-            a.part_ml[p * 2 + 1] = L;
-          }
-        }
+        const int t = i / a.G;
+        finish(a, rq.first + t, h * a.G + i - t * a.G, d, M, L, O);
       }
       __syncthreads();
     }
@@ -505,48 +563,65 @@ struct Rows {
   }
 };
 
-// Pieces of equal length, at least a step for each wave.
+// Pieces of equal length; more rows take longer pieces, since a piece's result is read and written once more.
+template <int NT>
 __device__ __forceinline__ int pieces(const AttArgs &a, long long all) {
-  return (int)min((long long)a.workers, max((all + kWaves - 1) / kWaves, 1ll));
+  return (int)min((long long)a.workers, max((all + NT - 1) / NT, 1ll));
 }
 __device__ __forceinline__ long long piece_start(long long all, int w, int n) { return all * w / n; }
 
-template <typename T, int D, int NT, bool CUT>
-__global__ void __launch_bounds__(kBlock, (D <= 128 && NT <= 2) ? 2 : 1) k_rows(AttArgs a) {
+// A workgroup for each row tile and key head, its waves over the keys in turn: few keys, one launch.
+template <typename T, int D, int NT>
+__global__ void __launch_bounds__(kBlock, (D <= 128 && NT <= 2) ? 2 : 1) k_rows_whole(AttArgs a) {
   typedef Rows<T, D, NT> K;
   __shared__ typename K::Shared sh;
-  if constexpr (!CUT) {
-    // a workgroup for each row tile and key head
-    const int tile = blockIdx.x % a.tiles_each, rest = blockIdx.x / a.tiles_each, h = rest % a.H, r = rest / a.H;
-    const Request rq = request(a, r);
-    const int rows = rq.n * a.G;
-    if (rows > a.rows_max || tile * K::kRows >= rows) return;
-    K::piece(a, r, rq, h, tile, 0, units(a, rq), -1, sh);
-    return;
-  }
-  __shared__ long long list_[kListed + 2], lds[kWaves];
-  const long long *list = a.plan;
-  if (!list) {
-    list_sums(a, [&](int r) { return units_of<K::kRows>(a, r); }, list_, lds);
-    list = list_;
-  }
-  const long long all = list[a.R];
-  const int n = pieces(a, all), w = blockIdx.x;
-  if (w >= n) return;
-  long long u = piece_start(all, w, n);
-  const long long end = piece_start(all, w + 1, n);
-  for (int place = 2 * w; u < end; ++place) {
-    const int r = find(list, a.R, u);
-    const Request rq = request(a, r);
-    const int each = units(a, rq), at = (int)((u - list[r]) / each), tiles = cdiv(rq.n * a.G, K::kRows);
-    const int k0 = (int)(u - list[r] - (long long)at * each), k1 = (int)min((long long)each, k0 + (end - u));
-    const bool whole = k0 == 0 && k1 == each;
-    K::piece(a, r, rq, at / tiles, at % tiles, k0, k1, whole ? -1 : min(place, 2 * w + 1), sh);
-    u += k1 - k0;
-  }
+  const int tile = blockIdx.x % a.tiles_each, rest = blockIdx.x / a.tiles_each, h = rest % a.H, r = rest / a.H;
+  const Request rq = request(a, r);
+  const int rows = rq.n * a.G;
+  if (rows > a.rows_max || tile * K::kRows >= rows) return;
+  K::whole(a, r, rq, h, tile, sh);
 }
 
-// Joins one row's pieces `first_part`, then `next_part`, next_part + stride, ... : a wave, lanes over the row.
+// A wave a piece.
+template <typename T, int D, int NT>
+__global__ void __launch_bounds__(64, (D <= 128 && NT <= 2) ? 2 : 1) k_rows(AttArgs a) {
+  typedef Rows<T, D, NT> K;
+  __shared__ long long list_[kListed + 1];
+  const long long *list = a.plan;
+  if (!list) {
+    list_sums(a, [&](int r) { return units_of<K::kRows>(a, r); }, list_);
+    list = list_;
+  }
+  const long long all = same(list[a.R]);
+  const int n = pieces<NT>(a, all), w = blockIdx.x;
+  Cut cut{};
+  if (w < n) {
+    long long u = piece_start(all, w, n);
+    const long long start = u, end = piece_start(all, w + 1, n);
+    for (int place = 2 * w; u < end; ++place) {
+      const int r = find(list, a.R, u);
+      const Request rq = request(a, r);
+      const long long begin = same(list[r]);
+      const int each = units(a, rq), at = (int)((u - begin) / each), tiles = cdiv(rq.n * a.G, K::kRows);
+      const long long tile0 = begin + (long long)at * each;
+      const int k0 = (int)(u - tile0), k1 = (int)min((long long)each, k0 + (end - u));
+      const int h = at / tiles, tile = at % tiles;
+      if (u == start && k0 > 0) {
+        // this piece's start cuts the tile: the first such cut is where the tile's pieces are joined
+        const long long prior = piece_start(all, w - 1, n);
+        if (prior <= tile0) {
+          const int last = (int)(((tile0 + each) * n - 1) / all);      // piece of the tile's last unit
+          cut = Cut{last - w + 2, prior < tile0 ? 1 : 0, tile * K::kRows, rq.n * a.G, rq.first, h * a.G, {0, 0}};
+        }
+      }
+      K::piece(a, r, rq, h, tile, k0, k1, k0 == 0 && k1 == each ? -1 : min(place, 2 * w + 1));
+      u += k1 - k0;
+    }
+  }
+  if (threadIdx.x == 0) a.cuts[w] = cut;
+}
+
+// Joins one row's n pieces, the first at p0 and the others from p1 on: a wave, lanes over the row.
 template <typename T, int D>
 __device__ __forceinline__ void join_row(const AttArgs &a, size_t p0, size_t p1, size_t stride, int n, int t, int head) {
   const int lane = threadIdx.x & 63;
@@ -560,41 +635,24 @@ __device__ __forceinline__ void join_row(const AttArgs &a, size_t p0, size_t p1,
   for (int d = 32; d > 0; d >>= 1) L += __shfl_xor(L, d);
   if (lane * 4 < D) {
     f4 O = f4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
+#pragma unroll 8
     for (int i = 0; i < n; ++i)
       O += *reinterpret_cast<const f4 *>(a.part_o + at(i) * D + lane * 4) * weight(a.part_ml[at(i) * 2], M);
     Rows<T, D, 1>::finish(a, t, head, lane * 4, M, L, O);
   }
 }
 
-// Workgroup (w - 1, y) joins rows 4 y .. 4 y + 3 of the row tile that the cut between pieces w - 1 and w falls into,
-// if it is the tile's first cut.
+// A wave joins a row of the tile that the cut at piece blockIdx.x + 1 leaves to it.
 template <typename T, int D, int NT>
 __global__ void __launch_bounds__(kBlock) k_rows_join(AttArgs a) {
   constexpr int kRows = 16 * NT;
-  __shared__ long long list_[kListed + 2], lds[kWaves];
-  const long long *list = a.plan;
-  if (!list) {
-    list_sums(a, [&](int r) { return units_of<kRows>(a, r); }, list_, lds);
-    list = list_;
-  }
-  const long long all = list[a.R];
-  const int n = pieces(a, all), w = blockIdx.x + 1;
-  if (w >= n) return;
-  const long long u = piece_start(all, w, n);
-  const int r = find(list, a.R, u);
-  const Request rq = request(a, r);
-  const int each = units(a, rq), at = (int)((u - list[r]) / each), tiles = cdiv(rq.n * a.G, kRows);
-  const long long begin = list[r] + (long long)at * each, end = begin + each;
-  const long long prior = piece_start(all, w - 1, n);
-  if (begin == u || prior > begin) return;
-  const int row = blockIdx.y * kWaves + (threadIdx.x >> 6), i = (at % tiles) * kRows + row;
-  if (i >= rq.n * a.G) return;
-  const int last = (int)((end * n - 1) / all);                        // piece of the tile's last unit
-  const int t = i / a.G, head = (at / tiles) * a.G + i - t * a.G;
-  // a piece that begins in the tile or at its start holds it as its first part, one that began before as its second
-  const size_t p0 = (size_t)(2 * (w - 1) + (prior < begin ? 1 : 0)) * kRows + row, p1 = (size_t)(2 * w) * kRows + row;
-  join_row<T, D>(a, p0, p1, 2 * kRows, last - w + 2, rq.first + t, head);
+  const int w = blockIdx.x + 1;
+  const Cut cut = a.cuts[w];
+  const int row = blockIdx.y * kWaves + (threadIdx.x >> 6), i = cut.row0 + row;
+  if (cut.n == 0 || i >= cut.rows) return;
+  const int t = i / a.G;
+  join_row<T, D>(a, (size_t)(2 * (w - 1) + cut.second) * kRows + row, (size_t)(2 * w) * kRows + row, 2 * kRows, cut.n,
+                 cut.first + t, cut.head + i - t * a.G);
 }
 
 // ------------------------------------------------------------------ k_tiles
@@ -608,7 +666,8 @@ struct Tiles {
     T k[kUnit][kPitchK];
     f16 v[D][kPitchV];
     float c[4], lv[4], iv[4];
-    int nans[kWaves];
+    int nans[kWaves];                // a wave's values hold a NaN that not every row sees
+    __attribute__((aligned(8))) uint16_t nan[D][4];   // which: a bit a key
   };
 
   struct Raw {
@@ -657,7 +716,34 @@ struct Tiles {
   }
 
   // `look`: some row of the workgroup does not see all of the tile.
-  static __device__ __forceinline__ void store(const AttArgs &a, const Raw &raw, bool look, Buffer &b) {
+  static __device__ __forceinline__ void store(const AttArgs &a, Raw &raw, bool look, Buffer &b) {
+    bool nans = false;
+    if (look) {
+      rarely();
+      unsigned any = 0;
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) any |= nan_bytes(raw.v[i][j]);
+      nans = __any(any != 0);
+      if (__syncthreads_or(nans)) {
+        // a NaN that some rows see and others do not is left out of the product; step() puts it into the rows
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+          const int e = threadIdx.x + i * kBlock;
+          if (kItems % kBlock != 0 && e >= kItems) continue;
+          unsigned bits = 0;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const unsigned n = nan_bytes(raw.v[i][j]);
+            raw.v[i][j] &= ~n;
+            bits |= ((n & 0x01010101u) * 0x01020408u >> 24) << (4 * j);
+          }
+          b.nan[e >> 2][e & 3] = (uint16_t)bits;
+        }
+      }
+    }
+    if ((threadIdx.x & 63) == 0) b.nans[threadIdx.x >> 6] = nans;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int e = threadIdx.x + i * kBlock;
@@ -676,22 +762,13 @@ struct Tiles {
       b.lv[threadIdx.x] = raw.ok ? log2_(vs) : kNegInf();
       b.iv[threadIdx.x] = raw.ok ? 1.f / vs : 0.f;
     }
-    unsigned any = 0;
-    if (look) {
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) any |= nan_bytes(raw.v[i][j]);
-    }
-    const bool nans = __any(any != 0);
-    if ((threadIdx.x & 63) == 0) b.nans[threadIdx.x >> 6] = nans;
   }
 
   struct State {
     typename Vec8<T>::type q[D / 16];
     f16v o[D / 32];
     float m, l;
-    int pos;
+    Span sees;
   };
 
   static __device__ __forceinline__ void step(const AttArgs &a, int base, int pos_min, int pos_max, const Buffer &b,
@@ -714,21 +791,19 @@ struct Tiles {
     }
     const bool masked = base + kUnit - 1 > pos_min || (a.window > 0 && base <= pos_max - a.window);
     if (masked) {
+      rarely();
+      const Span sees{st.sees.from - base - h * 16, st.sees.count};
 #pragma unroll
       for (int g = 0; g < 2; ++g)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int key = base + g * 32 + h * 16 + i;
-          const bool sees = key <= st.pos && (a.window <= 0 || key > st.pos - a.window);
-          x[g][i] = sees ? x[g][i] : kNegInf();
-        }
+        for (int i = 0; i < 16; ++i) x[g][i] = sees.has(g * 32 + i) ? x[g][i] : kNegInf();
     }
     float top = x[0][0];
 #pragma unroll
     for (int g = 0; g < 2; ++g)
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, x[g][i]);
-    top = fmaxf(top, __shfl_xor(top, 32));
+    top = across32(top, max_);
     if (__any(top > st.m)) {
       const float now = fmaxf(st.m, top), f = weight(st.m, now);
       st.m = now;
@@ -749,44 +824,27 @@ struct Tiles {
       }
       st.l = fmaf(sum, b.iv[g * 2 + h], st.l);
     }
-    const bool nans = masked && (b.nans[0] | b.nans[1] | b.nans[2] | b.nans[3]);
-    if (!nans) {
+    if (masked && (b.nans[0] | b.nans[1] | b.nans[2] | b.nans[3])) {
+      rarely();
+      unsigned long long seen = 0;
+#pragma unroll 1
+      for (int key = 0; key < kUnit; ++key) seen |= (unsigned long long)st.sees.has(base + key) << key;
 #pragma unroll
       for (int t = 0; t < D / 32; ++t)
 #pragma unroll
-        for (int g = 0; g < 2; ++g)
-#pragma unroll
-          for (int s = 0; s < 2; ++s)
-            st.o[t] = mfma32(*reinterpret_cast<const h8 *>(&b.v[t * 32 + c][g * 32 + h * 16 + s * 8]), w[g][s], st.o[t]);
-      return;
+        for (int i = 0; i < 16; ++i) {
+          const int d = t * 32 + (i >> 2) * 8 + h * 4 + (i & 3);
+          const unsigned long long nan = *reinterpret_cast<const unsigned long long *>(b.nan[d]);
+          st.o[t][i] = nan & seen ? __builtin_nanf("") : st.o[t][i];
+        }
     }
-    // a NaN that some rows see and others do not: it is left out of the product and put into the rows that see it
 #pragma unroll
-    for (int t = 0; t < D / 32; ++t) {
-      f16v hits;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) hits[i] = 0.f;
+    for (int t = 0; t < D / 32; ++t)
 #pragma unroll
       for (int g = 0; g < 2; ++g)
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          h8 vf = *reinterpret_cast<const h8 *>(&b.v[t * 32 + c][g * 32 + h * 16 + s * 8]), isnan, sees;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const bool n = vf[i] != vf[i];
-            const int key = base + g * 32 + h * 16 + s * 8 + i;
-            const bool y = key <= st.pos && (a.window <= 0 || key > st.pos - a.window);
-            isnan[i] = n ? (f16)1.f : (f16)0.f;
-            sees[i] = y ? (f16)1.f : (f16)0.f;
-            vf[i] = n ? (f16)0.f : vf[i];
-          }
-          hits = mfma32(isnan, sees, hits);
-          st.o[t] = mfma32(vf, w[g][s], st.o[t]);
-        }
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (hits[i] > 0.f) st.o[t][i] = __builtin_nanf("");
-    }
+        for (int s = 0; s < 2; ++s)
+          st.o[t] = mfma32(*reinterpret_cast<const h8 *>(&b.v[t * 32 + c][g * 32 + h * 16 + s * 8]), w[g][s], st.o[t]);
   }
 };
 
@@ -794,10 +852,10 @@ template <typename T, int D>
 __global__ void __launch_bounds__(kBlock, D <= 128 ? 2 : 1) k_tiles(AttArgs a) {
   typedef Tiles<T, D> K;
   __shared__ typename K::Buffer buf[2];
-  __shared__ long long list_[kListed + 2], lds[kWaves];
+  __shared__ long long list_[kListed + 1];
   const long long *list = a.plan ? a.plan + a.R + 1 : nullptr;
   if (!list) {
-    list_sums(a, [&](int r) { return tiles_of(a, r); }, list_, lds);
+    list_sums(a, [&](int r) { return tiles_of(a, r); }, list_);
     list = list_;
   }
   // neighbouring workgroups take different key heads, so that (for 8 heads) the workgroups of one XCD share one
@@ -821,7 +879,7 @@ __global__ void __launch_bounds__(kBlock, D <= 128 ? 2 : 1) k_tiles(AttArgs a) {
     u += (int)((long long)n * s / a.splits);
   }
   typename K::State st;
-  st.pos = in ? before + t : -1;
+  st.sees = span(a, in ? before + t : -1);
   st.m = kNegInf();
   st.l = 0.f;
 #pragma unroll
@@ -855,7 +913,7 @@ __global__ void __launch_bounds__(kBlock, D <= 128 ? 2 : 1) k_tiles(AttArgs a) {
     __syncthreads();
   }
   if (!in) return;
-  st.l += __shfl_xor(st.l, 32);
+  st.l = across32(st.l, add_);
   if (a.splits > 1) {
     const size_t p = (((size_t)at * a.H + h) * a.splits + blockIdx.y) * kTileRows + wave * 32 + c;
 #pragma unroll
@@ -881,10 +939,10 @@ __global__ void __launch_bounds__(kBlock, D <= 128 ? 2 : 1) k_tiles(AttArgs a) {
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kBlock) k_tiles_join(AttArgs a) {
-  __shared__ long long list_[kListed + 2], lds[kWaves];
+  __shared__ long long list_[kListed + 1];
   const long long *list = a.plan ? a.plan + a.R + 1 : nullptr;
   if (!list) {
-    list_sums(a, [&](int r) { return tiles_of(a, r); }, list_, lds);
+    list_sums(a, [&](int r) { return tiles_of(a, r); }, list_);
     list = list_;
   }
   const int h = blockIdx.x % a.H;
@@ -907,7 +965,8 @@ struct Shape {
   int tiles_each;
   long long tile_groups;             // bound of the row tiles of all requests
   int splits;
-  size_t plan, part_ml, part_o, bytes;
+  int join_rows;                     // rows of a row tile that may be in use
+  size_t plan, cuts, part_ml, part_o, bytes;
 };
 
 size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
@@ -927,7 +986,8 @@ festina_status shape_of(const festina_kv_cache *c, const festina_attention *t, S
   *s = Shape{};
   s->tiles = most > 64 && t->max_new > 1;
   const long long rows = s->tiles ? G : most;                         // with prompts about: the single tokens' rows
-  s->nt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  s->nt = rows <= 16 ? 1 : rows <= 32 || D > 128 ? 2 : 4;             // four tiles of 256 dims are more than registers hold
+  s->join_rows = (int)min(rows, 16ll * s->nt);
   if (s->tiles && G > 64) s->nt = 0;
   s->rows_max = s->tiles ? 16 * s->nt : INT_MAX;
   const long long keys = (long long)t->max_blocks * c->block_tokens;
@@ -941,7 +1001,7 @@ festina_status shape_of(const festina_kv_cache *c, const festina_attention *t, S
     if (s->tile_groups * H > INT_MAX) return FESTINA_ERR_UNSUPPORTED;
     // at least two workgroups a compute unit, of at least 16 steps each
     const long long groups = max(((long long)t->n_tokens * G + kTileRows - 1) / kTileRows, 1ll) * H;
-    const long long wanted = (kWorkers + groups - 1) / groups;
+    const long long wanted = (kGroups + groups - 1) / groups;
     s->splits = (int)max(min(wanted, keys / (16 * kUnit)), 1ll);
     if (s->splits > 1) {
       const size_t p = (size_t)s->tile_groups * H * s->splits * kTileRows;
@@ -949,7 +1009,8 @@ festina_status shape_of(const festina_kv_cache *c, const festina_attention *t, S
     }
   }
   s->plan = 0;
-  s->part_ml = up((size_t)2 * (t->n_requests + 1) * 8);
+  s->cuts = up((size_t)2 * (t->n_requests + 1) * 8);
+  s->part_ml = s->cuts + up((size_t)kWorkers * sizeof(Cut));
   s->part_o = s->part_ml + up(parts * 8);
   s->bytes = s->part_o + up(parts * D * 4);
   return FESTINA_OK;
@@ -958,11 +1019,11 @@ festina_status shape_of(const festina_kv_cache *c, const festina_attention *t, S
 template <typename T, int D, int NT>
 void run_rows(const AttArgs &a, const Shape &s, hipStream_t st) {
   if (!s.cut) {
-    k_rows<T, D, NT, false><<<(unsigned)(a.R * a.H * s.tiles_each), kBlock, 0, st>>>(a);
+    k_rows_whole<T, D, NT><<<(unsigned)(a.R * a.H * s.tiles_each), kBlock, 0, st>>>(a);
     return;
   }
-  k_rows<T, D, NT, true><<<a.workers, kBlock, 0, st>>>(a);
-  k_rows_join<T, D, NT><<<dim3(a.workers - 1, 16 * NT / kWaves), kBlock, 0, st>>>(a);
+  k_rows<T, D, NT><<<a.workers, 64, 0, st>>>(a);
+  k_rows_join<T, D, NT><<<dim3(a.workers - 1, (s.join_rows + kWaves - 1) / kWaves), kBlock, 0, st>>>(a);
 }
 
 template <typename T, int D>
@@ -975,7 +1036,9 @@ void run(AttArgs a, const Shape &s, long long *plan, hipStream_t st) {
   }
   if (s.nt == 1) run_rows<T, D, 1>(a, s, st);
   else if (s.nt == 2) run_rows<T, D, 2>(a, s, st);
-  else if (s.nt == 4) run_rows<T, D, 4>(a, s, st);
+  else if (s.nt == 4) {
+    if constexpr (D <= 128) run_rows<T, D, 4>(a, s, st);
+  }
   if (s.tiles) {
     k_tiles<T, D><<<dim3((unsigned)(s.tile_groups * a.H), s.splits), kBlock, 0, st>>>(a);
     if (s.splits > 1)
@@ -1044,6 +1107,7 @@ extern "C" festina_status festina_attend(const festina_kv_cache *cache, const fe
   a.v = cache->v;
   a.ks = cache->k_scale;
   a.vs = cache->v_scale;
+  a.cuts = reinterpret_cast<Cut *>(w + s.cuts);
   a.part_ml = reinterpret_cast<float *>(w + s.part_ml);
   a.part_o = reinterpret_cast<float *>(w + s.part_o);
   long long *plan = reinterpret_cast<long long *>(w + s.plan);

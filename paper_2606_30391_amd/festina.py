@@ -629,7 +629,7 @@ def _check(t, name, dtypes, shape=None):
         raise ValueError(f"{name}: a tensor in device memory is needed")
     if t.dtype not in dtypes:
         raise ValueError(f"{name}: dtype {t.dtype}, not {' or '.join(str(d) for d in dtypes)}")
-    if shape is not None and (tuple(t.shape) != tuple(shape) or not t.is_contiguous()):
+    if shape is not None and (t.shape != shape or not t.is_contiguous()):
         raise ValueError(f"{name}: a contiguous tensor of shape {tuple(shape)} is needed, not {tuple(t.shape)}")
 
 
@@ -651,13 +651,14 @@ class _Workspaces:
         self.by_stream = {}
 
     def get(self, n, stream, device):
+        """(address of at least n bytes for calls on `stream`, that stream's handle)."""
         import torch
-        key = _stream_handle(stream).value
-        ws = self.by_stream.get(key)
+        handle = _stream_handle(stream).value or 0
+        ws = self.by_stream.get(handle)
         if ws is None or ws.numel() < n:
             with _on(stream, device):
-                ws = self.by_stream[key] = torch.empty(max(n, 256), dtype=torch.uint8, device=device)
-        return ws
+                ws = self.by_stream[handle] = torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+        return ws.data_ptr(), handle
 
 
 class DeviceBlocks:
@@ -695,14 +696,14 @@ class DeviceBlocks:
                                    _ptr(self.served), _ptr(self.n_free_out))
 
     def extend(self, stream=None):
-        festina_extend_blocks(self.req, self.out, self._ws.get(self.ws_bytes, stream, self.table.device),
-                              self.ws_bytes, stream)
+        ws, handle = self._ws.get(self.ws_bytes, stream, self.table.device)
+        festina_extend_blocks(self.req, self.out, ws, self.ws_bytes, handle)
 
     def release(self, done, stream=None):
         import torch
         _check(done, "done", (torch.uint8, torch.bool), self.held.shape)
-        festina_release_blocks(self.req, done, self.out, self._ws.get(self.ws_bytes, stream, self.table.device),
-                               self.ws_bytes, stream)
+        ws, handle = self._ws.get(self.ws_bytes, stream, self.table.device)
+        festina_release_blocks(self.req, done, self.out, ws, self.ws_bytes, handle)
 
     def advance(self):
         self.held, self.length = self.length, self.held
@@ -726,7 +727,9 @@ class DeviceCache:
         _check(v_scale, "v_scale", (torch.float32,), (n, h))
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.cache = festina_kv_cache(n, bt, h, d, _ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale))
-        self._ws = _Workspaces()
+        self._ws, self._ws_bytes = _Workspaces(), {}
+        self._types = {torch.bfloat16: FESTINA_BF16, torch.float16: FESTINA_F16, torch.float32: FESTINA_F32}
+        self._halves, self._int32, self._rows = (torch.bfloat16, torch.float16), (torch.int32,), (h, d)
 
     @classmethod
     def empty(cls, n_blocks: int, block_tokens: int, n_kv_heads: int, head_dim: int, device="cuda"):
@@ -739,19 +742,17 @@ class DeviceCache:
     def store(self, k, v, slot, stream=None):
         """Store keys and values [tokens][kv heads][dim] (bfloat16, half or float32; any strides but the last)
         at the int32 slots [tokens]."""
-        import torch
-        types = {torch.bfloat16: FESTINA_BF16, torch.float16: FESTINA_F16, torch.float32: FESTINA_F32}
-        c = self.cache
         for name, x in (("k", k), ("v", v)):
-            _check(x, name, tuple(types))
-            if tuple(x.shape[1:]) != (c.n_kv_heads, c.head_dim) or x.dim() != 3 or (x.numel() and x.stride(2) != 1):
-                raise ValueError(f"{name}: [tokens][{c.n_kv_heads}][{c.head_dim}] with its last axis contiguous")
-        if k.dtype != v.dtype or k.shape[0] != v.shape[0]:
+            _check(x, name, self._types)
+            if x.dim() != 3 or x.shape[1:] != self._rows or (x.stride(2) != 1 and x.numel()):
+                raise ValueError(f"{name}: [tokens][{self._rows[0]}][{self._rows[1]}] with its last axis contiguous")
+        T = k.shape[0]
+        if k.dtype != v.dtype or v.shape[0] != T:
             raise ValueError("k and v: one type and number of tokens")
-        _check(slot, "slot", (torch.int32,), (k.shape[0],))
-        tokens = festina_kv_tokens(int(k.shape[0]), types[k.dtype], _ptr(k), _ptr(v), k.stride(0), k.stride(1),
-                                   v.stride(0), v.stride(1), _ptr(slot))
-        festina_store_kv(c, tokens, stream)
+        _check(slot, "slot", self._int32, (T,))
+        (kt, kh, _), (vt, vh, _) = k.stride(), v.stride()
+        festina_store_kv(self.cache, festina_kv_tokens(T, self._types[k.dtype], k.data_ptr(), v.data_ptr(), kt, kh, vt,
+                                                       vh, slot.data_ptr()), stream)
 
     def attend(self, q, table, length, first, max_new: int, scale=None, window: int = 0, out=None, lse=None,
                stream=None):
@@ -759,31 +760,41 @@ class DeviceCache:
         [requests][columns], length [requests] (new tokens included) and first [requests+1] are a step's
         (DeviceBlocks); max_new bounds the new tokens of one request.  out and lse are made where not given."""
         import torch
-        types = {torch.bfloat16: FESTINA_BF16, torch.float16: FESTINA_F16}
-        c = self.cache
-        _check(q, "q", tuple(types))
-        if q.dim() != 3 or q.shape[2] != c.head_dim or (q.numel() and q.stride(2) != 1):
-            raise ValueError(f"q: [tokens][heads][{c.head_dim}] with its last axis contiguous")
-        _check(table, "table", (torch.int32,), table.shape)
-        if table.dim() != 2:
-            raise ValueError("table: a tensor of two dimensions is needed")
-        R = int(table.shape[0])
-        _check(length, "length", (torch.int32,), (R,))
-        _check(first, "first", (torch.int32,), (R + 1,))
+        _check(q, "q", self._halves)
+        if q.dim() != 3 or q.shape[2] != self._rows[1] or (q.stride(2) != 1 and q.numel()):
+            raise ValueError(f"q: [tokens][heads][{self._rows[1]}] with its last axis contiguous")
+        _check(table, "table", self._int32)
+        if table.dim() != 2 or not table.is_contiguous():
+            raise ValueError("table: a contiguous tensor of two dimensions is needed")
+        T, heads, _ = q.shape
+        R, columns = table.shape
+        _check(length, "length", self._int32, (R,))
+        _check(first, "first", self._int32, (R + 1,))
         if out is None or lse is None:
             with _on(stream, q.device):
-                out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
-                lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if lse is None else lse
+                if out is None:
+                    out = torch.empty((T, heads, q.shape[2]), dtype=q.dtype, device=q.device)
+                if lse is None:
+                    lse = torch.empty((T, heads), dtype=torch.float32, device=q.device)
         _check(out, "out", (q.dtype,))
-        if out.shape != q.shape or (out.numel() and out.stride(2) != 1):
+        if out.shape != q.shape or (out.stride(2) != 1 and out.numel()):
             raise ValueError("out: q's shape with its last axis contiguous")
-        _check(lse, "lse", (torch.float32,), q.shape[:2])
-        att = festina_attention(R, int(table.shape[1]), int(q.shape[0]), int(q.shape[1]), int(max_new), types[q.dtype],
-                                int(window), float(c.head_dim ** -0.5 if scale is None else scale), _ptr(table),
-                                _ptr(length), _ptr(first), _ptr(q), q.stride(0), q.stride(1), _ptr(out), out.stride(0),
-                                out.stride(1), _ptr(lse))
-        n = festina_attend_workspace_bytes(c, att)
-        festina_attend(c, att, self._ws.get(n, stream, q.device), n, stream)
+        _check(lse, "lse", (torch.float32,), (T, heads))
+        qt, qh, _ = q.stride()
+        ot, oh, _ = out.stride()
+        if scale is None:
+            scale = self._rows[1] ** -0.5
+        att = festina_attention(R, columns, T, heads, max_new, self._types[q.dtype], window, scale, table.data_ptr(),
+                                length.data_ptr(), first.data_ptr(), q.data_ptr(), qt, qh, out.data_ptr(), ot, oh,
+                                lse.data_ptr())
+        sizes = (R, columns, T, heads, max_new)
+        n = self._ws_bytes.get(sizes)
+        if n is None:
+            if len(self._ws_bytes) > 1024:
+                self._ws_bytes.clear()
+            n = self._ws_bytes[sizes] = festina_attend_workspace_bytes(self.cache, att)
+        ws, handle = self._ws.get(n, stream, q.device)
+        festina_attend(self.cache, att, ws, n, handle)
         return out, lse
 
 
@@ -904,14 +915,15 @@ def festina_blocks_workspace_bytes(n_requests: int, max_tokens: int) -> int:
 
 
 def festina_extend_blocks(req, out, workspace, workspace_bytes, stream=None) -> None:
-    st = lib().festina_extend_blocks(C.byref(req), C.byref(out), _ptr(workspace), int(workspace_bytes),
+    """workspace: the address of device memory (here and in the calls below)."""
+    st = lib().festina_extend_blocks(C.byref(req), C.byref(out), workspace, int(workspace_bytes),
                                      _stream_handle(stream))
     if st != FESTINA_OK:
         raise FestinaError(st, "festina_extend_blocks")
 
 
 def festina_release_blocks(req, done, out, workspace, workspace_bytes, stream=None) -> None:
-    st = lib().festina_release_blocks(C.byref(req), _ptr(done), C.byref(out), _ptr(workspace), int(workspace_bytes),
+    st = lib().festina_release_blocks(C.byref(req), _ptr(done), C.byref(out), workspace, int(workspace_bytes),
                                       _stream_handle(stream))
     if st != FESTINA_OK:
         raise FestinaError(st, "festina_release_blocks")
@@ -928,7 +940,7 @@ def festina_attend_workspace_bytes(cache, att) -> int:
 
 
 def festina_attend(cache, att, workspace, workspace_bytes, stream=None) -> None:
-    st = lib().festina_attend(C.byref(cache), C.byref(att), _ptr(workspace), int(workspace_bytes),
+    st = lib().festina_attend(C.byref(cache), C.byref(att), workspace, int(workspace_bytes),
                               _stream_handle(stream))
     if st != FESTINA_OK:
         raise FestinaError(st, "festina_attend")
