@@ -9,14 +9,17 @@
 // min(T[r] - add[r], total).  Its i-th new block is free_ids[n_free - 1 - (B[r] - need[r] + i)].
 //
 // k_extend_small   one workgroup: the sums in LDS, then a thread per token (small steps, where launches count).
-// k_extend_sums, k_extend_scan, k_extend_fill   the sums of each kChunk requests; each chunk's running sums
-//   from those of the chunks before it; then the slots, kFill tokens a workgroup.  The scan leaves for each
-//   workgroup of the fill the request that its first token belongs to, so that no search crosses
-//   the whole list: a thread searches the few requests of its stretch in LDS.
-// k_release_sums, k_release_fill   the same two sums for release, then a thread per returned id.
+// k_extend_scan    the running sums of kChunk requests a workgroup, after the sums of all requests before them:
+//   from k_extend_sums, one number a chunk, or, for few requests, summed by the workgroup itself, which
+//   saves a launch.  It leaves what the fill needs of a request, and for each stretch of kFill tokens the
+//   request that its first token belongs to, so that no search crosses the whole list.
+// k_extend_fill    the slots, kFill tokens a workgroup.  A wave's 256 tokens mostly lie in one request: then
+//   everything about the request is uniform and a lane makes four slots from one or two block ids.
+//   Where they do not, each lane searches the few requests of its stretch in LDS.
+// k_release        a thread per returned id, after the same sums.
 //
-// All arithmetic is on integers; the largest T is taken by an atomic maximum, which does not
-// depend on order.  Bound by the bytes of the slot map on large steps, by latency on small ones.
+// All arithmetic is on integers, so results do not depend on order.  Bound by the bytes of the slot map on
+// large steps, by latency on small ones.
 #include <hip/hip_runtime.h>
 
 #include <climits>
@@ -28,6 +31,8 @@
 namespace {
 
 constexpr int kChunk = 256;          // requests a workgroup of the sums and scans
+constexpr int kGive = 64;            // requests a workgroup of the release
+constexpr int kDirect = 16384;       // up to so many requests a workgroup sums all requests before its own
 constexpr int kFill = 2048;          // slots a workgroup of the fill
 constexpr int kSmall = 1024;         // threads of the one-workgroup kernel, a request each
 constexpr int kSmallTokens = 8192;   // and its slots
@@ -42,9 +47,16 @@ struct BlockArgs {
   const uint8_t *done;
   // workspace
   long long *sum_blocks, *sum_tokens;   // [chunks]
-  int32_t *total;                       // served tokens, last request with any, blocks they take, n_free
-  int32_t *before;                      // [R] blocks taken by the requests before r
+  int4 *ends;                           // [chunks] served tokens up to the chunk's last, that request, blocks taken
+  int32_t *n_free_in;                   // [1] the count before the call
+  int4 *about;                          // [R] see About
   int32_t *owner;                       // [fill workgroups] request of a stretch's first token
+};
+
+// What the fill needs of a request: token t stands at position t + shift; columns from `have` on are new, column c is
+// free_ids[top - c]; its length afterwards.
+struct About {
+  int32_t shift, have, top, length;
 };
 
 struct Demand {
@@ -95,22 +107,22 @@ __device__ __forceinline__ long long scan(long long x, long long *lds, long long
   return x + before;
 }
 
-// Where token t of request r goes; fills the table's new column when the token is its first.
-__device__ __forceinline__ int place(const BlockArgs &a, int r, int p, int have, int before, int n_free) {
-  const int c = p >> a.shift, o = p & ((1 << a.shift) - 1);
-  int id;
-  if (c >= have) {
-    id = a.free_ids[max(n_free - 1 - (before + c - have), 0)];
-    if (o == 0) a.table[(size_t)r * a.MB + c] = id;
-  } else {
-    id = a.table[(size_t)r * a.MB + c];
-  }
+// The block of column c of a request; the table's entry is filled where the column's first token is `begins`.
+__device__ __forceinline__ int block_at(const BlockArgs &a, int r, const About &q, int c, bool begins) {
+  if (c < q.have) return a.table[(size_t)r * a.MB + c];
+  const int id = a.free_ids[max(q.top - c, 0)];
+  if (begins) a.table[(size_t)r * a.MB + c] = id;
+  return id;
+}
+__device__ __forceinline__ int slot_of(const BlockArgs &a, int id, int o) {
   return (unsigned)id < (unsigned)a.NB ? (id << a.shift) + o : -1;
 }
 
-__global__ void __launch_bounds__(kSmall) k_extend_small(BlockArgs a) {
-  __shared__ long long lds[kSmall / 64];
-  __shared__ int first[kSmall + 1], held[kSmall], have[kSmall], before[kSmall];
+template <int N>
+__global__ void __launch_bounds__(N) k_extend_small(BlockArgs a) {
+  __shared__ long long lds[N / 64];
+  __shared__ int first[N + 1];
+  __shared__ About about[N];
   __shared__ int total, taken;
   const int r = threadIdx.x;
   const int n_free = free_count(a);
@@ -118,8 +130,8 @@ __global__ void __launch_bounds__(kSmall) k_extend_small(BlockArgs a) {
   if (r < a.R) d = demand(a, r);
   if (r == 0) total = taken = 0;
   long long unused;
-  const long long B = scan<kSmall>(d.need, lds, &unused);
-  const long long T = scan<kSmall>(d.takes, lds, &unused);
+  const long long B = scan<N>(d.need, lds, &unused);
+  const long long T = scan<N>(d.takes, lds, &unused);
   const bool served = d.fits && B <= n_free && T <= a.max_tokens;
   if (served) {
     atomicMax(&total, (int)T);
@@ -128,12 +140,11 @@ __global__ void __launch_bounds__(kSmall) k_extend_small(BlockArgs a) {
   __syncthreads();
   const int end = total;
   if (r < a.R) {
-    first[r] = (int)min(T - d.takes, (long long)end);
-    held[r] = d.held;
-    have[r] = d.have;
-    before[r] = (int)min(B - d.need, (long long)INT_MAX);
-    a.first[r] = first[r];
-    a.length[r] = served ? d.held + d.add : d.held;
+    const int f = (int)min(T - d.takes, (long long)end), len = served ? d.held + d.add : d.held;
+    first[r] = f;
+    about[r] = About{d.held - f, d.have, (int)(n_free - 1 - min(B - d.need, (long long)n_free) + d.have), len};
+    a.first[r] = f;
+    a.length[r] = len;
     a.served[r] = served;
   }
   if (r == 0) {
@@ -142,7 +153,7 @@ __global__ void __launch_bounds__(kSmall) k_extend_small(BlockArgs a) {
     *a.n_free_out = n_free - taken;
   }
   __syncthreads();
-  for (int t = threadIdx.x; t < a.max_tokens; t += kSmall) {
+  for (int t = threadIdx.x; t < a.max_tokens; t += N) {
     int s = -1;
     if (t < end) {
       int lo = 0, hi = a.R;                        // first[lo] <= t < first[hi]
@@ -150,7 +161,9 @@ __global__ void __launch_bounds__(kSmall) k_extend_small(BlockArgs a) {
         const int m = (lo + hi) >> 1;
         if (first[m] <= t) lo = m; else hi = m;
       }
-      s = place(a, lo, held[lo] + t - first[lo], have[lo], before[lo], n_free);
+      const About q = about[lo];
+      const int p = t + q.shift, o = p & ((1 << a.shift) - 1);
+      s = slot_of(a, block_at(a, lo, q, p >> a.shift, o == 0), o);
     }
     a.slot[t] = s;
   }
@@ -167,20 +180,29 @@ __global__ void __launch_bounds__(kChunk) k_extend_sums(BlockArgs a) {
   if (threadIdx.x == 0) {
     a.sum_blocks[blockIdx.x] = B;
     a.sum_tokens[blockIdx.x] = T;
-    if (blockIdx.x == 0) {
-      a.total[0] = a.total[1] = a.total[2] = 0;
-      a.total[3] = free_count(a);
-    }
   }
 }
 
+// The caller's arrays are only read here (length and n_free may be the ones to be overwritten): the fill writes them.
+template <bool DIRECT>
 __global__ void __launch_bounds__(kChunk) k_extend_scan(BlockArgs a) {
   __shared__ long long lds[kChunk / 64];
+  __shared__ int ends[3];
   const int r = blockIdx.x * kChunk + threadIdx.x;
   long long b = 0, t = 0, B0, T0, unused;
-  for (int i = threadIdx.x; i < (int)blockIdx.x; i += kChunk) {
-    b += a.sum_blocks[i];
-    t += a.sum_tokens[i];
+  if (threadIdx.x < 3) ends[threadIdx.x] = 0;
+  if (DIRECT) {
+#pragma unroll 4
+    for (int i = threadIdx.x; i < (int)blockIdx.x * kChunk; i += kChunk) {
+      const Demand d = demand(a, i);
+      b += d.need;
+      t += d.takes;
+    }
+  } else {
+    for (int i = threadIdx.x; i < (int)blockIdx.x; i += kChunk) {
+      b += a.sum_blocks[i];
+      t += a.sum_tokens[i];
+    }
   }
   scan<kChunk>(b, lds, &B0);
   scan<kChunk>(t, lds, &T0);
@@ -188,77 +210,117 @@ __global__ void __launch_bounds__(kChunk) k_extend_scan(BlockArgs a) {
   if (r < a.R) d = demand(a, r);
   const long long B = B0 + scan<kChunk>(d.need, lds, &unused);
   const long long T = T0 + scan<kChunk>(d.takes, lds, &unused);
-  const int n_free = a.total[3];
+  const int n_free = free_count(a);
   const bool served = d.fits && B <= n_free && T <= a.max_tokens;
   if (r < a.R) {
-    a.first[r] = (int)min(T - d.takes, (long long)a.max_tokens);   // the fill takes the least of this and the total
-    a.before[r] = (int)min(B - d.need, (long long)INT_MAX);
-    a.length[r] = served ? d.held + d.add : d.held;
+    const int f = (int)min(T - d.takes, (long long)a.max_tokens);   // the fill takes the least of this and the total
+    a.first[r] = f;
+    const int top = (int)(n_free - 1 - min(B - d.need, (long long)n_free) + d.have);
+    a.about[r] = make_int4(d.held - f, d.have, top, served ? d.held + d.add : d.held);
     a.served[r] = served;
   }
   if (served && d.takes) {
     const int f = (int)(T - d.takes), e = (int)T;
     for (int w = (f + kFill - 1) / kFill; w * kFill < e; ++w) a.owner[w] = r;
-    atomicMax(&a.total[0], e);
-    atomicMax(&a.total[1], r);
-    atomicMax(&a.total[2], (int)B);
+    atomicMax(&ends[0], e);
+    atomicMax(&ends[1], r);
+    atomicMax(&ends[2], (int)B);
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    a.ends[blockIdx.x] = make_int4(ends[0], ends[1], ends[2], 0);
+    if (blockIdx.x == 0) *a.n_free_in = n_free;
   }
 }
 
-__global__ void __launch_bounds__(256) k_extend_fill(BlockArgs a, int32_t fills, int32_t vec) {
+__global__ void __launch_bounds__(256) k_extend_fill(BlockArgs a, int32_t chunks, int32_t fills, int32_t vec) {
   constexpr int kList = kFill + 256;
-  __shared__ int first[kList + 1];
-  const int end = a.total[0], n_free = a.total[3];
+  __shared__ int first[kList];
+  __shared__ int ends[4][3];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int e0 = 0, e1 = 0, e2 = 0;
+  for (int i = threadIdx.x; i < chunks; i += 256) {
+    const int4 e = a.ends[i];
+    e0 = max(e0, e.x), e1 = max(e1, e.y), e2 = max(e2, e.z);
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) {
+    e0 = max(e0, __shfl_xor(e0, d));
+    e1 = max(e1, __shfl_xor(e1, d));
+    e2 = max(e2, __shfl_xor(e2, d));
+  }
+  if (lane == 0) ends[wave][0] = e0, ends[wave][1] = e1, ends[wave][2] = e2;
+  __syncthreads();
+  const int end = max(max(ends[0][0], ends[1][0]), max(ends[2][0], ends[3][0]));
+  const int last = max(max(ends[0][1], ends[1][1]), max(ends[2][1], ends[3][1]));
   // the scan's first tokens of requests that are not served lie past the end
   for (int i = blockIdx.x * 256 + threadIdx.x; i <= a.R; i += gridDim.x * 256) {
     if (i == a.R || a.first[i] > end) a.first[i] = end;
+    if (i < a.R) a.length[i] = a.about[i].w;
   }
-  if (blockIdx.x == 0 && threadIdx.x == 0) *a.n_free_out = n_free - a.total[2];
+  if (blockIdx.x == 0 && threadIdx.x == 0)
+    *a.n_free_out = *a.n_free_in - max(max(ends[0][2], ends[1][2]), max(ends[2][2], ends[3][2]));
+  const int bt = 1 << a.shift;
   for (int w = blockIdx.x; w < fills; w += gridDim.x) {
     const int t0 = w * kFill;
     int lo0 = 0, n = 0;
     if (t0 < end) {
       lo0 = a.owner[w];
-      n = (t0 + kFill < end ? a.owner[w + 1] : a.total[1]) - lo0 + 1;     // requests lo0 .. lo0 + n - 1
+      n = (t0 + kFill < end ? a.owner[w + 1] : last) - lo0 + 1;           // requests lo0 .. lo0 + n - 1
     }
     __syncthreads();
-    if (n <= kList)
-      for (int i = threadIdx.x; i < n; i += 256) first[i] = a.first[lo0 + i];
+    for (int i = threadIdx.x; i < min(n, kList); i += 256) first[i] = a.first[lo0 + i];
     __syncthreads();
-#pragma unroll
+    const auto start = [&](int i) { return i < kList ? first[i] : a.first[lo0 + i]; };
+    const auto owner = [&](int t, int lo) {            // the request of token t, lo0 + lo or later
+      int hi = n;
+      while (hi - lo > 1) {
+        const int m = (lo + hi) >> 1;
+        if (start(m) <= t) lo = m; else hi = m;
+      }
+      return lo;
+    };
+    int from = 0;
     for (int g = 0; g < kFill / 1024; ++g) {
-      const int t = t0 + g * 1024 + threadIdx.x * 4;
-      if (t >= a.max_tokens) break;
+      const int tw = t0 + g * 1024 + wave * 256, t = tw + lane * 4;       // the wave's tokens, the lane's
+      if (tw >= a.max_tokens) break;
       int s[4] = {-1, -1, -1, -1};
-      if (t < end) {
-        int lo = 0, hi = n;
-        while (hi - lo > 1) {
-          const int m = (lo + hi) >> 1;
-          const int f = n <= kList ? first[m] : a.first[lo0 + m];
-          if (f <= t) lo = m; else hi = m;
-        }
-        int r = -1, have = 0, before = 0, shift_p = 0, stop = t;       // stop: where request r's tokens end
+      if (tw < end) {
+        from = __builtin_amdgcn_readfirstlane(owner(tw, from));
+        const int tail = min(tw + 255, end - 1);
+        if (from + 1 >= n || start(from + 1) > tail) {
+          // one request
+          const int r = lo0 + from;
+          const int4 q4 = a.about[r];
+          const About q{q4.x, q4.y, q4.z, q4.w};
+          const int p = t + q.shift, c = p >> a.shift, o = p & (bt - 1);
+          if (t <= tail) {
+            const int id = block_at(a, r, q, c, o == 0);
+            const int over = o + 3 - (bt - 1), more = t + 3 <= tail ? over : over - (t + 3 - tail);
+            const int next = more > 0 ? block_at(a, r, q, c + 1, true) : 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (t + i >= end) break;
-          if (t + i >= stop) {
-            // the next request with tokens
-            int f, add;
-            r = r < 0 ? lo0 + lo : r + 1;
-            for (;;) {
-              f = a.first[r];
-              add = a.length[r];
-              const int next = r + 1 < a.R ? min(a.first[r + 1], end) : end;
-              stop = next;
-              if (next > t + i) break;
-              ++r;
-            }
-            const int held = add - (stop - f);      // served: length - its new tokens
-            have = blocks_of(held, a.shift);
-            before = a.before[r];
-            shift_p = held - f;
+            for (int i = 0; i < 4; ++i)
+              s[i] = t + i > tail ? -1 : o + i < bt ? slot_of(a, id, o + i) : slot_of(a, next, o + i - bt);
           }
-          s[i] = place(a, r, t + i + shift_p, have, before, n_free);
+        } else if (t < end) {
+          int i = owner(t, from), r = -1, stop = t, c = -1, id = 0;       // stop: where request r's tokens end
+          About q{};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            if (t + k >= end) break;
+            if (t + k >= stop) {
+              if (r >= 0) ++i;
+              while (i + 1 < n && start(i + 1) <= t + k) ++i;
+              stop = i + 1 < n ? min(start(i + 1), end) : end;
+              r = lo0 + i;
+              const int4 q4 = a.about[r];
+              q = About{q4.x, q4.y, q4.z, q4.w};
+              c = -1;
+            }
+            const int p = t + k + q.shift, o = p & (bt - 1);
+            if (p >> a.shift != c) id = block_at(a, r, q, c = p >> a.shift, o == 0);
+            s[k] = slot_of(a, id, o);
+          }
         }
       }
       if (vec && t + 4 <= a.max_tokens) {
@@ -286,63 +348,62 @@ __global__ void __launch_bounds__(kChunk) k_release_sums(BlockArgs a) {
   scan<kChunk>(r < a.R ? returned(a, r, &held) : 0, lds, &B);
   if (threadIdx.x == 0) {
     a.sum_blocks[blockIdx.x] = B;
-    if (blockIdx.x == 0) a.total[3] = free_count(a);
+    if (blockIdx.x == 0) *a.n_free_in = free_count(a);
   }
 }
 
-// One chunk of requests: `n_free` ids lie on the list already, `B0` come from the chunks before it.
-__device__ void give_back(const BlockArgs &a, int chunk, int n_free, long long B0, long long *lds, long long *ends) {
-  const int r = chunk * kChunk + threadIdx.x;
+// kGive requests a workgroup.  DIRECT: sums the requests before its own itself, where what is written is not what
+// is read; otherwise whole chunks from k_release_sums, and only the requests of its own chunk, whose
+// lengths this launch overwrites, from their own thread.
+template <bool DIRECT>
+__global__ void __launch_bounds__(kChunk) k_release(BlockArgs a) {
+  constexpr int kOwn = DIRECT ? kGive : kChunk;
+  __shared__ long long lds[kChunk / 64];
+  __shared__ long long ends[kOwn];
+  const int r0 = blockIdx.x * kOwn, r = r0 + threadIdx.x;
+  const int n_free = DIRECT ? free_count(a) : *a.n_free_in;
+  long long b = 0, B0, all;
   int held = 0;
-  const int n = r < a.R ? returned(a, r, &held) : 0;
-  long long all;
-  ends[threadIdx.x] = scan<kChunk>(n, lds, &all);
+  if (DIRECT) {
+#pragma unroll 4
+    for (int i = threadIdx.x; i < r0; i += kChunk) b += returned(a, i, &held);
+  } else {
+    for (int i = threadIdx.x; i < (int)blockIdx.x; i += kChunk) b += a.sum_blocks[i];
+  }
+  scan<kChunk>(b, lds, &B0);
+  const bool mine = threadIdx.x < kOwn && r < a.R;
+  const long long own = scan<kChunk>(mine ? returned(a, r, &held) : 0, lds, &all);
+  if (threadIdx.x < kOwn) ends[threadIdx.x] = own;
   __syncthreads();
   for (long long i = threadIdx.x; i < all; i += kChunk) {
-    int lo = -1, hi = kChunk - 1;                      // ends[lo] <= i < ends[hi]
+    int lo = -1, hi = kOwn - 1;                            // ends[lo] <= i < ends[hi]
     while (hi - lo > 1) {
       const int m = (lo + hi) >> 1;
       if (ends[m] <= i) lo = m; else hi = m;
     }
     const int c = (int)(i - (hi ? ends[hi - 1] : 0));
     const long long at = n_free + B0 + i;
-    if (at < a.NB) a.free_ids[at] = a.table[(size_t)(chunk * kChunk + hi) * a.MB + c];
+    if (at < a.NB) a.free_ids[at] = a.table[(size_t)(r0 + hi) * a.MB + c];
   }
-  if (r < a.R) a.length[r] = a.done[r] ? 0 : held;
-  if (chunk == (a.R - 1) / kChunk && threadIdx.x == 0)
-    *a.n_free_out = (int)min(n_free + B0 + all, (long long)a.NB);
-}
-
-__global__ void __launch_bounds__(kChunk) k_release_fill(BlockArgs a) {
-  __shared__ long long lds[kChunk / 64];
-  __shared__ long long ends[kChunk];
-  long long b = 0, B0;
-  for (int i = threadIdx.x; i < (int)blockIdx.x; i += kChunk) b += a.sum_blocks[i];
-  scan<kChunk>(b, lds, &B0);
-  give_back(a, blockIdx.x, a.total[3], B0, lds, ends);
-}
-
-// One chunk alone: every thread has read held and n_free (the scan's barrier) before any writes.
-__global__ void __launch_bounds__(kChunk) k_release_one(BlockArgs a) {
-  __shared__ long long lds[kChunk / 64];
-  __shared__ long long ends[kChunk];
-  give_back(a, 0, free_count(a), 0, lds, ends);
+  if (mine) a.length[r] = a.done[r] ? 0 : held;
+  if (threadIdx.x == 0 && r0 + kOwn >= a.R) *a.n_free_out = (int)min(n_free + B0 + all, (long long)a.NB);
 }
 
 struct Layout {
-  size_t sum_blocks, sum_tokens, total, before, owner, bytes;
+  size_t sum_blocks, sum_tokens, ends, n_free_in, about, owner, bytes;
 };
 
 size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 
 Layout layout(int R, int max_tokens) {
   Layout l;
-  const size_t chunks = ((size_t)R + kChunk - 1) / kChunk, fills = ((size_t)max_tokens + kFill - 1) / kFill;
+  const size_t chunks = R > 0 ? ((size_t)R + kChunk - 1) / kChunk : 1, fills = ((size_t)max_tokens + kFill - 1) / kFill;
   l.sum_blocks = 0;
   l.sum_tokens = up(chunks * 8);
-  l.total = l.sum_tokens + up(chunks * 8);
-  l.before = l.total + 256;
-  l.owner = l.before + up((size_t)R * 4);
+  l.ends = l.sum_tokens + up(chunks * 8);
+  l.n_free_in = l.ends + up(chunks * 16);
+  l.about = l.n_free_in + 256;
+  l.owner = l.about + up((size_t)R * 16);
   l.bytes = l.owner + up((fills + 1) * 4);
   return l;
 }
@@ -383,8 +444,9 @@ festina_status arguments(const festina_kv_requests *q, festina_kv_step *out, boo
   a->served = out->served;
   a->sum_blocks = reinterpret_cast<long long *>(w + l.sum_blocks);
   a->sum_tokens = reinterpret_cast<long long *>(w + l.sum_tokens);
-  a->total = reinterpret_cast<int32_t *>(w + l.total);
-  a->before = reinterpret_cast<int32_t *>(w + l.before);
+  a->ends = reinterpret_cast<int4 *>(w + l.ends);
+  a->n_free_in = reinterpret_cast<int32_t *>(w + l.n_free_in);
+  a->about = reinterpret_cast<int4 *>(w + l.about);
   a->owner = reinterpret_cast<int32_t *>(w + l.owner);
   return FESTINA_OK;
 }
@@ -402,15 +464,21 @@ extern "C" festina_status festina_extend_blocks(const festina_kv_requests *req, 
   const festina_status bad = arguments(req, out, true, workspace, workspace_bytes, &a);
   if (bad != FESTINA_OK) return bad;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if (a.R <= kSmall && a.max_tokens <= kSmallTokens) {
-    k_extend_small<<<1, kSmall, 0, st>>>(a);
+  if (a.R <= 64 && a.max_tokens <= 512) {
+    k_extend_small<64><<<1, 64, 0, st>>>(a);
+  } else if (a.R <= kSmall && a.max_tokens <= kSmallTokens) {
+    k_extend_small<kSmall><<<1, kSmall, 0, st>>>(a);
   } else {
     const int chunks = max((a.R + kChunk - 1) / kChunk, 1);
     const int fills = (a.max_tokens + kFill - 1) / kFill;
     const bool vec = (reinterpret_cast<uintptr_t>(a.slot) & 15) == 0;
-    k_extend_sums<<<chunks, kChunk, 0, st>>>(a);
-    k_extend_scan<<<chunks, kChunk, 0, st>>>(a);
-    k_extend_fill<<<min(max(max(fills, chunks), 1), 4096), 256, 0, st>>>(a, fills, vec);
+    if (a.R <= kDirect) {
+      k_extend_scan<true><<<chunks, kChunk, 0, st>>>(a);
+    } else {
+      k_extend_sums<<<chunks, kChunk, 0, st>>>(a);
+      k_extend_scan<false><<<chunks, kChunk, 0, st>>>(a);
+    }
+    k_extend_fill<<<min(max(max(fills, chunks), 1), 4096), 256, 0, st>>>(a, chunks, fills, vec);
   }
   return hipGetLastError() == hipSuccess ? FESTINA_OK : FESTINA_ERR_DEVICE;
 }
@@ -424,12 +492,14 @@ extern "C" festina_status festina_release_blocks(const festina_kv_requests *req,
   if (a.R > 0 && !done) return FESTINA_ERR_INVALID;
   a.done = done;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const int chunks = (a.R + kChunk - 1) / kChunk;
-  if (chunks <= 1) {
-    k_release_one<<<1, kChunk, 0, st>>>(a);
+  // one workgroup reads everything before it writes anything; several may only where they write elsewhere
+  const bool apart = a.length != a.held && a.n_free_out != a.n_free;
+  if (a.R <= kGive || (a.R <= kDirect * 2 && apart)) {
+    k_release<true><<<max((a.R + kGive - 1) / kGive, 1), kChunk, 0, st>>>(a);
   } else {
+    const int chunks = (a.R + kChunk - 1) / kChunk;
     k_release_sums<<<chunks, kChunk, 0, st>>>(a);
-    k_release_fill<<<chunks, kChunk, 0, st>>>(a);
+    k_release<false><<<chunks, kChunk, 0, st>>>(a);
   }
   return hipGetLastError() == hipSuccess ? FESTINA_OK : FESTINA_ERR_DEVICE;
 }

@@ -2,7 +2,8 @@
 //
 // k_store  a workgroup takes the runs (stretches of tokens in one block) that begin among its tokens, for one key
 //   head and either the keys or the values.  For each run: the largest finite magnitude over the run's
-//   elements, the block's scale from it, where that grew the older codes anew, then the new codes.
+//   elements (which stay in registers), the block's scale from it, where that grew the older codes anew, then
+//   the new codes.
 //   Keys are stored as they come ([token][dim]); values pass through LDS, 64 slots at a time, and leave with
 //   their tokens running fastest, 16 tokens of a row in one 16-byte store.
 //
@@ -38,32 +39,6 @@ struct StoreArgs {
   float *scale[2];
 };
 
-template <int TYPE>
-__device__ __forceinline__ void load8(const void *base, int64_t at, bool vec, float (&x)[8]) {
-  if constexpr (TYPE == FESTINA_F32) {
-    const float *p = static_cast<const float *>(base) + at;
-    if (vec) {
-      const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
-      x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = p[i];
-    }
-  } else {
-    const uint16_t *p = static_cast<const uint16_t *>(base) + at;
-    uint16_t u[8];
-    if (vec) {
-      *reinterpret_cast<uint4 *>(u) = *reinterpret_cast<const uint4 *>(p);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) u[i] = p[i];
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      x[i] = TYPE == FESTINA_BF16 ? __uint_as_float((unsigned)u[i] << 16) : (float)__builtin_bit_cast(_Float16, u[i]);
-  }
-}
-
 __device__ __forceinline__ bool finite(float x) { return __builtin_fabsf(x) < __builtin_inff(); }
 
 // Four codes; `inv` is the scale's reciprocal, a power of two.
@@ -92,22 +67,93 @@ __device__ __forceinline__ float scale_of(float amax) {
   return fminf(fmaxf(__uint_as_float((unsigned)max(e, 1) << 23), kScaleMin), kScaleMax);
 }
 
-template <int TYPE, int D>
-__device__ __forceinline__ void store_run(const StoreArgs &a, int which, int h, int t, int n, int slot, float *lds_max,
-                                          uint8_t *tile) {
-  constexpr int kVecs = D / 8, kPitch = D + 4;
+// Eight elements as they were read.
+template <int TYPE>
+struct Raw8 {
+  uint4 w[TYPE == FESTINA_F32 ? 2 : 1];
+};
+
+template <int TYPE>
+__device__ __forceinline__ Raw8<TYPE> read8(const void *base, int64_t at, bool vec) {
+  Raw8<TYPE> r;
+  if constexpr (TYPE == FESTINA_F32) {
+    const float *p = static_cast<const float *>(base) + at;
+    if (vec) {
+      r.w[0] = reinterpret_cast<const uint4 *>(p)[0];
+      r.w[1] = reinterpret_cast<const uint4 *>(p)[1];
+    } else {
+      unsigned u[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) u[i] = __float_as_uint(p[i]);
+      r.w[0] = make_uint4(u[0], u[1], u[2], u[3]);
+      r.w[1] = make_uint4(u[4], u[5], u[6], u[7]);
+    }
+  } else {
+    const uint16_t *p = static_cast<const uint16_t *>(base) + at;
+    if (vec) {
+      r.w[0] = *reinterpret_cast<const uint4 *>(p);
+    } else {
+      unsigned u[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) u[i] = p[2 * i] | (unsigned)p[2 * i + 1] << 16;
+      r.w[0] = make_uint4(u[0], u[1], u[2], u[3]);
+    }
+  }
+  return r;
+}
+
+template <int TYPE>
+__device__ __forceinline__ void values8(const Raw8<TYPE> &r, float (&x)[8]) {
+  if constexpr (TYPE == FESTINA_F32) {
+    const unsigned u[8] = {r.w[0].x, r.w[0].y, r.w[0].z, r.w[0].w, r.w[1].x, r.w[1].y, r.w[1].z, r.w[1].w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(u[i]);
+  } else {
+    const unsigned u[4] = {r.w[0].x, r.w[0].y, r.w[0].z, r.w[0].w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (TYPE == FESTINA_BF16) {
+        x[2 * i] = __uint_as_float(u[i] << 16);
+        x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+      } else {
+        x[2 * i] = (float)__builtin_bit_cast(_Float16, (uint16_t)u[i]);
+        x[2 * i + 1] = (float)__builtin_bit_cast(_Float16, (uint16_t)(u[i] >> 16));
+      }
+    }
+  }
+}
+
+// One run, for keys (WHICH = 0) or values.  The elements of its first kSlots tokens stay in registers between the
+// maximum and the codes; a longer run's others are read again.
+template <int TYPE, int D, int WHICH>
+__device__ __forceinline__ void store_run(const StoreArgs &a, int h, int t, int n, int slot, float *lds_max, uint8_t *tile) {
+  constexpr int kVecs = D / 8, kPitch = D + 4, kKept = kSlots * kVecs / kThreads;
   const int bt = 1 << a.shift, off = slot & (bt - 1);
   const size_t bh = (size_t)(slot >> a.shift) * a.H + h;
-  const int64_t ts = a.token_stride[which], row0 = (int64_t)h * a.head_stride[which] + (int64_t)t * ts;
-  const void *x = a.x[which];
-  const bool vec = a.vec[which];
-  uint8_t *codes = a.codes[which] + bh * D * bt;
-  const float old = a.scale[which][bh];
+  const int64_t ts = a.token_stride[WHICH], row0 = (int64_t)h * a.head_stride[WHICH] + (int64_t)t * ts;
+  const void *x = a.x[WHICH];
+  const bool vec = a.vec[WHICH];
+  uint8_t *codes = a.codes[WHICH] + bh * D * bt;
+  const float old = a.scale[WHICH][bh];
+  const auto read = [&](int i) { return read8<TYPE>(x, row0 + (int64_t)(i / kVecs) * ts + (i % kVecs) * 8, vec); };
+  Raw8<TYPE> kept[kKept];
   float v[8], amax = 0.f;
-  for (int i = threadIdx.x; i < n * kVecs; i += kThreads) {
-    load8<TYPE>(x, row0 + (int64_t)(i / kVecs) * ts + (i % kVecs) * 8, vec, v);
+#pragma unroll
+  for (int j = 0; j < kKept; ++j)
+    if ((int)threadIdx.x + j * kThreads < n * kVecs) kept[j] = read(threadIdx.x + j * kThreads);
+  const auto widen = [&]() {
 #pragma unroll
     for (int j = 0; j < 8; ++j) amax = fmaxf(amax, finite(v[j]) ? __builtin_fabsf(v[j]) : 0.f);
+  };
+#pragma unroll
+  for (int j = 0; j < kKept; ++j)
+    if ((int)threadIdx.x + j * kThreads < n * kVecs) {
+      values8<TYPE>(kept[j], v);
+      widen();
+    }
+  for (int i = threadIdx.x + kKept * kThreads; i < n * kVecs; i += kThreads) {
+    values8<TYPE>(read(i), v);
+    widen();
   }
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) amax = fmaxf(amax, __shfl_xor(amax, d));
@@ -117,10 +163,10 @@ __device__ __forceinline__ void store_run(const StoreArgs &a, int which, int h, 
   float scale = scale_of(amax);
   if (off > 0) scale = fmaxf(scale, old);
   const float inv = 1.f / scale;                       // exact
-  if (threadIdx.x == 0) a.scale[which][bh] = scale;
+  if (threadIdx.x == 0) a.scale[WHICH][bh] = scale;
   if (off > 0 && scale > old) {
     const float ratio = old / scale;
-    if (which == 0) {
+    if (WHICH == 0) {
       uint4 *p = reinterpret_cast<uint4 *>(codes);
       for (int i = threadIdx.x; i < off * D / 16; i += kThreads) {
         uint4 c = p[i];
@@ -143,23 +189,42 @@ __device__ __forceinline__ void store_run(const StoreArgs &a, int which, int h, 
       }
     }
   }
-  if (which == 0) {
-    for (int i = threadIdx.x; i < n * kVecs; i += kThreads) {
-      const int k = i / kVecs, d = (i % kVecs) * 8;
-      load8<TYPE>(x, row0 + (int64_t)k * ts + d, vec, v);
-      *reinterpret_cast<uint2 *>(codes + (size_t)(off + k) * D + d) = make_uint2(encode4(v, inv), encode4(v + 4, inv));
+  if (WHICH == 0) {
+    const auto put = [&](int i) {
+      *reinterpret_cast<uint2 *>(codes + (size_t)off * D + (size_t)i * 8) = make_uint2(encode4(v, inv), encode4(v + 4, inv));
+    };
+#pragma unroll
+    for (int j = 0; j < kKept; ++j)
+      if ((int)threadIdx.x + j * kThreads < n * kVecs) {
+        values8<TYPE>(kept[j], v);
+        put(threadIdx.x + j * kThreads);
+      }
+    for (int i = threadIdx.x + kKept * kThreads; i < n * kVecs; i += kThreads) {
+      values8<TYPE>(read(i), v);
+      put(i);
     }
     __syncthreads();                                   // lds_max serves the next run
     return;
   }
   for (int s0 = off & ~(kSlots - 1); s0 < off + n; s0 += kSlots) {     // slots s0 .. s0 + kSlots - 1 of the block
     const int lo = max(off, s0), hi = min(off + n, s0 + kSlots);
-    for (int i = threadIdx.x; i < (hi - lo) * kVecs; i += kThreads) {
-      const int k = lo + i / kVecs, d = (i % kVecs) * 8;
-      load8<TYPE>(x, row0 + (int64_t)(k - off) * ts + d, vec, v);
-      unsigned *p = reinterpret_cast<unsigned *>(tile + (k - s0) * kPitch + d);
+    const int i0 = (lo - off) * kVecs, i1 = (hi - off) * kVecs;        // the run's elements among them
+    const auto put = [&](int i) {
+      unsigned *p = reinterpret_cast<unsigned *>(tile + (off + i / kVecs - s0) * kPitch + (i % kVecs) * 8);
       p[0] = encode4(v, inv);
       p[1] = encode4(v + 4, inv);
+    };
+#pragma unroll
+    for (int j = 0; j < kKept; ++j) {
+      const int i = threadIdx.x + j * kThreads;
+      if (i >= i0 && i < i1) {
+        values8<TYPE>(kept[j], v);
+        put(i);
+      }
+    }
+    for (int i = max(i0, kKept * kThreads) + threadIdx.x; i < i1; i += kThreads) {
+      values8<TYPE>(read(i), v);
+      put(i);
     }
     __syncthreads();
     for (int i = threadIdx.x; i < D; i += kThreads) {                  // D / 4 groups of rows x 4 groups of slots
@@ -198,21 +263,32 @@ template <int TYPE, int D>
 __global__ void __launch_bounds__(kThreads) k_store(StoreArgs a) {
   __shared__ float lds_max[kThreads / 64];
   __shared__ __attribute__((aligned(16))) uint8_t tile[kSlots * (D + 4)];
-  const int h = blockIdx.y, which = blockIdx.z, bt = 1 << a.shift;
-  const int t0 = blockIdx.x * a.span, t1 = min(t0 + a.span, a.T);
-  for (int t = t0; t < t1; ++t) {                      // everything here is the same in all threads
-    const int slot = a.slot[t];
-    if ((unsigned)slot >= (unsigned)a.slots) continue;
-    if (t > 0 && (slot & (bt - 1)) != 0 && a.slot[t - 1] == slot - 1) continue;
+  // heads vary fastest: a token's heads lie beside each other in what is read
+  const int h = blockIdx.x % a.H, which = blockIdx.y, bt = 1 << a.shift, lane = threadIdx.x & 63;
+  const int64_t t0 = (int64_t)(blockIdx.x / a.H) * a.span;
+  // the first tokens of runs among this workgroup's: every wave finds them all
+  const int64_t tl = t0 + lane;
+  int mine = -1, prior = -2;
+  if (lane < a.span && tl < a.T) {
+    mine = a.slot[tl];
+    if (tl > 0) prior = a.slot[tl - 1];
+  }
+  unsigned long long begins =
+      __ballot((unsigned)mine < (unsigned)a.slots && ((mine & (bt - 1)) == 0 || prior != mine - 1));
+  while (begins) {
+    const int b = __builtin_ctzll(begins);
+    begins &= begins - 1;
+    const int slot = __builtin_amdgcn_readlane(mine, b), t = (int)t0 + b;
     const int most = min(bt - (slot & (bt - 1)), a.T - t);
-    int n = 1;
-    for (int i = 0; i < most; i += 64) {               // the run ends at the first slot that does not follow
-      const int k = i + (threadIdx.x & 63);
+    int n = 0;
+    for (;;) {                                         // the run ends at the first slot that does not follow
+      const int k = n + lane;
       const unsigned long long follows = __ballot(k < most && a.slot[min(t + k, a.T - 1)] == slot + k);
-      n = i + (follows == ~0ull ? 64 : __builtin_ctzll(~follows));
+      n += follows == ~0ull ? 64 : __builtin_ctzll(~follows);
       if (follows != ~0ull) break;
     }
-    store_run<TYPE, D>(a, which, h, t, n, slot, lds_max, tile);
+    if (which == 0) store_run<TYPE, D, 0>(a, h, t, n, slot, lds_max, tile);
+    else store_run<TYPE, D, 1>(a, h, t, n, slot, lds_max, tile);
   }
 }
 
@@ -261,8 +337,9 @@ extern "C" festina_status festina_store_kv(const festina_kv_cache *cache, const 
   a.scale[0] = cache->k_scale;
   a.scale[1] = cache->v_scale;
   a.span = a.T <= 2048 ? 1 : 16;
-  const long long groups = ((long long)a.T + a.span - 1) / a.span;
-  const dim3 grid((unsigned)groups, a.H, 2);
+  const long long groups = ((long long)a.T + a.span - 1) / a.span * a.H;
+  if (groups > INT_MAX) return FESTINA_ERR_UNSUPPORTED;
+  const dim3 grid((unsigned)groups, 2);
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (tokens->dtype == FESTINA_BF16) launch<FESTINA_BF16>(a, cache->head_dim, grid, st);
   else if (tokens->dtype == FESTINA_F16) launch<FESTINA_F16>(a, cache->head_dim, grid, st);
