@@ -13,9 +13,9 @@
 //   from k_extend_sums, one number a chunk, or, for few requests, summed by the workgroup itself, which
 //   saves a launch.  It leaves what the fill needs of a request, and for each stretch of kFill tokens the
 //   request that its first token belongs to, so that no search crosses the whole list.
-// k_extend_fill    the slots, kFill tokens a workgroup.  A wave's 256 tokens mostly lie in one request: then
-//   everything about the request is uniform and a lane makes four slots from one or two block ids.
-//   Where they do not, each lane searches the few requests of its stretch in LDS.
+// k_extend_fill    the slots, kFill tokens a wave.  Mostly they lie in one request: then everything about the
+//   request is uniform, and a lane makes 16 slots, four at a time from one or two block ids, with all loads
+//   in flight together.  Where they do not, each lane searches the few requests of its stretch in LDS.
 // k_release        a thread per returned id, after the same sums.
 //
 // All arithmetic is on integers, so results do not depend on order.  Bound by the bytes of the slot map on
@@ -33,7 +33,7 @@ namespace {
 constexpr int kChunk = 256;          // requests a workgroup of the sums and scans
 constexpr int kGive = 64;            // requests a workgroup of the release
 constexpr int kDirect = 16384;       // up to so many requests a workgroup sums all requests before its own
-constexpr int kFill = 2048;          // slots a workgroup of the fill
+constexpr int kFill = 1024;          // slots a wave of the fill
 constexpr int kSmall = 1024;         // threads of the one-workgroup kernel, a request each
 constexpr int kSmallTokens = 8192;   // and its slots
 constexpr int kMaxRequests = 1 << 20;
@@ -50,7 +50,8 @@ struct BlockArgs {
   int4 *ends;                           // [chunks] served tokens up to the chunk's last, that request, blocks taken
   int32_t *n_free_in;                   // [1] the count before the call
   int4 *about;                          // [R] see About
-  int32_t *owner;                       // [fill workgroups] request of a stretch's first token
+  int32_t *owner;                       // [fill stretches] request of a stretch's first token
+  bool vec;                             // held, add (and done) may be read four at a time
 };
 
 // What the fill needs of a request: token t stands at position t + shift; columns from `have` on are new, column c is
@@ -70,10 +71,10 @@ __device__ __forceinline__ int blocks_of(int tokens, int shift) {
   return (int)(((unsigned)tokens + (1u << shift) - 1) >> shift);
 }
 
-__device__ __forceinline__ Demand demand(const BlockArgs &a, int r) {
+__device__ __forceinline__ Demand demand_of(const BlockArgs &a, int held, int add) {
   Demand d;
-  d.held = a.held[r];
-  d.add = a.add[r];
+  d.held = held;
+  d.add = add;
   const long long room = (long long)a.MB << a.shift;
   d.fits = d.held >= 0 && d.add >= 0 && (long long)d.held + d.add <= room;
   d.have = d.fits ? blocks_of(d.held, a.shift) : 0;
@@ -81,6 +82,8 @@ __device__ __forceinline__ Demand demand(const BlockArgs &a, int r) {
   d.takes = d.fits ? d.add : 0;
   return d;
 }
+
+__device__ __forceinline__ Demand demand(const BlockArgs &a, int r) { return demand_of(a, a.held[r], a.add[r]); }
 
 __device__ __forceinline__ int free_count(const BlockArgs &a) { return min(max(*a.n_free, 0), a.NB); }
 
@@ -107,6 +110,17 @@ __device__ __forceinline__ long long scan(long long x, long long *lds, long long
   return x + before;
 }
 
+// A wave's last served request, if it has one: the sums up to it and its index (the served ones come first).
+__device__ __forceinline__ void last_served(bool served, int tokens, int r, int blocks, int (&out)[3]) {
+  const unsigned long long m = __ballot(served);
+  const int lane = threadIdx.x & 63;
+  if (m ? lane == 63 - __builtin_clzll(m) : lane == 0) {
+    out[0] = m ? tokens : 0;
+    out[1] = m ? r : 0;
+    out[2] = m ? blocks : 0;
+  }
+}
+
 // The block of column c of a request; the table's entry is filled where the column's first token is `begins`.
 __device__ __forceinline__ int block_at(const BlockArgs &a, int r, const About &q, int c, bool begins) {
   if (c < q.have) return a.table[(size_t)r * a.MB + c];
@@ -123,22 +137,20 @@ __global__ void __launch_bounds__(N) k_extend_small(BlockArgs a) {
   __shared__ long long lds[N / 64];
   __shared__ int first[N + 1];
   __shared__ About about[N];
-  __shared__ int total, taken;
+  __shared__ int ends[N / 64][3];
   const int r = threadIdx.x;
   const int n_free = free_count(a);
   Demand d{0, 0, 0, 0, 0, false};
   if (r < a.R) d = demand(a, r);
-  if (r == 0) total = taken = 0;
   long long unused;
   const long long B = scan<N>(d.need, lds, &unused);
   const long long T = scan<N>(d.takes, lds, &unused);
   const bool served = d.fits && B <= n_free && T <= a.max_tokens;
-  if (served) {
-    atomicMax(&total, (int)T);
-    atomicMax(&taken, (int)B);
-  }
+  last_served(served, (int)T, r, (int)B, ends[threadIdx.x >> 6]);
   __syncthreads();
-  const int end = total;
+  int end = 0, taken = 0;
+#pragma unroll
+  for (int w = 0; w < N / 64; ++w) end = max(end, ends[w][0]), taken = max(taken, ends[w][2]);
   if (r < a.R) {
     const int f = (int)min(T - d.takes, (long long)end), len = served ? d.held + d.add : d.held;
     first[r] = f;
@@ -187,17 +199,25 @@ __global__ void __launch_bounds__(kChunk) k_extend_sums(BlockArgs a) {
 template <bool DIRECT>
 __global__ void __launch_bounds__(kChunk) k_extend_scan(BlockArgs a) {
   __shared__ long long lds[kChunk / 64];
-  __shared__ int ends[3];
-  const int r = blockIdx.x * kChunk + threadIdx.x;
+  __shared__ int ends[kChunk / 64][3];
+  const int r = blockIdx.x * kChunk + threadIdx.x, r0 = blockIdx.x * kChunk;
   long long b = 0, t = 0, B0, T0, unused;
-  if (threadIdx.x < 3) ends[threadIdx.x] = 0;
-  if (DIRECT) {
+  const auto count = [&](int held, int add) {
+    const Demand d = demand_of(a, held, add);
+    b += d.need;
+    t += d.takes;
+  };
+  Demand d{0, 0, 0, 0, 0, false};
+  if (r < a.R) d = demand(a, r);
+  const int n_free = free_count(a);
+  if (DIRECT && a.vec) {
 #pragma unroll 4
-    for (int i = threadIdx.x; i < (int)blockIdx.x * kChunk; i += kChunk) {
-      const Demand d = demand(a, i);
-      b += d.need;
-      t += d.takes;
+    for (int i = threadIdx.x * 4; i < r0; i += kChunk * 4) {
+      const int4 h = *reinterpret_cast<const int4 *>(a.held + i), n = *reinterpret_cast<const int4 *>(a.add + i);
+      count(h.x, n.x), count(h.y, n.y), count(h.z, n.z), count(h.w, n.w);
     }
+  } else if (DIRECT) {
+    for (int i = threadIdx.x; i < r0; i += kChunk) count(a.held[i], a.add[i]);
   } else {
     for (int i = threadIdx.x; i < (int)blockIdx.x; i += kChunk) {
       b += a.sum_blocks[i];
@@ -206,11 +226,8 @@ __global__ void __launch_bounds__(kChunk) k_extend_scan(BlockArgs a) {
   }
   scan<kChunk>(b, lds, &B0);
   scan<kChunk>(t, lds, &T0);
-  Demand d{0, 0, 0, 0, 0, false};
-  if (r < a.R) d = demand(a, r);
   const long long B = B0 + scan<kChunk>(d.need, lds, &unused);
   const long long T = T0 + scan<kChunk>(d.takes, lds, &unused);
-  const int n_free = free_count(a);
   const bool served = d.fits && B <= n_free && T <= a.max_tokens;
   if (r < a.R) {
     const int f = (int)min(T - d.takes, (long long)a.max_tokens);   // the fill takes the least of this and the total
@@ -221,56 +238,84 @@ __global__ void __launch_bounds__(kChunk) k_extend_scan(BlockArgs a) {
   }
   if (served && d.takes) {
     const int f = (int)(T - d.takes), e = (int)T;
-    for (int w = (f + kFill - 1) / kFill; w * kFill < e; ++w) a.owner[w] = r;
-    atomicMax(&ends[0], e);
-    atomicMax(&ends[1], r);
-    atomicMax(&ends[2], (int)B);
+    for (int w = (f + kFill - 1) / kFill; w < (e + kFill - 1) / kFill; ++w) a.owner[w] = r;
   }
+  last_served(served && d.takes, (int)T, r, (int)B, ends[threadIdx.x >> 6]);
   __syncthreads();
   if (threadIdx.x == 0) {
-    a.ends[blockIdx.x] = make_int4(ends[0], ends[1], ends[2], 0);
+    int4 e = make_int4(0, 0, 0, 0);
+#pragma unroll
+    for (int w = 0; w < kChunk / 64; ++w)
+      e = make_int4(max(e.x, ends[w][0]), max(e.y, ends[w][1]), max(e.z, ends[w][2]), 0);
+    a.ends[blockIdx.x] = e;
     if (blockIdx.x == 0) *a.n_free_in = n_free;
   }
 }
 
 __global__ void __launch_bounds__(256) k_extend_fill(BlockArgs a, int32_t chunks, int32_t fills, int32_t vec) {
-  constexpr int kList = kFill + 256;
-  __shared__ int first[kList];
-  __shared__ int ends[4][3];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int e0 = 0, e1 = 0, e2 = 0;
-  for (int i = threadIdx.x; i < chunks; i += 256) {
+  constexpr int kList = kFill + 64, kGroups = kFill / 256;
+  __shared__ int lists[4][kList];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, bt = 1 << a.shift;
+  int *first = lists[wave];
+  int end = 0, last = 0, taken = 0;
+  for (int i = lane; i < chunks; i += 64) {
     const int4 e = a.ends[i];
-    e0 = max(e0, e.x), e1 = max(e1, e.y), e2 = max(e2, e.z);
+    end = max(end, e.x), last = max(last, e.y), taken = max(taken, e.z);
   }
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) {
-    e0 = max(e0, __shfl_xor(e0, d));
-    e1 = max(e1, __shfl_xor(e1, d));
-    e2 = max(e2, __shfl_xor(e2, d));
+    end = max(end, __shfl_xor(end, d));
+    last = max(last, __shfl_xor(last, d));
+    taken = max(taken, __shfl_xor(taken, d));
   }
-  if (lane == 0) ends[wave][0] = e0, ends[wave][1] = e1, ends[wave][2] = e2;
-  __syncthreads();
-  const int end = max(max(ends[0][0], ends[1][0]), max(ends[2][0], ends[3][0]));
-  const int last = max(max(ends[0][1], ends[1][1]), max(ends[2][1], ends[3][1]));
-  // the scan's first tokens of requests that are not served lie past the end
-  for (int i = blockIdx.x * 256 + threadIdx.x; i <= a.R; i += gridDim.x * 256) {
-    if (i == a.R || a.first[i] > end) a.first[i] = end;
-    if (i < a.R) a.length[i] = a.about[i].w;
-  }
-  if (blockIdx.x == 0 && threadIdx.x == 0)
-    *a.n_free_out = *a.n_free_in - max(max(ends[0][2], ends[1][2]), max(ends[2][2], ends[3][2]));
-  const int bt = 1 << a.shift;
-  for (int w = blockIdx.x; w < fills; w += gridDim.x) {
-    const int t0 = w * kFill;
-    int lo0 = 0, n = 0;
-    if (t0 < end) {
-      lo0 = a.owner[w];
-      n = (t0 + kFill < end ? a.owner[w + 1] : last) - lo0 + 1;           // requests lo0 .. lo0 + n - 1
+  end = __builtin_amdgcn_readfirstlane(end);
+  const auto put = [&](int t, const int (&s)[4]) {
+    if (vec && t + 4 <= a.max_tokens) {
+      *reinterpret_cast<int4 *>(a.slot + t) = make_int4(s[0], s[1], s[2], s[3]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (t + i < a.max_tokens) a.slot[t + i] = s[i];
     }
-    __syncthreads();
-    for (int i = threadIdx.x; i < min(n, kList); i += 256) first[i] = a.first[lo0 + i];
-    __syncthreads();
+  };
+  for (int w = blockIdx.x * 4 + wave; w < fills; w += gridDim.x * 4) {
+    const int t0 = w * kFill;
+    int lo0 = 0, n = 0;                                // requests lo0 .. lo0 + n - 1
+    if (t0 < end) {
+      lo0 = __builtin_amdgcn_readfirstlane(a.owner[w]);
+      n = __builtin_amdgcn_readfirstlane(t0 + kFill < end ? a.owner[w + 1] : last) - lo0 + 1;
+    }
+    // Four slots from the lane's token t on, all of request r; tokens past `tail` get none.
+    const auto quad = [&](int r, const About &q, int t, int tail) {
+      const int p = t + q.shift, c = p >> a.shift, o = p & (bt - 1), over = o + 3 - (bt - 1) - max(t + 3 - tail, 0);
+      int2 id = make_int2(-1, -1);
+      if (t <= tail) {
+        id.x = block_at(a, r, q, c, o == 0);
+        if (over > 0) id.y = block_at(a, r, q, c + 1, true);
+      }
+      return id;
+    };
+    const auto slots = [&](const About &q, int t, int tail, int2 id) {
+      const int o = (t + q.shift) & (bt - 1);
+      int s[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        s[i] = t + i > tail ? -1 : o + i < bt ? slot_of(a, id.x, o + i) : slot_of(a, id.y, o + i - bt);
+      put(t, s);
+    };
+    if (n <= 1) {                                      // one request, or none
+      const int4 q4 = n ? a.about[lo0] : make_int4(0, 0, 0, 0);
+      const About q{q4.x, q4.y, q4.z, q4.w};
+      const int tail = n ? min(t0 + kFill, end) - 1 : -1;
+      int2 id[kGroups];
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) id[g] = quad(lo0, q, t0 + g * 256 + lane * 4, tail);
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) slots(q, t0 + g * 256 + lane * 4, tail, id[g]);
+      continue;
+    }
+    for (int i = lane; i < min(n, kList); i += 64) first[i] = a.first[lo0 + i];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     const auto start = [&](int i) { return i < kList ? first[i] : a.first[lo0 + i]; };
     const auto owner = [&](int t, int lo) {            // the request of token t, lo0 + lo or later
       int hi = n;
@@ -281,63 +326,55 @@ __global__ void __launch_bounds__(256) k_extend_fill(BlockArgs a, int32_t chunks
       return lo;
     };
     int from = 0;
-    for (int g = 0; g < kFill / 1024; ++g) {
-      const int tw = t0 + g * 1024 + wave * 256, t = tw + lane * 4;       // the wave's tokens, the lane's
+    for (int g = 0; g < kGroups; ++g) {
+      const int tw = t0 + g * 256, t = tw + lane * 4, tail = min(tw + 255, end - 1);
       if (tw >= a.max_tokens) break;
+      if (tw < end) from = __builtin_amdgcn_readfirstlane(owner(tw, from));
+      if (tw < end && (from + 1 >= n || start(from + 1) > tail)) {
+        const int4 q4 = a.about[lo0 + from];
+        const About q{q4.x, q4.y, q4.z, q4.w};
+        slots(q, t, tail, quad(lo0 + from, q, t, tail));
+        continue;
+      }
       int s[4] = {-1, -1, -1, -1};
-      if (tw < end) {
-        from = __builtin_amdgcn_readfirstlane(owner(tw, from));
-        const int tail = min(tw + 255, end - 1);
-        if (from + 1 >= n || start(from + 1) > tail) {
-          // one request
-          const int r = lo0 + from;
-          const int4 q4 = a.about[r];
-          const About q{q4.x, q4.y, q4.z, q4.w};
-          const int p = t + q.shift, c = p >> a.shift, o = p & (bt - 1);
-          if (t <= tail) {
-            const int id = block_at(a, r, q, c, o == 0);
-            const int over = o + 3 - (bt - 1), more = t + 3 <= tail ? over : over - (t + 3 - tail);
-            const int next = more > 0 ? block_at(a, r, q, c + 1, true) : 0;
+      if (t < end) {
+        int i = owner(t, from), r = -1, stop = t, c = -1, id = 0;         // stop: where request r's tokens end
+        About q{};
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              s[i] = t + i > tail ? -1 : o + i < bt ? slot_of(a, id, o + i) : slot_of(a, next, o + i - bt);
+        for (int k = 0; k < 4; ++k) {
+          if (t + k >= end) break;
+          if (t + k >= stop) {
+            if (r >= 0) ++i;
+            while (i + 1 < n && start(i + 1) <= t + k) ++i;
+            stop = i + 1 < n ? min(start(i + 1), end) : end;
+            r = lo0 + i;
+            const int4 q4 = a.about[r];
+            q = About{q4.x, q4.y, q4.z, q4.w};
+            c = -1;
           }
-        } else if (t < end) {
-          int i = owner(t, from), r = -1, stop = t, c = -1, id = 0;       // stop: where request r's tokens end
-          About q{};
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            if (t + k >= end) break;
-            if (t + k >= stop) {
-              if (r >= 0) ++i;
-              while (i + 1 < n && start(i + 1) <= t + k) ++i;
-              stop = i + 1 < n ? min(start(i + 1), end) : end;
-              r = lo0 + i;
-              const int4 q4 = a.about[r];
-              q = About{q4.x, q4.y, q4.z, q4.w};
-              c = -1;
-            }
-            const int p = t + k + q.shift, o = p & (bt - 1);
-            if (p >> a.shift != c) id = block_at(a, r, q, c = p >> a.shift, o == 0);
-            s[k] = slot_of(a, id, o);
-          }
+          const int p = t + k + q.shift, o = p & (bt - 1);
+          if (p >> a.shift != c) id = block_at(a, r, q, c = p >> a.shift, o == 0);
+          s[k] = slot_of(a, id, o);
         }
       }
-      if (vec && t + 4 <= a.max_tokens) {
-        *reinterpret_cast<int4 *>(a.slot + t) = make_int4(s[0], s[1], s[2], s[3]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (t + i < a.max_tokens) a.slot[t + i] = s[i];
-      }
+      put(t, s);
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
+  // the scan's first tokens of requests that are not served lie past the end
+  for (int i = blockIdx.x * 256 + threadIdx.x; i <= a.R; i += gridDim.x * 256) {
+    if (i == a.R || a.first[i] > end) a.first[i] = end;
+    if (i < a.R) a.length[i] = a.about[i].w;
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.n_free_out = *a.n_free_in - taken;
 }
 
-__device__ __forceinline__ int returned(const BlockArgs &a, int r, int *held) {
+__device__ __forceinline__ long long returned_of(const BlockArgs &a, int held, unsigned done) {
+  return done && held >= 0 && held <= ((long long)a.MB << a.shift) ? blocks_of(held, a.shift) : 0;
+}
+__device__ __forceinline__ long long returned(const BlockArgs &a, int r, int *held) {
   *held = a.held[r];
-  const bool ok = *held >= 0 && *held <= ((long long)a.MB << a.shift);
-  return a.done[r] && ok ? blocks_of(*held, a.shift) : 0;
+  return returned_of(a, *held, a.done[r]);
 }
 
 __global__ void __launch_bounds__(kChunk) k_release_sums(BlockArgs a) {
@@ -364,8 +401,15 @@ __global__ void __launch_bounds__(kChunk) k_release(BlockArgs a) {
   const int n_free = DIRECT ? free_count(a) : *a.n_free_in;
   long long b = 0, B0, all;
   int held = 0;
-  if (DIRECT) {
+  if (DIRECT && a.vec) {
 #pragma unroll 4
+    for (int i = threadIdx.x * 4; i < r0; i += kChunk * 4) {
+      const int4 x = *reinterpret_cast<const int4 *>(a.held + i);
+      const unsigned done = *reinterpret_cast<const unsigned *>(a.done + i);
+      b += returned_of(a, x.x, done & 0xffu) + returned_of(a, x.y, done & 0xff00u) +
+           returned_of(a, x.z, done & 0xff0000u) + returned_of(a, x.w, done & 0xff000000u);
+    }
+  } else if (DIRECT) {
     for (int i = threadIdx.x; i < r0; i += kChunk) b += returned(a, i, &held);
   } else {
     for (int i = threadIdx.x; i < (int)blockIdx.x; i += kChunk) b += a.sum_blocks[i];
@@ -472,13 +516,14 @@ extern "C" festina_status festina_extend_blocks(const festina_kv_requests *req, 
     const int chunks = max((a.R + kChunk - 1) / kChunk, 1);
     const int fills = (a.max_tokens + kFill - 1) / kFill;
     const bool vec = (reinterpret_cast<uintptr_t>(a.slot) & 15) == 0;
+    a.vec = ((reinterpret_cast<uintptr_t>(a.held) | reinterpret_cast<uintptr_t>(a.add)) & 15) == 0;
     if (a.R <= kDirect) {
       k_extend_scan<true><<<chunks, kChunk, 0, st>>>(a);
     } else {
       k_extend_sums<<<chunks, kChunk, 0, st>>>(a);
       k_extend_scan<false><<<chunks, kChunk, 0, st>>>(a);
     }
-    k_extend_fill<<<min(max(max(fills, chunks), 1), 4096), 256, 0, st>>>(a, chunks, fills, vec);
+    k_extend_fill<<<min(max(max((fills + 3) / 4, chunks), 1), 8192), 256, 0, st>>>(a, chunks, fills, vec);
   }
   return hipGetLastError() == hipSuccess ? FESTINA_OK : FESTINA_ERR_DEVICE;
 }
@@ -491,6 +536,7 @@ extern "C" festina_status festina_release_blocks(const festina_kv_requests *req,
   if (bad != FESTINA_OK) return bad;
   if (a.R > 0 && !done) return FESTINA_ERR_INVALID;
   a.done = done;
+  a.vec = ((reinterpret_cast<uintptr_t>(a.held) & 15) | (reinterpret_cast<uintptr_t>(done) & 3)) == 0;
   hipStream_t st = static_cast<hipStream_t>(stream);
   // one workgroup reads everything before it writes anything; several may only where they write elsewhere
   const bool apart = a.length != a.held && a.n_free_out != a.n_free;

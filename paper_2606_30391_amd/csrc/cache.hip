@@ -336,7 +336,9 @@ extern "C" festina_status festina_store_kv(const festina_kv_cache *cache, const 
   a.codes[1] = cache->v;
   a.scale[0] = cache->k_scale;
   a.scale[1] = cache->v_scale;
-  a.span = a.T <= 2048 ? 1 : 16;
+  // few tokens: a workgroup each, so that runs of single tokens are not done one after the other; many: enough that
+  // most workgroups have a run to store (they are dispatched at a rate that empty ones take their share of)
+  a.span = (int)min(max((long long)a.T * a.H / 4096, 1ll), (long long)kSlots);
   const long long groups = ((long long)a.T + a.span - 1) / a.span * a.H;
   if (groups > INT_MAX) return FESTINA_ERR_UNSUPPORTED;
   const dim3 grid((unsigned)groups, 2);
