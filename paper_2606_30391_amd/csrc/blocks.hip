@@ -13,9 +13,9 @@
 //   from k_extend_sums, one number a chunk, or, for few requests, summed by the workgroup itself, which
 //   saves a launch.  It leaves what the fill needs of a request, and for each stretch of kFill tokens the
 //   request that its first token belongs to, so that no search crosses the whole list.
-// k_extend_fill    the slots, kFill tokens a wave.  Mostly they lie in one request: then everything about the
-//   request is uniform, and a lane makes 16 slots, four at a time from one or two block ids, with all loads
-//   in flight together.  Where they do not, each lane searches the few requests of its stretch in LDS.
+// k_extend_fill    the slots, a stretch of 256 or 1,024 tokens a wave.  Where they lie in one request, everything
+//   about it is uniform, and a lane makes its slots four at a time from one or two block ids, with all loads in
+//   flight together.  Where they do not, each lane searches the few requests of its stretch in LDS.
 // k_release        a thread per returned id, after the same sums.
 //
 // All arithmetic is on integers, so results do not depend on order.  Bound by the bytes of the slot map on
@@ -33,7 +33,10 @@ namespace {
 constexpr int kChunk = 256;          // requests a workgroup of the sums and scans
 constexpr int kGive = 64;            // requests a workgroup of the release
 constexpr int kDirect = 16384;       // up to so many requests a workgroup sums all requests before its own
-constexpr int kFill = 1024;          // slots a wave of the fill
+// Slots a wave of the fill, in groups of 256: long stretches from the size on that gives every wave slot of the chip
+// one (2.2 M slots of 4,096 requests 13 us with long stretches, 10 with short ones; 42.5 M: 65 and 82).
+constexpr int kGroupsMost = 4;
+constexpr int kLongFills = 8 << 20;
 constexpr int kSmall = 1024;         // threads of the one-workgroup kernel, a request each
 constexpr int kSmallTokens = 8192;   // and its slots
 constexpr int kMaxRequests = 1 << 20;
@@ -51,6 +54,7 @@ struct BlockArgs {
   int32_t *n_free_in;                   // [1] the count before the call
   int4 *about;                          // [R] see About
   int32_t *owner;                       // [fill stretches] request of a stretch's first token
+  int32_t fill;                         // slots of a stretch
   bool vec;                             // held, add (and done) may be read four at a time
 };
 
@@ -75,8 +79,8 @@ __device__ __forceinline__ Demand demand_of(const BlockArgs &a, int held, int ad
   Demand d;
   d.held = held;
   d.add = add;
-  const long long room = (long long)a.MB << a.shift;
-  d.fits = d.held >= 0 && d.add >= 0 && (long long)d.held + d.add <= room;
+  const int room = a.MB << a.shift;                    // fits 32 bits
+  d.fits = held >= 0 && add >= 0 && held <= room && add <= room - held;
   d.have = d.fits ? blocks_of(d.held, a.shift) : 0;
   d.need = d.fits ? blocks_of(d.held + d.add, a.shift) - d.have : 0;
   d.takes = d.fits ? d.add : 0;
@@ -238,7 +242,7 @@ __global__ void __launch_bounds__(kChunk) k_extend_scan(BlockArgs a) {
   }
   if (served && d.takes) {
     const int f = (int)(T - d.takes), e = (int)T;
-    for (int w = (f + kFill - 1) / kFill; w < (e + kFill - 1) / kFill; ++w) a.owner[w] = r;
+    for (int w = (int)(((unsigned)f + a.fill - 1) / a.fill); w * (long long)a.fill < e; ++w) a.owner[w] = r;
   }
   last_served(served && d.takes, (int)T, r, (int)B, ends[threadIdx.x >> 6]);
   __syncthreads();
@@ -252,8 +256,9 @@ __global__ void __launch_bounds__(kChunk) k_extend_scan(BlockArgs a) {
   }
 }
 
+template <int kGroups>
 __global__ void __launch_bounds__(256) k_extend_fill(BlockArgs a, int32_t chunks, int32_t fills, int32_t vec) {
-  constexpr int kList = kFill + 64, kGroups = kFill / 256;
+  constexpr int kFill = kGroups * 256, kList = kFill + 64;
   __shared__ int lists[4][kList];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, bt = 1 << a.shift;
   int *first = lists[wave];
@@ -369,10 +374,11 @@ __global__ void __launch_bounds__(256) k_extend_fill(BlockArgs a, int32_t chunks
   if (blockIdx.x == 0 && threadIdx.x == 0) *a.n_free_out = *a.n_free_in - taken;
 }
 
-__device__ __forceinline__ long long returned_of(const BlockArgs &a, int held, unsigned done) {
-  return done && held >= 0 && held <= ((long long)a.MB << a.shift) ? blocks_of(held, a.shift) : 0;
+// At most 2^27 blocks.
+__device__ __forceinline__ int returned_of(const BlockArgs &a, int held, unsigned done) {
+  return done && held >= 0 && held <= (a.MB << a.shift) ? blocks_of(held, a.shift) : 0;
 }
-__device__ __forceinline__ long long returned(const BlockArgs &a, int r, int *held) {
+__device__ __forceinline__ int returned(const BlockArgs &a, int r, int *held) {
   *held = a.held[r];
   return returned_of(a, *held, a.done[r]);
 }
@@ -402,7 +408,7 @@ __global__ void __launch_bounds__(kChunk) k_release(BlockArgs a) {
   long long b = 0, B0, all;
   int held = 0;
   if (DIRECT && a.vec) {
-#pragma unroll 4
+#pragma unroll 8
     for (int i = threadIdx.x * 4; i < r0; i += kChunk * 4) {
       const int4 x = *reinterpret_cast<const int4 *>(a.held + i);
       const unsigned done = *reinterpret_cast<const unsigned *>(a.done + i);
@@ -419,15 +425,24 @@ __global__ void __launch_bounds__(kChunk) k_release(BlockArgs a) {
   const long long own = scan<kChunk>(mine ? returned(a, r, &held) : 0, lds, &all);
   if (threadIdx.x < kOwn) ends[threadIdx.x] = own;
   __syncthreads();
-  for (long long i = threadIdx.x; i < all; i += kChunk) {
-    int lo = -1, hi = kOwn - 1;                            // ends[lo] <= i < ends[hi]
-    while (hi - lo > 1) {
-      const int m = (lo + hi) >> 1;
-      if (ends[m] <= i) lo = m; else hi = m;
+  for (long long i0 = threadIdx.x; i0 < all; i0 += 4 * kChunk) {
+    int id[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {                          // four ids in flight
+      const long long i = i0 + k * kChunk;
+      int lo = -1, hi = kOwn - 1;                          // ends[lo] <= i < ends[hi]
+      while (hi - lo > 1) {
+        const int m = (lo + hi) >> 1;
+        if (ends[m] <= i) lo = m; else hi = m;
+      }
+      const int c = (int)(i - (hi ? ends[hi - 1] : 0));
+      if (i < all) id[k] = a.table[(size_t)(r0 + hi) * a.MB + c];
     }
-    const int c = (int)(i - (hi ? ends[hi - 1] : 0));
-    const long long at = n_free + B0 + i;
-    if (at < a.NB) a.free_ids[at] = a.table[(size_t)(r0 + hi) * a.MB + c];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const long long i = i0 + k * kChunk, at = n_free + B0 + i;
+      if (i < all && at < a.NB) a.free_ids[at] = id[k];
+    }
   }
   if (mine) a.length[r] = a.done[r] ? 0 : held;
   if (threadIdx.x == 0 && r0 + kOwn >= a.R) *a.n_free_out = (int)min(n_free + B0 + all, (long long)a.NB);
@@ -441,7 +456,7 @@ size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 
 Layout layout(int R, int max_tokens) {
   Layout l;
-  const size_t chunks = R > 0 ? ((size_t)R + kChunk - 1) / kChunk : 1, fills = ((size_t)max_tokens + kFill - 1) / kFill;
+  const size_t chunks = R > 0 ? ((size_t)R + kChunk - 1) / kChunk : 1, fills = ((size_t)max_tokens + 255) / 256;
   l.sum_blocks = 0;
   l.sum_tokens = up(chunks * 8);
   l.ends = l.sum_tokens + up(chunks * 8);
@@ -514,7 +529,8 @@ extern "C" festina_status festina_extend_blocks(const festina_kv_requests *req, 
     k_extend_small<kSmall><<<1, kSmall, 0, st>>>(a);
   } else {
     const int chunks = max((a.R + kChunk - 1) / kChunk, 1);
-    const int fills = (a.max_tokens + kFill - 1) / kFill;
+    a.fill = a.max_tokens >= kLongFills ? kGroupsMost * 256 : 256;
+    const int fills = (int)(((long long)a.max_tokens + a.fill - 1) / a.fill);
     const bool vec = (reinterpret_cast<uintptr_t>(a.slot) & 15) == 0;
     a.vec = ((reinterpret_cast<uintptr_t>(a.held) | reinterpret_cast<uintptr_t>(a.add)) & 15) == 0;
     if (a.R <= kDirect) {
@@ -523,7 +539,9 @@ extern "C" festina_status festina_extend_blocks(const festina_kv_requests *req, 
       k_extend_sums<<<chunks, kChunk, 0, st>>>(a);
       k_extend_scan<false><<<chunks, kChunk, 0, st>>>(a);
     }
-    k_extend_fill<<<min(max(max((fills + 3) / 4, chunks), 1), 8192), 256, 0, st>>>(a, chunks, fills, vec);
+    const int grid = min(max(max((fills + 3) / 4, chunks), 1), 8192);
+    if (a.fill > 256) k_extend_fill<kGroupsMost><<<grid, 256, 0, st>>>(a, chunks, fills, vec);
+    else k_extend_fill<1><<<grid, 256, 0, st>>>(a, chunks, fills, vec);
   }
   return hipGetLastError() == hipSuccess ? FESTINA_OK : FESTINA_ERR_DEVICE;
 }

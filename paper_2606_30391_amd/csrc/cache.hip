@@ -41,12 +41,16 @@ struct StoreArgs {
 
 __device__ __forceinline__ bool finite(float x) { return __builtin_fabsf(x) < __builtin_inff(); }
 
-// Four codes; `inv` is the scale's reciprocal, a power of two.
-__device__ __forceinline__ unsigned encode4(const float *x, float inv) {
+// Four codes; `inv` is the scale's reciprocal, a power of two.  Elements of at most 448 times the scale need nothing
+// else (the conversion keeps NaN); `careful` where some may be larger or infinite.
+__device__ __forceinline__ unsigned encode4(const float *x, float inv, bool careful) {
   float y[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    y[i] = finite(x[i]) ? fminf(fmaxf(x[i] * inv, -448.f), 448.f) : __builtin_nanf("");
+  for (int i = 0; i < 4; ++i) y[i] = x[i] * inv;
+  if (careful) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = finite(x[i]) ? fminf(fmaxf(y[i], -448.f), 448.f) : __builtin_nanf("");
+  }
   int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
   w = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
   return (unsigned)w;
@@ -141,26 +145,40 @@ __device__ __forceinline__ void store_run(const StoreArgs &a, int h, int t, int 
 #pragma unroll
   for (int j = 0; j < kKept; ++j)
     if ((int)threadIdx.x + j * kThreads < n * kVecs) kept[j] = read(threadIdx.x + j * kThreads);
-  const auto widen = [&]() {
+  const auto join = [&]() {                            // over the workgroup
 #pragma unroll
-    for (int j = 0; j < 8; ++j) amax = fmaxf(amax, finite(v[j]) ? __builtin_fabsf(v[j]) : 0.f);
+    for (int d = 32; d > 0; d >>= 1) amax = fmaxf(amax, __shfl_xor(amax, d));
+    if ((threadIdx.x & 63) == 0) lds_max[threadIdx.x >> 6] = amax;
+    __syncthreads();
+    amax = fmaxf(fmaxf(lds_max[0], lds_max[1]), fmaxf(lds_max[2], lds_max[3]));
   };
+  // the maximum leaves NaN out by itself
 #pragma unroll
   for (int j = 0; j < kKept; ++j)
     if ((int)threadIdx.x + j * kThreads < n * kVecs) {
       values8<TYPE>(kept[j], v);
-      widen();
+#pragma unroll
+      for (int k = 0; k < 8; ++k) amax = fmaxf(amax, __builtin_fabsf(v[k]));
     }
   for (int i = threadIdx.x + kKept * kThreads; i < n * kVecs; i += kThreads) {
     values8<TYPE>(read(i), v);
-    widen();
-  }
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) amax = fmaxf(amax, __shfl_xor(amax, d));
-  if ((threadIdx.x & 63) == 0) lds_max[threadIdx.x >> 6] = amax;
-  __syncthreads();
-  amax = fmaxf(fmaxf(lds_max[0], lds_max[1]), fmaxf(lds_max[2], lds_max[3]));
+    for (int k = 0; k < 8; ++k) amax = fmaxf(amax, __builtin_fabsf(v[k]));
+  }
+  join();
+  bool careful = !finite(amax);
+  if (careful) {                                       // infinities: once more without them
+    __syncthreads();
+    amax = 0.f;
+    for (int i = threadIdx.x; i < n * kVecs; i += kThreads) {
+      values8<TYPE>(read(i), v);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) amax = fmaxf(amax, finite(v[k]) ? __builtin_fabsf(v[k]) : 0.f);
+    }
+    join();
+  }
   float scale = scale_of(amax);
+  careful |= scale == kScaleMax;
   if (off > 0) scale = fmaxf(scale, old);
   const float inv = 1.f / scale;                       // exact
   if (threadIdx.x == 0) a.scale[WHICH][bh] = scale;
@@ -191,7 +209,7 @@ __device__ __forceinline__ void store_run(const StoreArgs &a, int h, int t, int 
   }
   if (WHICH == 0) {
     const auto put = [&](int i) {
-      *reinterpret_cast<uint2 *>(codes + (size_t)off * D + (size_t)i * 8) = make_uint2(encode4(v, inv), encode4(v + 4, inv));
+      *reinterpret_cast<uint2 *>(codes + (size_t)off * D + (size_t)i * 8) = make_uint2(encode4(v, inv, careful), encode4(v + 4, inv, careful));
     };
 #pragma unroll
     for (int j = 0; j < kKept; ++j)
@@ -211,8 +229,8 @@ __device__ __forceinline__ void store_run(const StoreArgs &a, int h, int t, int 
     const int i0 = (lo - off) * kVecs, i1 = (hi - off) * kVecs;        // the run's elements among them
     const auto put = [&](int i) {
       unsigned *p = reinterpret_cast<unsigned *>(tile + (off + i / kVecs - s0) * kPitch + (i % kVecs) * 8);
-      p[0] = encode4(v, inv);
-      p[1] = encode4(v + 4, inv);
+      p[0] = encode4(v, inv, careful);
+      p[1] = encode4(v + 4, inv, careful);
     };
 #pragma unroll
     for (int j = 0; j < kKept; ++j) {
