@@ -5,18 +5,18 @@
 // and one pass over the keys keeps, for each query row, the running maximum m of y_j = x_j + log2 vs_j, the sum
 // l = sum 2^(y_j - m) / vs_j and the vector o = sum 2^(y_j - m) vc_j; then out = o / l and
 // lse = (m + log2 l) ln 2.  Folding vs into the exponent costs nothing (the scaling of the logit
-// is a fused multiply-add either way), leaves weights of at most 1 for the second product, and lets the codes
+// is a fused multiply-add either way), leaves weights of bounded size for the second product, and lets the codes
 // be its other operand as they are.
 //
 // Both products run on the matrix cores, keys (and values' dims) as rows and queries as columns: S' = K Q' and
 // O' = V' P'.  A column then stays in the same lanes through both, so P goes from the first product's
 // result straight into the second's operand: the keys of a tile are dealt to the first product's rows in the
 // order in which the second wants them, and no value crosses lanes but the maximum and the sum.  Codes are
-// converted exactly (e4m3 fits bfloat16 and half); q keeps its own type, the weights (at most 1) and the value
+// converted exactly (e4m3 fits bfloat16 and half); q keeps its own type, the weights and the value
 // codes are taken in half precision, whose 11 bits leave less error than the outputs' rounding; sums are
 // float32.
 //
-// k_rows    up to 64 query rows a request and key head (single tokens, short runs): 16 NT rows against 64 keys
+// k_rows    up to 64 query rows (16 to 64, as registers allow) a request and key head (single tokens, short runs): 16 NT rows against 64 keys
 //   per wave and step, operands loaded from the cache into the lanes that use them.  Bound by the cache's bytes.
 //   All requests' keys form one line of 64-key units, cut into equal pieces, one a wave, so that
 //   ragged lengths leave no wave behind; a row tile that a cut falls into is joined by k_rows_join.
@@ -30,6 +30,7 @@
 #include <climits>
 #include <cstddef>
 #include <cstdint>
+#include <cstdlib>
 
 #include "festina.h"
 #include "kv.h"
@@ -55,7 +56,6 @@ constexpr int kBlock = 64 * kWaves;
 constexpr int kWorkers = 2048;       // pieces that k_rows cuts the keys into: two waves a SIMD
 constexpr int kGroups = 512;         // workgroups of k_tiles that fill the chip: two a compute unit
 constexpr int kListed = 512;         // requests whose running sums a workgroup forms by itself
-constexpr int kTileRows = 128;
 constexpr int kMaxRequests = 1 << 20;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -68,6 +68,7 @@ struct AttArgs {
   int32_t rows_max;                  // requests of at most so many rows are k_rows' (the others k_tiles')
   int32_t tiles_each;                // k_rows without cuts: row tiles a request
   int32_t workers, splits;
+  int32_t tile_rows;                 // query rows a workgroup of k_tiles
   float scale;                       // times log2 e
   const int32_t *table, *length, *first;
   const void *q;
@@ -129,7 +130,7 @@ __device__ __forceinline__ long long units_of(const AttArgs &a, int r) {
 
 __device__ __forceinline__ long long tiles_of(const AttArgs &a, int r) {
   const int rows = request(a, r).n * a.G;
-  return rows > a.rows_max ? cdiv(rows, kTileRows) : 0;
+  return rows > a.rows_max ? cdiv(rows, a.tile_rows) : 0;
 }
 
 // Running sums over a workgroup of N threads: returns the exclusive sum and the whole.
@@ -280,6 +281,22 @@ __device__ __forceinline__ unsigned below(int n, int w) {
   return k >= 4 ? ~0u : k <= 0 ? 0u : (1u << (8 * k)) - 1;
 }
 
+// A row's weights are taken relative to a reference m that follows its maximum only in strides: logits are formed
+// relative to it, and while none exceeds it by more than 2^kSlack nothing has to be rescaled (weights of up
+// to 2^8 are as exact in half precision as those of up to 1).  -inf: no key seen yet, logits are relative to 0.
+constexpr float kSlack = 8.f;
+__device__ __forceinline__ bool raises(float top, float m) { return top > (m == kNegInf() ? kNegInf() : kSlack); }
+// Takes `top` (relative to m) as the new reference where it raises it, else sets it to 0; scales l and returns the
+// factor for the row's other sums.
+__device__ __forceinline__ float raise(float &top, float &m, float &l) {
+  const bool fresh = m == kNegInf();
+  if (!raises(top, m)) top = 0.f;
+  else m = fresh ? top : m + top;
+  const float f = fresh ? 1.f : exp2_(-top);
+  l *= f;
+  return f;
+}
+
 // Weight of a piece with maximum m in a row whose maximum is M.
 __device__ __forceinline__ float weight(float m, float M) { return m == kNegInf() ? 0.f : exp2_(m - M); }
 
@@ -361,15 +378,16 @@ struct Rows {
       }
     }
     const float c = a.scale * s.ks, vs = fminf(fmaxf(s.vs, kScaleMin), kScaleMax);
-    const float lv = log2_(vs), iv = 1.f / vs;
+    const float lv = log2_(vs), iv = __builtin_amdgcn_rcpf(vs);
     const bool masked = base + kUnit - 1 > pos_min || (a.window > 0 && base <= pos_max - a.window) || __any(!s.ok);
     h8 w[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
+      const float shift = st.m[nt] == kNegInf() ? lv : lv - st.m[nt];
 #pragma unroll
       for (int u = 0; u < 4; ++u)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[nt][u][i] = fmaf(x[nt][u][i], c, lv);
+        for (int i = 0; i < 4; ++i) x[nt][u][i] = fmaf(x[nt][u][i], c, shift);
       if (masked) {
         rarely();
         const Span sees{st.sees[nt].from - base - 16 * g, s.ok ? st.sees[nt].count : 0};
@@ -384,21 +402,20 @@ struct Rows {
 #pragma unroll
         for (int i = 0; i < 4; ++i) top = fmaxf(top, x[nt][u][i]);
       top = across32(across16(top, max_), max_);
-      const float was = st.m[nt];
-      if (__any(top > was)) {
-        const float now = fmaxf(was, top), f = weight(was, now);
-        st.m[nt] = now;
-        st.l[nt] *= f;
+      if (__any(raises(top, st.m[nt]))) {
+        rarely();
+        const float f = raise(top, st.m[nt], st.l[nt]);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) x[nt][u] -= top;
 #pragma unroll
         for (int t = 0; t < D / 16; ++t) st.o[nt][t] *= f;
       }
-      const float m = st.m[nt] == kNegInf() ? 0.f : st.m[nt];
       float sum = 0.f;
 #pragma unroll
       for (int u = 0; u < 4; ++u)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float p = exp2_(x[nt][u][i] - m);
+          const float p = exp2_(x[nt][u][i]);
           sum += p;
           w[nt][u >> 1][(u & 1) * 4 + i] = (f16)p;
         }
@@ -657,110 +674,133 @@ __global__ void __launch_bounds__(kBlock) k_rows_join(AttArgs a) {
 
 // ------------------------------------------------------------------ k_tiles
 
-template <typename T, int D>
+template <typename T, int D, int W>
 struct Tiles {
+  static constexpr int kThreads = 64 * W, kTileRows = 32 * W;
   static constexpr int kPitchK = D + 8, kPitchV = kUnit + 8;
-  static constexpr int kLoads = (kUnit * D / 16 + kBlock - 1) / kBlock, kItems = kUnit * D / 16;
+  static constexpr int kItems = kUnit * D / 16, kLoads = (kItems + kThreads - 1) / kThreads;
+  static constexpr bool kEven = kItems % kThreads == 0;
 
   struct Buffer {
     T k[kUnit][kPitchK];
     f16 v[D][kPitchV];
     float c[4], lv[4], iv[4];
-    int nans[kWaves];                // a wave's values hold a NaN that not every row sees
+    int nans[W];                     // a wave's values hold a NaN that not every row sees
     __attribute__((aligned(8))) uint16_t nan[D][4];   // which: a bit a key
   };
 
-  struct Raw {
-    u4 k[kLoads], v[kLoads];
+  // What a thread stages of each tile: kLoads 16-byte pieces of the keys and of the values.  Block ids are read a tile
+  // ahead of the codes.
+  struct Stage {
+    const uint8_t *k[kLoads], *v[kLoads];              // the pieces in block 0
+    int key_k[kLoads], key_v;                          // their first keys in a tile
+    int id_k[kLoads], id_v, id_s;                      // the next tile's blocks
+    u4 raw_k[kLoads], raw_v[kLoads];
     float ks, vs;
     bool ok;
   };
 
-  static __device__ __forceinline__ int block_of(const AttArgs &a, const int32_t *table, int key) {
-    return table[min(key >> a.shift, a.MB - 1)];
-  }
+  static __device__ __forceinline__ bool has(int i) { return kEven || (int)threadIdx.x + i * kThreads < kItems; }
 
-  static __device__ __forceinline__ void load(const AttArgs &a, const int32_t *table, int h, int length, int base, Raw &raw) {
+  static __device__ __forceinline__ void begin(const AttArgs &a, int h, Stage &g) {
     const int bt = 1 << a.shift;
+    g.key_v = (threadIdx.x & 3) * 16;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int e = threadIdx.x + i * kBlock;
-      raw.k[i] = raw.v[i] = u4{0u, 0u, 0u, 0u};
-      if (kItems % kBlock != 0 && e >= kItems) continue;
-      const int key = base + e / (D / 16);
-      int id = block_of(a, table, key);
-      if ((unsigned)id < (unsigned)a.NB)
-        raw.k[i] = *reinterpret_cast<const u4 *>(a.k + (((size_t)id * a.H + h) * bt + (key & (bt - 1))) * D + e % (D / 16) * 16);
-      const int from = base + (e & 3) * 16;
-      id = block_of(a, table, from);
-      if ((unsigned)id < (unsigned)a.NB) {
-        u4 v = *reinterpret_cast<const u4 *>(a.v + (((size_t)id * a.H + h) * D + (e >> 2)) * bt + (from & (bt - 1)));
-        const int n = length - from;                   // what lies behind the last token may be anything
-        if (n < 16) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) v[j] &= below(n, j);
-        }
-        raw.v[i] = v;
-      }
-    }
-    raw.ok = false;
-    raw.ks = raw.vs = 1.f;
-    if (threadIdx.x < 4) {
-      const int id = block_of(a, table, base + threadIdx.x * 16);
-      raw.ok = (unsigned)id < (unsigned)a.NB;
-      if (raw.ok) {
-        raw.ks = a.ks[(size_t)id * a.H + h];
-        raw.vs = a.vs[(size_t)id * a.H + h];
-      }
+      const int e = threadIdx.x + i * kThreads;
+      g.key_k[i] = e / (D / 16);
+      g.k[i] = a.k + (size_t)h * bt * D + (g.key_k[i] & (bt - 1)) * D + e % (D / 16) * 16;
+      g.v[i] = a.v + (size_t)h * bt * D + (size_t)(has(i) ? e >> 2 : 0) * bt + (g.key_v & (bt - 1));
     }
   }
 
-  // `look`: some row of the workgroup does not see all of the tile.
-  static __device__ __forceinline__ void store(const AttArgs &a, Raw &raw, bool look, Buffer &b) {
+  static __device__ __forceinline__ void blocks(const AttArgs &a, const int32_t *table, int base, Stage &g) {
+    const auto at = [&](int key) { return table[min(key >> a.shift, a.MB - 1)]; };
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) g.id_k[i] = at(base + min(g.key_k[i], kUnit - 1));
+    g.id_v = at(base + g.key_v);
+    g.id_s = at(base + (threadIdx.x & 3) * 16);
+  }
+
+  // The codes of the tile whose blocks were read; `within`: its first key's place in a block longer than a tile.
+  static __device__ __forceinline__ void load(const AttArgs &a, int h, int within, Stage &g) {
+    const unsigned stride = (unsigned)a.H * D << a.shift;              // bytes of a block: below 2^27
+    bool ok = (unsigned)g.id_v < (unsigned)a.NB;
+    const size_t at_v = (size_t)(unsigned)(ok ? g.id_v : 0) * stride + within;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const bool ok_k = (unsigned)g.id_k[i] < (unsigned)a.NB;
+      g.raw_k[i] = g.raw_v[i] = u4{0u, 0u, 0u, 0u};
+      if (has(i)) {
+        g.raw_k[i] = *reinterpret_cast<const u4 *>(g.k[i] + (size_t)(unsigned)(ok_k ? g.id_k[i] : 0) * stride + within * D);
+        g.raw_v[i] = *reinterpret_cast<const u4 *>(g.v[i] + at_v);
+      }
+      ok &= ok_k;
+    }
+    if (__any(!ok)) {                                  // a block that is not there reads as zeros
+      rarely();
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        if ((unsigned)g.id_k[i] >= (unsigned)a.NB) g.raw_k[i] = u4{0u, 0u, 0u, 0u};
+        if ((unsigned)g.id_v >= (unsigned)a.NB) g.raw_v[i] = u4{0u, 0u, 0u, 0u};
+      }
+    }
+    if (threadIdx.x < 64) {
+      g.ok = (unsigned)g.id_s < (unsigned)a.NB;
+      const size_t at = (size_t)(g.ok ? g.id_s : 0) * a.H + h;
+      g.ks = a.ks[at];
+      g.vs = a.vs[at];
+    }
+  }
+
+  // Into LDS.  `n`: keys of the tile that there are; `look`: some row of the workgroup does not see all of them.
+  static __device__ __forceinline__ void store(const AttArgs &a, int n, bool look, Stage &g, Buffer &b) {
     bool nans = false;
-    if (look) {
+    if (look || n < kUnit) {
       rarely();
       unsigned any = 0;
 #pragma unroll
       for (int i = 0; i < kLoads; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) any |= nan_bytes(raw.v[i][j]);
+        for (int j = 0; j < 4; ++j) {
+          g.raw_v[i][j] &= below(n - g.key_v, j);      // what lies behind the last token may be anything
+          any |= nan_bytes(g.raw_v[i][j]);
+        }
       nans = __any(any != 0);
       if (__syncthreads_or(nans)) {
         // a NaN that some rows see and others do not is left out of the product; step() puts it into the rows
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-          const int e = threadIdx.x + i * kBlock;
-          if (kItems % kBlock != 0 && e >= kItems) continue;
+          if (!has(i)) continue;
           unsigned bits = 0;
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const unsigned n = nan_bytes(raw.v[i][j]);
-            raw.v[i][j] &= ~n;
-            bits |= ((n & 0x01010101u) * 0x01020408u >> 24) << (4 * j);
+            const unsigned x = nan_bytes(g.raw_v[i][j]);
+            g.raw_v[i][j] &= ~x;
+            bits |= ((x & 0x01010101u) * 0x01020408u >> 24) << (4 * j);
           }
-          b.nan[e >> 2][e & 3] = (uint16_t)bits;
+          b.nan[(threadIdx.x + i * kThreads) >> 2][threadIdx.x & 3] = (uint16_t)bits;
         }
       }
     }
     if ((threadIdx.x & 63) == 0) b.nans[threadIdx.x >> 6] = nans;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int e = threadIdx.x + i * kBlock;
-      if (kItems % kBlock != 0 && e >= kItems) continue;
-      const int key = e / (D / 16), d = e % (D / 16) * 16, vd = e >> 2, from = (e & 3) * 16;
+      if (!has(i)) continue;
+      const int e = threadIdx.x + i * kThreads, d = e % (D / 16) * 16;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        *reinterpret_cast<typename Vec8<T>::type *>(&b.k[key][d + j * 8]) = decode8<T>(raw.k[i][2 * j], raw.k[i][2 * j + 1]);
-        *reinterpret_cast<h8 *>(&b.v[vd][from + j * 8]) = decode8<f16>(raw.v[i][2 * j], raw.v[i][2 * j + 1]);
+        *reinterpret_cast<typename Vec8<T>::type *>(&b.k[e / (D / 16)][d + j * 8]) =
+            decode8<T>(g.raw_k[i][2 * j], g.raw_k[i][2 * j + 1]);
+        *reinterpret_cast<h8 *>(&b.v[e >> 2][g.key_v + j * 8]) = decode8<f16>(g.raw_v[i][2 * j], g.raw_v[i][2 * j + 1]);
       }
     }
     if (threadIdx.x < 4) {
       // a block that is not there: its codes are zeros and its logits -inf
-      const float vs = fminf(fmaxf(raw.vs, kScaleMin), kScaleMax);
-      b.c[threadIdx.x] = raw.ok ? a.scale * raw.ks : 0.f;
-      b.lv[threadIdx.x] = raw.ok ? log2_(vs) : kNegInf();
-      b.iv[threadIdx.x] = raw.ok ? 1.f / vs : 0.f;
+      const float vs = fminf(fmaxf(g.vs, kScaleMin), kScaleMax);
+      b.c[threadIdx.x] = g.ok ? a.scale * g.ks : 0.f;
+      b.lv[threadIdx.x] = g.ok ? log2_(vs) : kNegInf();
+      b.iv[threadIdx.x] = g.ok ? __builtin_amdgcn_rcpf(vs) : 0.f;
     }
   }
 
@@ -777,17 +817,19 @@ struct Tiles {
     // row c of a first product is key 16 (c / 4 % 2) + 4 (c / 8) + c % 4 of its 32
     const int key_row = ((c >> 2) & 1) * 16 + (c >> 3) * 4 + (c & 3);
     f16v x[2];
+    float iv[2];
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
+      const float cc = b.c[g * 2 + h], lv = b.lv[g * 2 + h], shift = st.m == kNegInf() ? lv : lv - st.m;
+      iv[g] = b.iv[g * 2 + h];
       f16v s;
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
       for (int i = 0; i < D / 16; ++i)
         s = mfma32(*reinterpret_cast<const typename Vec8<T>::type *>(&b.k[g * 32 + key_row][i * 16 + h * 8]), st.q[i], s);
-      const float cc = b.c[g * 2 + h], lv = b.lv[g * 2 + h];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) x[g][i] = fmaf(s[i], cc, lv);
+      for (int i = 0; i < 16; ++i) x[g][i] = fmaf(s[i], cc, shift);
     }
     const bool masked = base + kUnit - 1 > pos_min || (a.window > 0 && base <= pos_max - a.window);
     if (masked) {
@@ -804,27 +846,31 @@ struct Tiles {
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, x[g][i]);
     top = across32(top, max_);
-    if (__any(top > st.m)) {
-      const float now = fmaxf(st.m, top), f = weight(st.m, now);
-      st.m = now;
-      st.l *= f;
+    if (__any(raises(top, st.m))) {
+      rarely();
+      const float f = raise(top, st.m, st.l);
+#pragma unroll
+      for (int g = 0; g < 2; ++g) x[g] -= top;
 #pragma unroll
       for (int t = 0; t < D / 32; ++t) st.o[t] *= f;
     }
-    const float m = st.m == kNegInf() ? 0.f : st.m;
     h8 w[2][2];
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const float p = exp2_(x[g][i] - m);
+        const float p = exp2_(x[g][i]);
         sum += p;
         w[g][i >> 3][i & 7] = (f16)p;
       }
-      st.l = fmaf(sum, b.iv[g * 2 + h], st.l);
+      st.l = fmaf(sum, iv[g], st.l);
     }
-    if (masked && (b.nans[0] | b.nans[1] | b.nans[2] | b.nans[3])) {
+    bool nans = false;
+    if (masked)
+#pragma unroll
+      for (int i = 0; i < W; ++i) nans |= b.nans[i] != 0;
+    if (nans) {
       rarely();
       unsigned long long seen = 0;
 #pragma unroll 1
@@ -848,9 +894,9 @@ struct Tiles {
   }
 };
 
-template <typename T, int D>
-__global__ void __launch_bounds__(kBlock, D <= 128 ? 2 : 1) k_tiles(AttArgs a) {
-  typedef Tiles<T, D> K;
+template <typename T, int D, int W>
+__global__ void __launch_bounds__(64 * W, D <= 128 ? 2 : 1) k_tiles(AttArgs a) {
+  typedef Tiles<T, D, W> K;
   __shared__ typename K::Buffer buf[2];
   __shared__ long long list_[kListed + 1];
   const long long *list = a.plan ? a.plan + a.R + 1 : nullptr;
@@ -865,11 +911,11 @@ __global__ void __launch_bounds__(kBlock, D <= 128 ? 2 : 1) k_tiles(AttArgs a) {
   if (at < 0) return;
   const int r = find(list, a.R, at);
   const Request rq = request(a, r);
-  const int rows = rq.n * a.G, row0 = (int)(at - list[r]) * kTileRows, before = rq.length - rq.n;
+  const int rows = rq.n * a.G, row0 = (int)(at - list[r]) * K::kTileRows, before = rq.length - rq.n;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 31, half = lane >> 5;
   const int wave0 = row0 + wave * 32, i = wave0 + c, t = i / a.G;
   const bool in = i < rows;
-  const int pos_lo = before + row0 / a.G, pos_hi = before + (min(row0 + kTileRows, rows) - 1) / a.G;
+  const int pos_lo = before + row0 / a.G, pos_hi = before + (min(row0 + K::kTileRows, rows) - 1) / a.G;
   const int pos_min = before + wave0 / a.G, pos_max = before + (min(wave0 + 32, rows) - 1) / a.G;
   int u = a.window > 0 ? max(pos_lo - a.window + 1, 0) / kUnit : 0;
   int end = pos_hi < 0 ? u : max(cdiv(pos_hi + 1, kUnit), u);
@@ -895,27 +941,36 @@ __global__ void __launch_bounds__(kBlock, D <= 128 ? 2 : 1) k_tiles(AttArgs a) {
     st.q[s] = __builtin_bit_cast(typename Vec8<T>::type, raw);
   }
   const int32_t *table = a.table + (size_t)r * a.MB;
+  const int bt1 = (1 << a.shift) - 1;
   const auto look = [&](int unit) {
     return unit * kUnit + kUnit - 1 > pos_lo || (a.window > 0 && unit * kUnit <= pos_hi - a.window);
   };
-  typename K::Raw raw;
+  typename K::Stage g;
+  const auto load = [&](int unit) { K::load(a, h, a.shift > 6 ? unit * kUnit & bt1 : 0, g); };
+  const auto store = [&](int unit) { K::store(a, rq.length - unit * kUnit, look(unit), g, buf[unit & 1]); };
   if (u < end) {
-    K::load(a, table, h, rq.length, u * kUnit, raw);
-    K::store(a, raw, look(u), buf[u & 1]);
+    K::begin(a, h, g);
+    K::blocks(a, table, u * kUnit, g);
+    load(u);
+    K::blocks(a, table, (u + 1) * kUnit, g);
+    store(u);
   }
   __syncthreads();
   for (; u < end; ++u) {
-    if (u + 1 < end) K::load(a, table, h, rq.length, (u + 1) * kUnit, raw);
+    if (u + 1 < end) {
+      load(u + 1);
+      K::blocks(a, table, (u + 2) * kUnit, g);
+    }
     const int base = u * kUnit;
     if (wave0 < rows && base <= pos_max && (a.window <= 0 || base + kUnit - 1 > pos_min - a.window))
       K::step(a, base, pos_min, pos_max, buf[u & 1], st);
-    if (u + 1 < end) K::store(a, raw, look(u + 1), buf[(u + 1) & 1]);
+    if (u + 1 < end) store(u + 1);
     __syncthreads();
   }
   if (!in) return;
   st.l = across32(st.l, add_);
   if (a.splits > 1) {
-    const size_t p = (((size_t)at * a.H + h) * a.splits + blockIdx.y) * kTileRows + wave * 32 + c;
+    const size_t p = (((size_t)at * a.H + h) * a.splits + blockIdx.y) * K::kTileRows + wave * 32 + c;
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
@@ -950,10 +1005,10 @@ __global__ void __launch_bounds__(kBlock) k_tiles_join(AttArgs a) {
   if (at < 0) return;
   const int r = find(list, a.R, at);
   const Request rq = request(a, r);
-  const int row = blockIdx.y * kWaves + (threadIdx.x >> 6), i = (int)(at - list[r]) * kTileRows + row, t = i / a.G;
+  const int row = blockIdx.y * kWaves + (threadIdx.x >> 6), i = (int)(at - list[r]) * a.tile_rows + row, t = i / a.G;
   if (i >= rq.n * a.G) return;
-  const size_t p = ((size_t)at * a.H + h) * a.splits * kTileRows + row;
-  join_row<T, D>(a, p, p + kTileRows, kTileRows, a.splits, rq.first + t, h * a.G + i - t * a.G);
+  const size_t p = ((size_t)at * a.H + h) * a.splits * a.tile_rows + row;
+  join_row<T, D>(a, p, p + a.tile_rows, a.tile_rows, a.splits, rq.first + t, h * a.G + i - t * a.G);
 }
 
 // ------------------------------------------------------------------ host
@@ -963,6 +1018,7 @@ struct Shape {
   int rows_max;
   bool cut, tiles;                   // k_rows with pieces; k_tiles runs
   int tiles_each;
+  int tile_rows;
   long long tile_groups;             // bound of the row tiles of all requests
   int splits;
   int join_rows;                     // rows of a row tile that may be in use
@@ -970,6 +1026,9 @@ struct Shape {
 };
 
 size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
+
+// Row tiles that k_rows keeps in registers, nothing spilled to memory.
+constexpr int row_tiles_most(int D) { return D <= 96 ? 4 : D <= 128 ? 2 : 1; }
 
 festina_status shape_of(const festina_kv_cache *c, const festina_attention *t, Shape *s) {
   const festina_status bad = check_cache(c);
@@ -983,12 +1042,13 @@ festina_status shape_of(const festina_kv_cache *c, const festina_attention *t, S
     return FESTINA_ERR_UNSUPPORTED;
   const int G = t->n_heads / c->n_kv_heads, H = c->n_kv_heads, D = c->head_dim;
   const long long most = (long long)t->max_new * G;                   // rows of one request and key head
+  const int nt_most = row_tiles_most(D);
   *s = Shape{};
-  s->tiles = most > 64 && t->max_new > 1;
+  s->tiles = most > 16 * nt_most && t->max_new > 1;
   const long long rows = s->tiles ? G : most;                         // with prompts about: the single tokens' rows
-  s->nt = rows <= 16 ? 1 : rows <= 32 || D > 128 ? 2 : 4;             // four tiles of 256 dims are more than registers hold
+  s->nt = rows <= 16 ? 1 : min(rows <= 32 ? 2 : 4, nt_most);
   s->join_rows = (int)min(rows, 16ll * s->nt);
-  if (s->tiles && G > 64) s->nt = 0;
+  if (s->tiles && G > 16 * nt_most) s->nt = 0;
   s->rows_max = s->tiles ? 16 * s->nt : INT_MAX;
   const long long keys = (long long)t->max_blocks * c->block_tokens;
   s->tiles_each = (int)((rows + 16 * s->nt - 1) / max(16 * s->nt, 1));
@@ -997,14 +1057,15 @@ festina_status shape_of(const festina_kv_cache *c, const festina_attention *t, S
   size_t parts = 0;
   if (s->nt && s->cut) parts = (size_t)2 * kWorkers * 16 * s->nt;
   if (s->tiles) {
-    s->tile_groups = ((long long)t->n_tokens * G + kTileRows - 1) / kTileRows + t->n_requests;
+    s->tile_rows = getenv("FST_W8") && D <= 128 ? 256 : 128;
+    s->tile_groups = ((long long)t->n_tokens * G + s->tile_rows - 1) / s->tile_rows + t->n_requests;
     if (s->tile_groups * H > INT_MAX) return FESTINA_ERR_UNSUPPORTED;
     // at least two workgroups a compute unit, of at least 16 steps each
-    const long long groups = max(((long long)t->n_tokens * G + kTileRows - 1) / kTileRows, 1ll) * H;
+    const long long groups = max(((long long)t->n_tokens * G + s->tile_rows - 1) / s->tile_rows, 1ll) * H;
     const long long wanted = (kGroups + groups - 1) / groups;
     s->splits = (int)max(min(wanted, keys / (16 * kUnit)), 1ll);
     if (s->splits > 1) {
-      const size_t p = (size_t)s->tile_groups * H * s->splits * kTileRows;
+      const size_t p = (size_t)s->tile_groups * H * s->splits * s->tile_rows;
       parts = p > parts ? p : parts;
     }
   }
@@ -1035,14 +1096,17 @@ void run(AttArgs a, const Shape &s, long long *plan, hipStream_t st) {
     a.plan = plan;
   }
   if (s.nt == 1) run_rows<T, D, 1>(a, s, st);
-  else if (s.nt == 2) run_rows<T, D, 2>(a, s, st);
-  else if (s.nt == 4) {
-    if constexpr (D <= 128) run_rows<T, D, 4>(a, s, st);
-  }
+  if constexpr (row_tiles_most(D) >= 2)
+    if (s.nt == 2) run_rows<T, D, 2>(a, s, st);
+  if constexpr (row_tiles_most(D) >= 4)
+    if (s.nt == 4) run_rows<T, D, 4>(a, s, st);
   if (s.tiles) {
-    k_tiles<T, D><<<dim3((unsigned)(s.tile_groups * a.H), s.splits), kBlock, 0, st>>>(a);
+    if constexpr (D <= 128)
+      if (s.tile_rows == 256) k_tiles<T, D, 8><<<dim3((unsigned)(s.tile_groups * a.H), s.splits), 512, 0, st>>>(a);
+    if (s.tile_rows == 128)
+      k_tiles<T, D, 4><<<dim3((unsigned)(s.tile_groups * a.H), s.splits), kBlock, 0, st>>>(a);
     if (s.splits > 1)
-      k_tiles_join<T, D><<<dim3((unsigned)(s.tile_groups * a.H), kTileRows / kWaves), kBlock, 0, st>>>(a);
+      k_tiles_join<T, D><<<dim3((unsigned)(s.tile_groups * a.H), s.tile_rows / kWaves), kBlock, 0, st>>>(a);
   }
 }
 
@@ -1092,6 +1156,7 @@ extern "C" festina_status festina_attend(const festina_kv_cache *cache, const fe
   a.tiles_each = s.tiles_each;
   a.workers = kWorkers;
   a.splits = s.splits;
+  a.tile_rows = s.tile_rows;
   a.scale = att->scale * 1.44269504088896341f;
   a.table = att->block_table;
   a.length = att->length;
