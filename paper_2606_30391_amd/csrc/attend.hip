@@ -682,10 +682,10 @@ struct Tiles {
   static constexpr bool kEven = kItems % kThreads == 0;
 
   struct Buffer {
-    T k[kUnit][kPitchK];
-    f16 v[D][kPitchV];
+    __attribute__((aligned(16))) T k[kUnit][kPitchK];
+    __attribute__((aligned(16))) f16 v[D][kPitchV];
     float c[4], lv[4], iv[4];
-    int nans[W];                     // a wave's values hold a NaN that not every row sees
+    int nans;                        // the values hold a NaN that not every row sees
     __attribute__((aligned(8))) uint16_t nan[D][4];   // which: a bit a key
   };
 
@@ -755,7 +755,7 @@ struct Tiles {
 
   // Into LDS.  `n`: keys of the tile that there are; `look`: some row of the workgroup does not see all of them.
   static __device__ __forceinline__ void store(const AttArgs &a, int n, bool look, Stage &g, Buffer &b) {
-    bool nans = false;
+    int nans = 0;
     if (look || n < kUnit) {
       rarely();
       unsigned any = 0;
@@ -766,8 +766,8 @@ struct Tiles {
           g.raw_v[i][j] &= below(n - g.key_v, j);      // what lies behind the last token may be anything
           any |= nan_bytes(g.raw_v[i][j]);
         }
-      nans = __any(any != 0);
-      if (__syncthreads_or(nans)) {
+      nans = __syncthreads_or(any != 0);
+      if (nans) {
         // a NaN that some rows see and others do not is left out of the product; step() puts it into the rows
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
@@ -783,7 +783,7 @@ struct Tiles {
         }
       }
     }
-    if ((threadIdx.x & 63) == 0) b.nans[threadIdx.x >> 6] = nans;
+    if (threadIdx.x == 0) b.nans = nans;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       if (!has(i)) continue;
@@ -817,19 +817,37 @@ struct Tiles {
     // row c of a first product is key 16 (c / 4 % 2) + 4 (c / 8) + c % 4 of its 32
     const int key_row = ((c >> 2) & 1) * 16 + (c >> 3) * 4 + (c & 3);
     f16v x[2];
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[g][i] = 0.f;
+    // two chains of products side by side, each operand read from LDS a step before it is used
+    typedef typename Vec8<T>::type Vec;
+    const auto keys = [&](int g, int i) { return *reinterpret_cast<const Vec *>(&b.k[g * 32 + key_row][i * 16 + h * 8]); };
+    Vec kf[2][2];
+#pragma unroll
+    for (int g = 0; g < 2; ++g) kf[0][g] = keys(g, 0);
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+      if (i + 1 < D / 16)
+#pragma unroll
+        for (int g = 0; g < 2; ++g) kf[(i + 1) & 1][g] = keys(g, i + 1);
+#pragma unroll
+      for (int g = 0; g < 2; ++g) x[g] = mfma32(kf[i & 1][g], st.q[i], x[g]);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+    }
     float iv[2];
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       const float cc = b.c[g * 2 + h], lv = b.lv[g * 2 + h], shift = st.m == kNegInf() ? lv : lv - st.m;
       iv[g] = b.iv[g * 2 + h];
-      f16v s;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = 0.f;
-#pragma unroll
-      for (int i = 0; i < D / 16; ++i)
-        s = mfma32(*reinterpret_cast<const typename Vec8<T>::type *>(&b.k[g * 32 + key_row][i * 16 + h * 8]), st.q[i], s);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) x[g][i] = fmaf(s[i], cc, shift);
+      for (int i = 0; i < 16; ++i) x[g][i] = fmaf(x[g][i], cc, shift);
     }
     const bool masked = base + kUnit - 1 > pos_min || (a.window > 0 && base <= pos_max - a.window);
     if (masked) {
@@ -866,11 +884,7 @@ struct Tiles {
       }
       st.l = fmaf(sum, iv[g], st.l);
     }
-    bool nans = false;
-    if (masked)
-#pragma unroll
-      for (int i = 0; i < W; ++i) nans |= b.nans[i] != 0;
-    if (nans) {
+    if (b.nans) {
       rarely();
       unsigned long long seen = 0;
 #pragma unroll 1
@@ -884,18 +898,25 @@ struct Tiles {
           st.o[t][i] = nan & seen ? __builtin_nanf("") : st.o[t][i];
         }
     }
+    // as many chains as there are tiles of 32 dims
+    constexpr int kT = D / 32;
+    const auto values = [&](int j, int t) { return *reinterpret_cast<const h8 *>(&b.v[t * 32 + c][(j >> 1) * 32 + h * 16 + (j & 1) * 8]); };
+    h8 vf[2][kT];
 #pragma unroll
-    for (int t = 0; t < D / 32; ++t)
+    for (int t = 0; t < kT; ++t) vf[0][t] = values(0, t);
 #pragma unroll
-      for (int g = 0; g < 2; ++g)
+    for (int j = 0; j < 4; ++j) {
+      if (j < 3)
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
-          st.o[t] = mfma32(*reinterpret_cast<const h8 *>(&b.v[t * 32 + c][g * 32 + h * 16 + s * 8]), w[g][s], st.o[t]);
+        for (int t = 0; t < kT; ++t) vf[(j + 1) & 1][t] = values(j + 1, t);
+#pragma unroll
+      for (int t = 0; t < kT; ++t) st.o[t] = mfma32(vf[j & 1][t], w[j >> 1][j & 1], st.o[t]);
+    }
   }
 };
 
 template <typename T, int D, int W>
-__global__ void __launch_bounds__(64 * W, D <= 128 ? 2 : 1) k_tiles(AttArgs a) {
+__global__ void __launch_bounds__(64 * W, D <= 64 && W == 4 ? 3 : D <= 128 ? 2 : 1) k_tiles(AttArgs a) {
   typedef Tiles<T, D, W> K;
   __shared__ typename K::Buffer buf[2];
   __shared__ long long list_[kListed + 1];

@@ -176,6 +176,15 @@ def test_nan_in_values_reaches_only_the_rows_that_see_it(new, window):
     c.check(window=window, label="NaN values")
 
 
+@pytest.mark.parametrize("place", [560, 561, 575, 576, 590, 599, 512])
+def test_nan_in_values_of_a_tile_that_only_some_rows_see_whole(place):
+    """40 tokens from 560 on: the tile of keys 512-575 is cut by the first tokens' view and seen whole by the last's."""
+    rng = np.random.default_rng(place)
+    c = Case(rng, [(600, 40)], D=64, bt=32)
+    c.v[c.table[0, place // 32], 0, 5, place % 32] = 0x7F
+    c.check(label=f"NaN value at {place}")
+
+
 @pytest.mark.parametrize("new", [1, 4, 40])
 def test_nan_in_keys_reaches_only_the_rows_that_see_it(new):
     rng = np.random.default_rng(new + 90)
