@@ -116,6 +116,7 @@ __device__ __forceinline__ int units(const AttArgs &a, const Request &q) {
 }
 
 // A value that is the same in all lanes, kept once.
+__device__ __forceinline__ int same(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ long long same(long long x) {
   const unsigned lo = __builtin_amdgcn_readfirstlane((int)x), hi = __builtin_amdgcn_readfirstlane((int)(x >> 32));
   return (long long)((unsigned long long)hi << 32 | lo);
@@ -536,7 +537,7 @@ struct Rows {
 
   // A workgroup's keys: its waves' parts of each row joined in LDS.
   static __device__ __forceinline__ void whole(const AttArgs &a, int r, const Request &rq, int h, int tile, Shared &sh) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = same((int)threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
     const int rows = rq.n * a.G, row0 = tile * kRows;
     State st;
     scan_keys(a, r, rq, h, tile, wave, units(a, rq), kWaves, st);
@@ -858,12 +859,13 @@ struct Tiles {
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[g][i] = sees.has(g * 32 + i) ? x[g][i] : kNegInf();
     }
-    float top = x[0][0];
+    float tops[4] = {x[0][0], x[0][1], x[1][0], x[1][1]};
 #pragma unroll
-    for (int g = 0; g < 2; ++g)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, x[g][i]);
-    top = across32(top, max_);
+    for (int i = 2; i < 16; ++i) {
+      tops[i & 1] = fmaxf(tops[i & 1], x[0][i]);
+      tops[2 + (i & 1)] = fmaxf(tops[2 + (i & 1)], x[1][i]);
+    }
+    float top = across32(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), max_);
     if (__any(raises(top, st.m))) {
       rarely();
       const float f = raise(top, st.m, st.l);
@@ -875,14 +877,14 @@ struct Tiles {
     h8 w[2][2];
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
-      float sum = 0.f;
+      float sum[2];
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const float p = exp2_(x[g][i]);
-        sum += p;
+        sum[i & 1] = i < 2 ? p : sum[i & 1] + p;
         w[g][i >> 3][i & 7] = (f16)p;
       }
-      st.l = fmaf(sum, iv[g], st.l);
+      st.l = fmaf(sum[0] + sum[1], iv[g], st.l);
     }
     if (b.nans) {
       rarely();
@@ -928,12 +930,12 @@ __global__ void __launch_bounds__(64 * W, D <= 64 && W == 4 ? 3 : D <= 128 ? 2 :
   // neighbouring workgroups take different key heads, so that (for 8 heads) the workgroups of one XCD share one
   // head's keys in its L2; a request's last rows, which see most keys, come first
   const int h = blockIdx.x % a.H;
-  const long long at = min(list[a.R], (long long)(gridDim.x / a.H)) - 1 - blockIdx.x / a.H;
+  const long long at = same(min(list[a.R], (long long)(gridDim.x / a.H)) - 1 - blockIdx.x / a.H);
   if (at < 0) return;
   const int r = find(list, a.R, at);
   const Request rq = request(a, r);
-  const int rows = rq.n * a.G, row0 = (int)(at - list[r]) * K::kTileRows, before = rq.length - rq.n;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 31, half = lane >> 5;
+  const int rows = rq.n * a.G, row0 = (int)(at - same(list[r])) * K::kTileRows, before = rq.length - rq.n;
+  const int lane = threadIdx.x & 63, wave = same((int)threadIdx.x >> 6), c = lane & 31, half = lane >> 5;
   const int wave0 = row0 + wave * 32, i = wave0 + c, t = i / a.G;
   const bool in = i < rows;
   const int pos_lo = before + row0 / a.G, pos_hi = before + (min(row0 + K::kTileRows, rows) - 1) / a.G;
