@@ -675,156 +675,185 @@ __global__ void __launch_bounds__(kBlock) k_rows_join(AttArgs a) {
 
 // ------------------------------------------------------------------ k_tiles
 
+// A tile of 64 keys in LDS.
+template <typename T, int D>
+struct KeyTile {
+  static constexpr int kPitch = D + 8;
+  __attribute__((aligned(16))) T k[kUnit][kPitch];
+  float c[4], lv[4], iv[4];          // for 16 keys each: scale, log2 and reciprocal of the values' scale
+};
+
+// Its values.
+template <int D, int W>
+struct ValueTile {
+  static constexpr int kPitch = kUnit + 8;
+  __attribute__((aligned(16))) f16 v[D][kPitch];
+  __attribute__((aligned(16))) int nans[W];          // a wave staged a NaN that not every row sees
+  __attribute__((aligned(8))) uint16_t nan[D][4];    // which: a bit a key
+};
+
+// What a thread stages of each tile: a 16-byte piece of the keys and one of the values, `kLoads` times.
 template <typename T, int D, int W>
-struct Tiles {
-  static constexpr int kThreads = 64 * W, kTileRows = 32 * W;
-  static constexpr int kPitchK = D + 8, kPitchV = kUnit + 8;
-  static constexpr int kItems = kUnit * D / 16, kLoads = (kItems + kThreads - 1) / kThreads;
-  static constexpr bool kEven = kItems % kThreads == 0;
+struct Stage {
+  static constexpr int kThreads = 64 * W, kItems = kUnit * D / 16, kLoads = (kItems + kThreads - 1) / kThreads;
 
-  struct Buffer {
-    __attribute__((aligned(16))) T k[kUnit][kPitchK];
-    __attribute__((aligned(16))) f16 v[D][kPitchV];
-    float c[4], lv[4], iv[4];
-    int nans;                        // the values hold a NaN that not every row sees
-    __attribute__((aligned(8))) uint16_t nan[D][4];   // which: a bit a key
-  };
+  const uint8_t *k[kLoads], *v[kLoads];              // the pieces in block 0
+  int id_k[kLoads], id_v[kLoads], id_s;              // the blocks of the next tile
+  u4 raw_k[kLoads], raw_v[kLoads];
+  float ks, vs;
+  bool ok;
 
-  // What a thread stages of each tile: kLoads 16-byte pieces of the keys and of the values.  Block ids are read a tile
-  // ahead of the codes.
-  struct Stage {
-    const uint8_t *k[kLoads], *v[kLoads];              // the pieces in block 0
-    int key_k[kLoads], key_v;                          // their first keys in a tile
-    int id_k[kLoads], id_v, id_s;                      // the next tile's blocks
-    u4 raw_k[kLoads], raw_v[kLoads];
-    float ks, vs;
-    bool ok;
-  };
+  // keys to the first threads, values to the last, so that all have some where there are fewer pieces than threads
+  static __device__ __forceinline__ int key_item(int i) { return threadIdx.x + i * kThreads; }
+  static __device__ __forceinline__ int value_item(int i) { return kThreads - 1 - threadIdx.x + i * kThreads; }
+  static __device__ __forceinline__ bool has(int item) { return kItems % kThreads == 0 || item < kItems; }
+  static __device__ __forceinline__ int key_of(int item) { return item / (D / 16); }
+  static __device__ __forceinline__ int key_of_value(int item) { return (item & 3) * 16; }
 
-  static __device__ __forceinline__ bool has(int i) { return kEven || (int)threadIdx.x + i * kThreads < kItems; }
-
-  static __device__ __forceinline__ void begin(const AttArgs &a, int h, Stage &g) {
+  __device__ __forceinline__ void begin(const AttArgs &a, int h) {
     const int bt = 1 << a.shift;
-    g.key_v = (threadIdx.x & 3) * 16;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int e = threadIdx.x + i * kThreads;
-      g.key_k[i] = e / (D / 16);
-      g.k[i] = a.k + (size_t)h * bt * D + (g.key_k[i] & (bt - 1)) * D + e % (D / 16) * 16;
-      g.v[i] = a.v + (size_t)h * bt * D + (size_t)(has(i) ? e >> 2 : 0) * bt + (g.key_v & (bt - 1));
+      const int x = key_item(i), y = has(value_item(i)) ? value_item(i) : 0;
+      k[i] = a.k + (size_t)h * bt * D + (key_of(x) & (bt - 1)) * D + x % (D / 16) * 16;
+      v[i] = a.v + (size_t)h * bt * D + (size_t)(y >> 2) * bt + (key_of_value(y) & (bt - 1));
     }
   }
 
-  static __device__ __forceinline__ void blocks(const AttArgs &a, const int32_t *table, int base, Stage &g) {
-    const auto at = [&](int key) { return table[min(key >> a.shift, a.MB - 1)]; };
+  static __device__ __forceinline__ int block_at(const AttArgs &a, const int32_t *table, int key) {
+    return table[min(key >> a.shift, a.MB - 1)];
+  }
+  __device__ __forceinline__ void key_blocks(const AttArgs &a, const int32_t *table, int base) {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) g.id_k[i] = at(base + min(g.key_k[i], kUnit - 1));
-    g.id_v = at(base + g.key_v);
-    g.id_s = at(base + (threadIdx.x & 3) * 16);
+    for (int i = 0; i < kLoads; ++i) id_k[i] = block_at(a, table, base + min(key_of(key_item(i)), kUnit - 1));
+    id_s = block_at(a, table, base + (threadIdx.x & 3) * 16);
+  }
+  __device__ __forceinline__ void value_blocks(const AttArgs &a, const int32_t *table, int base) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) id_v[i] = block_at(a, table, base + key_of_value(value_item(i)));
   }
 
-  // The codes of the tile whose blocks were read; `within`: its first key's place in a block longer than a tile.
-  static __device__ __forceinline__ void load(const AttArgs &a, int h, int within, Stage &g) {
-    const unsigned stride = (unsigned)a.H * D << a.shift;              // bytes of a block: below 2^27
-    bool ok = (unsigned)g.id_v < (unsigned)a.NB;
-    const size_t at_v = (size_t)(unsigned)(ok ? g.id_v : 0) * stride + within;
+  // The codes of the tile at `base`, whose blocks were read.  A block that is not there reads as zeros.
+  static __device__ __forceinline__ unsigned block_bytes(const AttArgs &a) { return (unsigned)a.H * D << a.shift; }   // below 2^27
+  static __device__ __forceinline__ int within(const AttArgs &a, int base) {   // its place in a block longer than a tile
+    return a.shift > 6 ? base & ((1 << a.shift) - 1) : 0;
+  }
+  __device__ __forceinline__ void load_keys(const AttArgs &a, int h, int base) {
+    bool all = true;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const bool ok_k = (unsigned)g.id_k[i] < (unsigned)a.NB;
-      g.raw_k[i] = g.raw_v[i] = u4{0u, 0u, 0u, 0u};
-      if (has(i)) {
-        g.raw_k[i] = *reinterpret_cast<const u4 *>(g.k[i] + (size_t)(unsigned)(ok_k ? g.id_k[i] : 0) * stride + within * D);
-        g.raw_v[i] = *reinterpret_cast<const u4 *>(g.v[i] + at_v);
-      }
-      ok &= ok_k;
+      const bool there = (unsigned)id_k[i] < (unsigned)a.NB;
+      all &= there;
+      raw_k[i] = u4{0u, 0u, 0u, 0u};
+      if (has(key_item(i)))
+        raw_k[i] = *reinterpret_cast<const u4 *>(k[i] + (size_t)(unsigned)(there ? id_k[i] : 0) * block_bytes(a) + within(a, base) * D);
     }
-    if (__any(!ok)) {                                  // a block that is not there reads as zeros
+    if (__any(!all)) {
       rarely();
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        if ((unsigned)g.id_k[i] >= (unsigned)a.NB) g.raw_k[i] = u4{0u, 0u, 0u, 0u};
-        if ((unsigned)g.id_v >= (unsigned)a.NB) g.raw_v[i] = u4{0u, 0u, 0u, 0u};
-      }
-    }
-    if (threadIdx.x < 64) {
-      g.ok = (unsigned)g.id_s < (unsigned)a.NB;
-      const size_t at = (size_t)(g.ok ? g.id_s : 0) * a.H + h;
-      g.ks = a.ks[at];
-      g.vs = a.vs[at];
-    }
-  }
-
-  // Into LDS.  `n`: keys of the tile that there are; `look`: some row of the workgroup does not see all of them.
-  static __device__ __forceinline__ void store(const AttArgs &a, int n, bool look, Stage &g, Buffer &b) {
-    int nans = 0;
-    if (look || n < kUnit) {
-      rarely();
-      unsigned any = 0;
 #pragma unroll
       for (int i = 0; i < kLoads; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          g.raw_v[i][j] &= below(n - g.key_v, j);      // what lies behind the last token may be anything
-          any |= nan_bytes(g.raw_v[i][j]);
-        }
-      nans = __syncthreads_or(any != 0);
-      if (nans) {
-        // a NaN that some rows see and others do not is left out of the product; step() puts it into the rows
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-          if (!has(i)) continue;
-          unsigned bits = 0;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const unsigned x = nan_bytes(g.raw_v[i][j]);
-            g.raw_v[i][j] &= ~x;
-            bits |= ((x & 0x01010101u) * 0x01020408u >> 24) << (4 * j);
-          }
-          b.nan[(threadIdx.x + i * kThreads) >> 2][threadIdx.x & 3] = (uint16_t)bits;
-        }
-      }
+        if ((unsigned)id_k[i] >= (unsigned)a.NB) raw_k[i] = u4{0u, 0u, 0u, 0u};
     }
-    if (threadIdx.x == 0) b.nans = nans;
+    if (threadIdx.x < 64) {
+      ok = (unsigned)id_s < (unsigned)a.NB;
+      const size_t at = (size_t)(ok ? id_s : 0) * a.H + h;
+      ks = a.ks[at];
+      vs = a.vs[at];
+    }
+  }
+  __device__ __forceinline__ void load_values(const AttArgs &a, int base) {
+    bool all = true;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      if (!has(i)) continue;
-      const int e = threadIdx.x + i * kThreads, d = e % (D / 16) * 16;
+      const bool there = (unsigned)id_v[i] < (unsigned)a.NB;
+      all &= there;
+      raw_v[i] = u4{0u, 0u, 0u, 0u};
+      if (has(value_item(i)))
+        raw_v[i] = *reinterpret_cast<const u4 *>(v[i] + (size_t)(unsigned)(there ? id_v[i] : 0) * block_bytes(a) + within(a, base));
+    }
+    if (__any(!all)) {
+      rarely();
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        *reinterpret_cast<typename Vec8<T>::type *>(&b.k[e / (D / 16)][d + j * 8]) =
-            decode8<T>(g.raw_k[i][2 * j], g.raw_k[i][2 * j + 1]);
-        *reinterpret_cast<h8 *>(&b.v[e >> 2][g.key_v + j * 8]) = decode8<f16>(g.raw_v[i][2 * j], g.raw_v[i][2 * j + 1]);
-      }
+      for (int i = 0; i < kLoads; ++i)
+        if ((unsigned)id_v[i] >= (unsigned)a.NB) raw_v[i] = u4{0u, 0u, 0u, 0u};
+    }
+  }
+
+  __device__ __forceinline__ void store_keys(const AttArgs &a, KeyTile<T, D> &b) const {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int x = key_item(i), d = x % (D / 16) * 16;
+      if (!has(x)) continue;
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        *reinterpret_cast<typename Vec8<T>::type *>(&b.k[key_of(x)][d + j * 8]) = decode8<T>(raw_k[i][2 * j], raw_k[i][2 * j + 1]);
     }
     if (threadIdx.x < 4) {
       // a block that is not there: its codes are zeros and its logits -inf
-      const float vs = fminf(fmaxf(g.vs, kScaleMin), kScaleMax);
-      b.c[threadIdx.x] = g.ok ? a.scale * g.ks : 0.f;
-      b.lv[threadIdx.x] = g.ok ? log2_(vs) : kNegInf();
-      b.iv[threadIdx.x] = g.ok ? __builtin_amdgcn_rcpf(vs) : 0.f;
+      const float s = fminf(fmaxf(vs, kScaleMin), kScaleMax);
+      b.c[threadIdx.x] = ok ? a.scale * ks : 0.f;
+      b.lv[threadIdx.x] = ok ? log2_(s) : kNegInf();
+      b.iv[threadIdx.x] = ok ? __builtin_amdgcn_rcpf(s) : 0.f;
     }
   }
 
-  struct State {
-    typename Vec8<T>::type q[D / 16];
-    f16v o[D / 32];
-    float m, l;
-    Span sees;
-  };
+  // `n`: keys of the tile that there are; `look`: some row of the workgroup does not see all of them.
+  __device__ __forceinline__ void store_values(int n, bool look, ValueTile<D, W> &b) {
+    if (look) {
+      rarely();
+      unsigned any = 0;
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int y = value_item(i);
+        unsigned bits = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          // what lies behind the last token may be anything; a NaN that some rows see and others do not is left out of
+          // the product and put into the rows that see it
+          raw_v[i][j] &= below(n - key_of_value(y), j);
+          const unsigned x = nan_bytes(raw_v[i][j]);
+          raw_v[i][j] &= ~x;
+          bits |= ((x & 0x01010101u) * 0x01020408u >> 24) << (4 * j);
+        }
+        if (has(y)) b.nan[y >> 2][y & 3] = (uint16_t)bits;
+        any |= has(y) ? bits : 0u;
+      }
+      const int nans = __any(any != 0);
+      if ((threadIdx.x & 63) == 0) b.nans[threadIdx.x >> 6] = nans;
+    }
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int y = value_item(i);
+      if (!has(y)) continue;
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        *reinterpret_cast<h8 *>(&b.v[y >> 2][key_of_value(y) + j * 8]) = decode8<f16>(raw_v[i][2 * j], raw_v[i][2 * j + 1]);
+    }
+  }
+};
 
-  static __device__ __forceinline__ void step(const AttArgs &a, int base, int pos_min, int pos_max, const Buffer &b,
-                                              State &st) {
+// 32 query rows of a wave: columns of the products.
+template <typename T, int D>
+struct TileRows {
+  typedef typename Vec8<T>::type Vec;
+
+  Vec q[D / 16];
+  f16v o[D / 32];
+  f16v x[2];                         // logits of a tile, 32 keys each
+  h8 w[2][2];                        // its weights
+  float m, l;
+  Span sees;
+
+  // x = K Q': two chains of products side by side, each operand read from LDS a step before it is used
+  __device__ __forceinline__ void products(const KeyTile<T, D> &b) {
     const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5;
     // row c of a first product is key 16 (c / 4 % 2) + 4 (c / 8) + c % 4 of its 32
     const int key_row = ((c >> 2) & 1) * 16 + (c >> 3) * 4 + (c & 3);
-    f16v x[2];
+    const auto keys = [&](int g, int i) { return *reinterpret_cast<const Vec *>(&b.k[g * 32 + key_row][i * 16 + h * 8]); };
 #pragma unroll
     for (int g = 0; g < 2; ++g)
 #pragma unroll
       for (int i = 0; i < 16; ++i) x[g][i] = 0.f;
-    // two chains of products side by side, each operand read from LDS a step before it is used
-    typedef typename Vec8<T>::type Vec;
-    const auto keys = [&](int g, int i) { return *reinterpret_cast<const Vec *>(&b.k[g * 32 + key_row][i * 16 + h * 8]); };
     Vec kf[2][2];
 #pragma unroll
     for (int g = 0; g < 2; ++g) kf[0][g] = keys(g, 0);
@@ -834,7 +863,7 @@ struct Tiles {
 #pragma unroll
         for (int g = 0; g < 2; ++g) kf[(i + 1) & 1][g] = keys(g, i + 1);
 #pragma unroll
-      for (int g = 0; g < 2; ++g) x[g] = mfma32(kf[i & 1][g], st.q[i], x[g]);
+      for (int g = 0; g < 2; ++g) x[g] = mfma32(kf[i & 1][g], q[i], x[g]);
     }
     __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
 #pragma unroll
@@ -842,22 +871,26 @@ struct Tiles {
       __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
       __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
     }
+  }
+
+  // w = 2^(logits - m), l; `masked`: some row does not see all of the tile
+  __device__ __forceinline__ void weights(const KeyTile<T, D> &b, int base, bool masked) {
+    const int h = (threadIdx.x & 63) >> 5;
     float iv[2];
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
-      const float cc = b.c[g * 2 + h], lv = b.lv[g * 2 + h], shift = st.m == kNegInf() ? lv : lv - st.m;
+      const float cc = b.c[g * 2 + h], lv = b.lv[g * 2 + h], shift = m == kNegInf() ? lv : lv - m;
       iv[g] = b.iv[g * 2 + h];
 #pragma unroll
       for (int i = 0; i < 16; ++i) x[g][i] = fmaf(x[g][i], cc, shift);
     }
-    const bool masked = base + kUnit - 1 > pos_min || (a.window > 0 && base <= pos_max - a.window);
     if (masked) {
       rarely();
-      const Span sees{st.sees.from - base - h * 16, st.sees.count};
+      const Span s{sees.from - base - h * 16, sees.count};
 #pragma unroll
       for (int g = 0; g < 2; ++g)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[g][i] = sees.has(g * 32 + i) ? x[g][i] : kNegInf();
+        for (int i = 0; i < 16; ++i) x[g][i] = s.has(g * 32 + i) ? x[g][i] : kNegInf();
     }
     float tops[4] = {x[0][0], x[0][1], x[1][0], x[1][1]};
 #pragma unroll
@@ -866,15 +899,14 @@ struct Tiles {
       tops[2 + (i & 1)] = fmaxf(tops[2 + (i & 1)], x[1][i]);
     }
     float top = across32(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), max_);
-    if (__any(raises(top, st.m))) {
+    if (__any(raises(top, m))) {
       rarely();
-      const float f = raise(top, st.m, st.l);
+      const float f = raise(top, m, l);
 #pragma unroll
       for (int g = 0; g < 2; ++g) x[g] -= top;
 #pragma unroll
-      for (int t = 0; t < D / 32; ++t) st.o[t] *= f;
+      for (int t = 0; t < D / 32; ++t) o[t] *= f;
     }
-    h8 w[2][2];
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       float sum[2];
@@ -884,23 +916,33 @@ struct Tiles {
         sum[i & 1] = i < 2 ? p : sum[i & 1] + p;
         w[g][i >> 3][i & 7] = (f16)p;
       }
-      st.l = fmaf(sum[0] + sum[1], iv[g], st.l);
+      l = fmaf(sum[0] + sum[1], iv[g], l);
     }
-    if (b.nans) {
+  }
+
+  // o += V' w: as many chains as there are tiles of 32 dims; `look` as for Stage::store_values
+  template <int W>
+  __device__ __forceinline__ void sums(const ValueTile<D, W> &b, int base, bool look) {
+    const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5;
+    if (look) {
       rarely();
-      unsigned long long seen = 0;
+      int nans = 0;
+#pragma unroll
+      for (int i = 0; i < W; ++i) nans |= b.nans[i];
+      if (__any(nans)) {
+        unsigned long long seen = 0;
 #pragma unroll 1
-      for (int key = 0; key < kUnit; ++key) seen |= (unsigned long long)st.sees.has(base + key) << key;
+        for (int key = 0; key < kUnit; ++key) seen |= (unsigned long long)sees.has(base + key) << key;
 #pragma unroll
-      for (int t = 0; t < D / 32; ++t)
+        for (int t = 0; t < D / 32; ++t)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int d = t * 32 + (i >> 2) * 8 + h * 4 + (i & 3);
-          const unsigned long long nan = *reinterpret_cast<const unsigned long long *>(b.nan[d]);
-          st.o[t][i] = nan & seen ? __builtin_nanf("") : st.o[t][i];
-        }
+          for (int i = 0; i < 16; ++i) {
+            const int d = t * 32 + (i >> 2) * 8 + h * 4 + (i & 3);
+            const unsigned long long nan = *reinterpret_cast<const unsigned long long *>(b.nan[d]);
+            o[t][i] = nan & seen ? __builtin_nanf("") : o[t][i];
+          }
+      }
     }
-    // as many chains as there are tiles of 32 dims
     constexpr int kT = D / 32;
     const auto values = [&](int j, int t) { return *reinterpret_cast<const h8 *>(&b.v[t * 32 + c][(j >> 1) * 32 + h * 16 + (j & 1) * 8]); };
     h8 vf[2][kT];
@@ -912,16 +954,28 @@ struct Tiles {
 #pragma unroll
         for (int t = 0; t < kT; ++t) vf[(j + 1) & 1][t] = values(j + 1, t);
 #pragma unroll
-      for (int t = 0; t < kT; ++t) st.o[t] = mfma32(vf[j & 1][t], w[j >> 1][j & 1], st.o[t]);
+      for (int t = 0; t < kT; ++t) o[t] = mfma32(vf[j & 1][t], w[j >> 1][j & 1], o[t]);
     }
   }
 };
 
-template <typename T, int D, int W>
-__global__ void __launch_bounds__(64 * W, D <= 64 && W == 4 ? 3 : D <= 128 ? 2 : 1) k_tiles(AttArgs a) {
-  typedef Tiles<T, D, W> K;
-  __shared__ typename K::Buffer buf[2];
-  __shared__ long long list_[kListed + 1];
+// A workgroup's row tile: which request, head and rows, and the tiles of keys that it goes over.
+struct TileWork {
+  Request rq;
+  long long at;
+  int h, r, rows, row0;
+  int pos_lo, pos_hi;                // first and last row's positions
+  int begin, end;                    // units
+  bool none;
+
+  __device__ __forceinline__ bool look(const AttArgs &a, int unit) const {
+    return unit * kUnit + kUnit - 1 > pos_lo || (a.window > 0 && unit * kUnit <= pos_hi - a.window);
+  }
+};
+
+template <int ROWS>
+__device__ __forceinline__ TileWork tile_work(const AttArgs &a, long long *list_) {
+  TileWork k{};
   const long long *list = a.plan ? a.plan + a.R + 1 : nullptr;
   if (!list) {
     list_sums(a, [&](int r) { return tiles_of(a, r); }, list_);
@@ -929,90 +983,145 @@ __global__ void __launch_bounds__(64 * W, D <= 64 && W == 4 ? 3 : D <= 128 ? 2 :
   }
   // neighbouring workgroups take different key heads, so that (for 8 heads) the workgroups of one XCD share one
   // head's keys in its L2; a request's last rows, which see most keys, come first
-  const int h = blockIdx.x % a.H;
-  const long long at = same(min(list[a.R], (long long)(gridDim.x / a.H)) - 1 - blockIdx.x / a.H);
-  if (at < 0) return;
-  const int r = find(list, a.R, at);
-  const Request rq = request(a, r);
-  const int rows = rq.n * a.G, row0 = (int)(at - same(list[r])) * K::kTileRows, before = rq.length - rq.n;
-  const int lane = threadIdx.x & 63, wave = same((int)threadIdx.x >> 6), c = lane & 31, half = lane >> 5;
-  const int wave0 = row0 + wave * 32, i = wave0 + c, t = i / a.G;
-  const bool in = i < rows;
-  const int pos_lo = before + row0 / a.G, pos_hi = before + (min(row0 + K::kTileRows, rows) - 1) / a.G;
-  const int pos_min = before + wave0 / a.G, pos_max = before + (min(wave0 + 32, rows) - 1) / a.G;
-  int u = a.window > 0 ? max(pos_lo - a.window + 1, 0) / kUnit : 0;
-  int end = pos_hi < 0 ? u : max(cdiv(pos_hi + 1, kUnit), u);
-  if (a.splits > 1) {
-    const int n = end - u, s = blockIdx.y;
-    end = u + (int)((long long)n * (s + 1) / a.splits);
-    u += (int)((long long)n * s / a.splits);
-  }
-  typename K::State st;
-  st.sees = span(a, in ? before + t : -1);
-  st.m = kNegInf();
-  st.l = 0.f;
+  k.h = blockIdx.x % a.H;
+  k.at = same(min(list[a.R], (long long)(gridDim.x / a.H)) - 1 - blockIdx.x / a.H);
+  k.none = k.at < 0;
+  if (k.none) return k;
+  k.r = find(list, a.R, k.at);
+  k.rq = request(a, k.r);
+  k.rows = k.rq.n * a.G;
+  k.row0 = (int)(k.at - same(list[k.r])) * ROWS;
+  const int before = k.rq.length - k.rq.n;
+  k.pos_lo = before + k.row0 / a.G;
+  k.pos_hi = before + (min(k.row0 + ROWS, k.rows) - 1) / a.G;
+  const int u = a.window > 0 ? max(k.pos_lo - a.window + 1, 0) / kUnit : 0;
+  const int n = k.pos_hi < 0 ? 0 : max(cdiv(k.pos_hi + 1, kUnit) - u, 0);
+  k.begin = u + (int)((long long)n * blockIdx.y / a.splits);
+  k.end = u + (int)((long long)n * (blockIdx.y + 1) / a.splits);
+  return k;
+}
+
+// One wave's rows: where they stand, their queries, and where their results go.
+template <typename T, int D, int ROWS>
+struct TileWave {
+  int i, t, pos_min, pos_max;
+  bool in, live;
+
+  __device__ __forceinline__ void begin(const AttArgs &a, const TileWork &k, TileRows<T, D> &st) {
+    const int lane = threadIdx.x & 63, wave0 = k.row0 + same((int)threadIdx.x >> 6) * 32, before = k.rq.length - k.rq.n;
+    i = wave0 + (lane & 31);
+    t = i / a.G;
+    in = i < k.rows;
+    live = wave0 < k.rows;
+    pos_min = before + wave0 / a.G;
+    pos_max = before + (min(wave0 + 32, k.rows) - 1) / a.G;
+    st.sees = span(a, in ? before + t : -1);
+    st.m = kNegInf();
+    st.l = 0.f;
 #pragma unroll
-  for (int d = 0; d < D / 32; ++d)
+    for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-    for (int y = 0; y < 16; ++y) st.o[d][y] = 0.f;
-  const T *q = static_cast<const T *>(a.q) + (int64_t)(rq.first + (in ? t : 0)) * a.q_token +
-               (int64_t)(h * a.G + (in ? i - t * a.G : 0)) * a.q_head;
+      for (int y = 0; y < 16; ++y) st.o[d][y] = 0.f;
+    const T *q = static_cast<const T *>(a.q) + (int64_t)(k.rq.first + (in ? t : 0)) * a.q_token +
+                 (int64_t)(k.h * a.G + (in ? i - t * a.G : 0)) * a.q_head;
 #pragma unroll
-  for (int s = 0; s < D / 16; ++s) {
-    u4 raw = *reinterpret_cast<const u4 *>(q + s * 16 + half * 8);
-    if (!in) raw = u4{0u, 0u, 0u, 0u};
-    st.q[s] = __builtin_bit_cast(typename Vec8<T>::type, raw);
-  }
-  const int32_t *table = a.table + (size_t)r * a.MB;
-  const int bt1 = (1 << a.shift) - 1;
-  const auto look = [&](int unit) {
-    return unit * kUnit + kUnit - 1 > pos_lo || (a.window > 0 && unit * kUnit <= pos_hi - a.window);
-  };
-  typename K::Stage g;
-  const auto load = [&](int unit) { K::load(a, h, a.shift > 6 ? unit * kUnit & bt1 : 0, g); };
-  const auto store = [&](int unit) { K::store(a, rq.length - unit * kUnit, look(unit), g, buf[unit & 1]); };
-  if (u < end) {
-    K::begin(a, h, g);
-    K::blocks(a, table, u * kUnit, g);
-    load(u);
-    K::blocks(a, table, (u + 1) * kUnit, g);
-    store(u);
-  }
-  __syncthreads();
-  for (; u < end; ++u) {
-    if (u + 1 < end) {
-      load(u + 1);
-      K::blocks(a, table, (u + 2) * kUnit, g);
+    for (int s = 0; s < D / 16; ++s) {
+      u4 raw = *reinterpret_cast<const u4 *>(q + s * 16 + (lane >> 5) * 8);
+      if (!in) raw = u4{0u, 0u, 0u, 0u};
+      st.q[s] = __builtin_bit_cast(typename Vec8<T>::type, raw);
     }
-    const int base = u * kUnit;
-    if (wave0 < rows && base <= pos_max && (a.window <= 0 || base + kUnit - 1 > pos_min - a.window))
-      K::step(a, base, pos_min, pos_max, buf[u & 1], st);
-    if (u + 1 < end) store(u + 1);
-    __syncthreads();
   }
-  if (!in) return;
-  st.l = across32(st.l, add_);
-  if (a.splits > 1) {
-    const size_t p = (((size_t)at * a.H + h) * a.splits + blockIdx.y) * K::kTileRows + wave * 32 + c;
+  // Some row sees some of the tile; some row does not see all of it.
+  __device__ __forceinline__ bool sees(const AttArgs &a, int base) const {
+    return live && base <= pos_max && (a.window <= 0 || base + kUnit - 1 > pos_min - a.window);
+  }
+  __device__ __forceinline__ bool masked(const AttArgs &a, int base) const {
+    return base + kUnit - 1 > pos_min || (a.window > 0 && base <= pos_max - a.window);
+  }
+  __device__ __forceinline__ void end(const AttArgs &a, const TileWork &k, TileRows<T, D> &st) const {
+    const int half = (threadIdx.x & 63) >> 5;
+    st.l = across32(st.l, add_);
+    if (!in) return;
+    if (a.splits > 1) {
+      const size_t p = (((size_t)k.at * a.H + k.h) * a.splits + blockIdx.y) * ROWS + i - k.row0;
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+          *reinterpret_cast<f4 *>(a.part_o + p * D + d * 32 + y * 8 + half * 4) =
+              f4{st.o[d][y * 4], st.o[d][y * 4 + 1], st.o[d][y * 4 + 2], st.o[d][y * 4 + 3]};
+      if (half == 0) {
+        a.part_ml[p * 2] = st.m;
+        a.part_ml[p * 2 + 1] = st.l;
+      }
+      return;
+    }
+    const int head = k.h * a.G + i - t * a.G;
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
       for (int y = 0; y < 4; ++y)
-        *reinterpret_cast<f4 *>(a.part_o + p * D + d * 32 + y * 8 + half * 4) =
-            f4{st.o[d][y * 4], st.o[d][y * 4 + 1], st.o[d][y * 4 + 2], st.o[d][y * 4 + 3]};
-    if (half == 0) {
-      a.part_ml[p * 2] = st.m;
-      a.part_ml[p * 2 + 1] = st.l;
-    }
-    return;
+        Rows<T, D, 1>::finish(a, k.rq.first + t, head, d * 32 + y * 8 + half * 4, st.m, st.l,
+                              f4{st.o[d][y * 4], st.o[d][y * 4 + 1], st.o[d][y * 4 + 2], st.o[d][y * 4 + 3]});
   }
-  const int head = h * a.G + i - t * a.G;
-#pragma unroll
-  for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-    for (int y = 0; y < 4; ++y)
-      Rows<T, D, 1>::finish(a, rq.first + t, head, d * 32 + y * 8 + half * 4, st.m, st.l,
-                            f4{st.o[d][y * 4], st.o[d][y * 4 + 1], st.o[d][y * 4 + 2], st.o[d][y * 4 + 3]});
+};
+
+// A barrier for what lies in LDS alone: loads from memory stay in flight across it.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// Each tile is staged while the one before is worked on.
+template <typename T, int D, int W>
+__global__ void __launch_bounds__(64 * W, D <= 64 && W == 4 ? 3 : D <= 128 ? 2 : 1) k_tiles(AttArgs a) {
+  constexpr int ROWS = 32 * W;
+  __shared__ KeyTile<T, D> keys[2];
+  __shared__ ValueTile<D, W> values[2];
+  __shared__ long long list_[kListed + 1];
+  const TileWork k = tile_work<ROWS>(a, list_);
+  if (k.none) return;
+  TileRows<T, D> st;
+  TileWave<T, D, ROWS> wave;
+  wave.begin(a, k, st);
+  const int32_t *table = a.table + (size_t)k.r * a.MB;
+  Stage<T, D, W> g;
+  const auto blocks = [&](int u) {
+    g.key_blocks(a, table, u * kUnit);
+    g.value_blocks(a, table, u * kUnit);
+  };
+  const auto load = [&](int u) {
+    g.load_keys(a, k.h, u * kUnit);
+    g.load_values(a, u * kUnit);
+  };
+  const auto store = [&](int u) {
+    g.store_keys(a, keys[u & 1]);
+    g.store_values(k.rq.length - u * kUnit, k.look(a, u), values[u & 1]);
+  };
+  if (k.begin < k.end) {
+    g.begin(a, k.h);
+    blocks(k.begin);
+    load(k.begin);
+    blocks(k.begin + 1);
+    store(k.begin);
+  }
+  lds_barrier();
+  for (int u = k.begin; u < k.end; ++u) {
+    const int base = u * kUnit;
+    if (u + 1 < k.end) {
+      load(u + 1);
+      blocks(u + 2);
+    }
+    if (wave.sees(a, base)) {
+      st.products(keys[u & 1]);
+      st.weights(keys[u & 1], base, wave.masked(a, base));
+      st.sums(values[u & 1], base, k.look(a, u));
+    }
+    if (u + 1 < k.end) store(u + 1);
+    lds_barrier();
+  }
+  wave.end(a, k, st);
 }
 
 template <typename T, int D>
