@@ -30,7 +30,6 @@
 #include <climits>
 #include <cstddef>
 #include <cstdint>
-#include <cstdlib>
 
 #include "festina.h"
 #include "kv.h"
@@ -53,7 +52,10 @@ typedef unsigned u2 __attribute__((ext_vector_type(2)));
 constexpr int kUnit = 64;            // keys of a step
 constexpr int kWaves = 4;
 constexpr int kBlock = 64 * kWaves;
-constexpr int kWorkers = 2048;       // pieces that k_rows cuts the keys into: two waves a SIMD
+// Waves of k_rows on a SIMD, and the pieces that it cuts the keys into: one for each wave of 256 compute units.  (Three
+// waves of 128 dims and one row tile, 168 registers each, were slower: 64 requests up to 32,768 tokens 473 us against 440.)
+constexpr int waves_of(int D, int NT) { return D > 128 || NT > 2 ? 1 : 2; }
+constexpr int workers_of(int D, int NT) { return 1024 * waves_of(D, NT); }
 constexpr int kGroups = 512;         // workgroups of k_tiles that fill the chip: two a compute unit
 constexpr int kListed = 512;         // requests whose running sums a workgroup forms by itself
 constexpr int kMaxRequests = 1 << 20;
@@ -602,7 +604,7 @@ __global__ void __launch_bounds__(kBlock, (D <= 128 && NT <= 2) ? 2 : 1) k_rows_
 
 // A wave a piece.
 template <typename T, int D, int NT>
-__global__ void __launch_bounds__(64, (D <= 128 && NT <= 2) ? 2 : 1) k_rows(AttArgs a) {
+__global__ void __launch_bounds__(64, waves_of(D, NT)) k_rows(AttArgs a) {
   typedef Rows<T, D, NT> K;
   __shared__ long long list_[kListed + 1];
   const long long *list = a.plan;
@@ -639,25 +641,42 @@ __global__ void __launch_bounds__(64, (D <= 128 && NT <= 2) ? 2 : 1) k_rows(AttA
   if (threadIdx.x == 0) a.cuts[w] = cut;
 }
 
-// Joins one row's n pieces, the first at p0 and the others from p1 on: a wave, lanes over the row.
+// Joins one row's n pieces, the first at p0 and the others from p1 on: a wave, lanes over the row, eight pieces' loads in
+// flight at a time.
 template <typename T, int D>
 __device__ __forceinline__ void join_row(const AttArgs &a, size_t p0, size_t p1, size_t stride, int n, int t, int head) {
-  const int lane = threadIdx.x & 63;
-  const auto at = [&](int i) { return i == 0 ? p0 : p1 + (size_t)(i - 1) * stride; };
+  constexpr int kAtOnce = 8;
+  const int d = (threadIdx.x & 63) * 4;
+  if (d >= D) return;
   float M = kNegInf(), L = 0.f;
-  for (int i = lane; i < n; i += 64) M = fmaxf(M, a.part_ml[at(i) * 2]);
+  f4 O = f4{0.f, 0.f, 0.f, 0.f};
+  for (int i0 = 0; i0 < n; i0 += kAtOnce) {
+    f4 o[kAtOnce];
+    float2 ml[kAtOnce];
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor(M, d));
-  for (int i = lane; i < n; i += 64) L = fmaf(a.part_ml[at(i) * 2 + 1], weight(a.part_ml[at(i) * 2], M), L);
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int i = min(i0 + k, n - 1);
+      const size_t at = i == 0 ? p0 : p1 + (size_t)(i - 1) * stride;
+      ml[k] = *reinterpret_cast<const float2 *>(a.part_ml + at * 2);
+      o[k] = *reinterpret_cast<const f4 *>(a.part_o + at * D + d);
+    }
+    float now = M;
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) L += __shfl_xor(L, d);
-  if (lane * 4 < D) {
-    f4 O = f4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-    for (int i = 0; i < n; ++i)
-      O += *reinterpret_cast<const f4 *>(a.part_o + at(i) * D + lane * 4) * weight(a.part_ml[at(i) * 2], M);
-    Rows<T, D, 1>::finish(a, t, head, lane * 4, M, L, O);
+    for (int k = 0; k < kAtOnce; ++k) now = fmaxf(now, ml[k].x);
+    const float f = weight(M, now);
+    M = now;
+    L *= f;
+    O *= f;
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const float g = i0 + k < n ? weight(ml[k].x, M) : 0.f;
+      if (i0 + k < n) {
+        L = fmaf(ml[k].y, g, L);
+        O += o[k] * g;
+      }
+    }
   }
+  Rows<T, D, 1>::finish(a, t, head, d, M, L, O);
 }
 
 // A wave joins a row of the tile that the cut at piece blockIdx.x + 1 leaves to it.
@@ -779,7 +798,7 @@ struct Stage {
     }
   }
 
-  __device__ __forceinline__ void store_keys(const AttArgs &a, KeyTile<T, D> &b) const {
+  __device__ __forceinline__ void put_keys(KeyTile<T, D> &b) const {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int x = key_item(i), d = x % (D / 16) * 16;
@@ -788,6 +807,8 @@ struct Stage {
       for (int j = 0; j < 2; ++j)
         *reinterpret_cast<typename Vec8<T>::type *>(&b.k[key_of(x)][d + j * 8]) = decode8<T>(raw_k[i][2 * j], raw_k[i][2 * j + 1]);
     }
+  }
+  __device__ __forceinline__ void put_scales(const AttArgs &a, KeyTile<T, D> &b) const {
     if (threadIdx.x < 4) {
       // a block that is not there: its codes are zeros and its logits -inf
       const float s = fminf(fmaxf(vs, kScaleMin), kScaleMax);
@@ -797,10 +818,9 @@ struct Stage {
     }
   }
 
-  // `n`: keys of the tile that there are; `look`: some row of the workgroup does not see all of them.
-  __device__ __forceinline__ void store_values(int n, bool look, ValueTile<D, W> &b) {
-    if (look) {
-      rarely();
+  // `n`: keys of the tile that there are.  For tiles of which some row of the workgroup does not see all.
+  __device__ __forceinline__ void clean_values(int n, ValueTile<D, W> &b) {
+    {
       unsigned any = 0;
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
@@ -821,6 +841,8 @@ struct Stage {
       const int nans = __any(any != 0);
       if ((threadIdx.x & 63) == 0) b.nans[threadIdx.x >> 6] = nans;
     }
+  }
+  __device__ __forceinline__ void put_values(ValueTile<D, W> &b) const {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int y = value_item(i);
@@ -1096,8 +1118,13 @@ __global__ void __launch_bounds__(64 * W, D <= 64 && W == 4 ? 3 : D <= 128 ? 2 :
     g.load_values(a, u * kUnit);
   };
   const auto store = [&](int u) {
-    g.store_keys(a, keys[u & 1]);
-    g.store_values(k.rq.length - u * kUnit, k.look(a, u), values[u & 1]);
+    g.put_keys(keys[u & 1]);
+    g.put_scales(a, keys[u & 1]);
+    if (k.look(a, u)) {
+      rarely();
+      g.clean_values(k.rq.length - u * kUnit, values[u & 1]);
+    }
+    g.put_values(values[u & 1]);
   };
   if (k.begin < k.end) {
     g.begin(a, k.h);
@@ -1187,9 +1214,13 @@ festina_status shape_of(const festina_kv_cache *c, const festina_attention *t, S
   s->cut = keys > 2 * kWaves * kUnit;
   if (!s->cut && (long long)t->n_requests * H * max(s->tiles_each, 1) > INT_MAX) return FESTINA_ERR_UNSUPPORTED;
   size_t parts = 0;
-  if (s->nt && s->cut) parts = (size_t)2 * kWorkers * 16 * s->nt;
+  if (s->nt && s->cut) parts = (size_t)2 * workers_of(D, s->nt) * 16 * s->nt;
   if (s->tiles) {
-    s->tile_rows = getenv("FST_W8") && D <= 128 ? 256 : 128;
+    // 256 rows a workgroup stage each tile half as often for a row, where registers allow and enough workgroups are
+    // left: a prompt of 8,192 tokens (32 heads over 8 of 128 dims) 641 us against 662 with 128; 9,215 tokens of 16
+    // heads of 64 dims, with three smaller workgroups a compute unit, 183 against 234 the other way
+    const long long rows_all = (long long)t->n_tokens * G * H;
+    s->tile_rows = (D == 96 || D == 128) && rows_all >= 256ll * kGroups ? 256 : 128;
     s->tile_groups = ((long long)t->n_tokens * G + s->tile_rows - 1) / s->tile_rows + t->n_requests;
     if (s->tile_groups * H > INT_MAX) return FESTINA_ERR_UNSUPPORTED;
     // at least two workgroups a compute unit, of at least 16 steps each
@@ -1203,14 +1234,15 @@ festina_status shape_of(const festina_kv_cache *c, const festina_attention *t, S
   }
   s->plan = 0;
   s->cuts = up((size_t)2 * (t->n_requests + 1) * 8);
-  s->part_ml = s->cuts + up((size_t)kWorkers * sizeof(Cut));
+  s->part_ml = s->cuts + up((size_t)workers_of(D, max(s->nt, 1)) * sizeof(Cut));
   s->part_o = s->part_ml + up(parts * 8);
   s->bytes = s->part_o + up(parts * D * 4);
   return FESTINA_OK;
 }
 
 template <typename T, int D, int NT>
-void run_rows(const AttArgs &a, const Shape &s, hipStream_t st) {
+void run_rows(AttArgs a, const Shape &s, hipStream_t st) {
+  a.workers = workers_of(D, NT);
   if (!s.cut) {
     k_rows_whole<T, D, NT><<<(unsigned)(a.R * a.H * s.tiles_each), kBlock, 0, st>>>(a);
     return;
@@ -1233,10 +1265,10 @@ void run(AttArgs a, const Shape &s, long long *plan, hipStream_t st) {
   if constexpr (row_tiles_most(D) >= 4)
     if (s.nt == 4) run_rows<T, D, 4>(a, s, st);
   if (s.tiles) {
-    if constexpr (D <= 128)
-      if (s.tile_rows == 256) k_tiles<T, D, 8><<<dim3((unsigned)(s.tile_groups * a.H), s.splits), 512, 0, st>>>(a);
-    if (s.tile_rows == 128)
-      k_tiles<T, D, 4><<<dim3((unsigned)(s.tile_groups * a.H), s.splits), kBlock, 0, st>>>(a);
+    const dim3 grid((unsigned)(s.tile_groups * a.H), s.splits);
+    if constexpr (D == 96 || D == 128)
+      if (s.tile_rows == 256) k_tiles<T, D, 8><<<grid, 512, 0, st>>>(a);
+    if (s.tile_rows == 128) k_tiles<T, D, 4><<<grid, kBlock, 0, st>>>(a);
     if (s.splits > 1)
       k_tiles_join<T, D><<<dim3((unsigned)(s.tile_groups * a.H), s.tile_rows / kWaves), kBlock, 0, st>>>(a);
   }
@@ -1286,7 +1318,6 @@ extern "C" festina_status festina_attend(const festina_kv_cache *cache, const fe
   a.window = att->window;
   a.rows_max = s.rows_max;
   a.tiles_each = s.tiles_each;
-  a.workers = kWorkers;
   a.splits = s.splits;
   a.tile_rows = s.tile_rows;
   a.scale = att->scale * 1.44269504088896341f;

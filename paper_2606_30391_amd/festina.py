@@ -652,13 +652,15 @@ class _Workspaces:
 
     def get(self, n, stream, device):
         """(address of at least n bytes for calls on `stream`, that stream's handle)."""
-        import torch
         handle = _stream_handle(stream).value or 0
-        ws = self.by_stream.get(handle)
-        if ws is None or ws.numel() < n:
+        ws, at, size = self.by_stream.get(handle, (None, 0, -1))
+        if size < n:
+            import torch
             with _on(stream, device):
-                ws = self.by_stream[handle] = torch.empty(max(n, 256), dtype=torch.uint8, device=device)
-        return ws.data_ptr(), handle
+                ws = torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+            at = ws.data_ptr()
+            self.by_stream[handle] = ws, at, ws.numel()
+        return at, handle
 
 
 class DeviceBlocks:
@@ -728,8 +730,10 @@ class DeviceCache:
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.cache = festina_kv_cache(n, bt, h, d, _ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale))
         self._ws, self._ws_bytes = _Workspaces(), {}
-        self._types = {torch.bfloat16: FESTINA_BF16, torch.float16: FESTINA_F16, torch.float32: FESTINA_F32}
-        self._halves, self._int32, self._rows = (torch.bfloat16, torch.float16), (torch.int32,), (h, d)
+        self._halves = {torch.bfloat16: FESTINA_BF16, torch.float16: FESTINA_F16}
+        self._types = {**self._halves, torch.float32: FESTINA_F32}
+        self._int32, self._f32, self._rows, self._scale = (torch.int32,), torch.float32, (h, d), d ** -0.5
+        self._empty, self._attend, self._cache_ref = torch.empty, lib().festina_attend, C.byref(self.cache)
 
     @classmethod
     def empty(cls, n_blocks: int, block_tokens: int, n_kv_heads: int, head_dim: int, device="cuda"):
@@ -759,34 +763,51 @@ class DeviceCache:
         """Attention of the queries [tokens][heads][dim] (bfloat16 or half) over the cache: (out, lse).  table
         [requests][columns], length [requests] (new tokens included) and first [requests+1] are a step's
         (DeviceBlocks); max_new bounds the new tokens of one request.  out and lse are made where not given."""
-        import torch
-        _check(q, "q", self._halves)
-        if q.dim() != 3 or q.shape[2] != self._rows[1] or (q.stride(2) != 1 and q.numel()):
-            raise ValueError(f"q: [tokens][heads][{self._rows[1]}] with its last axis contiguous")
-        _check(table, "table", self._int32)
+        # every check by itself: _check() where one fails names what is wrong (a decode step's kernels take about as
+        # long as this function's host work, so it keeps to a few attribute reads a tensor)
+        dim = self._rows[1]
+        dtype = q.dtype
+        kind = self._halves.get(dtype)
+        i32 = self._int32[0]
+        if kind is None or not q.is_cuda:
+            _check(q, "q", self._halves)
+        if q.dim() != 3 or q.shape[2] != dim or (q.stride(2) != 1 and q.numel()):
+            raise ValueError(f"q: [tokens][heads][{dim}] with its last axis contiguous")
+        if table.dtype is not i32 or not table.is_cuda:
+            _check(table, "table", self._int32)
         if table.dim() != 2 or not table.is_contiguous():
             raise ValueError("table: a contiguous tensor of two dimensions is needed")
         T, heads, _ = q.shape
         R, columns = table.shape
-        _check(length, "length", self._int32, (R,))
-        _check(first, "first", self._int32, (R + 1,))
-        if out is None or lse is None:
+        if length.dtype is not i32 or not length.is_cuda or length.dim() != 1 or len(length) != R or \
+                not length.is_contiguous():
+            _check(length, "length", self._int32, (R,))
+        if first.dtype is not i32 or not first.is_cuda or first.dim() != 1 or len(first) != R + 1 or \
+                not first.is_contiguous():
+            _check(first, "first", self._int32, (R + 1,))
+        if stream is None:
+            if out is None:
+                out = self._empty((T, heads, dim), dtype=dtype, device=q.device)
+            if lse is None:
+                lse = self._empty((T, heads), dtype=self._f32, device=q.device)
+        elif out is None or lse is None:
             with _on(stream, q.device):
-                if out is None:
-                    out = torch.empty((T, heads, q.shape[2]), dtype=q.dtype, device=q.device)
-                if lse is None:
-                    lse = torch.empty((T, heads), dtype=torch.float32, device=q.device)
-        _check(out, "out", (q.dtype,))
+                return self.attend(q, table, length, first, max_new, scale, window,
+                                   self._empty((T, heads, dim), dtype=dtype, device=q.device) if out is None else out,
+                                   self._empty((T, heads), dtype=self._f32, device=q.device) if lse is None else lse,
+                                   stream)
+        if out.dtype is not dtype or not out.is_cuda:
+            _check(out, "out", (dtype,))
         if out.shape != q.shape or (out.stride(2) != 1 and out.numel()):
             raise ValueError("out: q's shape with its last axis contiguous")
-        _check(lse, "lse", (torch.float32,), (T, heads))
+        if lse.dtype is not self._f32 or not lse.is_cuda or lse.dim() != 2 or not lse.is_contiguous() or \
+                lse.shape[0] != T or lse.shape[1] != heads:
+            _check(lse, "lse", (self._f32,), (T, heads))
         qt, qh, _ = q.stride()
         ot, oh, _ = out.stride()
-        if scale is None:
-            scale = self._rows[1] ** -0.5
-        att = festina_attention(R, columns, T, heads, max_new, self._types[q.dtype], window, scale, table.data_ptr(),
-                                length.data_ptr(), first.data_ptr(), q.data_ptr(), qt, qh, out.data_ptr(), ot, oh,
-                                lse.data_ptr())
+        att = festina_attention(R, columns, T, heads, max_new, kind, window, self._scale if scale is None else scale,
+                                table.data_ptr(), length.data_ptr(), first.data_ptr(), q.data_ptr(), qt, qh,
+                                out.data_ptr(), ot, oh, lse.data_ptr())
         sizes = (R, columns, T, heads, max_new)
         n = self._ws_bytes.get(sizes)
         if n is None:
@@ -794,7 +815,9 @@ class DeviceCache:
                 self._ws_bytes.clear()
             n = self._ws_bytes[sizes] = festina_attend_workspace_bytes(self.cache, att)
         ws, handle = self._ws.get(n, stream, q.device)
-        festina_attend(self.cache, att, ws, n, handle)
+        st = self._attend(self._cache_ref, C.byref(att), ws, n, handle)
+        if st != FESTINA_OK:
+            raise FestinaError(st, "festina_attend")
         return out, lse
 
 

@@ -136,6 +136,24 @@ def test_prompts_over_a_long_cache(requests, max_new):
     Case(rng, requests, D=128, H=2, G=2, bt=16).check(max_new=max_new)
 
 
+@pytest.mark.parametrize("D,dtype", [(96, "f16"), (128, "bf16")])
+def test_large_prompts(D, dtype):
+    """As many rows (heads x tokens) as have tiles of 256 rows: three key heads of 64 compared."""
+    rng = np.random.default_rng(D)
+    H, G = 64, 8
+    c = Case(rng, [(500, 200), (77, 77), (1, 1)], D=D, H=H, G=G, bt=64, dtype=dtype)
+    for place in (320, 383, 384, 499):                        # a NaN that some rows see
+        c.v[c.table[0, place // 64], 40, 7, place % 64] = 0x7F
+    print(f"[gpu] attend large prompt D={D}", flush=True)
+    out, lse = c.cache().attend(c.q, *c.tensors(), max_new=200)
+    torch.cuda.synchronize()
+    for h in (0, 40, 63):
+        one = Case(rng, [(1, 1)], D=D, H=1, G=G, dtype=dtype)
+        one.k, one.v, one.ks, one.vs = (x[:, h:h + 1] for x in (c.k, c.v, c.ks, c.vs))
+        one.table, one.length, one.first, one.q = c.table, c.length, c.first, c.q[:, h * G:(h + 1) * G]
+        one.compare(out[:, h * G:(h + 1) * G], lse[:, h * G:(h + 1) * G], one.want())
+
+
 @pytest.mark.parametrize("window", [1, 16, 63, 200, 10 ** 9])
 def test_windows(window):
     rng = np.random.default_rng(window % 1000)
@@ -269,7 +287,7 @@ def test_the_result_does_not_depend_on_the_workspace_or_the_bound():
         cache = c.cache()
         print("[gpu] attend workspace", flush=True)
         a = cache.attend(c.q, *c.tensors(), max_new=90)
-        for ws in cache._ws.by_stream.values():
+        for ws, _, _ in cache._ws.by_stream.values():
             ws.fill_(255)
         b = cache.attend(c.q, *c.tensors(), max_new=90)
         torch.cuda.synchronize()
