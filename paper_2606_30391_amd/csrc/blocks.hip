@@ -15,7 +15,8 @@
 //   request that its first token belongs to, so that no search crosses the whole list.
 // k_extend_fill    the slots, a stretch of 256 or 1,024 tokens a wave.  Where they lie in one request, everything
 //   about it is uniform, and a lane makes its slots four at a time from one or two block ids, with all loads in
-//   flight together.  Where they do not, each lane searches the few requests of its stretch in LDS.
+//   flight together.  Where they do not, each lane searches the few requests of its stretch in LDS, in steps
+//   that all groups of the stretch take together, so that their loads wait once (4,096 requests: 14.7 -> 13.9 us).
 // k_release        a thread per returned id, after the same sums.
 //
 // All arithmetic is on integers, so results do not depend on order.  Bound by the bytes of the slot map on
@@ -50,7 +51,8 @@ struct BlockArgs {
   const uint8_t *done;
   // workspace
   long long *sum_blocks, *sum_tokens;   // [chunks]
-  int4 *ends;                           // [chunks] served tokens up to the chunk's last, that request, blocks taken
+  int4 *ends;                           // served tokens, the last request with any, the blocks they take: of each chunk
+                                        // of a direct scan, else of all in ends[0]
   int32_t *n_free_in;                   // [1] the count before the call
   int4 *about;                          // [R] see About
   int32_t *owner;                       // [fill stretches] request of a stretch's first token
@@ -196,6 +198,7 @@ __global__ void __launch_bounds__(kChunk) k_extend_sums(BlockArgs a) {
   if (threadIdx.x == 0) {
     a.sum_blocks[blockIdx.x] = B;
     a.sum_tokens[blockIdx.x] = T;
+    if (blockIdx.x == 0) a.ends[0] = make_int4(0, 0, 0, 0);
   }
 }
 
@@ -251,7 +254,12 @@ __global__ void __launch_bounds__(kChunk) k_extend_scan(BlockArgs a) {
 #pragma unroll
     for (int w = 0; w < kChunk / 64; ++w)
       e = make_int4(max(e.x, ends[w][0]), max(e.y, ends[w][1]), max(e.z, ends[w][2]), 0);
-    a.ends[blockIdx.x] = e;
+    if (DIRECT) {
+      a.ends[blockIdx.x] = e;
+    } else if (e.x) {                                  // one maximum a workgroup, whatever their order
+      int *all = reinterpret_cast<int *>(a.ends);
+      atomicMax(all, e.x), atomicMax(all + 1, e.y), atomicMax(all + 2, e.z);
+    }
     if (blockIdx.x == 0) *a.n_free_in = n_free;
   }
 }
@@ -263,15 +271,20 @@ __global__ void __launch_bounds__(256) k_extend_fill(BlockArgs a, int32_t chunks
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, bt = 1 << a.shift;
   int *first = lists[wave];
   int end = 0, last = 0, taken = 0;
-  for (int i = lane; i < chunks; i += 64) {
-    const int4 e = a.ends[i];
-    end = max(end, e.x), last = max(last, e.y), taken = max(taken, e.z);
-  }
+  if (chunks == 1) {
+    const int4 e = a.ends[0];
+    end = e.x, last = e.y, taken = e.z;
+  } else {
+    for (int i = lane; i < chunks; i += 64) {
+      const int4 e = a.ends[i];
+      end = max(end, e.x), last = max(last, e.y), taken = max(taken, e.z);
+    }
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) {
-    end = max(end, __shfl_xor(end, d));
-    last = max(last, __shfl_xor(last, d));
-    taken = max(taken, __shfl_xor(taken, d));
+    for (int d = 32; d > 0; d >>= 1) {
+      end = max(end, __shfl_xor(end, d));
+      last = max(last, __shfl_xor(last, d));
+      taken = max(taken, __shfl_xor(taken, d));
+    }
   }
   end = __builtin_amdgcn_readfirstlane(end);
   const auto put = [&](int t, const int (&s)[4]) {
@@ -285,11 +298,10 @@ __global__ void __launch_bounds__(256) k_extend_fill(BlockArgs a, int32_t chunks
   };
   for (int w = blockIdx.x * 4 + wave; w < fills; w += gridDim.x * 4) {
     const int t0 = w * kFill;
-    int lo0 = 0, n = 0;                                // requests lo0 .. lo0 + n - 1
-    if (t0 < end) {
-      lo0 = __builtin_amdgcn_readfirstlane(a.owner[w]);
-      n = __builtin_amdgcn_readfirstlane(t0 + kFill < end ? a.owner[w + 1] : last) - lo0 + 1;
-    }
+    // requests lo0 .. lo0 + n - 1 (what is read for stretches past the end is not used)
+    int lo0 = __builtin_amdgcn_readfirstlane(a.owner[w]), n = __builtin_amdgcn_readfirstlane(a.owner[w + 1]);
+    n = t0 >= end ? 0 : (t0 + kFill < end ? n : __builtin_amdgcn_readfirstlane(last)) - lo0 + 1;
+    if (n == 0) lo0 = 0;
     // Four slots from the lane's token t on, all of request r; tokens past `tail` get none.
     const auto quad = [&](int r, const About &q, int t, int tail) {
       const int p = t + q.shift, c = p >> a.shift, o = p & (bt - 1), over = o + 3 - (bt - 1) - max(t + 3 - tail, 0);
@@ -302,10 +314,15 @@ __global__ void __launch_bounds__(256) k_extend_fill(BlockArgs a, int32_t chunks
     };
     const auto slots = [&](const About &q, int t, int tail, int2 id) {
       const int o = (t + q.shift) & (bt - 1);
+      // the slot that the lane's first token has, or would have, in either block; none stays below 0 with 3 added
+      const int in0 = (unsigned)id.x < (unsigned)a.NB ? (id.x << a.shift) + o : INT_MIN;
+      const int in1 = (unsigned)id.y < (unsigned)a.NB ? (id.y << a.shift) + o - bt : INT_MIN;
       int s[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        s[i] = t + i > tail ? -1 : o + i < bt ? slot_of(a, id.x, o + i) : slot_of(a, id.y, o + i - bt);
+      for (int i = 0; i < 4; ++i) s[i] = max((o + i < bt ? in0 : in1) + i, -1);
+      if (t + 3 > tail)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[i] = t + i > tail ? -1 : s[i];
       put(t, s);
     };
     if (n <= 1) {                                      // one request, or none
@@ -321,45 +338,75 @@ __global__ void __launch_bounds__(256) k_extend_fill(BlockArgs a, int32_t chunks
     }
     for (int i = lane; i < min(n, kList); i += 64) first[i] = a.first[lo0 + i];
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    const auto start = [&](int i) { return i < kList ? first[i] : a.first[lo0 + i]; };
-    const auto owner = [&](int t, int lo) {            // the request of token t, lo0 + lo or later
-      int hi = n;
-      while (hi - lo > 1) {
-        const int m = (lo + hi) >> 1;
-        if (start(m) <= t) lo = m; else hi = m;
-      }
-      return lo;
-    };
-    int from = 0;
+    // where request lo0 + i's tokens begin, the end behind the last; a lane's four tokens lie in one request, in two, or
+    // (single tokens side by side) in more, which is left for later
+    const auto start = [&](int i) { return min(i >= n ? end : i < kList ? first[i] : a.first[lo0 + i], end); };
+    int of[kGroups], then[kGroups], stop[kGroups], stop2[kGroups];
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) of[g] = 0;
+    for (int s = 1 << (31 - __builtin_clz(n)); s; s >>= 1)                // the last request that begins at or before t
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g)
+        if (of[g] + s < n && start(of[g] + s) <= t0 + g * 256 + lane * 4) of[g] += s;
+    int4 about[kGroups], about2[kGroups];
+#pragma unroll
     for (int g = 0; g < kGroups; ++g) {
-      const int tw = t0 + g * 256, t = tw + lane * 4, tail = min(tw + 255, end - 1);
-      if (tw >= a.max_tokens) break;
-      if (tw < end) from = __builtin_amdgcn_readfirstlane(owner(tw, from));
-      if (tw < end && (from + 1 >= n || start(from + 1) > tail)) {
-        const int4 q4 = a.about[lo0 + from];
-        const About q{q4.x, q4.y, q4.z, q4.w};
-        slots(q, t, tail, quad(lo0 + from, q, t, tail));
-        continue;
+      const int t = t0 + g * 256 + lane * 4;
+      stop[g] = start(of[g] + 1);
+      then[g] = of[g] + 1;
+      stop2[g] = end;
+      about[g] = about2[g] = make_int4(0, 0, 0, 0);
+      if (t < end) about[g] = a.about[lo0 + of[g]];
+      if (t + 3 >= stop[g] && stop[g] < end) {
+        while (start(then[g] + 1) <= stop[g]) ++then[g];                  // the request of token `stop`
+        stop2[g] = start(then[g] + 1);
+        about2[g] = a.about[lo0 + then[g]];
       }
-      int s[4] = {-1, -1, -1, -1};
-      if (t < end) {
-        int i = owner(t, from), r = -1, stop = t, c = -1, id = 0;         // stop: where request r's tokens end
+    }
+    int2 id[kGroups], id2[kGroups];
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      const int t = t0 + g * 256 + lane * 4;
+      id[g] = quad(lo0 + of[g], About{about[g].x, about[g].y, about[g].z, about[g].w}, t, stop[g] - 1);
+      id2[g] = make_int2(-1, -1);
+      if (t + 3 >= stop[g] && stop[g] < end) {
+        const About q{about2[g].x, about2[g].y, about2[g].z, about2[g].w};
+        const int p = stop[g] + q.shift, c = p >> a.shift, p1 = min(t + 3, stop2[g] - 1) + q.shift;
+        id2[g].x = block_at(a, lo0 + then[g], q, c, (p & (bt - 1)) == 0);
+        if (p1 >> a.shift != c) id2[g].y = block_at(a, lo0 + then[g], q, c + 1, true);
+      }
+    }
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      const int t = t0 + g * 256 + lane * 4;
+      if (t >= a.max_tokens) break;
+      const int o = (t + about[g].x) & (bt - 1), c2 = (stop[g] + about2[g].x) >> a.shift;
+      int s[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int p2 = t + k + about2[g].x;
+        s[k] = t + k < stop[g] ? (o + k < bt ? slot_of(a, id[g].x, o + k) : slot_of(a, id[g].y, o + k - bt))
+                               : slot_of(a, p2 >> a.shift == c2 ? id2[g].x : id2[g].y, p2 & (bt - 1));
+        if (t + k >= end) s[k] = -1;
+      }
+      if (t + 3 >= stop2[g] && stop2[g] < end) {
+        int i = then[g], r = -1, c = -1, block = 0, next = stop2[g];      // next: where request r's tokens end
         About q{};
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          if (t + k >= end) break;
-          if (t + k >= stop) {
-            if (r >= 0) ++i;
-            while (i + 1 < n && start(i + 1) <= t + k) ++i;
-            stop = i + 1 < n ? min(start(i + 1), end) : end;
+          if (t + k < stop2[g] || t + k >= end) continue;
+          if (t + k >= next || r < 0) {
+            ++i;
+            while (start(i + 1) <= t + k) ++i;
+            next = start(i + 1);
             r = lo0 + i;
             const int4 q4 = a.about[r];
             q = About{q4.x, q4.y, q4.z, q4.w};
             c = -1;
           }
-          const int p = t + k + q.shift, o = p & (bt - 1);
-          if (p >> a.shift != c) id = block_at(a, r, q, c = p >> a.shift, o == 0);
-          s[k] = slot_of(a, id, o);
+          const int p = t + k + q.shift, at = p & (bt - 1);
+          if (p >> a.shift != c) block = block_at(a, r, q, c = p >> a.shift, at == 0);
+          s[k] = slot_of(a, block, at);
         }
       }
       put(t, s);
@@ -463,7 +510,7 @@ Layout layout(int R, int max_tokens) {
   l.n_free_in = l.ends + up(chunks * 16);
   l.about = l.n_free_in + 256;
   l.owner = l.about + up((size_t)R * 16);
-  l.bytes = l.owner + up((fills + 1) * 4);
+  l.bytes = l.owner + up((fills + 2) * 4);
   return l;
 }
 
@@ -540,8 +587,9 @@ extern "C" festina_status festina_extend_blocks(const festina_kv_requests *req, 
       k_extend_scan<false><<<chunks, kChunk, 0, st>>>(a);
     }
     const int grid = min(max(max((fills + 3) / 4, chunks), 1), 8192);
-    if (a.fill > 256) k_extend_fill<kGroupsMost><<<grid, 256, 0, st>>>(a, chunks, fills, vec);
-    else k_extend_fill<1><<<grid, 256, 0, st>>>(a, chunks, fills, vec);
+    const int ends = a.R <= kDirect ? chunks : 1;
+    if (a.fill > 256) k_extend_fill<kGroupsMost><<<grid, 256, 0, st>>>(a, ends, fills, vec);
+    else k_extend_fill<1><<<grid, 256, 0, st>>>(a, ends, fills, vec);
   }
   return hipGetLastError() == hipSuccess ? FESTINA_OK : FESTINA_ERR_DEVICE;
 }
