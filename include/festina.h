@@ -562,7 +562,7 @@ typedef struct festina_kv_step {
 size_t festina_blocks_workspace_bytes(int32_t n_requests, int32_t max_tokens);
 
 /* Blocks and slots for the step's new tokens.  Workspace 256-byte aligned, clobbered; one kernel
- * launch on `stream` for a small step, three otherwise. */
+ * launch on `stream` for up to 1,024 requests and 8,192 tokens, two up to 16,384 requests, three beyond. */
 festina_status festina_extend_blocks(const festina_kv_requests *req, festina_kv_step *out, void *workspace,
                                      size_t workspace_bytes, void *stream);
 
