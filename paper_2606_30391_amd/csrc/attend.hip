@@ -573,7 +573,7 @@ struct Rows {
   }
 
   static __device__ __forceinline__ void finish(const AttArgs &a, int t, int head, int d, float M, float L, f4 O) {
-    const bool none = M == kNegInf();
+    const bool none = M == kNegInf() && L == L;     // (NaN logits leave the maximum alone)
     const float f = none ? 0.f : 1.f / L;
     float x[4];
 #pragma unroll

@@ -416,3 +416,16 @@ def test_binding_checks_its_tensors():
             cache.attend(**{**ok, key: bad})
     with pytest.raises(F.FestinaError):
         cache.attend(**{**ok, "q": c.q[:, :7]})               # no multiple of the key heads
+
+
+@pytest.mark.parametrize("requests", [[(40, 1), (300, 1)], [(513, 1), (2000, 1), (64, 1)], [(700, 3)], [(400, 100), (65, 1)],
+                                      [(6000, 40)]])
+def test_a_nan_query_has_nan_and_no_other_row_has(requests):
+    """One launch, pieces and their join, row tiles, prompts, prompts split over the keys: a row whose logits are all
+    NaN is no row without keys."""
+    rng = np.random.default_rng(len(requests) + requests[0][0])
+    c = Case(rng, requests)
+    T = c.q.shape[0]
+    c.q[T // 2, 3, 17] = float("nan")
+    c.q[T - 1, 0, 5] = float("nan")
+    c.check()
