@@ -289,6 +289,7 @@ __device__ __forceinline__ unsigned below(int n, int w) {
 // to 2^8 are as exact in half precision as those of up to 1).  -inf: no key seen yet, logits are relative to 0.
 constexpr float kSlack = 8.f;
 __device__ __forceinline__ bool raises(float top, float m) { return top > (m == kNegInf() ? kNegInf() : kSlack); }
+constexpr float kMostSum = 256.f;    // the same for k_tiles, on the sum of a lane's weights of 32 keys
 // Takes `top` (relative to m) as the new reference where it raises it, else sets it to 0; scales l and returns the
 // factor for the row's other sums.
 __device__ __forceinline__ float raise(float &top, float &m, float &l) {
@@ -717,6 +718,7 @@ struct Stage {
   static constexpr int kThreads = 64 * W, kItems = kUnit * D / 16, kLoads = (kItems + kThreads - 1) / kThreads;
 
   const uint8_t *k[kLoads], *v[kLoads];              // the pieces in block 0
+  unsigned at_k[kLoads], at_v[kLoads], at_s;         // where their blocks stand in a tile's part of the table, in bytes
   int id_k[kLoads], id_v[kLoads], id_s;              // the blocks of the next tile
   u4 raw_k[kLoads], raw_v[kLoads];
   float ks, vs;
@@ -736,20 +738,25 @@ struct Stage {
       const int x = key_item(i), y = has(value_item(i)) ? value_item(i) : 0;
       k[i] = a.k + (size_t)h * bt * D + (key_of(x) & (bt - 1)) * D + x % (D / 16) * 16;
       v[i] = a.v + (size_t)h * bt * D + (size_t)(y >> 2) * bt + (key_of_value(y) & (bt - 1));
+      at_k[i] = (min(key_of(x), kUnit - 1) >> a.shift) * 4;
+      at_v[i] = (key_of_value(y) >> a.shift) * 4;
     }
+    at_s = ((threadIdx.x & 3) * 16 >> a.shift) * 4;
   }
 
-  static __device__ __forceinline__ int block_at(const AttArgs &a, const int32_t *table, int key) {
-    return table[min(key >> a.shift, a.MB - 1)];
-  }
-  __device__ __forceinline__ void key_blocks(const AttArgs &a, const int32_t *table, int base) {
+  // A tile begins at a multiple of 64 keys, so a key's column is the tile's first one and its own part: offsets of less
+  // than 2^29 bytes from the row's start, of which only the tile's part changes.
+  __device__ __forceinline__ void blocks(const AttArgs &a, const int32_t *table, int base) {
+    const unsigned from = (unsigned)(base >> a.shift) * 4, last = (unsigned)(a.MB - 1) * 4;
+    const auto block_at = [&](unsigned at) {
+      return *reinterpret_cast<const int32_t *>(reinterpret_cast<const char *>(table) + min(from + at, last));
+    };
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) id_k[i] = block_at(a, table, base + min(key_of(key_item(i)), kUnit - 1));
-    id_s = block_at(a, table, base + (threadIdx.x & 3) * 16);
-  }
-  __device__ __forceinline__ void value_blocks(const AttArgs &a, const int32_t *table, int base) {
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) id_v[i] = block_at(a, table, base + key_of_value(value_item(i)));
+    for (int i = 0; i < kLoads; ++i) {
+      id_k[i] = block_at(at_k[i]);
+      id_v[i] = block_at(at_v[i]);
+    }
+    id_s = block_at(at_s);
   }
 
   // The codes of the tile at `base`, whose blocks were read.  A block that is not there reads as zeros.
@@ -765,7 +772,7 @@ struct Stage {
       all &= there;
       raw_k[i] = u4{0u, 0u, 0u, 0u};
       if (has(key_item(i)))
-        raw_k[i] = *reinterpret_cast<const u4 *>(k[i] + (size_t)(unsigned)(there ? id_k[i] : 0) * block_bytes(a) + within(a, base) * D);
+        raw_k[i] = *reinterpret_cast<const u4 *>(k[i] + (size_t)min((unsigned)id_k[i], (unsigned)a.NB - 1) * block_bytes(a) + within(a, base) * D);
     }
     if (__any(!all)) {
       rarely();
@@ -788,7 +795,7 @@ struct Stage {
       all &= there;
       raw_v[i] = u4{0u, 0u, 0u, 0u};
       if (has(value_item(i)))
-        raw_v[i] = *reinterpret_cast<const u4 *>(v[i] + (size_t)(unsigned)(there ? id_v[i] : 0) * block_bytes(a) + within(a, base));
+        raw_v[i] = *reinterpret_cast<const u4 *>(v[i] + (size_t)min((unsigned)id_v[i], (unsigned)a.NB - 1) * block_bytes(a) + within(a, base));
     }
     if (__any(!all)) {
       rarely();
@@ -863,7 +870,7 @@ struct TileRows {
   f16v o[D / 32];
   f16v x[2];                         // logits of a tile, 32 keys each
   h8 w[2][2];                        // its weights
-  float m, l;
+  float ref, l, most;                // the reference (0 where no key was seen), the largest sum that leaves it
   Span sees;
 
   // x = K Q': two chains of products side by side, each operand read from LDS a step before it is used
@@ -895,14 +902,12 @@ struct TileRows {
     }
   }
 
-  // w = 2^(logits - m), l; `masked`: some row does not see all of the tile
-  __device__ __forceinline__ void weights(const KeyTile<T, D> &b, int base, bool masked) {
+  // The logits relative to the reference; `masked`: some row does not see all of the tile
+  __device__ __forceinline__ void logits(const KeyTile<T, D> &b, int base, bool masked) {
     const int h = (threadIdx.x & 63) >> 5;
-    float iv[2];
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
-      const float cc = b.c[g * 2 + h], lv = b.lv[g * 2 + h], shift = m == kNegInf() ? lv : lv - m;
-      iv[g] = b.iv[g * 2 + h];
+      const float cc = b.c[g * 2 + h], shift = b.lv[g * 2 + h] - ref;
 #pragma unroll
       for (int i = 0; i < 16; ++i) x[g][i] = fmaf(x[g][i], cc, shift);
     }
@@ -914,38 +919,51 @@ struct TileRows {
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[g][i] = s.has(g * 32 + i) ? x[g][i] : kNegInf();
     }
-    float tops[4] = {x[0][0], x[0][1], x[1][0], x[1][1]};
-#pragma unroll
-    for (int i = 2; i < 16; ++i) {
-      tops[i & 1] = fmaxf(tops[i & 1], x[0][i]);
-      tops[2 + (i & 1)] = fmaxf(tops[2 + (i & 1)], x[1][i]);
-    }
-    float top = across32(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), max_);
-    if (__any(raises(top, m))) {
-      rarely();
-      const float f = raise(top, m, l);
-#pragma unroll
-      for (int g = 0; g < 2; ++g) x[g] -= top;
-#pragma unroll
-      for (int t = 0; t < D / 32; ++t) o[t] *= f;
-    }
-#pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      float sum[2];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float p = exp2_(x[g][i]);
-        sum[i & 1] = i < 2 ? p : sum[i & 1] + p;
-        w[g][i >> 3][i & 7] = (f16)p;
-      }
-      l = fmaf(sum[0] + sum[1], iv[g], l);
-    }
   }
 
-  // o += V' w: as many chains as there are tiles of 32 dims; `look` as for Stage::store_values
+  // w = 2^logits of 32 keys, and their sum
+  template <int g>
+  __device__ __forceinline__ float powers() {
+    float sum[2];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float p = exp2_(x[g][i]);
+      sum[i & 1] = i < 2 ? p : sum[i & 1] + p;
+      w[g][i >> 3][i & 7] = (f16)p;
+    }
+    return sum[0] + sum[1];
+  }
+
+  // The weights and their part of l.  No weight is above their sum, so while that is small the reference holds and
+  // the logits' maximum need not be known.
+  template <int g>
+  __device__ __forceinline__ void weights(const KeyTile<T, D> &b) {
+    float sum = powers<g>();
+    if (__any(sum > most)) {
+      rarely();
+      float top = x[g][0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) top = fmaxf(top, x[g][i]);
+      top = across32(top, max_);
+      const bool fresh = most != kMostSum, up = top > (fresh ? kNegInf() : 0.f);
+      top = up ? top : 0.f;
+      const float f = fresh ? 1.f : exp2_(-top);
+      ref += top;
+      most = up ? kMostSum : most;
+      l *= f;
+#pragma unroll
+      for (int y = g; y < 2; ++y) x[y] -= top;
+#pragma unroll
+      for (int t = 0; t < D / 32; ++t) o[t] *= f;
+      sum = powers<g>();
+    }
+    l = fmaf(sum, b.iv[g * 2 + ((threadIdx.x & 63) >> 5)], l);
+  }
+
+  // A NaN among the values goes to the rows that see it; `look` as for Stage::clean_values
   template <int W>
-  __device__ __forceinline__ void sums(const ValueTile<D, W> &b, int base, bool look) {
-    const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5;
+  __device__ __forceinline__ void nans(const ValueTile<D, W> &b, int base, bool look) {
+    const int h = (threadIdx.x & 63) >> 5;
     if (look) {
       rarely();
       int nans = 0;
@@ -965,19 +983,23 @@ struct TileRows {
           }
       }
     }
+  }
+
+  // o += V' w over 32 keys: as many chains as there are tiles of 32 dims
+  template <int g, int W>
+  __device__ __forceinline__ void sums(const ValueTile<D, W> &b) {
+    const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5;
     constexpr int kT = D / 32;
     const auto values = [&](int j, int t) { return *reinterpret_cast<const h8 *>(&b.v[t * 32 + c][(j >> 1) * 32 + h * 16 + (j & 1) * 8]); };
     h8 vf[2][kT];
 #pragma unroll
-    for (int t = 0; t < kT; ++t) vf[0][t] = values(0, t);
+    for (int j = 0; j < 2; ++j)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (j < 3)
+      for (int t = 0; t < kT; ++t) vf[j][t] = values(2 * g + j, t);
 #pragma unroll
-        for (int t = 0; t < kT; ++t) vf[(j + 1) & 1][t] = values(j + 1, t);
+    for (int j = 0; j < 2; ++j)
 #pragma unroll
-      for (int t = 0; t < kT; ++t) o[t] = mfma32(vf[j & 1][t], w[j >> 1][j & 1], o[t]);
-    }
+      for (int t = 0; t < kT; ++t) o[t] = mfma32(vf[j][t], w[g][j], o[t]);
   }
 };
 
@@ -1038,8 +1060,8 @@ struct TileWave {
     pos_min = before + wave0 / a.G;
     pos_max = before + (min(wave0 + 32, k.rows) - 1) / a.G;
     st.sees = span(a, in ? before + t : -1);
-    st.m = kNegInf();
-    st.l = 0.f;
+    st.ref = st.l = 0.f;
+    st.most = st.sees.count > 0 ? -1.f : __builtin_inff();
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
@@ -1063,6 +1085,7 @@ struct TileWave {
   __device__ __forceinline__ void end(const AttArgs &a, const TileWork &k, TileRows<T, D> &st) const {
     const int half = (threadIdx.x & 63) >> 5;
     st.l = across32(st.l, add_);
+    const float m = st.most == kMostSum ? st.ref : kNegInf();
     if (!in) return;
     if (a.splits > 1) {
       const size_t p = (((size_t)k.at * a.H + k.h) * a.splits + blockIdx.y) * ROWS + i - k.row0;
@@ -1073,7 +1096,7 @@ struct TileWave {
           *reinterpret_cast<f4 *>(a.part_o + p * D + d * 32 + y * 8 + half * 4) =
               f4{st.o[d][y * 4], st.o[d][y * 4 + 1], st.o[d][y * 4 + 2], st.o[d][y * 4 + 3]};
       if (half == 0) {
-        a.part_ml[p * 2] = st.m;
+        a.part_ml[p * 2] = m;
         a.part_ml[p * 2 + 1] = st.l;
       }
       return;
@@ -1083,7 +1106,7 @@ struct TileWave {
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
       for (int y = 0; y < 4; ++y)
-        Rows<T, D, 1>::finish(a, k.rq.first + t, head, d * 32 + y * 8 + half * 4, st.m, st.l,
+        Rows<T, D, 1>::finish(a, k.rq.first + t, head, d * 32 + y * 8 + half * 4, m, st.l,
                               f4{st.o[d][y * 4], st.o[d][y * 4 + 1], st.o[d][y * 4 + 2], st.o[d][y * 4 + 3]});
   }
 };
@@ -1109,10 +1132,7 @@ __global__ void __launch_bounds__(64 * W, D <= 64 && W == 4 ? 3 : D <= 128 ? 2 :
   wave.begin(a, k, st);
   const int32_t *table = a.table + (size_t)k.r * a.MB;
   Stage<T, D, W> g;
-  const auto blocks = [&](int u) {
-    g.key_blocks(a, table, u * kUnit);
-    g.value_blocks(a, table, u * kUnit);
-  };
+  const auto blocks = [&](int u) { g.blocks(a, table, u * kUnit); };
   const auto load = [&](int u) {
     g.load_keys(a, k.h, u * kUnit);
     g.load_values(a, u * kUnit);
@@ -1142,8 +1162,12 @@ __global__ void __launch_bounds__(64 * W, D <= 64 && W == 4 ? 3 : D <= 128 ? 2 :
     }
     if (wave.sees(a, base)) {
       st.products(keys[u & 1]);
-      st.weights(keys[u & 1], base, wave.masked(a, base));
-      st.sums(values[u & 1], base, k.look(a, u));
+      st.logits(keys[u & 1], base, wave.masked(a, base));
+      st.nans(values[u & 1], base, k.look(a, u));
+      st.template weights<0>(keys[u & 1]);
+      st.template sums<0>(values[u & 1]);
+      st.template weights<1>(keys[u & 1]);
+      st.template sums<1>(values[u & 1]);
     }
     if (u + 1 < k.end) store(u + 1);
     lds_barrier();
