@@ -23,8 +23,14 @@ namespace {
 
 using namespace festina_kv;
 
-constexpr int kThreads = 256;
-constexpr int kSlots = 64;           // slots of a block that the values' transpose takes at a time
+// A run has a workgroup of N threads: the fewest, of 64, 128 and 256, whose registers hold a block's rows of one head in at most
+// four pieces of eight elements a thread, else 256; slots_of() rows are held, and pass through the values' transpose, at a
+// time.  More threads have little to load each and a barrier to wait for, and more pieces leave too few waves on a SIMD.  32 prompts,
+// 41,100 tokens of 8 heads of 128, us: blocks of 16 slots 61 (256 threads: 122), of 32 59 (78); 16,900 tokens of 12 heads
+// of 64, blocks of 32 27 (40); 16,900 of 12 heads of 256, blocks of 128 136 (161 with eight pieces a thread).  512 threads
+// were slower (256 dims, blocks of 64: 137 against 100).
+constexpr int slots_of(int D, int N) { return N * 32 / D >= 64 ? 64 : N * 32 / D / 16 * 16; }
+constexpr int kSpanMost = 64;
 
 typedef float f2 __attribute__((ext_vector_type(2)));
 
@@ -129,9 +135,9 @@ __device__ __forceinline__ void values8(const Raw8<TYPE> &r, float (&x)[8]) {
 
 // One run, for keys (WHICH = 0) or values.  The elements of its first kSlots tokens stay in registers between the
 // maximum and the codes; a longer run's others are read again.
-template <int TYPE, int D, int WHICH>
+template <int TYPE, int D, int N, int WHICH>
 __device__ __forceinline__ void store_run(const StoreArgs &a, int h, int t, int n, int slot, float *lds_max, uint8_t *tile) {
-  constexpr int kVecs = D / 8, kPitch = D + 4, kKept = kSlots * kVecs / kThreads;
+  constexpr int kSlots = slots_of(D, N), kVecs = D / 8, kPitch = D + 4, kKept = kSlots * kVecs / N;
   const int bt = 1 << a.shift, off = slot & (bt - 1);
   const size_t bh = (size_t)(slot >> a.shift) * a.H + h;
   const int64_t ts = a.token_stride[WHICH], row0 = (int64_t)h * a.head_stride[WHICH] + (int64_t)t * ts;
@@ -144,23 +150,25 @@ __device__ __forceinline__ void store_run(const StoreArgs &a, int h, int t, int 
   float v[8], amax = 0.f;
 #pragma unroll
   for (int j = 0; j < kKept; ++j)
-    if ((int)threadIdx.x + j * kThreads < n * kVecs) kept[j] = read(threadIdx.x + j * kThreads);
+    if ((int)threadIdx.x + j * N < n * kVecs) kept[j] = read(threadIdx.x + j * N);
   const auto join = [&]() {                            // over the workgroup
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) amax = fmaxf(amax, __shfl_xor(amax, d));
     if ((threadIdx.x & 63) == 0) lds_max[threadIdx.x >> 6] = amax;
     __syncthreads();
-    amax = fmaxf(fmaxf(lds_max[0], lds_max[1]), fmaxf(lds_max[2], lds_max[3]));
+    amax = lds_max[0];
+#pragma unroll
+    for (int w = 1; w < N / 64; ++w) amax = fmaxf(amax, lds_max[w]);
   };
   // the maximum leaves NaN out by itself
 #pragma unroll
   for (int j = 0; j < kKept; ++j)
-    if ((int)threadIdx.x + j * kThreads < n * kVecs) {
+    if ((int)threadIdx.x + j * N < n * kVecs) {
       values8<TYPE>(kept[j], v);
 #pragma unroll
       for (int k = 0; k < 8; ++k) amax = fmaxf(amax, __builtin_fabsf(v[k]));
     }
-  for (int i = threadIdx.x + kKept * kThreads; i < n * kVecs; i += kThreads) {
+  for (int i = threadIdx.x + kKept * N; i < n * kVecs; i += N) {
     values8<TYPE>(read(i), v);
 #pragma unroll
     for (int k = 0; k < 8; ++k) amax = fmaxf(amax, __builtin_fabsf(v[k]));
@@ -170,7 +178,7 @@ __device__ __forceinline__ void store_run(const StoreArgs &a, int h, int t, int 
   if (careful) {                                       // infinities: once more without them
     __syncthreads();
     amax = 0.f;
-    for (int i = threadIdx.x; i < n * kVecs; i += kThreads) {
+    for (int i = threadIdx.x; i < n * kVecs; i += N) {
       values8<TYPE>(read(i), v);
 #pragma unroll
       for (int k = 0; k < 8; ++k) amax = fmaxf(amax, finite(v[k]) ? __builtin_fabsf(v[k]) : 0.f);
@@ -186,14 +194,14 @@ __device__ __forceinline__ void store_run(const StoreArgs &a, int h, int t, int 
     const float ratio = old / scale;
     if (WHICH == 0) {
       uint4 *p = reinterpret_cast<uint4 *>(codes);
-      for (int i = threadIdx.x; i < off * D / 16; i += kThreads) {
+      for (int i = threadIdx.x; i < off * D / 16; i += N) {
         uint4 c = p[i];
         c.x = recode4(c.x, ratio), c.y = recode4(c.y, ratio), c.z = recode4(c.z, ratio), c.w = recode4(c.w, ratio);
         p[i] = c;
       }
     } else {
       const int words = (off + 3) / 4;
-      for (int i = threadIdx.x; i < D * words; i += kThreads) {
+      for (int i = threadIdx.x; i < D * words; i += N) {
         const int d = i / words, o = (i - d * words) * 4;
         uint8_t *p = codes + (size_t)d * bt + o;
         const unsigned c = recode4(*reinterpret_cast<const unsigned *>(p), ratio);
@@ -213,11 +221,11 @@ __device__ __forceinline__ void store_run(const StoreArgs &a, int h, int t, int 
     };
 #pragma unroll
     for (int j = 0; j < kKept; ++j)
-      if ((int)threadIdx.x + j * kThreads < n * kVecs) {
+      if ((int)threadIdx.x + j * N < n * kVecs) {
         values8<TYPE>(kept[j], v);
-        put(threadIdx.x + j * kThreads);
+        put(threadIdx.x + j * N);
       }
-    for (int i = threadIdx.x + kKept * kThreads; i < n * kVecs; i += kThreads) {
+    for (int i = threadIdx.x + kKept * N; i < n * kVecs; i += N) {
       values8<TYPE>(read(i), v);
       put(i);
     }
@@ -234,19 +242,20 @@ __device__ __forceinline__ void store_run(const StoreArgs &a, int h, int t, int 
     };
 #pragma unroll
     for (int j = 0; j < kKept; ++j) {
-      const int i = threadIdx.x + j * kThreads;
+      const int i = threadIdx.x + j * N;
       if (i >= i0 && i < i1) {
         values8<TYPE>(kept[j], v);
         put(i);
       }
     }
-    for (int i = max(i0, kKept * kThreads) + threadIdx.x; i < i1; i += kThreads) {
+    for (int i = max(i0, kKept * N) + threadIdx.x; i < i1; i += N) {
       values8<TYPE>(read(i), v);
       put(i);
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < D; i += kThreads) {                  // D / 4 groups of rows x 4 groups of slots
-      const int g = i & 3, d = (i >> 2) * 4, s = s0 + g * 16;
+    constexpr int kSixteens = kSlots / 16;
+    for (int i = threadIdx.x; i < D / 4 * kSixteens; i += N) {         // groups of four rows x groups of 16 slots
+      const int g = i % kSixteens, d = i / kSixteens * 4, s = s0 + g * 16;
       if (s >= hi || s + 16 <= lo) continue;
       unsigned w[4][4];                                                // [row][word of four slots]
 #pragma unroll
@@ -277,10 +286,10 @@ __device__ __forceinline__ void store_run(const StoreArgs &a, int h, int t, int 
   }
 }
 
-template <int TYPE, int D>
-__global__ void __launch_bounds__(kThreads) k_store(StoreArgs a) {
-  __shared__ float lds_max[kThreads / 64];
-  __shared__ __attribute__((aligned(16))) uint8_t tile[kSlots * (D + 4)];
+template <int TYPE, int D, int N>
+__global__ void __launch_bounds__(N) k_store(StoreArgs a) {
+  __shared__ float lds_max[N / 64];
+  __shared__ __attribute__((aligned(16))) uint8_t tile[slots_of(D, N) * (D + 4)];
   // heads vary fastest: a token's heads lie beside each other in what is read
   const int h = blockIdx.x % a.H, which = blockIdx.y, bt = 1 << a.shift, lane = threadIdx.x & 63;
   const int64_t t0 = (int64_t)(blockIdx.x / a.H) * a.span;
@@ -305,18 +314,26 @@ __global__ void __launch_bounds__(kThreads) k_store(StoreArgs a) {
       n += follows == ~0ull ? 64 : __builtin_ctzll(~follows);
       if (follows != ~0ull) break;
     }
-    if (which == 0) store_run<TYPE, D, 0>(a, h, t, n, slot, lds_max, tile);
-    else store_run<TYPE, D, 1>(a, h, t, n, slot, lds_max, tile);
+    if (which == 0) store_run<TYPE, D, N, 0>(a, h, t, n, slot, lds_max, tile);
+    else store_run<TYPE, D, N, 1>(a, h, t, n, slot, lds_max, tile);
   }
 }
 
+template <int TYPE, int D>
+void launch(const StoreArgs &a, dim3 grid, hipStream_t st) {
+  constexpr int kLeast = D < 256 ? 64 : 128;           // of threads, for blocks of 16
+  const int bt = 1 << a.shift;
+  if (bt <= slots_of(D, kLeast)) k_store<TYPE, D, kLeast><<<grid, kLeast, 0, st>>>(a);
+  else if (D > 64 && D < 256 && bt <= slots_of(D, 2 * kLeast)) k_store<TYPE, D, 2 * kLeast><<<grid, 2 * kLeast, 0, st>>>(a);
+  else k_store<TYPE, D, D == 64 ? 128 : 256><<<grid, D == 64 ? 128 : 256, 0, st>>>(a);
+}
 template <int TYPE>
 void launch(const StoreArgs &a, int D, dim3 grid, hipStream_t st) {
   switch (D) {
-    case 64: k_store<TYPE, 64><<<grid, kThreads, 0, st>>>(a); break;
-    case 96: k_store<TYPE, 96><<<grid, kThreads, 0, st>>>(a); break;
-    case 128: k_store<TYPE, 128><<<grid, kThreads, 0, st>>>(a); break;
-    default: k_store<TYPE, 256><<<grid, kThreads, 0, st>>>(a); break;
+    case 64: launch<TYPE, 64>(a, grid, st); break;
+    case 96: launch<TYPE, 96>(a, grid, st); break;
+    case 128: launch<TYPE, 128>(a, grid, st); break;
+    default: launch<TYPE, 256>(a, grid, st); break;
   }
 }
 
@@ -356,7 +373,7 @@ extern "C" festina_status festina_store_kv(const festina_kv_cache *cache, const 
   a.scale[1] = cache->v_scale;
   // few tokens: a workgroup each, so that runs of single tokens are not done one after the other; many: enough that
   // most workgroups have a run to store (they are dispatched at a rate that empty ones take their share of)
-  a.span = (int)min(max((long long)a.T * a.H / 4096, 1ll), (long long)kSlots);
+  a.span = (int)min(max((long long)a.T * a.H / 4096, 1ll), (long long)kSpanMost);
   const long long groups = ((long long)a.T + a.span - 1) / a.span * a.H;
   if (groups > INT_MAX) return FESTINA_ERR_UNSUPPORTED;
   const dim3 grid((unsigned)groups, 2);
