@@ -549,7 +549,7 @@ typedef struct festina_kv_requests {
  * New columns of the served requests' rows are filled with the blocks taken.  length and served are
  * also what a serving loop needs to carry on. */
 typedef struct festina_kv_step {
-  int32_t max_tokens;                /* entries of slot, >= 0: the step's token budget */
+  int32_t max_tokens;                /* entries of slot, 0 .. 2^31 - 4097: the step's token budget */
   int32_t *first;                    /* [R + 1] */
   int32_t *slot;                     /* [max_tokens] */
   int32_t *length;                   /* [R] */

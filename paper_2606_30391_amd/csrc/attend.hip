@@ -59,6 +59,7 @@ constexpr int workers_of(int D, int NT) { return 1024 * waves_of(D, NT); }
 constexpr int kGroups = 512;         // workgroups of k_tiles that fill the chip: two a compute unit
 constexpr int kListed = 512;         // requests whose running sums a workgroup forms by itself
 constexpr int kMaxRequests = 1 << 20;
+constexpr long long kThreadsMost = UINT_MAX;     // along one axis of a grid
 constexpr float kLn2 = 0.6931471805599453f;
 
 template <typename T> struct Vec8;
@@ -680,17 +681,19 @@ __device__ __forceinline__ void join_row(const AttArgs &a, size_t p0, size_t p1,
   Rows<T, D, 1>::finish(a, t, head, d, M, L, O);
 }
 
-// A wave joins a row of the tile that the cut at piece blockIdx.x + 1 leaves to it.
+// A wave joins rows of the tile that the cut at piece blockIdx.x + 1 leaves to it: one where the grid has a wave a row.
 template <typename T, int D, int NT>
 __global__ void __launch_bounds__(kBlock) k_rows_join(AttArgs a) {
   constexpr int kRows = 16 * NT;
   const int w = blockIdx.x + 1;
   const Cut cut = a.cuts[w];
-  const int row = blockIdx.y * kWaves + (threadIdx.x >> 6), i = cut.row0 + row;
-  if (cut.n == 0 || i >= cut.rows) return;
-  const int t = i / a.G;
-  join_row<T, D>(a, (size_t)(2 * (w - 1) + cut.second) * kRows + row, (size_t)(2 * w) * kRows + row, 2 * kRows, cut.n,
-                 cut.first + t, cut.head + i - t * a.G);
+  if (cut.n == 0) return;
+  for (int row = blockIdx.y * kWaves + (threadIdx.x >> 6); row < kRows; row += gridDim.y * kWaves) {
+    const int i = cut.row0 + row, t = i / a.G;
+    if (i >= cut.rows) return;
+    join_row<T, D>(a, (size_t)(2 * (w - 1) + cut.second) * kRows + row, (size_t)(2 * w) * kRows + row, 2 * kRows, cut.n,
+                   cut.first + t, cut.head + i - t * a.G);
+  }
 }
 
 // ------------------------------------------------------------------ k_tiles
@@ -1204,7 +1207,7 @@ struct Shape {
   int tile_rows;
   long long tile_groups;             // bound of the row tiles of all requests
   int splits;
-  int join_rows;                     // rows of a row tile that may be in use
+  int join_rows;                     // rows of a row tile that are mostly in use: the join's waves
   size_t plan, cuts, part_ml, part_o, bytes;
 };
 
@@ -1236,7 +1239,7 @@ festina_status shape_of(const festina_kv_cache *c, const festina_attention *t, S
   const long long keys = (long long)t->max_blocks * c->block_tokens;
   s->tiles_each = (int)((rows + 16 * s->nt - 1) / max(16 * s->nt, 1));
   s->cut = keys > 2 * kWaves * kUnit;
-  if (!s->cut && (long long)t->n_requests * H * max(s->tiles_each, 1) > INT_MAX) return FESTINA_ERR_UNSUPPORTED;
+  if (!s->cut && (long long)t->n_requests * H * max(s->tiles_each, 1) > kThreadsMost / kBlock) return FESTINA_ERR_UNSUPPORTED;
   size_t parts = 0;
   if (s->nt && s->cut) parts = (size_t)2 * workers_of(D, s->nt) * 16 * s->nt;
   if (s->tiles) {
@@ -1246,7 +1249,7 @@ festina_status shape_of(const festina_kv_cache *c, const festina_attention *t, S
     const long long rows_all = (long long)t->n_tokens * G * H;
     s->tile_rows = (D == 96 || D == 128) && rows_all >= 256ll * kGroups ? 256 : 128;
     s->tile_groups = ((long long)t->n_tokens * G + s->tile_rows - 1) / s->tile_rows + t->n_requests;
-    if (s->tile_groups * H > INT_MAX) return FESTINA_ERR_UNSUPPORTED;
+    if (s->tile_groups * H > kThreadsMost / (2 * s->tile_rows)) return FESTINA_ERR_UNSUPPORTED;
     // at least two workgroups a compute unit, of at least 16 steps each
     const long long groups = max(((long long)t->n_tokens * G + s->tile_rows - 1) / s->tile_rows, 1ll) * H;
     const long long wanted = (kGroups + groups - 1) / groups;

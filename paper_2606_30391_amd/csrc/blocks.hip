@@ -41,6 +41,7 @@ constexpr int kLongFills = 8 << 20;
 constexpr int kSmall = 1024;         // threads of the one-workgroup kernel, a request each
 constexpr int kSmallTokens = 8192;   // and its slots
 constexpr int kMaxRequests = 1 << 20;
+constexpr int kMaxTokens = INT_MAX - 4096;     // the last stretch of the fill is counted in 32 bits
 
 struct BlockArgs {
   int32_t R, MB, shift, NB, max_tokens;
@@ -523,6 +524,7 @@ festina_status arguments(const festina_kv_requests *q, festina_kv_step *out, boo
   if (bt < 16 || bt > 256 || (bt & (bt - 1))) return FESTINA_ERR_UNSUPPORTED;
   if ((long long)q->n_blocks * bt > INT_MAX || (long long)q->max_blocks * bt > INT_MAX || q->n_requests > kMaxRequests)
     return FESTINA_ERR_UNSUPPORTED;
+  if (extend && out->max_tokens > kMaxTokens) return FESTINA_ERR_UNSUPPORTED;
   if (!q->n_free || !out->n_free_out) return FESTINA_ERR_INVALID;
   if (q->n_requests > 0) {
     if (!q->held || !q->block_table || !q->free_ids || !out->length) return FESTINA_ERR_INVALID;
@@ -560,7 +562,7 @@ festina_status arguments(const festina_kv_requests *q, festina_kv_step *out, boo
 }  // namespace
 
 extern "C" size_t festina_blocks_workspace_bytes(int32_t n_requests, int32_t max_tokens) {
-  if (n_requests < 0 || n_requests > kMaxRequests || max_tokens < 0) return 0;
+  if (n_requests < 0 || n_requests > kMaxRequests || max_tokens < 0 || max_tokens > kMaxTokens) return 0;
   return layout(n_requests, max_tokens).bytes;
 }
 

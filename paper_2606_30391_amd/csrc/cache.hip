@@ -375,7 +375,7 @@ extern "C" festina_status festina_store_kv(const festina_kv_cache *cache, const 
   // most workgroups have a run to store (they are dispatched at a rate that empty ones take their share of)
   a.span = (int)min(max((long long)a.T * a.H / 4096, 1ll), (long long)kSpanMost);
   const long long groups = ((long long)a.T + a.span - 1) / a.span * a.H;
-  if (groups > INT_MAX) return FESTINA_ERR_UNSUPPORTED;
+  if (groups > UINT_MAX / 256) return FESTINA_ERR_UNSUPPORTED;   // threads along one axis of a grid
   const dim3 grid((unsigned)groups, 2);
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (tokens->dtype == FESTINA_BF16) launch<FESTINA_BF16>(a, cache->head_dim, grid, st);

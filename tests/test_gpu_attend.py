@@ -136,6 +136,13 @@ def test_prompts_over_a_long_cache(requests, max_new):
     Case(rng, requests, D=128, H=2, G=2, bt=16).check(max_new=max_new)
 
 
+@pytest.mark.parametrize("D,G,bt", [(64, 4, 32), (96, 1, 128), (128, 2, 16), (256, 3, 64)])
+def test_a_few_tokens_over_long_caches_beside_a_prompt(D, G, bt):
+    """A prompt's step in which other requests add two to five tokens: their rows, more than a single token's, are cut too."""
+    rng = np.random.default_rng(D + G)
+    Case(rng, [(2500, 100), (4096, 3), (3001, 2), (100, 100), (2049, 5), (2000, 1)], D=D, G=G, bt=bt).check()
+
+
 @pytest.mark.parametrize("D,dtype", [(96, "f16"), (128, "bf16")])
 def test_large_prompts(D, dtype):
     """As many rows (heads x tokens) as have tiles of 256 rows: three key heads of 64 compared."""

@@ -119,6 +119,9 @@ def test_blocks_reject_bad_arguments_before_launch(lib):
         setattr(s[i], field, None)
         assert _extend(*s) == F.FESTINA_ERR_INVALID, field
     assert _extend(*_blocks(tokens=-1)) == F.FESTINA_ERR_INVALID
+    assert _extend(*_blocks(tokens=2 ** 31 - 4096), n=1 << 40) == F.FESTINA_ERR_UNSUPPORTED
+    assert _extend(*_blocks(tokens=2 ** 31 - 4097), n=1 << 40) == F.FESTINA_ERR_DEVICE
+    assert F.festina_blocks_workspace_bytes(8, 2 ** 31 - 4096) == 0 < F.festina_blocks_workspace_bytes(8, 2 ** 31 - 4097)
     assert _release(q, o, done=None) == F.FESTINA_ERR_INVALID
     assert F.lib().festina_extend_blocks(None, C.byref(o), WS, need, None) == F.FESTINA_ERR_INVALID
     assert F.lib().festina_release_blocks(C.byref(q), FAKE, None, WS, need, None) == F.FESTINA_ERR_INVALID
@@ -153,6 +156,7 @@ def test_store_rejects_bad_arguments_before_launch(lib):
         t = tokens()
         setattr(t, field, value)
         assert call(_cache(), t) == F.FESTINA_ERR_INVALID, field
+    assert call(_cache(H=1024), tokens(T=2 ** 31 - 1)) == F.FESTINA_ERR_UNSUPPORTED    # more workgroups than a launch has
     t = tokens(T=0)
     t.k = t.v = t.slot = None
     assert call(_cache(), t) == F.FESTINA_OK                                 # no tokens: nothing launched
@@ -183,6 +187,10 @@ def test_attend_rejects_bad_arguments_before_launch(lib):
                      (dict(R=(1 << 20) + 1), 3), (dict(MB=1 << 26), 3), (dict(T=1 << 29), 3)]:
         assert call(_cache(), att(**kw)) == want, kw
         assert F.festina_attend_workspace_bytes(_cache(), att(**kw)) == 0
+    wide = _cache(H=32)                                                      # more workgroups than a launch has
+    for new in (1, 64):
+        assert call(wide, att(R=1 << 20, T=1 << 20, heads=32, new=new)) == F.FESTINA_ERR_UNSUPPORTED
+        assert call(wide, att(R=1 << 18, T=1 << 18, heads=32, new=new)) == F.FESTINA_ERR_DEVICE
     for field, value in [("block_table", None), ("length", None), ("first", None), ("q", None), ("out", None),
                          ("q", C.c_void_p(0x1008)), ("out", C.c_void_p(0x1004)), ("q_token_stride", 12),
                          ("q_head_stride", -64), ("out_head_stride", 68), ("scale", float("nan"))]:
