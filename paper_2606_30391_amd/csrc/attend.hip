@@ -20,10 +20,14 @@
 //   per wave and step, operands loaded from the cache into the lanes that use them.  Bound by the cache's bytes.
 //   All requests' keys form one line of 64-key units, cut into equal pieces, one a wave, so that
 //   ragged lengths leave no wave behind; a row tile that a cut falls into is joined by k_rows_join.
-// k_rows_whole   the same for short tables: a workgroup a row tile, joined in LDS, one launch.
+//   64 requests up to 32,768 tokens, 8 heads of 128: 2.15 GB in 433 us, 4.96 TB/s, what a large copy reaches too.
+// k_rows_whole   the same for short tables: a workgroup a row tile, joined in LDS, one launch.  One request of 403 tokens: 7 us,
+//   a launch and a few round trips to memory.
 // k_tiles   prompts: 128 query rows a workgroup, tiles of 64 keys converted once into LDS (two buffers, the next
 //   tile's loads in flight meanwhile) and read by four waves of 32 rows.  Bound by the matrix cores and the exponentials.
 //   Few tiles over a long cache are split over the keys and joined by k_tiles_join.
+//   8,192 tokens, 32 heads over 8 of 128: 550 GFLOP in 559 us (983 TFLOP/s; a large library product 1,189), matrix cores
+//   41% of the cycles, VALU issue 38%.  9,012 tokens of 16 heads of 64: 182 us, 28% and 52%: half the products an exponential.
 // k_plan    running sums of the requests' units and tiles, for many requests.
 #include <hip/hip_runtime.h>
 
@@ -643,21 +647,22 @@ __global__ void __launch_bounds__(64, waves_of(D, NT)) k_rows(AttArgs a) {
   if (threadIdx.x == 0) a.cuts[w] = cut;
 }
 
-// Joins one row's n pieces, the first at p0 and the others from p1 on: a wave, lanes over the row, eight pieces' loads in
-// flight at a time.
+// Joins one row's n pieces, the first at p0 and the others from p1 on: a wave, as many groups of lanes as a row leaves
+// room for each taking every kSides-th piece, eight of them with their loads in flight at a time.
+// (32 requests, a token each, up to 8,192 held: 24.1 -> 21.5 us against a piece a time for the whole wave; sixteen in flight 22.2.)
 template <typename T, int D>
 __device__ __forceinline__ void join_row(const AttArgs &a, size_t p0, size_t p1, size_t stride, int n, int t, int head) {
-  constexpr int kAtOnce = 8;
-  const int d = (threadIdx.x & 63) * 4;
+  constexpr int kAtOnce = 8, kLanes = D <= 64 ? 16 : D <= 128 ? 32 : 64, kSides = 64 / kLanes;
+  const int lane = threadIdx.x & 63, side = lane / kLanes, d = lane % kLanes * 4;
   if (d >= D) return;
   float M = kNegInf(), L = 0.f;
   f4 O = f4{0.f, 0.f, 0.f, 0.f};
-  for (int i0 = 0; i0 < n; i0 += kAtOnce) {
+  for (int i0 = side; i0 < n; i0 += kAtOnce * kSides) {
     f4 o[kAtOnce];
     float2 ml[kAtOnce];
 #pragma unroll
     for (int k = 0; k < kAtOnce; ++k) {
-      const int i = min(i0 + k, n - 1);
+      const int i = min(i0 + k * kSides, n - 1);
       const size_t at = i == 0 ? p0 : p1 + (size_t)(i - 1) * stride;
       ml[k] = *reinterpret_cast<const float2 *>(a.part_ml + at * 2);
       o[k] = *reinterpret_cast<const f4 *>(a.part_o + at * D + d);
@@ -671,14 +676,24 @@ __device__ __forceinline__ void join_row(const AttArgs &a, size_t p0, size_t p1,
     O *= f;
 #pragma unroll
     for (int k = 0; k < kAtOnce; ++k) {
-      const float g = i0 + k < n ? weight(ml[k].x, M) : 0.f;
-      if (i0 + k < n) {
+      const bool there = i0 + k * kSides < n;
+      const float g = there ? weight(ml[k].x, M) : 0.f;
+      if (there) {
         L = fmaf(ml[k].y, g, L);
         O += o[k] * g;
       }
     }
   }
-  Rows<T, D, 1>::finish(a, t, head, d, M, L, O);
+  // the sides' sums; one without a piece has M = -inf and adds nothing
+#pragma unroll
+  for (int x = kLanes; x < 64; x <<= 1) {
+    const float other = __shfl_xor(M, x), now = fmaxf(M, other), f = weight(M, now), g = weight(other, now);
+    M = now;
+    L = fmaf(__shfl_xor(L, x), g, L * f);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) O[i] = fmaf(__shfl_xor(O[i], x), g, O[i] * f);
+  }
+  if (side == 0) Rows<T, D, 1>::finish(a, t, head, d, M, L, O);
 }
 
 // A wave joins rows of the tile that the cut at piece blockIdx.x + 1 leaves to it: one where the grid has a wave a row.
@@ -1239,12 +1254,13 @@ festina_status shape_of(const festina_kv_cache *c, const festina_attention *t, S
   const long long keys = (long long)t->max_blocks * c->block_tokens;
   s->tiles_each = (int)((rows + 16 * s->nt - 1) / max(16 * s->nt, 1));
   s->cut = keys > 2 * kWaves * kUnit;
-  if (!s->cut && (long long)t->n_requests * H * max(s->tiles_each, 1) > kThreadsMost / kBlock) return FESTINA_ERR_UNSUPPORTED;
+  if (s->nt && !s->cut && (long long)t->n_requests * H * s->tiles_each > kThreadsMost / kBlock)
+    return FESTINA_ERR_UNSUPPORTED;
   size_t parts = 0;
   if (s->nt && s->cut) parts = (size_t)2 * workers_of(D, s->nt) * 16 * s->nt;
   if (s->tiles) {
     // 256 rows a workgroup stage each tile half as often for a row, where registers allow and enough workgroups are
-    // left: a prompt of 8,192 tokens (32 heads over 8 of 128 dims) 641 us against 662 with 128; 9,215 tokens of 16
+    // left: a prompt of 8,192 tokens (32 heads over 8 of 128 dims) 641 us against 662 with 128; 9,012 tokens of 16
     // heads of 64 dims, with three smaller workgroups a compute unit, 183 against 234 the other way
     const long long rows_all = (long long)t->n_tokens * G * H;
     s->tile_rows = (D == 96 || D == 128) && rows_all >= 256ll * kGroups ? 256 : 128;
