@@ -29,7 +29,8 @@ using namespace festina_kv;
 // time.  More threads have little to load each and a barrier to wait for, and more pieces leave too few waves on a SIMD.  32 prompts,
 // 41,100 tokens of 8 heads of 128, us: blocks of 16 slots 61 (256 threads: 122), of 32 59 (78); 16,900 tokens of 12 heads
 // of 64, blocks of 32 27 (40); 16,900 of 12 heads of 256, blocks of 128 136 (161 with eight pieces a thread).  512 threads
-// were slower (256 dims, blocks of 64: 137 against 100).
+// were slower (256 dims, blocks of 64: 137 against 100), and so were reads that mark the elements as
+// not to be kept (12 heads of 64: 32 against 28).
 constexpr int slots_of(int D, int N) { return N * 32 / D >= 64 ? 64 : N * 32 / D / 16 * 16; }
 constexpr int kSpanMost = 64;
 
