@@ -644,23 +644,41 @@ def _on(stream, device):
     return torch.cuda.stream(stream)
 
 
+def _capturing(stream, device):
+    """Whether `stream` (None: the current one) is being captured into a graph."""
+    import torch
+    if stream is None:
+        return torch.cuda.is_current_stream_capturing()
+    with _on(stream, device):
+        return torch.cuda.is_current_stream_capturing()
+
+
 class _Workspaces:
-    """Device scratch, one for each stream that calls come on, so that they may overlap."""
+    """Device scratch, one for each stream that calls come on, so that they may overlap.  A call that is captured gets
+    its own from the graph's memory: a graph keeps the address that it captured, while a stream's scratch is replaced
+    when a call needs more, and graphs captured on one stream may be replayed on several."""
 
     def __init__(self):
         self.by_stream = {}
 
     def get(self, n, stream, device):
-        """(address of at least n bytes for calls on `stream`, that stream's handle)."""
+        """(at least n bytes for calls on `stream`, to be held until the launch; their address; the stream's handle)."""
         handle = _stream_handle(stream).value or 0
+        if handle and _capturing(stream, device):            # (the null stream cannot be captured; asking takes 1 us)
+            ws = self._make(n, stream, device)
+            return ws, ws.data_ptr(), handle
         ws, at, size = self.by_stream.get(handle, (None, 0, -1))
         if size < n:
-            import torch
-            with _on(stream, device):
-                ws = torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+            ws = self._make(n, stream, device)
             at = ws.data_ptr()
             self.by_stream[handle] = ws, at, ws.numel()
-        return at, handle
+        return ws, at, handle
+
+    @staticmethod
+    def _make(n, stream, device):
+        import torch
+        with _on(stream, device):
+            return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
 
 
 class DeviceBlocks:
@@ -698,13 +716,13 @@ class DeviceBlocks:
                                    _ptr(self.served), _ptr(self.n_free_out))
 
     def extend(self, stream=None):
-        ws, handle = self._ws.get(self.ws_bytes, stream, self.table.device)
+        held, ws, handle = self._ws.get(self.ws_bytes, stream, self.table.device)
         festina_extend_blocks(self.req, self.out, ws, self.ws_bytes, handle)
 
     def release(self, done, stream=None):
         import torch
         _check(done, "done", (torch.uint8, torch.bool), self.held.shape)
-        ws, handle = self._ws.get(self.ws_bytes, stream, self.table.device)
+        held, ws, handle = self._ws.get(self.ws_bytes, stream, self.table.device)
         festina_release_blocks(self.req, done, self.out, ws, self.ws_bytes, handle)
 
     def advance(self):
@@ -716,7 +734,9 @@ class DeviceBlocks:
 class DeviceCache:
     """One layer's key/value cache in 8 bits (festina_kv_cache): uint8 codes k [n_blocks][kv heads][block tokens]
     [dim], v [n_blocks][kv heads][dim][block tokens] and float32 scales k_scale, v_scale [n_blocks][kv heads],
-    device tensors used in place (``DeviceCache.empty`` makes them)."""
+    device tensors used in place (``DeviceCache.empty`` makes them).  Scratch is the object's own, one for each stream;
+    what torch.cuda.graph captures has scratch of its graph's memory (a graph captured by other means: festina_attend
+    with a workspace that the caller keeps)."""
 
     def __init__(self, k, v, k_scale, v_scale):
         import torch
@@ -814,7 +834,7 @@ class DeviceCache:
             if len(self._ws_bytes) > 1024:
                 self._ws_bytes.clear()
             n = self._ws_bytes[sizes] = festina_attend_workspace_bytes(self.cache, att)
-        ws, handle = self._ws.get(n, stream, q.device)
+        held, ws, handle = self._ws.get(n, stream, q.device)
         st = self._attend(self._cache_ref, C.byref(att), ws, n, handle)
         if st != FESTINA_OK:
             raise FestinaError(st, "festina_attend")

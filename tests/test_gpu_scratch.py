@@ -1,0 +1,105 @@
+"""GPU tests of the binding's scratch and of tensors on other streams: graphs beside eager calls and beside each other."""
+import numpy as np
+import pytest
+
+from test_gpu_attend import Case
+
+torch = pytest.importorskip("torch")
+pytestmark = [pytest.mark.gpu,
+              pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a GPU")]
+
+LONG = [([(3000, 1), (50, 1), (700, 1)], 1), ([(3000, 60), (50, 1)], 60)]
+
+
+def _captured(cache, c, t, new, stream=None):
+    """(graph, out, lse) of one attention call, warmed up on the stream that it is captured on."""
+    out = torch.empty_like(c.q)
+    lse = torch.empty(c.q.shape[:2], device="cuda")
+    side = stream or torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        cache.attend(c.q, *t, max_new=new, out=out, lse=lse)
+    side.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=stream):
+        cache.attend(c.q, *t, max_new=new, out=out, lse=lse)
+    return g, out, lse
+
+
+@pytest.mark.parametrize("requests,new", LONG)
+def test_a_graph_beside_a_larger_eager_call_on_its_stream(requests, new):
+    """The call after the capture needs more scratch; a replay then writes to none of the tensors made since."""
+    rng = np.random.default_rng(new)
+    c = Case(rng, requests, D=64)
+    big = Case(rng, [(2600, 90)] * 4 + [(600, 1)] * 300, D=64)
+    s = torch.cuda.Stream()
+    cache, t = c.cache(), c.tensors()
+    print(f"[gpu] graph beside a larger eager call {requests}", flush=True)
+    want = cache.attend(c.q, *t, max_new=new)
+    torch.cuda.synchronize()
+    g, out, lse = _captured(cache, c, t, new, s)
+    other = big.cache()
+    other._ws = cache._ws                                    # the scratch that the graph's stream has
+    with torch.cuda.stream(s):
+        before = {k: v[2] for k, v in cache._ws.by_stream.items()}
+        other.attend(big.q, *big.tensors(), max_new=90)
+        assert cache._ws.by_stream[s.cuda_stream][2] > before[s.cuda_stream]
+        fresh = [torch.full((n,), 90, dtype=torch.uint8, device="cuda") for n in sorted(set(before.values())) for _ in range(3)]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        out.fill_(float("nan"))
+        lse.fill_(float("nan"))
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+        assert all(bool((x == 90).all()) for x in fresh)
+
+
+@pytest.mark.parametrize("requests,new", LONG)
+def test_two_graphs_replayed_on_two_streams(requests, new):
+    rng = np.random.default_rng(new + 1)
+    c = Case(rng, requests, D=64)
+    cache, t = c.cache(), c.tensors()
+    d = Case(rng, requests, D=64)                            # other queries over the same cache
+    print(f"[gpu] two graphs at once {requests}", flush=True)
+    want = [cache.attend(x.q, *t, max_new=new) for x in (c, d)]
+    graphs = [_captured(cache, x, t, new) for x in (c, d)]
+    streams = [torch.cuda.Stream() for _ in graphs]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for _, out, lse in graphs:
+            out.fill_(float("nan"))
+            lse.fill_(float("nan"))
+        torch.cuda.synchronize()
+        for _ in range(20):
+            for (g, _, _), s in zip(graphs, streams):
+                with torch.cuda.stream(s):
+                    g.replay()
+        torch.cuda.synchronize()
+        for (_, out, lse), w in zip(graphs, want):
+            assert torch.equal(out, w[0]) and torch.equal(lse, w[1])
+
+
+def test_block_plans_captured_twice_have_scratch_of_their_own():
+    from paper_2606_30391_amd import festina as F
+    i32 = lambda x: torch.as_tensor(np.asarray(x, np.int32)).cuda()
+    R = 3000
+    b = F.DeviceBlocks(i32(np.zeros(R)), i32(np.full(R, 3)), i32(np.full((R, 1), -1)), i32(np.arange(R)), i32([R]), 16, 3 * R)
+    print("[gpu] two graphs of a block plan", flush=True)
+    b.extend()
+    torch.cuda.synchronize()
+    want = b.slot.clone()
+    kept = dict(b._ws.by_stream)
+    graphs = []
+    for _ in range(2):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            b.extend()
+    assert b._ws.by_stream.keys() == kept.keys()             # neither is a stream's
+    for g in graphs:
+        b.slot.fill_(-7)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(b.slot, want)

@@ -213,3 +213,22 @@ def test_binding_refuses_tensors_of_host_memory_and_wrong_types(lib):
         F.DeviceCache(torch.zeros((2, 1, 16, 64), dtype=torch.uint8), None, None, None)
     with pytest.raises(ValueError, match="two dimensions"):
         F.DeviceBlocks(i, i, i, i, i[:1], 16, 8)
+
+
+def test_a_captured_call_has_scratch_of_its_own(monkeypatch):
+    """What a graph captured must neither be replaced by a larger call nor shared with another graph."""
+    import contextlib
+    import torch.cuda
+    capturing = [False]
+    monkeypatch.setattr(F, "_on", lambda stream, device: contextlib.nullcontext())
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing[0])
+    w = F._Workspaces()
+    eager = w.get(1000, 5, "cpu")
+    assert w.get(900, 5, "cpu")[1] == eager[1] and eager[2] == 5
+    capturing[0] = True
+    graphs = [w.get(1000, 5, "cpu") for _ in range(2)]
+    assert len({eager[1], graphs[0][1], graphs[1][1]}) == 3
+    assert all(g[0].data_ptr() == g[1] and g[0].numel() >= 1000 for g in graphs)
+    capturing[0] = False
+    assert w.get(1000, 5, "cpu")[1] == eager[1]              # the stream's own is as it was
+    assert w.get(2000, 5, "cpu")[1] not in (graphs[0][1], graphs[1][1])
