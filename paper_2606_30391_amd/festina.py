@@ -653,6 +653,15 @@ def _capturing(stream, device):
         return torch.cuda.is_current_stream_capturing()
 
 
+def _used_on(stream, *tensors):
+    """Tell torch that work on `stream` (a torch stream) reads or writes these tensors: their memory is not given to others
+    before that work is done, also where the caller drops them right after the call.  Not for a raw handle: its owner
+    may end that stream at any time, so the owner keeps the tensors too."""
+    if stream is not None and not isinstance(stream, int):
+        for t in tensors:
+            t.record_stream(stream)
+
+
 class _Workspaces:
     """Device scratch, one for each stream that calls come on, so that they may overlap.  A call that is captured gets
     its own from the graph's memory: a graph keeps the address that it captured, while a stream's scratch is replaced
@@ -688,7 +697,10 @@ class DeviceBlocks:
     extend() gives every request blocks and slots for its add new tokens: table, and first [R+1],
     slot [max_tokens], length [R], served [R], n_free_out [1].  release(done) returns the blocks of the
     requests whose uint8 done is not 0: free_ids, length, n_free_out.  advance() makes length and n_free_out
-    the next step's held and n_free (no work on the device)."""
+    the next step's held and n_free (no work on the device).
+
+    A call with stream= (a torch stream, or a raw handle) comes after what is on that stream, and waits for no other.
+    With a raw handle the tensors have to outlive the call's work."""
 
     def __init__(self, held, add, table, free_ids, n_free, block_tokens: int, max_tokens: int):
         import torch
@@ -718,12 +730,18 @@ class DeviceBlocks:
     def extend(self, stream=None):
         held, ws, handle = self._ws.get(self.ws_bytes, stream, self.table.device)
         festina_extend_blocks(self.req, self.out, ws, self.ws_bytes, handle)
+        _used_on(stream, *self._tensors())
 
     def release(self, done, stream=None):
         import torch
         _check(done, "done", (torch.uint8, torch.bool), self.held.shape)
         held, ws, handle = self._ws.get(self.ws_bytes, stream, self.table.device)
         festina_release_blocks(self.req, done, self.out, ws, self.ws_bytes, handle)
+        _used_on(stream, done, *self._tensors())
+
+    def _tensors(self):
+        return (self.held, self.add, self.table, self.free_ids, self.n_free, self.first, self.slot, self.length, self.served,
+                self.n_free_out)
 
     def advance(self):
         self.held, self.length = self.length, self.held
@@ -736,7 +754,7 @@ class DeviceCache:
     [dim], v [n_blocks][kv heads][dim][block tokens] and float32 scales k_scale, v_scale [n_blocks][kv heads],
     device tensors used in place (``DeviceCache.empty`` makes them).  Scratch is the object's own, one for each stream;
     what torch.cuda.graph captures has scratch of its graph's memory (a graph captured by other means: festina_attend
-    with a workspace that the caller keeps)."""
+    with a workspace that the caller keeps).  stream= as for DeviceBlocks."""
 
     def __init__(self, k, v, k_scale, v_scale):
         import torch
@@ -777,6 +795,7 @@ class DeviceCache:
         (kt, kh, _), (vt, vh, _) = k.stride(), v.stride()
         festina_store_kv(self.cache, festina_kv_tokens(T, self._types[k.dtype], k.data_ptr(), v.data_ptr(), kt, kh, vt,
                                                        vh, slot.data_ptr()), stream)
+        _used_on(stream, k, v, slot, self.k, self.v, self.k_scale, self.v_scale)
 
     def attend(self, q, table, length, first, max_new: int, scale=None, window: int = 0, out=None, lse=None,
                stream=None):
@@ -838,6 +857,8 @@ class DeviceCache:
         st = self._attend(self._cache_ref, C.byref(att), ws, n, handle)
         if st != FESTINA_OK:
             raise FestinaError(st, "festina_attend")
+        if stream is not None:
+            _used_on(stream, q, table, length, first, out, lse, self.k, self.v, self.k_scale, self.v_scale)
         return out, lse
 
 

@@ -103,3 +103,64 @@ def test_block_plans_captured_twice_have_scratch_of_their_own():
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(b.slot, want)
+
+
+def _busy(stream):
+    """Work of some milliseconds on `stream`."""
+    with torch.cuda.stream(stream):
+        x = torch.randn((8192, 8192), device="cuda").bfloat16()
+        for _ in range(20):
+            x = x @ x
+
+
+def _dropped(stream, make, call):
+    """`call` gets tensors that are dropped right after it, while `stream` has not come to it; others are made since."""
+    kept = make()
+    again = [x.clone() for x in kept]
+    sizes = [x.numel() * x.element_size() for x in again]
+    old = [x.untyped_storage().data_ptr() for x in again]
+    torch.cuda.synchronize()
+    _busy(stream)
+    call(*again)
+    done = torch.cuda.Event()
+    done.record(stream)
+    del again
+    fresh = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in sizes]
+    assert not done.query(), "the stream had nothing to do"
+    assert not {x.data_ptr() for x in fresh} & set(old)
+    torch.cuda.synchronize()
+    return kept
+
+
+def test_tensors_dropped_after_a_call_on_another_stream():
+    """A call's inputs keep their memory until the other stream has read them."""
+    from paper_2606_30391_amd import festina as F
+    rng = np.random.default_rng(41)
+    c = Case(rng, [(700, 1), (3000, 1)] + [(40, 1)] * 300, D=64)
+    cache, t = c.cache(), c.tensors()
+    s = torch.cuda.Stream()
+    print("[gpu] tensors dropped after calls on another stream", flush=True)
+    want = cache.attend(c.q, *t, max_new=1)
+    got = []
+    _dropped(s, lambda: (c.q, *t), lambda q, a, b, f: got.extend(cache.attend(q, a, b, f, max_new=1, stream=s)))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+    H, D, bt, T = 2, 64, 32, 2000
+    new = F.DeviceCache.empty(64, bt, H, D)
+    k, v = (torch.randn((T, H, D), device="cuda") for _ in range(2))
+    slot = torch.arange(T, dtype=torch.int32, device="cuda")
+    new.store(k, v, slot)
+    torch.cuda.synchronize()
+    want = [x.clone() for x in (new.k, new.v, new.k_scale, new.v_scale)]
+    for x in (new.k, new.v, new.k_scale, new.v_scale):
+        x.zero_()
+    _dropped(s, lambda: (k, v, slot), lambda *x: new.store(*x, stream=s))
+    blocks = T // bt                                         # (whole ones: what lies behind the last token was left alone)
+    for x, y in zip((new.k, new.v, new.k_scale, new.v_scale), want):
+        assert torch.equal(x[:blocks], y[:blocks])
+
+    i32 = lambda x: torch.as_tensor(np.asarray(x, np.int32)).cuda()
+    R = 3000
+    b = F.DeviceBlocks(i32(np.full(R, 5)), i32(np.zeros(R)), i32(np.arange(R)[:, None]), i32(np.full(R, -1)), i32([0]), 16, 0)
+    _dropped(s, lambda: (torch.ones(R, dtype=torch.uint8, device="cuda"),), lambda d: b.release(d, stream=s))
+    assert int(b.n_free_out) == R and torch.equal(b.free_ids, torch.arange(R, dtype=torch.int32, device="cuda"))
