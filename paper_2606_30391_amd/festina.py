@@ -852,7 +852,9 @@ class DeviceCache:
         if n is None:
             if len(self._ws_bytes) > 1024:
                 self._ws_bytes.clear()
-            n = self._ws_bytes[sizes] = festina_attend_workspace_bytes(self.cache, att)
+            n = festina_attend_workspace_bytes(self.cache, att)
+            if n:                                            # 0: refused below, for something that may not be a size
+                self._ws_bytes[sizes] = n
         held, ws, handle = self._ws.get(n, stream, q.device)
         st = self._attend(self._cache_ref, C.byref(att), ws, n, handle)
         if st != FESTINA_OK:

@@ -164,3 +164,18 @@ def test_tensors_dropped_after_a_call_on_another_stream():
     b = F.DeviceBlocks(i32(np.full(R, 5)), i32(np.zeros(R)), i32(np.arange(R)[:, None]), i32(np.full(R, -1)), i32([0]), 16, 0)
     _dropped(s, lambda: (torch.ones(R, dtype=torch.uint8, device="cuda"),), lambda d: b.release(d, stream=s))
     assert int(b.n_free_out) == R and torch.equal(b.free_ids, torch.arange(R, dtype=torch.int32, device="cuda"))
+
+
+@pytest.mark.parametrize("bad", [{"window": -1}, {"scale": float("nan")}])
+def test_a_refused_call_leaves_nothing_behind(bad):
+    """The first call of its sizes on a cache is refused; the same call without the fault is answered."""
+    from paper_2606_30391_amd import festina as F
+    rng = np.random.default_rng(51)
+    c = Case(rng, [(20, 2), (30, 1)], D=64)
+    cache, t = c.cache(), c.tensors()
+    print(f"[gpu] a call after a refused one {bad}", flush=True)
+    with pytest.raises(F.FestinaError):
+        cache.attend(c.q, *t, max_new=2, **bad)
+    out, lse = cache.attend(c.q, *t, max_new=2)
+    torch.cuda.synchronize()
+    c.compare(out, lse, c.want())
