@@ -842,6 +842,8 @@ class DeviceCache:
         if lse.dtype is not self._f32 or not lse.is_cuda or lse.dim() != 2 or not lse.is_contiguous() or \
                 lse.shape[0] != T or lse.shape[1] != heads:
             _check(lse, "lse", (self._f32,), (T, heads))
+        if max_new >> 31 or window >> 31:                    # past the struct's 32 bits, where ctypes would cut them off
+            max_new, window = max(-1, min(max_new, 0x7FFFFFFF)), max(-1, min(window, 0x7FFFFFFF))
         qt, qh, _ = q.stride()
         ot, oh, _ = out.stride()
         att = festina_attention(R, columns, T, heads, max_new, kind, window, self._scale if scale is None else scale,

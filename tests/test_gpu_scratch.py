@@ -179,3 +179,19 @@ def test_a_refused_call_leaves_nothing_behind(bad):
     out, lse = cache.attend(c.q, *t, max_new=2)
     torch.cuda.synchronize()
     c.compare(out, lse, c.want())
+
+
+def test_windows_and_bounds_past_32_bits():
+    """2^32 + 5 is no window of 5, and neither is a negative one."""
+    from paper_2606_30391_amd import festina as F
+    rng = np.random.default_rng(52)
+    c = Case(rng, [(200, 2), (30, 1)], D=64)
+    cache, t = c.cache(), c.tensors()
+    print("[gpu] windows past 32 bits", flush=True)
+    for new, window in ((2, 2 ** 32 + 5), (2 ** 32 + 1, 0), (2 ** 31, 2 ** 31), (2, 2 ** 31 - 1)):
+        out, lse = cache.attend(c.q, *t, max_new=new, window=window)
+        torch.cuda.synchronize()
+        c.compare(out, lse, c.want())
+    for kw in ({"max_new": 2, "window": 5 - 2 ** 32}, {"max_new": 2 - 2 ** 32}):
+        with pytest.raises(F.FestinaError):
+            cache.attend(c.q, *t, **kw)
