@@ -772,6 +772,7 @@ class DeviceCache:
         self._types = {**self._halves, torch.float32: FESTINA_F32}
         self._int32, self._f32, self._rows, self._scale = (torch.int32,), torch.float32, (h, d), d ** -0.5
         self._empty, self._attend, self._cache_ref = torch.empty, lib().festina_attend, C.byref(self.cache)
+        self._graded = torch.is_grad_enabled
 
     @classmethod
     def empty(cls, n_blocks: int, block_tokens: int, n_kv_heads: int, head_dim: int, device="cuda"):
@@ -783,7 +784,7 @@ class DeviceCache:
 
     def store(self, k, v, slot, stream=None):
         """Store keys and values [tokens][kv heads][dim] (bfloat16, half or float32; any strides but the last)
-        at the int32 slots [tokens]."""
+        at the int32 slots [tokens].  What is held has no gradient."""
         for name, x in (("k", k), ("v", v)):
             _check(x, name, self._types)
             if x.dim() != 3 or x.shape[1:] != self._rows or (x.stride(2) != 1 and x.numel()):
@@ -801,7 +802,8 @@ class DeviceCache:
                stream=None):
         """Attention of the queries [tokens][heads][dim] (bfloat16 or half) over the cache: (out, lse).  table
         [requests][columns], length [requests] (new tokens included) and first [requests+1] are a step's
-        (DeviceBlocks); max_new bounds the new tokens of one request.  out and lse are made where not given."""
+        (DeviceBlocks); max_new bounds the new tokens of one request.  out and lse are made where not given.  For serving:
+        queries that ask for a gradient are refused."""
         # every check by itself: _check() where one fails names what is wrong (a decode step's kernels take about as
         # long as this function's host work, so it keeps to a few attribute reads a tensor)
         dim = self._rows[1]
@@ -810,6 +812,8 @@ class DeviceCache:
         i32 = self._int32[0]
         if kind is None or not q.is_cuda:
             _check(q, "q", self._halves)
+        if q.requires_grad and self._graded():
+            raise ValueError("q: no gradient passes through a cache in 8 bits (call under torch.no_grad())")
         if q.dim() != 3 or q.shape[2] != dim or (q.stride(2) != 1 and q.numel()):
             raise ValueError(f"q: [tokens][heads][{dim}] with its last axis contiguous")
         if table.dtype is not i32 or not table.is_cuda:

@@ -195,3 +195,18 @@ def test_windows_and_bounds_past_32_bits():
     for kw in ({"max_new": 2, "window": 5 - 2 ** 32}, {"max_new": 2 - 2 ** 32}):
         with pytest.raises(F.FestinaError):
             cache.attend(c.q, *t, **kw)
+
+
+def test_queries_that_ask_for_a_gradient_are_refused():
+    rng = np.random.default_rng(53)
+    c = Case(rng, [(200, 2), (30, 1)], D=64)
+    cache, t = c.cache(), c.tensors()
+    print("[gpu] queries that ask for a gradient", flush=True)
+    want = cache.attend(c.q, *t, max_new=2)
+    q = c.q.clone().requires_grad_()
+    with pytest.raises(ValueError, match="gradient"):
+        cache.attend(q, *t, max_new=2)
+    with torch.no_grad():
+        out, lse = cache.attend(q, *t, max_new=2)
+    torch.cuda.synchronize()
+    assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
