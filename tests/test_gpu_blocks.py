@@ -202,3 +202,24 @@ def test_binding_checks_its_tensors():
         b.release(i(4))
     with pytest.raises(F.FestinaError):
         F.DeviceBlocks(**{**good, "block_tokens": 24}).extend()
+
+
+@pytest.mark.parametrize("busy", [[0, -1], [0, 1, -2, -1], [5, -1]])
+def test_a_million_idle_requests_cost_no_walk(busy):
+    """Requests without tokens between two with some, all in one stretch of the fill: right, and found by few reads."""
+    from paper_2606_30391_amd import festina as F
+    R, bt = 1 << 20, 16
+    held, add = np.full(R, 16), np.zeros(R, int)
+    add[busy] = 37
+    table = np.full((R, 4), -1)
+    table[:, 0] = np.arange(R) % 64
+    free = np.arange(64)
+    print(f"[gpu] extend a million idle requests {busy}", flush=True)
+    b, _ = _check_extend(held, add, table, free, 64, bt, 200)
+    begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    begin.record()
+    b.extend()
+    end.record()
+    torch.cuda.synchronize()
+    print(f"{begin.elapsed_time(end):.3f} ms")
+    assert begin.elapsed_time(end) < 10                     # all launches take 0.06; a read after the other 120
