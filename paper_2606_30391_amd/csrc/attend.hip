@@ -25,7 +25,8 @@
 //   a launch and a few round trips to memory.
 // k_tiles   prompts: 128 query rows a workgroup, tiles of 64 keys converted once into LDS (two buffers, the next
 //   tile's loads in flight meanwhile) and read by four waves of 32 rows.  Bound by the matrix cores and the exponentials.
-//   Few tiles over a long cache are split over the keys and joined by k_tiles_join.
+//   Few tiles over a long cache are split over the keys (how far, the kernel decides, which knows how many there are) and
+//   joined by k_tiles_join.
 //   8,192 tokens, 32 heads over 8 of 128: 550 GFLOP in 559 us (983 TFLOP/s; a large library product 1,189), matrix cores
 //   41% of the cycles, VALU issue 38%.  9,012 tokens of 16 heads of 64: 182 us, 28% and 52%: half the products an exponential.
 // k_plan    running sums of the requests' units and tiles, for many requests.
@@ -61,6 +62,7 @@ constexpr int kBlock = 64 * kWaves;
 constexpr int waves_of(int D, int NT) { return D > 128 || NT > 2 ? 1 : 2; }
 constexpr int workers_of(int D, int NT) { return 1024 * waves_of(D, NT); }
 constexpr int kGroups = 512;         // workgroups of k_tiles that fill the chip: two a compute unit
+constexpr int kJoins = 2048;         // and of its join: eight
 constexpr int kListed = 512;         // requests whose running sums a workgroup forms by itself
 constexpr int kMaxRequests = 1 << 20;
 constexpr long long kThreadsMost = UINT_MAX;     // along one axis of a grid
@@ -74,7 +76,8 @@ struct AttArgs {
   int32_t R, MB, T, Hq, H, G, shift, NB, window;
   int32_t rows_max;                  // requests of at most so many rows are k_rows' (the others k_tiles')
   int32_t tiles_each;                // k_rows without cuts: row tiles a request
-  int32_t workers, splits;
+  int32_t workers;
+  int32_t tiles_most, splits_most;   // k_tiles: bounds of all row tiles and of the parts of one's keys
   int32_t tile_rows;                 // query rows a workgroup of k_tiles
   float scale;                       // times log2 e
   const int32_t *table, *length, *first;
@@ -88,6 +91,8 @@ struct AttArgs {
   const long long *plan;             // [2][R + 1] running sums of units and of tiles, or NULL
   float *part_o, *part_ml;           // pieces: unnormalised rows; (m, l)
   struct Cut *cuts;                  // [workers]
+  int4 *joins;                       // what k_tiles_join needs: (groups, splits), then for each row tile the request's
+                                     // first token, the tile's first row, the request's rows
 };
 
 // What k_rows_join needs of the row tile that begins a join at a piece's start; n = 0: none.
@@ -1032,10 +1037,27 @@ struct TileRows {
   }
 };
 
+// All requests' row tiles, and the parts that the keys of each are cut into: as many as give two workgroups a compute unit,
+// at the next whole number (1,900 tokens of 32 heads over 8 of 128 dims, 480 workgroups, on 8,192: one part 260 us, two
+// 294), and above it for 64 dims, where a compute unit holds three (1,900 tokens of 16 heads, 240 workgroups: three parts
+// 114 us, two 128).  Single tokens have none, so only the sums on the device tell; less than 2 kGroups workgroups have a part.
+struct Tiling {
+  int tiles, groups, splits;         // groups: tiles of all key heads
+};
+template <int D>
+__device__ __forceinline__ Tiling tiling(const AttArgs &a, const long long *list) {
+  Tiling t;
+  t.tiles = same((int)min(list[a.R], (long long)a.tiles_most));
+  t.groups = t.tiles * a.H;
+  t.splits = t.groups > 0 && t.groups < kGroups ? min((kGroups + (D <= 64 ? t.groups - 1 : t.groups / 2)) / t.groups, a.splits_most) : 1;
+  return t;
+}
+
 // A workgroup's row tile: which request, head and rows, and the tiles of keys that it goes over.
 struct TileWork {
   Request rq;
-  long long at;
+  int at;                            // row tile
+  int splits, part;
   int h, r, rows, row0;
   int pos_lo, pos_hi;                // first and last row's positions
   int begin, end;                    // units
@@ -1046,7 +1068,7 @@ struct TileWork {
   }
 };
 
-template <int ROWS>
+template <int D, int ROWS>
 __device__ __forceinline__ TileWork tile_work(const AttArgs &a, long long *list_) {
   TileWork k{};
   const long long *list = a.plan ? a.plan + a.R + 1 : nullptr;
@@ -1054,23 +1076,33 @@ __device__ __forceinline__ TileWork tile_work(const AttArgs &a, long long *list_
     list_sums(a, [&](int r) { return tiles_of(a, r); }, list_);
     list = list_;
   }
+  const Tiling all = tiling<D>(a, list);
+  k.splits = all.splits;
+  if (a.splits_most > 1 && blockIdx.x == 0 && threadIdx.x == 0) a.joins[0] = make_int4(all.groups, all.splits, 0, 0);
+  int i = blockIdx.x;
+  if (all.splits > 1) {
+    k.part = i / all.groups;
+    i -= k.part * all.groups;
+  }
   // neighbouring workgroups take different key heads, so that (for 8 heads) the workgroups of one XCD share one
   // head's keys in its L2; a request's last rows, which see most keys, come first
-  k.h = blockIdx.x % a.H;
-  k.at = same(min(list[a.R], (long long)(gridDim.x / a.H)) - 1 - blockIdx.x / a.H);
-  k.none = k.at < 0;
+  k.h = i % a.H;
+  k.at = all.tiles - 1 - i / a.H;
+  k.none = k.at < 0 || k.part >= all.splits;
   if (k.none) return k;
   k.r = find(list, a.R, k.at);
   k.rq = request(a, k.r);
   k.rows = k.rq.n * a.G;
-  k.row0 = (int)(k.at - same(list[k.r])) * ROWS;
+  k.row0 = (k.at - (int)same(list[k.r])) * ROWS;
   const int before = k.rq.length - k.rq.n;
   k.pos_lo = before + k.row0 / a.G;
   k.pos_hi = before + (min(k.row0 + ROWS, k.rows) - 1) / a.G;
+  if (k.splits > 1 && k.part == 0 && k.h == 0 && threadIdx.x == 0)
+    a.joins[1 + k.at] = make_int4(k.rq.first, k.row0, k.rows, 0);
   const int u = a.window > 0 ? max(k.pos_lo - a.window + 1, 0) / kUnit : 0;
   const int n = k.pos_hi < 0 ? 0 : max(cdiv(k.pos_hi + 1, kUnit) - u, 0);
-  k.begin = u + (int)((long long)n * blockIdx.y / a.splits);
-  k.end = u + (int)((long long)n * (blockIdx.y + 1) / a.splits);
+  k.begin = u + (int)((long long)n * k.part / k.splits);
+  k.end = u + (int)((long long)n * (k.part + 1) / k.splits);
   return k;
 }
 
@@ -1116,8 +1148,8 @@ struct TileWave {
     st.l = across32(st.l, add_);
     const float m = st.most == kMostSum ? st.ref : kNegInf();
     if (!in) return;
-    if (a.splits > 1) {
-      const size_t p = (((size_t)k.at * a.H + k.h) * a.splits + blockIdx.y) * ROWS + i - k.row0;
+    if (k.splits > 1) {
+      const size_t p = ((size_t)(k.at * a.H + k.h) * k.splits + k.part) * ROWS + i - k.row0;
 #pragma unroll
       for (int d = 0; d < D / 32; ++d)
 #pragma unroll
@@ -1154,7 +1186,7 @@ __global__ void __launch_bounds__(64 * W, D <= 64 && W == 4 ? 3 : D <= 128 ? 2 :
   __shared__ KeyTile<T, D> keys[2];
   __shared__ ValueTile<D, W> values[2];
   __shared__ long long list_[kListed + 1];
-  const TileWork k = tile_work<ROWS>(a, list_);
+  const TileWork k = tile_work<D, ROWS>(a, list_);
   if (k.none) return;
   TileRows<T, D> st;
   TileWave<T, D, ROWS> wave;
@@ -1204,23 +1236,20 @@ __global__ void __launch_bounds__(64 * W, D <= 64 && W == 4 ? 3 : D <= 128 ? 2 :
   wave.end(a, k, st);
 }
 
+// A wave a row, in turn; nothing where the keys were not cut.
 template <typename T, int D>
 __global__ void __launch_bounds__(kBlock) k_tiles_join(AttArgs a) {
-  __shared__ long long list_[kListed + 1];
-  const long long *list = a.plan ? a.plan + a.R + 1 : nullptr;
-  if (!list) {
-    list_sums(a, [&](int r) { return tiles_of(a, r); }, list_);
-    list = list_;
+  const int4 all = a.joins[0];
+  const int groups = all.x, splits = all.y;
+  if (splits == 1) return;
+  for (int i = blockIdx.x * kWaves + (threadIdx.x >> 6); i < groups * a.tile_rows; i += gridDim.x * kWaves) {
+    const int group = i / a.tile_rows, row = i - group * a.tile_rows;
+    const int4 tile = a.joins[1 + group / a.H];
+    const int y = tile.y + row, t = y / a.G;
+    if (y >= tile.z) continue;
+    const size_t p = (size_t)group * splits * a.tile_rows + row;
+    join_row<T, D>(a, p, p + a.tile_rows, a.tile_rows, splits, tile.x + t, group % a.H * a.G + y - t * a.G);
   }
-  const int h = blockIdx.x % a.H;
-  const long long at = min(list[a.R], (long long)(gridDim.x / a.H)) - 1 - blockIdx.x / a.H;
-  if (at < 0) return;
-  const int r = find(list, a.R, at);
-  const Request rq = request(a, r);
-  const int row = blockIdx.y * kWaves + (threadIdx.x >> 6), i = (int)(at - list[r]) * a.tile_rows + row, t = i / a.G;
-  if (i >= rq.n * a.G) return;
-  const size_t p = ((size_t)at * a.H + h) * a.splits * a.tile_rows + row;
-  join_row<T, D>(a, p, p + a.tile_rows, a.tile_rows, a.splits, rq.first + t, h * a.G + i - t * a.G);
 }
 
 // ------------------------------------------------------------------ host
@@ -1231,10 +1260,11 @@ struct Shape {
   bool cut, tiles;                   // k_rows with pieces; k_tiles runs
   int tiles_each;
   int tile_rows;
-  long long tile_groups;             // bound of the row tiles of all requests
-  int splits;
+  long long tiles_most;              // bound of the row tiles of all requests
+  int splits_most;                   // and of the parts of one's keys
+  long long tile_groups, join_groups;   // workgroups of k_tiles, of k_tiles_join
   int join_rows;                     // rows of a row tile that are mostly in use: the join's waves
-  size_t plan, cuts, part_ml, part_o, bytes;
+  size_t plan, cuts, joins, part_ml, part_o, bytes;
 };
 
 size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
@@ -1275,20 +1305,27 @@ festina_status shape_of(const festina_kv_cache *c, const festina_attention *t, S
     // heads of 64 dims, with three smaller workgroups a compute unit, 183 against 234 the other way
     const long long rows_all = (long long)t->n_tokens * G * H;
     s->tile_rows = (D == 96 || D == 128) && rows_all >= 256ll * kGroups ? 256 : 128;
-    s->tile_groups = ((long long)t->n_tokens * G + s->tile_rows - 1) / s->tile_rows + t->n_requests;
-    if (s->tile_groups * H > kThreadsMost / (2 * s->tile_rows)) return FESTINA_ERR_UNSUPPORTED;
-    // at least two workgroups a compute unit, of at least 16 steps each
-    const long long groups = max(((long long)t->n_tokens * G + s->tile_rows - 1) / s->tile_rows, 1ll) * H;
-    const long long wanted = (kGroups + groups - 1) / groups;
-    s->splits = (int)max(min(wanted, keys / (16 * kUnit)), 1ll);
-    if (s->splits > 1) {
-      const size_t p = (size_t)s->tile_groups * H * s->splits * s->tile_rows;
-      parts = p > parts ? p : parts;
+    // whole row tiles, and one more a request that has more than rows_max rows, of which there are no more than tokens allow
+    const long long few = s->rows_max / G, requests = min((long long)t->n_requests, t->n_tokens / (few + 1));
+    s->tiles_most = max((long long)t->n_tokens * G / s->tile_rows + requests, 1ll);
+    if (s->tiles_most * H > kThreadsMost / (2 * s->tile_rows)) return FESTINA_ERR_UNSUPPORTED;
+    // parts of at least 16 steps each; none where, with every request but the prompts' having as many tokens as it may,
+    // prompts still fill the chip (tokens of no request would only leave them in one part)
+    const long long sure = ((long long)t->n_tokens - t->n_requests * few) * G / s->tile_rows * H;
+    s->splits_most = sure >= kGroups ? 1 : (int)max(min(keys / (16 * kUnit), (long long)kGroups), 1ll);
+    s->tile_groups = s->tiles_most * H;
+    if (s->splits_most > 1) {
+      const long long groups = s->tile_groups;
+      const size_t pieces = (size_t)min(groups * s->splits_most, kGroups + min(groups, (long long)kGroups));
+      s->join_groups = min(min(groups, (long long)kGroups) * s->tile_rows / kWaves, (long long)kJoins);
+      s->tile_groups = max(groups, (long long)pieces);
+      parts = max(parts, pieces * s->tile_rows);
     }
   }
   s->plan = 0;
   s->cuts = up((size_t)2 * (t->n_requests + 1) * 8);
-  s->part_ml = s->cuts + up((size_t)workers_of(D, max(s->nt, 1)) * sizeof(Cut));
+  s->joins = s->cuts + up((size_t)workers_of(D, max(s->nt, 1)) * sizeof(Cut));
+  s->part_ml = s->joins + up((kGroups + 1) * sizeof(int4));
   s->part_o = s->part_ml + up(parts * 8);
   s->bytes = s->part_o + up(parts * D * 4);
   return FESTINA_OK;
@@ -1319,12 +1356,12 @@ void run(AttArgs a, const Shape &s, long long *plan, hipStream_t st) {
   if constexpr (row_tiles_most(D) >= 4)
     if (s.nt == 4) run_rows<T, D, 4>(a, s, st);
   if (s.tiles) {
-    const dim3 grid((unsigned)(s.tile_groups * a.H), s.splits);
+    const unsigned grid = (unsigned)s.tile_groups;
     if constexpr (D == 96 || D == 128)
       if (s.tile_rows == 256) k_tiles<T, D, 8><<<grid, 512, 0, st>>>(a);
     if (s.tile_rows == 128) k_tiles<T, D, 4><<<grid, kBlock, 0, st>>>(a);
-    if (s.splits > 1)
-      k_tiles_join<T, D><<<dim3((unsigned)(s.tile_groups * a.H), s.tile_rows / kWaves), kBlock, 0, st>>>(a);
+    if (s.splits_most > 1)
+      k_tiles_join<T, D><<<(unsigned)s.join_groups, kBlock, 0, st>>>(a);
   }
 }
 
@@ -1372,7 +1409,8 @@ extern "C" festina_status festina_attend(const festina_kv_cache *cache, const fe
   a.window = att->window;
   a.rows_max = s.rows_max;
   a.tiles_each = s.tiles_each;
-  a.splits = s.splits;
+  a.tiles_most = (int)s.tiles_most;
+  a.splits_most = s.splits_most;
   a.tile_rows = s.tile_rows;
   a.scale = att->scale * 1.44269504088896341f;
   a.table = att->block_table;
@@ -1390,6 +1428,7 @@ extern "C" festina_status festina_attend(const festina_kv_cache *cache, const fe
   a.ks = cache->k_scale;
   a.vs = cache->v_scale;
   a.cuts = reinterpret_cast<Cut *>(w + s.cuts);
+  a.joins = reinterpret_cast<int4 *>(w + s.joins);
   a.part_ml = reinterpret_cast<float *>(w + s.part_ml);
   a.part_o = reinterpret_cast<float *>(w + s.part_o);
   long long *plan = reinterpret_cast<long long *>(w + s.plan);

@@ -436,3 +436,20 @@ def test_a_nan_query_has_nan_and_no_other_row_has(requests):
     c.q[T // 2, 3, 17] = float("nan")
     c.q[T - 1, 0, 5] = float("nan")
     c.check()
+
+
+@pytest.mark.parametrize("D,G,bt,dtype", [(64, 2, 32, "f16"), (96, 1, 64, "bf16"), (128, 4, 64, "bf16"), (256, 1, 128, "f16")])
+@pytest.mark.parametrize("chunk", [(2300, 60), (130, 130), (4100, 9)])
+def test_single_tokens_and_idle_requests_beside_a_chunk(D, G, bt, dtype, chunk):
+    """A step of many requests of which one has a prompt's chunk: its keys are cut into as many parts as it alone has."""
+    rng = np.random.default_rng(D + chunk[0])
+    requests = [(int(x), 1) for x in rng.integers(1, 90, 70)] + [(50, 0)] * 30 + [chunk] + [(2100, 1), (0, 0), (300, 4)]
+    Case(rng, requests, D=D, H=2, G=G, bt=bt, dtype=dtype).check()
+
+
+@pytest.mark.parametrize("columns", [16, 64, 1024])
+@pytest.mark.parametrize("requests", [[(700, 100)], [(40, 1)] * 5 + [(500, 300), (200, 200)], [(90, 90)] * 9])
+def test_prompts_in_tables_of_any_width(requests, columns):
+    """Parts of the keys follow the table's width; those past a request's own keys are empty."""
+    rng = np.random.default_rng(columns)
+    Case(rng, requests, D=64, H=2, G=2, bt=64, columns=columns).check()
