@@ -625,7 +625,9 @@ festina_status festina_store_kv(const festina_kv_cache *cache, const festina_kv_
  * A row that sees no key (p < 0) has out = 0 and lse = -inf.  Keys whose table entry lies
  * outside [0, NB) are not seen.  What is not seen (slots behind the last token, later tokens)
  * may hold anything, NaN included.  Rows of tokens that no request has are not written.
- * v_scale is taken within [2^-32, 2^32] (where festina_store_kv keeps it). */
+ * v_scale is taken within [2^-32, 2^32] (where festina_store_kv keeps it).  A weight is rounded by at
+ * most 2^-11 of itself or 2^-19 of the largest among its 64 keys (64 j .. 64 j + 63), each times its
+ * block's v_scale: blocks of 64 tokens and more do not touch each other, whatever their scales. */
 typedef struct festina_attention {
   int32_t n_requests;                /* R >= 0 */
   int32_t max_blocks;                /* MB >= 1 columns of the block table */

@@ -294,24 +294,38 @@ __device__ __forceinline__ unsigned below(int n, int w) {
   return k >= 4 ? ~0u : k <= 0 ? 0u : (1u << (8 * k)) - 1;
 }
 
-// A row's weights are taken relative to a reference m that follows its maximum only in strides: logits are formed
-// relative to it, and while none exceeds it by more than 2^kSlack nothing has to be rescaled (weights of up
-// to 2^8 are as exact in half precision as those of up to 1).  -inf: no key seen yet, logits are relative to 0.
-constexpr float kSlack = 8.f;
-__device__ __forceinline__ bool raises(float top, float m) { return top > (m == kNegInf() ? kNegInf() : kSlack); }
-constexpr float kMostSum = 256.f;    // the same for k_tiles, on the sum of a lane's weights of 32 keys
-// Takes `top` (relative to m) as the new reference where it raises it, else sets it to 0; scales l and returns the
-// factor for the row's other sums.
-__device__ __forceinline__ float raise(float &top, float &m, float &l) {
+// A row's weights are taken relative to a reference m that follows the keys at hand in strides: logits are formed relative
+// to it, and while the largest of a step lies between kLow and kSlack (in base 2) nothing has to be rescaled.  Else the
+// reference is placed kHead below that largest.  Half precision keeps 11 bits of weights of up to 2^15 and down to 2^-14 and
+// is off by at most 2^-25 below that: 2^-19 of the step's largest weight.  The reference goes down as well as up, so that keys
+// beside one of far more weight, or behind a block whose value scale (which weighs in the maximum) is far larger, are
+// not lost to the format; the sums, in 32 bits, may then be far larger than what is added to them.  -inf: no key seen
+// yet, logits are relative to 0.
+constexpr float kHead = 7.f, kSlack = 15.f, kLow = -6.f;
+// The same for k_tiles, on the sum of a lane's weights of 16 keys: 2^-6 .. 2^15, as one comparison of its bits.  (A sum of 0
+// is looked at too: a tile of which a row sees nothing.)
+constexpr unsigned kLeastSum = 0x3c800000, kSums = 0x47000000 - kLeastSum;
+// (Both ends cost 1% of a prompt of 8,192 tokens, 2% of units of 64 dims; a kHead of 10, which keeps three bits more, as much
+// again, since new maxima then move the reference more often.)
+// How far down the reference may go, by a row's sum of weights so far: the sums of values, at most 448 * 2^32 times
+// as large, stay below 2^104.
+__device__ __forceinline__ float down(float top, float l) { return fminf(fmaxf(top - kHead, log2_(l) - 60.f), 0.f); }
+__device__ __forceinline__ bool moves(float top, float m) {
+  return m == kNegInf() ? top > kNegInf() : top > kSlack || (top < kLow && top > kNegInf());
+}
+// Turns `top`, a row's largest logit relative to the reference, into how far the reference moves; scales l (of which each lane
+// has a part) and returns the factor for the row's other sums.
+__device__ __forceinline__ float move(float &top, float &m, float &l) {
   const bool fresh = m == kNegInf();
-  if (!raises(top, m)) top = 0.f;
-  else m = fresh ? top : m + top;
+  const float all = across32(across16(l, add_), add_);
+  if (!moves(top, m)) top = 0.f;
+  else top = top < kLow && !fresh ? down(top, all) : top - kHead, m = fresh ? top : m + top;
   const float f = fresh ? 1.f : exp2_(-top);
   l *= f;
   return f;
 }
 
-// Weight of a piece with maximum m in a row whose maximum is M.
+// Weight of a piece with reference m in a row whose largest is M.
 __device__ __forceinline__ float weight(float m, float M) { return m == kNegInf() ? 0.f : exp2_(m - M); }
 
 template <typename T>
@@ -423,9 +437,9 @@ struct Rows {
 #pragma unroll
         for (int i = 0; i < 4; ++i) top = fmaxf(top, x[nt][u][i]);
       top = across32(across16(top, max_), max_);
-      if (__any(raises(top, st.m[nt]))) {
+      if (__any(moves(top, st.m[nt]))) {
         rarely();
-        const float f = raise(top, st.m[nt], st.l[nt]);
+        const float f = move(top, st.m[nt], st.l[nt]);
 #pragma unroll
         for (int u = 0; u < 4; ++u) x[nt][u] -= top;
 #pragma unroll
@@ -904,7 +918,8 @@ struct TileRows {
   f16v o[D / 32];
   f16v x[2];                         // logits of a tile, 32 keys each
   h8 w[2][2];                        // its weights
-  float ref, l, most;                // the reference (0 where no key was seen), the largest sum that leaves it
+  float ref, l;                      // the reference (0 where no key was seen)
+  unsigned sums_kept;                // sums of kLeastSum and so many more leave it; 0 where no key was seen
   Span sees;
 
   // x = K Q': two chains of products side by side, each operand read from LDS a step before it is used
@@ -968,22 +983,23 @@ struct TileRows {
     return sum[0] + sum[1];
   }
 
-  // The weights and their part of l.  No weight is above their sum, so while that is small the reference holds and
-  // the logits' maximum need not be known.
+  // The weights and their part of l.  Their largest lies between a 16th of their sum and their sum, so while that is
+  // neither large nor small the reference holds and the logits' maximum need not be known.
   template <int g>
   __device__ __forceinline__ void weights(const KeyTile<T, D> &b) {
     float sum = powers<g>();
-    if (__any(sum > most)) {
+    if (__any(__float_as_uint(sum) - kLeastSum >= sums_kept) && __any(sum > 0.f || sums_kept == 0)) {
       rarely();
       float top = x[g][0];
 #pragma unroll
       for (int i = 1; i < 16; ++i) top = fmaxf(top, x[g][i]);
       top = across32(top, max_);
-      const bool fresh = most != kMostSum, up = top > (fresh ? kNegInf() : 0.f);
-      top = up ? top : 0.f;
+      const float all = across32(l, add_);
+      const bool fresh = sums_kept != kSums, up = top > (fresh ? kNegInf() : kHead);
+      top = up ? top - kHead : !fresh && top < kLow && top > kNegInf() ? down(top, all) : 0.f;
       const float f = fresh ? 1.f : exp2_(-top);
       ref += top;
-      most = up ? kMostSum : most;
+      sums_kept = up ? kSums : sums_kept;
       l *= f;
 #pragma unroll
       for (int y = g; y < 2; ++y) x[y] -= top;
@@ -1122,7 +1138,7 @@ struct TileWave {
     pos_max = before + (min(wave0 + 32, k.rows) - 1) / a.G;
     st.sees = span(a, in ? before + t : -1);
     st.ref = st.l = 0.f;
-    st.most = st.sees.count > 0 ? -1.f : __builtin_inff();
+    st.sums_kept = st.sees.count > 0 ? 0u : ~0u;
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
@@ -1146,7 +1162,7 @@ struct TileWave {
   __device__ __forceinline__ void end(const AttArgs &a, const TileWork &k, TileRows<T, D> &st) const {
     const int half = (threadIdx.x & 63) >> 5;
     st.l = across32(st.l, add_);
-    const float m = st.most == kMostSum ? st.ref : kNegInf();
+    const float m = st.sums_kept == kSums ? st.ref : kNegInf();
     if (!in) return;
     if (k.splits > 1) {
       const size_t p = ((size_t)(k.at * a.H + k.h) * k.splits + k.part) * ROWS + i - k.row0;
