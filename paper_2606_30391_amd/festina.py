@@ -752,11 +752,11 @@ class DeviceBlocks:
 class DeviceCache:
     """One layer's key/value cache in 8 bits (festina_kv_cache): uint8 codes k [n_blocks][kv heads][block tokens]
     [dim], v [n_blocks][kv heads][dim][block tokens] and float32 scales k_scale, v_scale [n_blocks][kv heads],
-    device tensors used in place (``DeviceCache.empty`` makes them).  Scratch is the object's own, one for each stream;
-    what torch.cuda.graph captures has scratch of its graph's memory (a graph captured by other means: festina_attend
+    device tensors used in place (``DeviceCache.empty`` makes them).  Scratch is the object's own, or shared with that of
+    the cache given as scratch_of (another layer's), one for each stream; what torch.cuda.graph captures has scratch of its graph's memory (a graph captured by other means: festina_attend
     with a workspace that the caller keeps).  stream= as for DeviceBlocks."""
 
-    def __init__(self, k, v, k_scale, v_scale):
+    def __init__(self, k, v, k_scale, v_scale, scratch_of=None):
         import torch
         _check(k, "k", (torch.uint8,), k.shape)
         if k.dim() != 4:
@@ -767,7 +767,7 @@ class DeviceCache:
         _check(v_scale, "v_scale", (torch.float32,), (n, h))
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.cache = festina_kv_cache(n, bt, h, d, _ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale))
-        self._ws, self._ws_bytes = _Workspaces(), {}
+        self._ws, self._ws_bytes = scratch_of._ws if scratch_of is not None else _Workspaces(), {}
         self._halves = {torch.bfloat16: FESTINA_BF16, torch.float16: FESTINA_F16}
         self._types = {**self._halves, torch.float32: FESTINA_F32}
         self._int32, self._f32, self._rows, self._scale = (torch.int32,), torch.float32, (h, d), d ** -0.5
@@ -775,12 +775,12 @@ class DeviceCache:
         self._graded = torch.is_grad_enabled
 
     @classmethod
-    def empty(cls, n_blocks: int, block_tokens: int, n_kv_heads: int, head_dim: int, device="cuda"):
+    def empty(cls, n_blocks: int, block_tokens: int, n_kv_heads: int, head_dim: int, device="cuda", scratch_of=None):
         import torch
         u8 = lambda *s: torch.empty(s, dtype=torch.uint8, device=device)
         f32 = lambda: torch.zeros((n_blocks, n_kv_heads), dtype=torch.float32, device=device)
         return cls(u8(n_blocks, n_kv_heads, block_tokens, head_dim), u8(n_blocks, n_kv_heads, head_dim, block_tokens),
-                   f32(), f32())
+                   f32(), f32(), scratch_of)
 
     def store(self, k, v, slot, stream=None):
         """Store keys and values [tokens][kv heads][dim] (bfloat16, half or float32; any strides but the last)

@@ -36,8 +36,10 @@ class Server:
         self.blocks = festina.DeviceBlocks(z(n_requests), z(n_requests), z(n_requests, columns), free,
                                            torch.full((1,), n_blocks, dtype=torch.int32, device=device),
                                            block_tokens, step_tokens)
-        self.caches = [festina.DeviceCache.empty(n_blocks, block_tokens, n_kv_heads, head_dim, device)
-                       for _ in range(n_layers)]
+        self.caches = []
+        for _ in range(n_layers):                            # a step's layers follow one another: one scratch for all
+            self.caches.append(festina.DeviceCache.empty(n_blocks, block_tokens, n_kv_heads, head_dim, device,
+                                                         self.caches[0] if self.caches else None))
 
     def step(self, add, qkv, window: int = 0):
         """One step with add[r] new tokens of request r (host integers): each layer's attention, a list.

@@ -87,3 +87,23 @@ def test_the_command_serves_the_busiest_gpu(capsys):
     said = capsys.readouterr().out
     print(said, flush=True)
     assert "prompts:" in said and "decode: 3 steps" in said
+
+
+def test_the_layers_share_one_scratch():
+    from paper_2606_30391_amd.serve import Server
+    gen = torch.Generator("cuda").manual_seed(6)
+    layers = 12
+    srv = Server(8, 4096, 600, 400, layers, 2, 64, 64)
+    add = [40] * 7 + [100]
+    data = [[torch.randn((sum(add), h, 64), generator=gen, device="cuda").bfloat16() for h in (8, 2, 2)]
+            for _ in range(layers)]
+    print("[gpu] twelve layers, one scratch", flush=True)
+    got = srv.step(add, lambda i: data[i])
+    torch.cuda.synchronize()
+    kept = [ws for c in srv.caches for ws, _, _ in c._ws.by_stream.values()]
+    assert len({ws.data_ptr() for ws in kept}) == 1
+    alone = Server(8, 4096, 600, 400, 1, 2, 64, 64)
+    for i in (0, 5, 11):                                     # each layer's rows as if it were alone
+        want = alone.step(add, lambda _: data[i])
+        assert torch.equal(got[i], want[0])
+        alone.finish(torch.ones(8, dtype=torch.uint8, device="cuda"))
