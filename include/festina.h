@@ -647,7 +647,8 @@ typedef struct festina_attention {
   float *lse;                        /* [T][n_heads] or NULL */
 } festina_attention;
 
-/* Bytes of device workspace of festina_attend (reads only sizes; 0 for invalid ones). */
+/* Bytes of device workspace of festina_attend (reads only sizes; 0 for invalid ones, and for ones beyond 2^30 keys of a
+ * table row or query rows, 2^20 requests, 65,536 query or 1,024 key heads, which are unsupported). */
 size_t festina_attend_workspace_bytes(const festina_kv_cache *cache, const festina_attention *att);
 
 /* Workspace 256-byte aligned, clobbered.  One to five kernel launches on `stream`. */

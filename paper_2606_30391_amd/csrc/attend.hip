@@ -20,15 +20,15 @@
 //   per wave and step, operands loaded from the cache into the lanes that use them.  Bound by the cache's bytes.
 //   All requests' keys form one line of 64-key units, cut into equal pieces, one a wave, so that
 //   ragged lengths leave no wave behind; a row tile that a cut falls into is joined by k_rows_join.
-//   64 requests up to 32,768 tokens, 8 heads of 128: 2.15 GB in 409 us, 5.3 TB/s (a large copy: 4.96).
+//   64 requests up to 32,768 tokens, 8 heads of 128: 2.15 GB in 413 us, 5.2 TB/s (a large copy: 4.96).
 // k_rows_whole   the same for short tables: a workgroup a row tile, joined in LDS, one launch.  One request of 403 tokens: 7 us,
 //   a launch and a few round trips to memory.
 // k_tiles   prompts: 128 query rows a workgroup, tiles of 64 keys converted once into LDS (two buffers, the next
 //   tile's loads in flight meanwhile) and read by four waves of 32 rows.  Bound by the matrix cores and the exponentials.
 //   Few tiles over a long cache are split over the keys (how far, the kernel decides, which knows how many there are) and
 //   joined by k_tiles_join.
-//   8,192 tokens, 32 heads over 8 of 128: 550 GFLOP in 559 us (983 TFLOP/s; a large library product 1,189), matrix cores
-//   41% of the cycles, VALU issue 38%.  9,012 tokens of 16 heads of 64: 182 us, 28% and 52%: half the products an exponential.
+//   8,192 tokens, 32 heads over 8 of 128: 550 GFLOP in 558 us (985 TFLOP/s; a large library product 1,189), matrix cores
+//   41% of the cycles, VALU issue 39%.  9,012 tokens of 16 heads of 64: 170 us, 27% and 52%: half the products an exponential.
 // k_plan    running sums of the requests' units and tiles, for many requests.
 #include <hip/hip_runtime.h>
 
