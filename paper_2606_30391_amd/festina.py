@@ -657,7 +657,7 @@ def _used_on(stream, *tensors):
     """Tell torch that work on `stream` (a torch stream) reads or writes these tensors: their memory is not given to others
     before that work is done, also where the caller drops them right after the call.  Not for a raw handle: its owner
     may end that stream at any time, so the owner keeps the tensors too."""
-    if stream is not None and not isinstance(stream, int):
+    if not isinstance(stream, int):
         for t in tensors:
             t.record_stream(stream)
 
@@ -730,14 +730,16 @@ class DeviceBlocks:
     def extend(self, stream=None):
         held, ws, handle = self._ws.get(self.ws_bytes, stream, self.table.device)
         festina_extend_blocks(self.req, self.out, ws, self.ws_bytes, handle)
-        _used_on(stream, *self._tensors())
+        if stream is not None:
+            _used_on(stream, *self._tensors())
 
     def release(self, done, stream=None):
         import torch
         _check(done, "done", (torch.uint8, torch.bool), self.held.shape)
         held, ws, handle = self._ws.get(self.ws_bytes, stream, self.table.device)
         festina_release_blocks(self.req, done, self.out, ws, self.ws_bytes, handle)
-        _used_on(stream, done, *self._tensors())
+        if stream is not None:
+            _used_on(stream, done, *self._tensors())
 
     def _tensors(self):
         return (self.held, self.add, self.table, self.free_ids, self.n_free, self.first, self.slot, self.length, self.served,
@@ -796,7 +798,8 @@ class DeviceCache:
         (kt, kh, _), (vt, vh, _) = k.stride(), v.stride()
         festina_store_kv(self.cache, festina_kv_tokens(T, self._types[k.dtype], k.data_ptr(), v.data_ptr(), kt, kh, vt,
                                                        vh, slot.data_ptr()), stream)
-        _used_on(stream, k, v, slot, self.k, self.v, self.k_scale, self.v_scale)
+        if stream is not None:
+            _used_on(stream, k, v, slot, self.k, self.v, self.k_scale, self.v_scale)
 
     def attend(self, q, table, length, first, max_new: int, scale=None, window: int = 0, out=None, lse=None,
                stream=None):
