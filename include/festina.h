@@ -574,6 +574,13 @@ festina_status festina_extend_blocks(const festina_kv_requests *req, festina_kv_
 festina_status festina_release_blocks(const festina_kv_requests *req, const uint8_t *done, festina_kv_step *out,
                                       void *workspace, size_t workspace_bytes, void *stream);
 
+/* The blocks behind the first keep[r] tokens of every request (columns ceil(keep / BT) .. ceil(held / BT) - 1) go onto
+ * free_ids as above, and its length becomes keep[r].  A request whose keep[r] is none of 0 .. held gives nothing and keeps its
+ * length, one with held > MB * BT gives nothing.  keep may be out's length.  Workspace and launches as for
+ * festina_release_blocks. */
+festina_status festina_trim_blocks(const festina_kv_requests *req, const int32_t *keep, festina_kv_step *out,
+                                   void *workspace, size_t workspace_bytes, void *stream);
+
 /* Element types of keys, values, queries and outputs. */
 #define FESTINA_BF16 0
 #define FESTINA_F16 1
@@ -654,6 +661,110 @@ size_t festina_attend_workspace_bytes(const festina_kv_cache *cache, const festi
 /* Workspace 256-byte aligned, clobbered.  One to five kernel launches on `stream`. */
 festina_status festina_attend(const festina_kv_cache *cache, const festina_attention *att, void *workspace,
                               size_t workspace_bytes, void *stream);
+
+/* ---- Steps of drafted tokens ----
+ *
+ * A request's new tokens of a step may be guesses at what follows, of which the step verifies several at once.  They form a
+ * tree of at most 64 nodes: node 0 is a token that is known (the last one chosen, not yet in the cache), and every
+ * node comes after its parent, the token that it would follow.  festina_extend_blocks gives the nodes slots as it does any
+ * new tokens, in the order of the nodes; a node's position is that of a token behind its ancestors, not its slot's.
+ * The calls of a step: festina_plan_drafts once; in each layer festina_rotate_heads, festina_store_kv and
+ * festina_attend_drafts; then festina_accept_drafts with the tokens that the model chose, festina_keep_tokens for
+ * all layers, and festina_trim_blocks.  A request with more than 64 new tokens is a run (a prompt beside the trees):
+ * each of its tokens follows the one before, and all are kept. */
+typedef struct festina_drafts {
+  int32_t n_requests;                /* R >= 0, at most 2^20 */
+  int32_t n_tokens;                  /* T >= 0 entries of the token arrays below */
+  const int32_t *first;              /* [R + 1] non-decreasing, as from festina_extend_blocks */
+  const int32_t *length;             /* [R] tokens in the cache, the new ones included */
+  const int32_t *parent;             /* [T] a token's parent, as an index among its request's new tokens: -1 .. its own
+                                      * index - 1 (others are taken as -1: no parent); not read for runs; NULL: each
+                                      * token's parent is the one before it */
+} festina_drafts;
+
+/* What the nodes see and where they stand: bit j of seen[t] (j < 64) is set when node j of t's request is t itself or an ancestor
+ * of it (0 for a run), and position[t] = length - n + the number of its ancestors, n being its request's new tokens (for a
+ * run: its index instead).  Either may be NULL.  Entries of tokens that no request has are not written.  One kernel launch
+ * on `stream`. */
+festina_status festina_plan_drafts(const festina_drafts *drafts, uint64_t *seen, int32_t *position, void *stream);
+
+/* Results (device memory, written by the call; length may be the drafts' own).  From node 0 on, which is always kept, the
+ * path goes to the first child whose token is the choice at the node, until there is none:
+ *   kept[r]   = nodes of the path (all tokens of a run, 0 without new tokens);
+ *   path[t]   = for the request's i-th new token t, i < kept: the path's i-th node (ascending); else -1;
+ *   next[r]   = the choice at the last node of the path, -1 without new tokens;
+ *   length[r] = tokens in the cache when only the path stays: drafts' length - n + kept.
+ * Entries of path of tokens that no request has are not written. */
+typedef struct festina_accepted {
+  int32_t *path;                     /* [T] */
+  int32_t *kept;                     /* [R] */
+  int32_t *next;                     /* [R] */
+  int32_t *length;                   /* [R] */
+} festina_accepted;
+
+/* token[t]: the drafted tokens; choice[t]: the token that the model chooses behind t.  One kernel launch on `stream`. */
+festina_status festina_accept_drafts(const festina_drafts *drafts, const int32_t *token, const int32_t *choice,
+                                     festina_accepted *out, void *stream);
+
+/* festina_attend for drafted tokens: bit j of seen[t] says that t sees node j of its request (seen: [T], 8-byte aligned, e.g. from
+ * festina_plan_drafts; bits from n on are taken as 0), and it sees the keys before the request's new tokens.  Its
+ * position is p = length - n + (set bits) - 1 (no set bit: length - n); with window > 0 it sees those keys j > p - window only,
+ * and the `window` last of its nodes.  seen is not read for runs, which see what festina_attend has them see.  Keys of
+ * nodes that a row does not see may hold anything.  All else as there; workspace from
+ * festina_attend_drafts_workspace_bytes. */
+size_t festina_attend_drafts_workspace_bytes(const festina_kv_cache *cache, const festina_attention *att);
+
+festina_status festina_attend_drafts(const festina_kv_cache *cache, const festina_attention *att, const uint64_t *seen,
+                                     void *workspace, size_t workspace_bytes, void *stream);
+
+/* The kept tokens of a step, e.g. as from festina_accept_drafts. */
+typedef struct festina_kept {
+  int32_t n_requests;                /* R >= 0, at most 2^20 */
+  int32_t max_blocks;                /* MB >= 1 columns of the block table */
+  int32_t n_tokens;                  /* T >= 0 entries of path */
+  const int32_t *block_table;        /* [R][MB] */
+  const int32_t *length;             /* [R] tokens in the cache, the new ones included */
+  const int32_t *first;              /* [R + 1] */
+  const int32_t *path;               /* [T] */
+  const int32_t *kept;               /* [R] */
+} festina_kept;
+
+/* Moves the kept tokens' keys and values together, in n_caches caches of the same sizes (the layers; HOST array):
+ * the request's token at position length - n + path[i] becomes the one at length - n + i, for i < kept[r].  For each block,
+ * head, and keys or values, the scale becomes the largest among those of the blocks that its tokens came from (its own for
+ * tokens that stay), and codes from a block of another scale are rounded anew, code' = e4m3(code * old / new), the older
+ * tokens' too (exact unless a code becomes subnormal; scales are the powers of two that festina_store_kv makes).  Slots behind
+ * the kept tokens are left as they are.  Left as it is a run, a request whose path is not ascending or leaves its new
+ * tokens, and one with length < n, length > MB * BT, or an id outside [0, NB) among its new tokens' blocks.  No two requests may
+ * share a block that their new tokens lie in.  No workspace; one kernel launch on `stream` for 64 caches. */
+festina_status festina_keep_tokens(const festina_kv_cache *caches, int32_t n_caches, const festina_kept *kept, void *stream);
+
+/* Norm and rotation of queries and keys, head by head.  head_dim is 64, 96, 128 or 256. */
+typedef struct festina_rotary {
+  int32_t head_dim;                  /* D */
+  int32_t rotated;                   /* elements that are rotated, the first of each head: a multiple of 16, 0 .. D */
+  int32_t interleaved;               /* pairs are elements 2i and 2i + 1, else i and i + rotated / 2 */
+  float eps;                         /* >= 0 */
+  const uint64_t *turn;              /* [rotated / 2] turns of pair i per position, times 2^64 (radians * 2^64 / 2 pi, modulo
+                                      * 2^64), device memory */
+  const float *q_weight, *k_weight;  /* [D], device memory, or NULL: no norm */
+} festina_rotary;
+
+typedef struct festina_heads {
+  int32_t n_tokens;                  /* T >= 0 */
+  int32_t n_heads, n_kv_heads;       /* heads of q and of k, >= 0 and at most 65,536 */
+  int32_t dtype;                     /* FESTINA_BF16, FESTINA_F16 or FESTINA_F32: q, k and the outputs */
+  const int32_t *position;           /* [T], any value */
+  const void *q, *k;                 /* [T][heads][D], last axis contiguous, any strides (in elements, >= 0) of the others */
+  int64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride;
+  void *q_out, *k_out;               /* as q and k: the same memory with the same strides, or memory apart from it */
+  int64_t q_out_token_stride, q_out_head_stride, k_out_token_stride, k_out_head_stride;
+} festina_heads;
+
+/* Each head's elements x become y = x / sqrt(mean(x^2) + eps) * weight (y = x where there is no weight), and every pair (a, b)
+ * of the rotated ones (a cos w - b sin w, b cos w + a sin w) with w = position * turn / 2^64 turns, exact modulo a turn; float32
+ * throughout, rounded once to the type.  No workspace; one kernel launch on `stream`. */
+festina_status festina_rotate_heads(const festina_rotary *rotary, const festina_heads *heads, void *stream);
 
 /* Static, NUL-terminated description of a status code. */
 const char *festina_status_string(festina_status status);

@@ -16,7 +16,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SRCS = [os.path.join(HERE, "csrc", n) for n in ("festina.hip", "fronts.hip", "sweep.hip", "preferred.hip",
                                                        "dispatch.hip", "transfer.hip", "blocks.hip", "cache.hip",
-                                                       "attend.hip")]
+                                                       "attend.hip", "drafts.hip", "rotate.hip")]
 HDRS = [os.path.join(HERE, "csrc", n) for n in ("fronts.h", "kv.h")]
 LIB = os.path.join(HERE, "libfestina.so")
 HASH_FILE = LIB + ".sources"

@@ -63,6 +63,7 @@ constexpr int waves_of(int D, int NT) { return D > 128 || NT > 2 ? 1 : 2; }
 constexpr int workers_of(int D, int NT) { return 1024 * waves_of(D, NT); }
 constexpr int kGroups = 512;         // workgroups of k_tiles that fill the chip: two a compute unit
 constexpr int kJoins = 2048;         // and of its join: eight
+constexpr int kNodes = 64;           // nodes of a draft tree: a request with more new tokens is a run
 constexpr int kListed = 512;         // requests whose running sums a workgroup forms by itself
 constexpr int kMaxRequests = 1 << 20;
 constexpr long long kThreadsMost = UINT_MAX;     // along one axis of a grid
@@ -86,6 +87,7 @@ struct AttArgs {
   void *out;
   int64_t out_token, out_head;
   float *lse;
+  const unsigned long long *seen;    // drafts: [T] which of its request's new tokens a row sees, else NULL
   const uint8_t *k, *v;
   const float *ks, *vs;
   const long long *plan;             // [2][R + 1] running sums of units and of tiles, or NULL
@@ -273,10 +275,68 @@ __device__ __forceinline__ float add_(float x, float y) { return x + y; }
 struct Span {
   int from, count;
   __device__ __forceinline__ bool has(int key) const { return (unsigned)(key - from) < (unsigned)count; }
+  __device__ __forceinline__ bool any() const { return count > 0; }
+  // The same keys counted from `base` on; none unless `there`.
+  __device__ __forceinline__ Span at(int base, bool there) const { return Span{from - base, there ? count : 0}; }
 };
 __device__ __forceinline__ Span span(const AttArgs &a, int pos) {
   const int from = a.window > 0 ? max(pos - a.window + 1, 0) : 0;
   return Span{from, max(pos - from + 1, 0)};
+}
+
+// Some of 64 keys.
+struct Bits {
+  unsigned long long word;
+  __device__ __forceinline__ bool has(int key) const { return word >> key & 1; }
+};
+// For rows of a draft tree: the keys from `from` to `nodes`, and of the 64 from there on those with a bit in `word`.
+struct TreeSpan {
+  int from, nodes;
+  unsigned long long word;
+  __device__ __forceinline__ bool any() const { return from < nodes || word != 0; }
+  // Which of the 64 keys from `base` on.
+  __device__ __forceinline__ Bits at(int base, bool there) const {
+    const int lo = min(max(from - base, 0), kNodes), s = nodes - base, hi = min(max(s, 0), kNodes);
+    unsigned long long m = hi > lo ? ~0ull >> (kNodes - hi + lo) << lo : 0ull;
+    m |= s <= -kNodes || s >= kNodes ? 0ull : s >= 0 ? word << s : word >> -s;
+    return Bits{there ? m : 0ull};
+  }
+  __device__ __forceinline__ bool has(int key) const { return at(key, true).has(0); }
+};
+
+template <bool TREE> struct Seen { typedef Span type; };
+template <> struct Seen<true> { typedef TreeSpan type; };
+
+// What token t of the request's new ones sees (nothing unless `in`).
+template <bool TREE>
+__device__ __forceinline__ typename Seen<TREE>::type sees_of(const AttArgs &a, const Request &q, int t, bool in) {
+  const int before = q.length - q.n;
+  if constexpr (!TREE) {
+    return span(a, in ? before + t : -1);
+  } else {
+    if (q.n > kNodes) {
+      const Span s = span(a, in ? before + t : -1);
+      return TreeSpan{s.from, s.from + s.count, 0ull};
+    }
+    unsigned long long word = in ? a.seen[q.first + t] : 0ull;
+    word &= ~0ull >> (kNodes - q.n);                   // (a request with rows has at least one)
+    const int pos = before + max(__builtin_popcountll(word) - 1, 0);
+    const int from = a.window > 0 ? max(pos - a.window + 1, 0) : 0;
+    if (a.window > 0)                                  // the nearest of its path, the node itself included
+      for (int n = __builtin_popcountll(word); n > a.window; --n) word &= word - 1;
+    if (before < 0) word = before > -kNodes ? word >> -before << -before : 0ull;
+    return TreeSpan{from, in ? before : 0, word};
+  }
+}
+// Bounds of the positions up to which the rows of tokens t0 .. t1 see their keys.
+struct Reach {
+  int lo, hi;
+};
+template <bool TREE>
+__device__ __forceinline__ Reach reach(const Request &q, int t0, int t1) {
+  const int before = q.length - q.n;
+  if (TREE && q.n <= kNodes) return Reach{before - 1, q.length - 1};
+  return Reach{before + t0, before + t1};
 }
 // Keeps a rare branch a branch: without it the compiler computes the masks of every step.
 __device__ __forceinline__ void rarely() { asm volatile(""); }
@@ -348,7 +408,7 @@ struct RowsStep {
   bool ok;
 };
 
-template <typename T, int D, int NT>
+template <typename T, int D, int NT, bool TREE = false>
 struct Rows {
   static constexpr int kRows = 16 * NT, kSteps = D / 32, kPitch = D + 4;
 
@@ -392,7 +452,7 @@ struct Rows {
     typename Vec8<T>::type q[NT][kSteps];
     f4 o[NT][D / 16];
     float m[NT], l[NT];
-    Span sees[NT];
+    typename Seen<TREE>::type sees[NT];
   };
 
   static __device__ __forceinline__ void step(const AttArgs &a, const Request &rq, int base, int pos_min, int pos_max,
@@ -425,7 +485,7 @@ struct Rows {
         for (int i = 0; i < 4; ++i) x[nt][u][i] = fmaf(x[nt][u][i], c, shift);
       if (masked) {
         rarely();
-        const Span sees{st.sees[nt].from - base - 16 * g, s.ok ? st.sees[nt].count : 0};
+        const auto sees = st.sees[nt].at(base + 16 * g, s.ok);
 #pragma unroll
         for (int u = 0; u < 4; ++u)
 #pragma unroll
@@ -485,9 +545,9 @@ struct Rows {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
               h8 sees;
+              const auto seen = st.sees[nt].at(base + 16 * g + 8 * i, s.ok);
 #pragma unroll
-              for (int j = 0; j < 8; ++j)
-                sees[j] = s.ok && st.sees[nt].has(base + 16 * g + 8 * i + j) ? (f16)1.f : (f16)0.f;
+              for (int j = 0; j < 8; ++j) sees[j] = seen.has(j) ? (f16)1.f : (f16)0.f;
               hits = mfma16(decode8<f16>(nan[2 * i] & kOnes, nan[2 * i + 1] & kOnes), sees, hits);
             }
 #pragma unroll
@@ -511,13 +571,13 @@ struct Rows {
   static __device__ __forceinline__ void scan_keys(const AttArgs &a, int r, const Request &rq, int h, int tile, int k0,
                                                    int k1, int stride, State &st) {
     const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-    const int rows = rq.n * a.G, row0 = tile * kRows, before = rq.length - rq.n;
-    const int pos_min = before + row0 / a.G, pos_max = before + (min(row0 + kRows, rows) - 1) / a.G;
+    const int rows = rq.n * a.G, row0 = tile * kRows;
+    const Reach to = reach<TREE>(rq, row0 / a.G, (min(row0 + kRows, rows) - 1) / a.G);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const int i = row0 + nt * 16 + c, t = i / a.G;
       const bool in = i < rows;
-      st.sees[nt] = span(a, in ? before + t : -1);
+      st.sees[nt] = sees_of<TREE>(a, rq, t, in);
       st.m[nt] = kNegInf();
       st.l[nt] = 0.f;
 #pragma unroll
@@ -541,7 +601,7 @@ struct Rows {
       RowsStep<D> s;
       load(a, ids, h, (u0 + u) * kUnit, s);
       ids = blocks(a, table, (u0 + u + stride) * kUnit);
-      step(a, rq, (u0 + u) * kUnit, pos_min, pos_max, s, st);
+      step(a, rq, (u0 + u) * kUnit, to.lo, to.hi, s, st);
     }
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) st.l[nt] = across32(across16(st.l[nt], add_), add_);
@@ -627,9 +687,9 @@ __device__ __forceinline__ int pieces(const AttArgs &a, long long all) {
 __device__ __forceinline__ long long piece_start(long long all, int w, int n) { return all * w / n; }
 
 // A workgroup for each row tile and key head, its waves over the keys in turn: few keys, one launch.
-template <typename T, int D, int NT>
+template <typename T, int D, int NT, bool TREE>
 __global__ void __launch_bounds__(kBlock, (D <= 128 && NT <= 2) ? 2 : 1) k_rows_whole(AttArgs a) {
-  typedef Rows<T, D, NT> K;
+  typedef Rows<T, D, NT, TREE> K;
   __shared__ typename K::Shared sh;
   const int tile = blockIdx.x % a.tiles_each, rest = blockIdx.x / a.tiles_each, h = rest % a.H, r = rest / a.H;
   const Request rq = request(a, r);
@@ -639,9 +699,9 @@ __global__ void __launch_bounds__(kBlock, (D <= 128 && NT <= 2) ? 2 : 1) k_rows_
 }
 
 // A wave a piece.
-template <typename T, int D, int NT>
+template <typename T, int D, int NT, bool TREE>
 __global__ void __launch_bounds__(64, waves_of(D, NT)) k_rows(AttArgs a) {
-  typedef Rows<T, D, NT> K;
+  typedef Rows<T, D, NT, TREE> K;
   __shared__ long long list_[kListed + 1];
   const long long *list = a.plan;
   if (!list) {
@@ -910,7 +970,7 @@ struct Stage {
 };
 
 // 32 query rows of a wave: columns of the products.
-template <typename T, int D>
+template <typename T, int D, bool TREE>
 struct TileRows {
   typedef typename Vec8<T>::type Vec;
 
@@ -920,7 +980,7 @@ struct TileRows {
   h8 w[2][2];                        // its weights
   float ref, l;                      // the reference (0 where no key was seen)
   unsigned sums_kept;                // sums of kLeastSum and so many more leave it; 0 where no key was seen
-  Span sees;
+  typename Seen<TREE>::type sees;
 
   // x = K Q': two chains of products side by side, each operand read from LDS a step before it is used
   __device__ __forceinline__ void products(const KeyTile<T, D> &b) {
@@ -962,7 +1022,7 @@ struct TileRows {
     }
     if (masked) {
       rarely();
-      const Span s{sees.from - base - h * 16, sees.count};
+      const auto s = sees.at(base + h * 16, true);
 #pragma unroll
       for (int g = 0; g < 2; ++g)
 #pragma unroll
@@ -1084,7 +1144,7 @@ struct TileWork {
   }
 };
 
-template <int D, int ROWS>
+template <int D, int ROWS, bool TREE>
 __device__ __forceinline__ TileWork tile_work(const AttArgs &a, long long *list_) {
   TileWork k{};
   const long long *list = a.plan ? a.plan + a.R + 1 : nullptr;
@@ -1110,9 +1170,9 @@ __device__ __forceinline__ TileWork tile_work(const AttArgs &a, long long *list_
   k.rq = request(a, k.r);
   k.rows = k.rq.n * a.G;
   k.row0 = (k.at - (int)same(list[k.r])) * ROWS;
-  const int before = k.rq.length - k.rq.n;
-  k.pos_lo = before + k.row0 / a.G;
-  k.pos_hi = before + (min(k.row0 + ROWS, k.rows) - 1) / a.G;
+  const Reach to = reach<TREE>(k.rq, k.row0 / a.G, (min(k.row0 + ROWS, k.rows) - 1) / a.G);
+  k.pos_lo = to.lo;
+  k.pos_hi = to.hi;
   if (k.splits > 1 && k.part == 0 && k.h == 0 && threadIdx.x == 0)
     a.joins[1 + k.at] = make_int4(k.rq.first, k.row0, k.rows, 0);
   const int u = a.window > 0 ? max(k.pos_lo - a.window + 1, 0) / kUnit : 0;
@@ -1123,22 +1183,23 @@ __device__ __forceinline__ TileWork tile_work(const AttArgs &a, long long *list_
 }
 
 // One wave's rows: where they stand, their queries, and where their results go.
-template <typename T, int D, int ROWS>
+template <typename T, int D, int ROWS, bool TREE>
 struct TileWave {
   int i, t, pos_min, pos_max;
   bool in, live;
 
-  __device__ __forceinline__ void begin(const AttArgs &a, const TileWork &k, TileRows<T, D> &st) {
-    const int lane = threadIdx.x & 63, wave0 = k.row0 + same((int)threadIdx.x >> 6) * 32, before = k.rq.length - k.rq.n;
+  __device__ __forceinline__ void begin(const AttArgs &a, const TileWork &k, TileRows<T, D, TREE> &st) {
+    const int lane = threadIdx.x & 63, wave0 = k.row0 + same((int)threadIdx.x >> 6) * 32;
     i = wave0 + (lane & 31);
     t = i / a.G;
     in = i < k.rows;
     live = wave0 < k.rows;
-    pos_min = before + wave0 / a.G;
-    pos_max = before + (min(wave0 + 32, k.rows) - 1) / a.G;
-    st.sees = span(a, in ? before + t : -1);
+    const Reach to = reach<TREE>(k.rq, wave0 / a.G, (min(wave0 + 32, k.rows) - 1) / a.G);
+    pos_min = to.lo;
+    pos_max = to.hi;
+    st.sees = sees_of<TREE>(a, k.rq, t, in);
     st.ref = st.l = 0.f;
-    st.sums_kept = st.sees.count > 0 ? 0u : ~0u;
+    st.sums_kept = st.sees.any() ? 0u : ~0u;
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
@@ -1159,7 +1220,7 @@ struct TileWave {
   __device__ __forceinline__ bool masked(const AttArgs &a, int base) const {
     return base + kUnit - 1 > pos_min || (a.window > 0 && base <= pos_max - a.window);
   }
-  __device__ __forceinline__ void end(const AttArgs &a, const TileWork &k, TileRows<T, D> &st) const {
+  __device__ __forceinline__ void end(const AttArgs &a, const TileWork &k, TileRows<T, D, TREE> &st) const {
     const int half = (threadIdx.x & 63) >> 5;
     st.l = across32(st.l, add_);
     const float m = st.sums_kept == kSums ? st.ref : kNegInf();
@@ -1196,16 +1257,16 @@ __device__ __forceinline__ void lds_barrier() {
 }
 
 // Each tile is staged while the one before is worked on.
-template <typename T, int D, int W>
+template <typename T, int D, int W, bool TREE>
 __global__ void __launch_bounds__(64 * W, D <= 64 && W == 4 ? 3 : D <= 128 ? 2 : 1) k_tiles(AttArgs a) {
   constexpr int ROWS = 32 * W;
   __shared__ KeyTile<T, D> keys[2];
   __shared__ ValueTile<D, W> values[2];
   __shared__ long long list_[kListed + 1];
-  const TileWork k = tile_work<D, ROWS>(a, list_);
+  const TileWork k = tile_work<D, ROWS, TREE>(a, list_);
   if (k.none) return;
-  TileRows<T, D> st;
-  TileWave<T, D, ROWS> wave;
+  TileRows<T, D, TREE> st;
+  TileWave<T, D, ROWS, TREE> wave;
   wave.begin(a, k, st);
   const int32_t *table = a.table + (size_t)k.r * a.MB;
   Stage<T, D, W> g;
@@ -1286,9 +1347,9 @@ struct Shape {
 size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Row tiles that k_rows keeps in registers, nothing spilled to memory.
-constexpr int row_tiles_most(int D) { return D <= 96 ? 4 : D <= 128 ? 2 : 1; }
+constexpr int row_tiles_most(int D, bool tree) { return tree && D > 64 ? 1 : D <= 96 ? 4 : D <= 128 ? 2 : 1; }
 
-festina_status shape_of(const festina_kv_cache *c, const festina_attention *t, Shape *s) {
+festina_status shape_of(const festina_kv_cache *c, const festina_attention *t, bool tree, Shape *s) {
   const festina_status bad = check_cache(c);
   if (bad != FESTINA_OK) return bad;
   if (!t || t->n_requests < 0 || t->max_blocks < 1 || t->n_tokens < 0 || t->n_heads < 1 || t->max_new < 1 || t->window < 0)
@@ -1300,7 +1361,7 @@ festina_status shape_of(const festina_kv_cache *c, const festina_attention *t, S
     return FESTINA_ERR_UNSUPPORTED;
   const int G = t->n_heads / c->n_kv_heads, H = c->n_kv_heads, D = c->head_dim;
   const long long most = (long long)t->max_new * G;                   // rows of one request and key head
-  const int nt_most = row_tiles_most(D);
+  const int nt_most = row_tiles_most(D, tree);
   *s = Shape{};
   s->tiles = most > 16 * nt_most && t->max_new > 1;
   const long long rows = s->tiles ? G : most;                         // with prompts about: the single tokens' rows
@@ -1347,38 +1408,44 @@ festina_status shape_of(const festina_kv_cache *c, const festina_attention *t, S
   return FESTINA_OK;
 }
 
-template <typename T, int D, int NT>
+template <typename T, int D, int NT, bool TREE>
 void run_rows(AttArgs a, const Shape &s, hipStream_t st) {
   a.workers = workers_of(D, NT);
   if (!s.cut) {
-    k_rows_whole<T, D, NT><<<(unsigned)(a.R * a.H * s.tiles_each), kBlock, 0, st>>>(a);
+    k_rows_whole<T, D, NT, TREE><<<(unsigned)(a.R * a.H * s.tiles_each), kBlock, 0, st>>>(a);
     return;
   }
-  k_rows<T, D, NT><<<a.workers, 64, 0, st>>>(a);
+  k_rows<T, D, NT, TREE><<<a.workers, 64, 0, st>>>(a);
   k_rows_join<T, D, NT><<<dim3(a.workers - 1, (s.join_rows + kWaves - 1) / kWaves), kBlock, 0, st>>>(a);
 }
 
-template <typename T, int D>
-void run(AttArgs a, const Shape &s, long long *plan, hipStream_t st) {
+template <typename T, int D, bool TREE>
+void run_kernels(AttArgs a, const Shape &s, long long *plan, hipStream_t st) {
   if (a.R > kListed) {
     if (s.nt == 1) k_plan<16><<<1, 1024, 0, st>>>(a, plan);
     else if (s.nt == 2) k_plan<32><<<1, 1024, 0, st>>>(a, plan);
     else k_plan<64><<<1, 1024, 0, st>>>(a, plan);
     a.plan = plan;
   }
-  if (s.nt == 1) run_rows<T, D, 1>(a, s, st);
-  if constexpr (row_tiles_most(D) >= 2)
-    if (s.nt == 2) run_rows<T, D, 2>(a, s, st);
-  if constexpr (row_tiles_most(D) >= 4)
-    if (s.nt == 4) run_rows<T, D, 4>(a, s, st);
+  if (s.nt == 1) run_rows<T, D, 1, TREE>(a, s, st);
+  if constexpr (row_tiles_most(D, TREE) >= 2)
+    if (s.nt == 2) run_rows<T, D, 2, TREE>(a, s, st);
+  if constexpr (row_tiles_most(D, TREE) >= 4)
+    if (s.nt == 4) run_rows<T, D, 4, TREE>(a, s, st);
   if (s.tiles) {
     const unsigned grid = (unsigned)s.tile_groups;
     if constexpr (D == 96 || D == 128)
-      if (s.tile_rows == 256) k_tiles<T, D, 8><<<grid, 512, 0, st>>>(a);
-    if (s.tile_rows == 128) k_tiles<T, D, 4><<<grid, kBlock, 0, st>>>(a);
+      if (s.tile_rows == 256) k_tiles<T, D, 8, TREE><<<grid, 512, 0, st>>>(a);
+    if (s.tile_rows == 128) k_tiles<T, D, 4, TREE><<<grid, kBlock, 0, st>>>(a);
     if (s.splits_most > 1)
       k_tiles_join<T, D><<<(unsigned)s.join_groups, kBlock, 0, st>>>(a);
   }
+}
+
+template <typename T, int D>
+void run(const AttArgs &a, const Shape &s, long long *plan, hipStream_t st) {
+  if (a.seen) run_kernels<T, D, true>(a, s, plan, st);
+  else run_kernels<T, D, false>(a, s, plan, st);
 }
 
 template <typename T>
@@ -1391,17 +1458,11 @@ void run_dim(const AttArgs &a, const Shape &s, int D, long long *plan, hipStream
   }
 }
 
-}  // namespace
-
-extern "C" size_t festina_attend_workspace_bytes(const festina_kv_cache *cache, const festina_attention *att) {
+// `seen` NULL: every request's new tokens are a run.
+festina_status attend(const festina_kv_cache *cache, const festina_attention *att, const uint64_t *seen, void *workspace,
+                      size_t workspace_bytes, void *stream) {
   Shape s;
-  return shape_of(cache, att, &s) == FESTINA_OK ? s.bytes : 0;
-}
-
-extern "C" festina_status festina_attend(const festina_kv_cache *cache, const festina_attention *att, void *workspace,
-                                         size_t workspace_bytes, void *stream) {
-  Shape s;
-  const festina_status bad = shape_of(cache, att, &s);
+  const festina_status bad = shape_of(cache, att, seen != nullptr, &s);
   if (bad != FESTINA_OK) return bad;
   if (att->n_requests == 0 || att->n_tokens == 0) return FESTINA_OK;
   if (!att->block_table || !att->length || !att->first || !att->q || !att->out) return FESTINA_ERR_INVALID;
@@ -1439,6 +1500,7 @@ extern "C" festina_status festina_attend(const festina_kv_cache *cache, const fe
   a.out_token = att->out_token_stride;
   a.out_head = att->out_head_stride;
   a.lse = att->lse;
+  a.seen = reinterpret_cast<const unsigned long long *>(seen);
   a.k = cache->k;
   a.v = cache->v;
   a.ks = cache->k_scale;
@@ -1452,4 +1514,28 @@ extern "C" festina_status festina_attend(const festina_kv_cache *cache, const fe
   if (att->dtype == FESTINA_BF16) run_dim<bf16>(a, s, cache->head_dim, plan, st);
   else run_dim<f16>(a, s, cache->head_dim, plan, st);
   return hipGetLastError() == hipSuccess ? FESTINA_OK : FESTINA_ERR_DEVICE;
+}
+
+}  // namespace
+
+extern "C" size_t festina_attend_workspace_bytes(const festina_kv_cache *cache, const festina_attention *att) {
+  Shape s;
+  return shape_of(cache, att, false, &s) == FESTINA_OK ? s.bytes : 0;
+}
+
+extern "C" festina_status festina_attend(const festina_kv_cache *cache, const festina_attention *att, void *workspace,
+                                         size_t workspace_bytes, void *stream) {
+  return attend(cache, att, nullptr, workspace, workspace_bytes, stream);
+}
+
+extern "C" size_t festina_attend_drafts_workspace_bytes(const festina_kv_cache *cache, const festina_attention *att) {
+  Shape s;
+  return shape_of(cache, att, true, &s) == FESTINA_OK ? s.bytes : 0;
+}
+
+extern "C" festina_status festina_attend_drafts(const festina_kv_cache *cache, const festina_attention *att,
+                                                const uint64_t *seen, void *workspace, size_t workspace_bytes,
+                                                void *stream) {
+  if (att && att->n_tokens > 0 && (!seen || (reinterpret_cast<uintptr_t>(seen) & 7))) return FESTINA_ERR_INVALID;
+  return attend(cache, att, seen, workspace, workspace_bytes, stream);
 }

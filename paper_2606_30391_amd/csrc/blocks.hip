@@ -1,5 +1,6 @@
 // blocks.hip -- MI355X (gfx950) kernels and C-ABI host dispatch of a serving step's cache blocks:
-// block tables and slot maps from request lengths, and the release of finished requests' blocks.
+// block tables and slot maps from request lengths, the release of finished requests' blocks and of those behind the
+// tokens that a request keeps.
 //
 // Request r holds held[r] tokens and adds add[r]; it needs
 //   need[r] = ceil((held + add) / BT) - ceil(held / BT)
@@ -17,7 +18,8 @@
 //   about it is uniform, and a lane makes its slots four at a time from one or two block ids, with all loads in
 //   flight together.  Where they do not, each lane searches the few requests of its stretch in LDS, in steps
 //   that all groups of the stretch take together, so that their loads wait once (4,096 requests: 14.7 -> 13.9 us).
-// k_release        a thread per returned id, after the same sums.
+// k_release        a thread per returned id, after the same sums; a request that keeps tokens returns the columns behind
+//   them, one that is done all.
 //
 // All arithmetic is on integers, so results do not depend on order.  Bound by the bytes of the slot map on
 // large steps (65,536 requests, 42.5 M slots: sums 5, scan 13, fill 57 us, 170 MB at 3.0 TB/s), by latency on small
@@ -53,6 +55,7 @@ struct BlockArgs {
   int32_t *first, *slot, *length, *n_free_out;
   uint8_t *served;
   const uint8_t *done;
+  const int32_t *keep;                  // a trim: the tokens that stay, in the place of done
   // workspace
   long long *sum_blocks, *sum_tokens;   // [chunks]
   int4 *ends;                           // served tokens, the last request with any, the blocks they take: of each chunk
@@ -439,17 +442,32 @@ __global__ void __launch_bounds__(256) k_extend_fill(BlockArgs a, int32_t chunks
 __device__ __forceinline__ int returned_of(const BlockArgs &a, int held, unsigned done) {
   return done && held >= 0 && held <= (a.MB << a.shift) ? blocks_of(held, a.shift) : 0;
 }
-__device__ __forceinline__ int returned(const BlockArgs &a, int r, int *held) {
+// Tokens that stay of `held`: all of them where `keep` is none of 0 .. held.
+__device__ __forceinline__ int stays_of(int held, int keep) { return keep >= 0 && keep <= held ? keep : held; }
+__device__ __forceinline__ int trimmed_of(const BlockArgs &a, int held, int keep) {
+  return held >= 0 && held <= (a.MB << a.shift) ? blocks_of(held, a.shift) - blocks_of(stays_of(held, keep), a.shift) : 0;
+}
+// Blocks that request r returns, the tokens that it holds, and those that stay.
+template <bool TRIM>
+__device__ __forceinline__ int returned(const BlockArgs &a, int r, int *held, int *stays) {
   *held = a.held[r];
-  return returned_of(a, *held, a.done[r]);
+  if (TRIM) {
+    const int keep = a.keep[r];
+    *stays = stays_of(*held, keep);
+    return trimmed_of(a, *held, keep);
+  }
+  const unsigned done = a.done[r];
+  *stays = done ? 0 : *held;
+  return returned_of(a, *held, done);
 }
 
+template <bool TRIM>
 __global__ void __launch_bounds__(kChunk) k_release_sums(BlockArgs a) {
   __shared__ long long lds[kChunk / 64];
   const int r = blockIdx.x * kChunk + threadIdx.x;
-  int held;
+  int held, stays;
   long long B;
-  scan<kChunk>(r < a.R ? returned(a, r, &held) : 0, lds, &B);
+  scan<kChunk>(r < a.R ? returned<TRIM>(a, r, &held, &stays) : 0, lds, &B);
   if (threadIdx.x == 0) {
     a.sum_blocks[blockIdx.x] = B;
     if (blockIdx.x == 0) *a.n_free_in = free_count(a);
@@ -459,16 +477,23 @@ __global__ void __launch_bounds__(kChunk) k_release_sums(BlockArgs a) {
 // kGive requests a workgroup.  DIRECT: sums the requests before its own itself, where what is written is not what
 // is read; otherwise whole chunks from k_release_sums, and only the requests of its own chunk, whose
 // lengths this launch overwrites, from their own thread.
-template <bool DIRECT>
+template <bool DIRECT, bool TRIM>
 __global__ void __launch_bounds__(kChunk) k_release(BlockArgs a) {
   constexpr int kOwn = DIRECT ? kGive : kChunk;
   __shared__ long long lds[kChunk / 64];
   __shared__ long long ends[kOwn];
+  __shared__ int from[TRIM ? kOwn : 1];                    // a request's first column that goes
   const int r0 = blockIdx.x * kOwn, r = r0 + threadIdx.x;
   const int n_free = DIRECT ? free_count(a) : *a.n_free_in;
   long long b = 0, B0, all;
-  int held = 0;
-  if (DIRECT && a.vec) {
+  int held = 0, stays = 0;
+  if (TRIM && DIRECT && a.vec) {
+#pragma unroll 8
+    for (int i = threadIdx.x * 4; i < r0; i += kChunk * 4) {
+      const int4 x = *reinterpret_cast<const int4 *>(a.held + i), y = *reinterpret_cast<const int4 *>(a.keep + i);
+      b += trimmed_of(a, x.x, y.x) + trimmed_of(a, x.y, y.y) + trimmed_of(a, x.z, y.z) + trimmed_of(a, x.w, y.w);
+    }
+  } else if (DIRECT && a.vec) {
 #pragma unroll 8
     for (int i = threadIdx.x * 4; i < r0; i += kChunk * 4) {
       const int4 x = *reinterpret_cast<const int4 *>(a.held + i);
@@ -477,14 +502,15 @@ __global__ void __launch_bounds__(kChunk) k_release(BlockArgs a) {
            returned_of(a, x.z, done & 0xff0000u) + returned_of(a, x.w, done & 0xff000000u);
     }
   } else if (DIRECT) {
-    for (int i = threadIdx.x; i < r0; i += kChunk) b += returned(a, i, &held);
+    for (int i = threadIdx.x; i < r0; i += kChunk) b += returned<TRIM>(a, i, &held, &stays);
   } else {
     for (int i = threadIdx.x; i < (int)blockIdx.x; i += kChunk) b += a.sum_blocks[i];
   }
   scan<kChunk>(b, lds, &B0);
   const bool mine = threadIdx.x < kOwn && r < a.R;
-  const long long own = scan<kChunk>(mine ? returned(a, r, &held) : 0, lds, &all);
+  const long long own = scan<kChunk>(mine ? returned<TRIM>(a, r, &held, &stays) : 0, lds, &all);
   if (threadIdx.x < kOwn) ends[threadIdx.x] = own;
+  if (TRIM && threadIdx.x < kOwn) from[threadIdx.x] = blocks_of(max(stays, 0), a.shift);
   __syncthreads();
   for (long long i0 = threadIdx.x; i0 < all; i0 += 4 * kChunk) {
     int id[4];
@@ -496,7 +522,7 @@ __global__ void __launch_bounds__(kChunk) k_release(BlockArgs a) {
         const int m = (lo + hi) >> 1;
         if (ends[m] <= i) lo = m; else hi = m;
       }
-      const int c = (int)(i - (hi ? ends[hi - 1] : 0));
+      const int c = (int)(i - (hi ? ends[hi - 1] : 0)) + (TRIM ? from[hi] : 0);
       if (i < all) id[k] = a.table[(size_t)(r0 + hi) * a.MB + c];
     }
 #pragma unroll
@@ -505,7 +531,7 @@ __global__ void __launch_bounds__(kChunk) k_release(BlockArgs a) {
       if (i < all && at < a.NB) a.free_ids[at] = id[k];
     }
   }
-  if (mine) a.length[r] = a.done[r] ? 0 : held;
+  if (mine) a.length[r] = stays;
   if (threadIdx.x == 0 && r0 + kOwn >= a.R) *a.n_free_out = (int)min(n_free + B0 + all, (long long)a.NB);
 }
 
@@ -609,6 +635,23 @@ extern "C" festina_status festina_extend_blocks(const festina_kv_requests *req, 
   return hipGetLastError() == hipSuccess ? FESTINA_OK : FESTINA_ERR_DEVICE;
 }
 
+namespace {
+
+template <bool TRIM>
+festina_status give_back(const BlockArgs &a, bool apart, hipStream_t st) {
+  // one workgroup reads everything before it writes anything; several may only where they write elsewhere
+  if (a.R <= kGive || (a.R <= kDirect * 2 && apart)) {
+    k_release<true, TRIM><<<max((a.R + kGive - 1) / kGive, 1), kChunk, 0, st>>>(a);
+  } else {
+    const int chunks = (a.R + kChunk - 1) / kChunk;
+    k_release_sums<TRIM><<<chunks, kChunk, 0, st>>>(a);
+    k_release<false, TRIM><<<chunks, kChunk, 0, st>>>(a);
+  }
+  return hipGetLastError() == hipSuccess ? FESTINA_OK : FESTINA_ERR_DEVICE;
+}
+
+}  // namespace
+
 extern "C" festina_status festina_release_blocks(const festina_kv_requests *req, const uint8_t *done,
                                                  festina_kv_step *out, void *workspace, size_t workspace_bytes,
                                                  void *stream) {
@@ -618,15 +661,17 @@ extern "C" festina_status festina_release_blocks(const festina_kv_requests *req,
   if (a.R > 0 && !done) return FESTINA_ERR_INVALID;
   a.done = done;
   a.vec = ((reinterpret_cast<uintptr_t>(a.held) & 15) | (reinterpret_cast<uintptr_t>(done) & 3)) == 0;
-  hipStream_t st = static_cast<hipStream_t>(stream);
-  // one workgroup reads everything before it writes anything; several may only where they write elsewhere
-  const bool apart = a.length != a.held && a.n_free_out != a.n_free;
-  if (a.R <= kGive || (a.R <= kDirect * 2 && apart)) {
-    k_release<true><<<max((a.R + kGive - 1) / kGive, 1), kChunk, 0, st>>>(a);
-  } else {
-    const int chunks = (a.R + kChunk - 1) / kChunk;
-    k_release_sums<<<chunks, kChunk, 0, st>>>(a);
-    k_release<false><<<chunks, kChunk, 0, st>>>(a);
-  }
-  return hipGetLastError() == hipSuccess ? FESTINA_OK : FESTINA_ERR_DEVICE;
+  return give_back<false>(a, a.length != a.held && a.n_free_out != a.n_free, static_cast<hipStream_t>(stream));
+}
+
+extern "C" festina_status festina_trim_blocks(const festina_kv_requests *req, const int32_t *keep, festina_kv_step *out,
+                                              void *workspace, size_t workspace_bytes, void *stream) {
+  BlockArgs a;
+  const festina_status bad = arguments(req, out, false, workspace, workspace_bytes, &a);
+  if (bad != FESTINA_OK) return bad;
+  if (a.R > 0 && !keep) return FESTINA_ERR_INVALID;
+  a.keep = keep;
+  a.vec = ((reinterpret_cast<uintptr_t>(a.held) | reinterpret_cast<uintptr_t>(keep)) & 15) == 0;
+  return give_back<true>(a, a.length != a.held && a.length != keep && a.n_free_out != a.n_free,
+                         static_cast<hipStream_t>(stream));
 }

@@ -3,7 +3,8 @@
 Argument marshalling only: every step of the search runs in the HIP library
 (``libfestina.so`` built from ``csrc/festina.hip``, ``csrc/fronts.hip``, ``csrc/sweep.hip``,
 ``csrc/preferred.hip``, ``csrc/dispatch.hip`` and ``csrc/transfer.hip``; the serving step's kernels
-from ``csrc/blocks.hip``, ``csrc/cache.hip`` and ``csrc/attend.hip``).  PyTorch provides device
+from ``csrc/blocks.hip``, ``csrc/cache.hip``, ``csrc/attend.hip``, ``csrc/drafts.hip`` and
+``csrc/rotate.hip``).  PyTorch provides device
 memory and streams.  There is no CPU fallback: if the library is missing this
 module raises.
 """
@@ -168,6 +169,34 @@ class festina_attention(C.Structure):
                 ("lse", C.c_void_p)]
 
 
+class festina_drafts(C.Structure):
+    _fields_ = [("n_requests", C.c_int32), ("n_tokens", C.c_int32), ("first", C.c_void_p), ("length", C.c_void_p),
+                ("parent", C.c_void_p)]
+
+
+class festina_accepted(C.Structure):
+    _fields_ = [("path", C.c_void_p), ("kept", C.c_void_p), ("next", C.c_void_p), ("length", C.c_void_p)]
+
+
+class festina_kept(C.Structure):
+    _fields_ = [("n_requests", C.c_int32), ("max_blocks", C.c_int32), ("n_tokens", C.c_int32),
+                ("block_table", C.c_void_p), ("length", C.c_void_p), ("first", C.c_void_p), ("path", C.c_void_p),
+                ("kept", C.c_void_p)]
+
+
+class festina_rotary(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("rotated", C.c_int32), ("interleaved", C.c_int32), ("eps", C.c_float),
+                ("turn", C.c_void_p), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p)]
+
+
+class festina_heads(C.Structure):
+    _fields_ = [("n_tokens", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("dtype", C.c_int32),
+                ("position", C.c_void_p), ("q", C.c_void_p), ("k", C.c_void_p), ("q_token_stride", C.c_int64),
+                ("q_head_stride", C.c_int64), ("k_token_stride", C.c_int64), ("k_head_stride", C.c_int64),
+                ("q_out", C.c_void_p), ("k_out", C.c_void_p), ("q_out_token_stride", C.c_int64),
+                ("q_out_head_stride", C.c_int64), ("k_out_token_stride", C.c_int64), ("k_out_head_stride", C.c_int64)]
+
+
 EXPORTED = ("festina_abi_version", "festina_status_string", "festina_placements_workspace_bytes",
             "festina_score_placements", "festina_score_placements_noalloc", "festina_migrations_workspace_bytes",
             "festina_score_migrations",
@@ -176,7 +205,9 @@ EXPORTED = ("festina_abi_version", "festina_status_string", "festina_placements_
             "festina_transfer_costs", "festina_request_moves", "festina_score_placements_timed",
             "festina_score_migrations_timed", "festina_dispatch_waves_workspace_bytes", "festina_dispatch_waves",
             "festina_blocks_workspace_bytes", "festina_extend_blocks", "festina_release_blocks", "festina_store_kv",
-            "festina_attend_workspace_bytes", "festina_attend")
+            "festina_attend_workspace_bytes", "festina_attend", "festina_trim_blocks", "festina_plan_drafts",
+            "festina_accept_drafts", "festina_attend_drafts_workspace_bytes", "festina_attend_drafts",
+            "festina_keep_tokens", "festina_rotate_heads")
 
 _lib = None
 
@@ -265,6 +296,21 @@ def lib():
         L.festina_attend_workspace_bytes.restype = C.c_size_t
         L.festina_attend.argtypes = [P(festina_kv_cache), P(festina_attention), C.c_void_p, C.c_size_t, C.c_void_p]
         L.festina_attend.restype = C.c_int
+        L.festina_trim_blocks.argtypes = L.festina_release_blocks.argtypes
+        L.festina_trim_blocks.restype = C.c_int
+        L.festina_plan_drafts.argtypes = [P(festina_drafts), C.c_void_p, C.c_void_p, C.c_void_p]
+        L.festina_plan_drafts.restype = C.c_int
+        L.festina_accept_drafts.argtypes = [P(festina_drafts), C.c_void_p, C.c_void_p, P(festina_accepted), C.c_void_p]
+        L.festina_accept_drafts.restype = C.c_int
+        L.festina_attend_drafts_workspace_bytes.argtypes = L.festina_attend_workspace_bytes.argtypes
+        L.festina_attend_drafts_workspace_bytes.restype = C.c_size_t
+        L.festina_attend_drafts.argtypes = [P(festina_kv_cache), P(festina_attention), C.c_void_p, C.c_void_p, C.c_size_t,
+                                            C.c_void_p]
+        L.festina_attend_drafts.restype = C.c_int
+        L.festina_keep_tokens.argtypes = [P(festina_kv_cache), C.c_int32, P(festina_kept), C.c_void_p]
+        L.festina_keep_tokens.restype = C.c_int
+        L.festina_rotate_heads.argtypes = [P(festina_rotary), P(festina_heads), C.c_void_p]
+        L.festina_rotate_heads.restype = C.c_int
         _lib = L
     return _lib
 
@@ -662,6 +708,17 @@ def _used_on(stream, *tensors):
             t.record_stream(stream)
 
 
+def _here(stream, *tensors):
+    """Refuse tensors of another device than the one that the call runs on: the current one, which a torch stream's has to be."""
+    import torch
+    now = torch.cuda.current_device()
+    at = now if stream is None or isinstance(stream, int) else stream.device_index
+    for t in tensors:
+        if t is not None and (t.device.index != now or at != now):
+            raise ValueError(f"tensors, stream and current device have to be one device (tensor on {t.device}, "
+                             f"stream on {at}, current {now})")
+
+
 class _Workspaces:
     """Device scratch, one for each stream that calls come on, so that they may overlap.  A call that is captured gets
     its own from the graph's memory: a graph keeps the address that it captured, while a stream's scratch is replaced
@@ -696,7 +753,8 @@ class DeviceBlocks:
 
     extend() gives every request blocks and slots for its add new tokens: table, and first [R+1],
     slot [max_tokens], length [R], served [R], n_free_out [1].  release(done) returns the blocks of the
-    requests whose uint8 done is not 0: free_ids, length, n_free_out.  advance() makes length and n_free_out
+    requests whose uint8 done is not 0: free_ids, length, n_free_out; trim(keep) those behind the tokens that each request
+    keeps.  advance() makes length and n_free_out
     the next step's held and n_free (no work on the device).
 
     A call with stream= (a torch stream, or a raw handle) comes after what is on that stream, and waits for no other.
@@ -741,6 +799,17 @@ class DeviceBlocks:
         if stream is not None:
             _used_on(stream, done, *self._tensors())
 
+    def trim(self, keep, stream=None):
+        """Give back the blocks behind the first keep[r] (int32, device) tokens of every request: free_ids, length (keep),
+        n_free_out."""
+        import torch
+        _check(keep, "keep", (torch.int32,), self.held.shape)
+        _here(stream, keep, self.held)
+        held, ws, handle = self._ws.get(self.ws_bytes, stream, self.table.device)
+        festina_trim_blocks(self.req, keep, self.out, ws, self.ws_bytes, handle)
+        if stream is not None:
+            _used_on(stream, keep, *self._tensors())
+
     def _tensors(self):
         return (self.held, self.add, self.table, self.free_ids, self.n_free, self.first, self.slot, self.length, self.served,
                 self.n_free_out)
@@ -774,6 +843,7 @@ class DeviceCache:
         self._types = {**self._halves, torch.float32: FESTINA_F32}
         self._int32, self._f32, self._rows, self._scale = (torch.int32,), torch.float32, (h, d), d ** -0.5
         self._empty, self._attend, self._cache_ref = torch.empty, lib().festina_attend, C.byref(self.cache)
+        self._attend_drafts, self._int64 = lib().festina_attend_drafts, (torch.int64,)
         self._graded = torch.is_grad_enabled
 
     @classmethod
@@ -802,11 +872,12 @@ class DeviceCache:
             _used_on(stream, k, v, slot, self.k, self.v, self.k_scale, self.v_scale)
 
     def attend(self, q, table, length, first, max_new: int, scale=None, window: int = 0, out=None, lse=None,
-               stream=None):
+               stream=None, seen=None):
         """Attention of the queries [tokens][heads][dim] (bfloat16 or half) over the cache: (out, lse).  table
         [requests][columns], length [requests] (new tokens included) and first [requests+1] are a step's
-        (DeviceBlocks); max_new bounds the new tokens of one request.  out and lse are made where not given.  For serving:
-        queries that ask for a gradient are refused."""
+        (DeviceBlocks); max_new bounds the new tokens of one request.  out and lse are made where not given.  seen
+        [tokens] (int64, DeviceDrafts.plan) says which of its request's new tokens each sees, where they are drafts.  For
+        serving: queries that ask for a gradient are refused."""
         # every check by itself: _check() where one fails names what is wrong (a decode step's kernels take about as
         # long as this function's host work, so it keeps to a few attribute reads a tensor)
         dim = self._rows[1]
@@ -841,7 +912,7 @@ class DeviceCache:
                 return self.attend(q, table, length, first, max_new, scale, window,
                                    self._empty((T, heads, dim), dtype=dtype, device=q.device) if out is None else out,
                                    self._empty((T, heads), dtype=self._f32, device=q.device) if lse is None else lse,
-                                   stream)
+                                   stream, seen)
         if out.dtype is not dtype or not out.is_cuda:
             _check(out, "out", (dtype,))
         if out.shape != q.shape or (out.stride(2) != 1 and out.numel()):
@@ -856,21 +927,176 @@ class DeviceCache:
         att = festina_attention(R, columns, T, heads, max_new, kind, window, self._scale if scale is None else scale,
                                 table.data_ptr(), length.data_ptr(), first.data_ptr(), q.data_ptr(), qt, qh,
                                 out.data_ptr(), ot, oh, lse.data_ptr())
-        sizes = (R, columns, T, heads, max_new)
+        if seen is not None:
+            _check(seen, "seen", self._int64, (T,))
+            _here(stream, q, seen)
+        sizes = (R, columns, T, heads, max_new) if seen is None else (R, columns, T, heads, max_new, 1)
         n = self._ws_bytes.get(sizes)
         if n is None:
             if len(self._ws_bytes) > 1024:
                 self._ws_bytes.clear()
-            n = festina_attend_workspace_bytes(self.cache, att)
+            n = (festina_attend_workspace_bytes if seen is None else festina_attend_drafts_workspace_bytes)(self.cache, att)
             if n:                                            # 0: refused below, for something that may not be a size
                 self._ws_bytes[sizes] = n
         held, ws, handle = self._ws.get(n, stream, q.device)
-        st = self._attend(self._cache_ref, C.byref(att), ws, n, handle)
+        if seen is None:
+            st = self._attend(self._cache_ref, C.byref(att), ws, n, handle)
+        else:
+            st = self._attend_drafts(self._cache_ref, C.byref(att), seen.data_ptr(), ws, n, handle)
         if st != FESTINA_OK:
-            raise FestinaError(st, "festina_attend")
+            raise FestinaError(st, "festina_attend" if seen is None else "festina_attend_drafts")
         if stream is not None:
-            _used_on(stream, q, table, length, first, out, lse, self.k, self.v, self.k_scale, self.v_scale)
+            _used_on(stream, q, table, length, first, out, lse, self.k, self.v, self.k_scale, self.v_scale,
+                     *(() if seen is None else (seen,)))
         return out, lse
+
+    def keep(self, table, length, first, path, kept, also=(), stream=None):
+        """Move the kept tokens of a step together, here and in the caches `also` (the other layers', of the same sizes): table,
+        length (new tokens included) and first are the step's, path [tokens] and kept [requests] (int32) as from
+        DeviceDrafts.accept."""
+        _check(table, "table", self._int32, table.shape)
+        if table.dim() != 2:
+            raise ValueError("table: a contiguous tensor of two dimensions is needed")
+        R, columns = table.shape
+        _check(length, "length", self._int32, (R,))
+        _check(first, "first", self._int32, (R + 1,))
+        _check(kept, "kept", self._int32, (R,))
+        _check(path, "path", self._int32, (path.numel(),))
+        caches = (self, *also)
+        if len({c.k.data_ptr() for c in caches}) != len(caches):
+            raise ValueError("also: each cache once (its tokens would be moved twice)")
+        _here(stream, table, length, first, path, kept, *(c.k for c in caches))
+        layers = (festina_kv_cache * len(caches))(*(c.cache for c in caches))
+        festina_keep_tokens(layers, len(caches), festina_kept(R, columns, path.numel(), _ptr(table), _ptr(length),
+                                                              _ptr(first), _ptr(path), _ptr(kept)), stream)
+        if stream is not None:
+            _used_on(stream, table, length, first, path, kept, *(x for c in caches for x in (c.k, c.v, c.k_scale, c.v_scale)))
+
+
+class DeviceDrafts:
+    """The draft trees of a step (festina_drafts): int32 device tensors parent [tokens] (an index among its request's new
+    tokens, -1 for node 0; None: each token's is the one before it) and, for accept(), token [tokens], used in place; tokens is
+    the most that a step may have.
+
+    plan() makes seen [tokens] (int64: bit j for node j; DeviceCache.attend) and position [tokens] (int32: DeviceRotary),
+    accept() path [tokens], kept [n_requests], next [n_requests] and length [n_requests].  stream= as for DeviceBlocks."""
+
+    def __init__(self, parent, token, n_requests: int, max_tokens=None, device=None):
+        import torch
+        given = [t for t in (parent, token) if t is not None]
+        if max_tokens is None or device is None:
+            if not given or not isinstance(given[0], torch.Tensor):
+                raise ValueError("parent, token: a tensor is needed, or max_tokens and device")
+            max_tokens = given[0].numel() if max_tokens is None else max_tokens
+            device = given[0].device if device is None else device
+        self.max_tokens, self.n_requests = int(max_tokens), int(n_requests)
+        if self.max_tokens < 0 or self.n_requests < 0:
+            raise ValueError("max_tokens and n_requests: not negative")
+        for name, t in (("parent", parent), ("token", token)):
+            if t is not None:
+                _check(t, name, (torch.int32,), (self.max_tokens,))
+        self.parent, self.token = parent, token
+        i32 = lambda n: torch.empty(n, dtype=torch.int32, device=device)
+        self.seen = torch.empty(self.max_tokens, dtype=torch.int64, device=device)
+        self.position, self.path = i32(self.max_tokens), i32(self.max_tokens)
+        self.kept, self.next, self.length = (i32(self.n_requests) for _ in range(3))
+        self.accepted = festina_accepted(_ptr(self.path), _ptr(self.kept), _ptr(self.next), _ptr(self.length))
+        self._int32 = (torch.int32,)
+
+    def _drafts(self, first, length, stream):
+        _check(first, "first", self._int32, (self.n_requests + 1,))
+        _check(length, "length", self._int32, (self.n_requests,))
+        _here(stream, first, length, self.seen)
+        return festina_drafts(self.n_requests, self.max_tokens, first.data_ptr(), length.data_ptr(),
+                              None if self.parent is None else self.parent.data_ptr())
+
+    def plan(self, first, length, stream=None):
+        """What the nodes see and where they stand; first and length are the step's (DeviceBlocks)."""
+        festina_plan_drafts(self._drafts(first, length, stream), self.seen, self.position, stream)
+        if stream is not None:
+            _used_on(stream, first, length, *self._tensors())
+
+    def accept(self, first, length, choice, stream=None):
+        """The nodes that the model's choice [max_tokens] (int32: the token chosen behind each) accepts."""
+        if self.token is None:
+            raise ValueError("token: the drafted tokens are needed")
+        _check(choice, "choice", self._int32, (self.max_tokens,))
+        festina_accept_drafts(self._drafts(first, length, stream), self.token, choice, self.accepted, stream)
+        if stream is not None:
+            _used_on(stream, first, length, choice, *self._tensors())
+
+    def _tensors(self):
+        return [t for t in (self.parent, self.token, self.seen, self.position, self.path, self.kept, self.next, self.length)
+                if t is not None]
+
+
+class DeviceRotary:
+    """Norm and rotation of queries and keys (festina_rotary): freq, radians per position of each rotated pair (host numbers,
+    at most head_dim / 2), weights of the heads' norms or None, and whether pairs are neighbours (interleaved) or half of the
+    rotated elements apart.  What a model's layers share of these is kept once and may be used by all."""
+
+    def __init__(self, freq, head_dim: int, q_weight=None, k_weight=None, eps: float = 1e-6, interleaved: bool = False,
+                 device="cuda"):
+        import torch
+        turn = np.array([_turn(float(f)) for f in np.asarray(freq, np.float64).reshape(-1)], np.uint64)
+        self.turn = torch.from_numpy(turn.view(np.int64)).to(device)
+        self.weights = []
+        for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+            if w is not None and tuple(w.shape) != (int(head_dim),):
+                raise ValueError(f"{name}: shape ({int(head_dim)},), not {tuple(w.shape)}")
+            self.weights.append(None if w is None else w.detach().to(device=device, dtype=torch.float32).contiguous().clone())
+        self.head_dim = int(head_dim)
+        self.rotary = festina_rotary(self.head_dim, 2 * len(turn), 1 if interleaved else 0, float(eps), _ptr(self.turn),
+                                     *(_ptr(w) for w in self.weights))
+        self._types = {torch.bfloat16: FESTINA_BF16, torch.float16: FESTINA_F16, torch.float32: FESTINA_F32}
+        self._int32, self._empty, self._graded = (torch.int32,), torch.empty, torch.is_grad_enabled
+        self._rotate, self._ref = lib().festina_rotate_heads, C.byref(self.rotary)
+
+    def apply(self, q, k, position, q_out=None, k_out=None, stream=None):
+        """(q_out, k_out): queries and keys [tokens][heads][head_dim] of one type (any strides but the last) at the int32
+        positions [tokens].  Outputs are made where not given, and may be q and k themselves.  For serving: inputs that ask
+        for a gradient are refused."""
+        T, D, device = q.shape[0], self.head_dim, q.device
+        if stream is not None and (q_out is None or k_out is None):
+            with _on(stream, device):
+                return self.apply(q, k, position, self._empty(q.shape, dtype=q.dtype, device=device) if q_out is None else q_out,
+                                  self._empty(k.shape, dtype=k.dtype, device=device) if k_out is None else k_out, stream)
+        if q_out is None:
+            q_out = self._empty(q.shape, dtype=q.dtype, device=device)
+        if k_out is None:
+            k_out = self._empty(k.shape, dtype=k.dtype, device=device)
+        for name, x, like in (("q", q, q), ("k", k, k), ("q_out", q_out, q), ("k_out", k_out, k)):
+            if not x.is_cuda or x.dtype not in self._types or x.dtype is not q.dtype:
+                _check(x, name, self._types if name == "q" else (q.dtype,))
+            if x.dim() != 3 or x.shape[0] != T or x.shape[2] != D or x.shape != like.shape or (x.stride(2) != 1 and x.numel()):
+                raise ValueError(f"{name}: [{T}][heads][{D}] with its last axis contiguous")
+            if x.requires_grad and self._graded():
+                raise ValueError(f"{name}: no gradient passes through (call under torch.no_grad())")
+        for name, x, y in (("q", q, q_out), ("k", k, k_out)):
+            if x.data_ptr() == y.data_ptr() and x.stride() != y.stride() and x.numel():
+                raise ValueError(f"{name}_out: {name}'s own memory with its strides, or other memory")
+            if x.numel() and any(s == 0 and n > 1 for s, n in zip(y.stride(), y.shape)):
+                raise ValueError(f"{name}_out: an element of its own for each of {name}")
+        _check(position, "position", self._int32, (T,))
+        _here(stream, q, k, q_out, k_out, position, self.turn)
+        (qt, qh, _), (kt, kh, _), (ot, oh, _), (pt, ph, _) = q.stride(), k.stride(), q_out.stride(), k_out.stride()
+        heads = festina_heads(T, q.shape[1], k.shape[1], self._types[q.dtype], position.data_ptr(), q.data_ptr(),
+                              k.data_ptr(), qt, qh, kt, kh, q_out.data_ptr(), k_out.data_ptr(), ot, oh, pt, ph)
+        st = self._rotate(self._ref, C.byref(heads), _stream_handle(stream))
+        if st != FESTINA_OK:
+            raise FestinaError(st, "festina_rotate_heads")
+        if stream is not None:
+            _used_on(stream, q, k, position, q_out, k_out, self.turn, *(w for w in self.weights if w is not None))
+        return q_out, k_out
+
+
+def _turn(radians: float) -> int:
+    """Radians as a part of a turn times 2^64, rounded to a whole number (the float taken as it is, pi to 60 digits)."""
+    from fractions import Fraction
+    if not np.isfinite(radians):
+        raise ValueError("freq: finite numbers")
+    turn = Fraction(radians) / (2 * Fraction(314159265358979323846264338327950288419716939937510582097494, 10 ** 59))
+    return round(turn * 2 ** 64) % 2 ** 64
 
 
 # ------------------------------------------------------------------ the ABI calls
@@ -1019,3 +1245,46 @@ def festina_attend(cache, att, workspace, workspace_bytes, stream=None) -> None:
                               _stream_handle(stream))
     if st != FESTINA_OK:
         raise FestinaError(st, "festina_attend")
+
+
+def festina_trim_blocks(req, keep, out, workspace, workspace_bytes, stream=None) -> None:
+    st = lib().festina_trim_blocks(C.byref(req), _ptr(keep), C.byref(out), workspace, int(workspace_bytes),
+                                   _stream_handle(stream))
+    if st != FESTINA_OK:
+        raise FestinaError(st, "festina_trim_blocks")
+
+
+def festina_plan_drafts(drafts, seen, position, stream=None) -> None:
+    st = lib().festina_plan_drafts(C.byref(drafts), _ptr(seen), _ptr(position), _stream_handle(stream))
+    if st != FESTINA_OK:
+        raise FestinaError(st, "festina_plan_drafts")
+
+
+def festina_accept_drafts(drafts, token, choice, out, stream=None) -> None:
+    st = lib().festina_accept_drafts(C.byref(drafts), _ptr(token), _ptr(choice), C.byref(out), _stream_handle(stream))
+    if st != FESTINA_OK:
+        raise FestinaError(st, "festina_accept_drafts")
+
+
+def festina_attend_drafts_workspace_bytes(cache, att) -> int:
+    return int(lib().festina_attend_drafts_workspace_bytes(C.byref(cache), C.byref(att)))
+
+
+def festina_attend_drafts(cache, att, seen, workspace, workspace_bytes, stream=None) -> None:
+    st = lib().festina_attend_drafts(C.byref(cache), C.byref(att), _ptr(seen), workspace, int(workspace_bytes),
+                                     _stream_handle(stream))
+    if st != FESTINA_OK:
+        raise FestinaError(st, "festina_attend_drafts")
+
+
+def festina_keep_tokens(caches, n_caches: int, kept, stream=None) -> None:
+    """caches: a ctypes array of festina_kv_cache."""
+    st = lib().festina_keep_tokens(caches, int(n_caches), C.byref(kept), _stream_handle(stream))
+    if st != FESTINA_OK:
+        raise FestinaError(st, "festina_keep_tokens")
+
+
+def festina_rotate_heads(rotary, heads, stream=None) -> None:
+    st = lib().festina_rotate_heads(C.byref(rotary), C.byref(heads), _stream_handle(stream))
+    if st != FESTINA_OK:
+        raise FestinaError(st, "festina_rotate_heads")

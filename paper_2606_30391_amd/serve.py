@@ -3,14 +3,18 @@
 ``Server`` holds the cache blocks of its requests and one cache a layer.  step() gives every request blocks and
 slots for its new tokens (festina_extend_blocks), then in each layer stores their keys and values through the slot
 map (festina_store_kv) and attends over the cache (festina_attend); finish() returns the blocks of finished requests
-(festina_release_blocks).  The block tables, slots and lengths stay on the device: a step has no wait for it.
+(festina_release_blocks).  verify() is a step whose new tokens are trees of drafted ones: each sees its own path
+(festina_plan_drafts, festina_attend_drafts), and what the model does not accept leaves the cache again
+(festina_accept_drafts, festina_keep_tokens, festina_trim_blocks).  Either normalises and rotates queries and keys when given a
+DeviceRotary (festina_rotate_heads).  The block tables, slots and lengths stay on the device: a step has no wait for it.
 
     python -m paper_2606_30391_amd.serve [--gpus 64] [--requests 1024] [--steps 64] [--layers 4] ...
 
 draws a dispatcher workload, lets festina_dispatch_requests place it, and serves the requests of the GPU that got
 most of them: their prompts in units of at most 2,048 tokens, then decode steps with a request leaving as its
-predicted output is made.  Queries, keys and values are random (no model is involved).  It prints what a step's
-cache and attention take, the part of a decode or prefill table's entry that grows with the tokens held.
+predicted output is made; with --draft N each decode step verifies a tree of N drafted tokens a request.  Queries, keys,
+values and choices are random (no model is involved).  It prints what a step's cache and attention take, the part of a decode or
+prefill table's entry that grows with the tokens held.
 """
 from __future__ import annotations
 
@@ -40,14 +44,43 @@ class Server:
         for _ in range(n_layers):                            # a step's layers follow one another: one scratch for all
             self.caches.append(festina.DeviceCache.empty(n_blocks, block_tokens, n_kv_heads, head_dim, device,
                                                          self.caches[0] if self.caches else None))
+        i32 = lambda: torch.zeros(max(step_tokens, 0), dtype=torch.int32, device=device)
+        self.runs = festina.DeviceDrafts(None, None, n_requests, step_tokens, self.blocks.table.device)
+        self.drafts, self.choice = festina.DeviceDrafts(i32(), i32(), n_requests), i32()
 
-    def step(self, add, qkv, window: int = 0):
+    def step(self, add, qkv, window: int = 0, rotary=None):
         """One step with add[r] new tokens of request r (host integers): each layer's attention, a list.
 
         qkv(layer) returns that layer's queries [tokens][heads][dim], keys and values [tokens][kv heads][dim] of the
         step's tokens, request after request; tokens is sum(add).  blocks.served says afterwards whose tokens were
         in the step: where blocks or step_tokens run out, those of the requests from there on are not, and their
-        rows of the output hold nothing."""
+        rows of the output hold nothing.  rotary (a DeviceRotary) is applied to the queries and keys at their positions."""
+        out = self._layers(self._begin(add), int(np.max(add, initial=1)), qkv, window, rotary)
+        self.blocks.advance()
+        return out
+
+    def verify(self, add, parent, token, qkv, choose, window: int = 0, rotary=None):
+        """One step of drafted tokens: add[r] nodes of request r's tree (host integers; 0: none), parent and token [tokens] theirs,
+        request after request (device int32; festina_drafts).  qkv as for step(); choose(outputs of the layers) returns the
+        tokens [tokens] (device int32) that the model chooses behind the nodes.  Returns the layers' outputs; drafts.next [requests]
+        is the token behind each request's accepted ones, drafts.kept their number, drafts.path which they were."""
+        b, d = self.blocks, self.drafts
+        tokens = self._begin(add)
+        d.parent[:tokens].copy_(parent)
+        d.token[:tokens].copy_(token)
+        d.plan(b.first, b.length)
+        out = self._layers(tokens, int(np.max(add, initial=1)), qkv, window, rotary, d)
+        self.choice[:tokens].copy_(choose(out))
+        d.accept(b.first, b.length, self.choice)
+        if self.caches:
+            self.caches[0].keep(b.table, b.length, b.first, d.path, d.kept, also=self.caches[1:])
+        b.advance()
+        b.trim(d.length)
+        b.advance()
+        return out
+
+    def _begin(self, add):
+        """Blocks and slots of a step; the number of its tokens."""
         import torch
         add = np.ascontiguousarray(add, np.int32)
         tokens, b = int(add.sum()), self.blocks
@@ -57,12 +90,20 @@ class Server:
         host.numpy()[:] = add
         b.add.copy_(host, non_blocking=True)
         b.extend()
-        out = []
+        return tokens
+
+    def _layers(self, tokens, longest, qkv, window, rotary, drafts=None):
+        b, out = self.blocks, []
+        seen = None if drafts is None else drafts.seen[:tokens]
+        if rotary is not None and drafts is None:
+            drafts = self.runs
+            drafts.plan(b.first, b.length)
         for layer, cache in enumerate(self.caches):
             q, k, v = qkv(layer)
+            if rotary is not None:
+                q, k = rotary.apply(q, k, drafts.position[:tokens])
             cache.store(k, v, b.slot[:tokens])
-            out.append(cache.attend(q, b.table, b.length, b.first, int(add.max(initial=1)), window=window)[0])
-        b.advance()
+            out.append(cache.attend(q, b.table, b.length, b.first, max(longest, 1), window=window, seen=seen)[0])
         return out
 
     def finish(self, done):
@@ -93,15 +134,17 @@ def main(argv=None):
                               ("--most", 32, "requests served at once"), ("--steps", 64, "decode steps"),
                               ("--layers", 4, "layers"), ("--heads", 32, "query heads"),
                               ("--kv-heads", 8, "key and value heads"), ("--dim", 128, "head dimension"),
-                              ("--block", 64, "tokens of a block")):
+                              ("--block", 64, "tokens of a block"), ("--draft", 0, "drafted tokens of a request and step, up to 64")):
         ap.add_argument(name, type=int, default=value, help=f"{what} ({value})")
     a = ap.parse_args(argv)
+    if not 0 <= a.draft <= 64:
+        ap.error("--draft: 0 to 64")
     g, prompt, output = busiest(a.requests, a.gpus, a.most)
     R = len(prompt)
-    total = prompt + np.minimum(output, a.steps)
+    total = prompt + np.minimum(output, a.steps) + 2 * a.draft
     n_blocks = int((-(-total // a.block)).sum())
     units = int(-(-prompt.max() // UNIT))
-    tokens = max(int(np.minimum(prompt, UNIT).sum()), R)
+    tokens = max(int(np.minimum(prompt, UNIT).sum()), R * max(a.draft, 1))
     srv = Server(R, int(total.max()), n_blocks, tokens, a.layers, a.kv_heads, a.dim, a.block)
     gen = torch.Generator("cuda").manual_seed(1)
     new = lambda h: torch.randn((tokens, h, a.dim), generator=gen, device="cuda").bfloat16()
@@ -128,15 +171,42 @@ def main(argv=None):
     print("prompts:", ", ".join(f"{b.elapsed_time(e):.2f}" for b, e in marks), "ms a step", flush=True)
 
     todo, marks = np.minimum(output, a.steps).astype(np.int64), []
+    chosen = torch.randint(0, 2, (tokens,), generator=gen, device="cuda", dtype=torch.int32)
+    drafted = torch.randint(0, 2, (tokens,), generator=gen, device="cuda", dtype=torch.int32)
+    parent = torch.from_numpy(np.tile(np.maximum(np.arange(max(a.draft, 1)) - 2, -1) + (np.arange(max(a.draft, 1)) == 1),
+                                      R).astype(np.int32)).cuda()        # two guesses a node, side by side
+    made = 0
+
+    def verified(add):
+        n = int(add.sum())
+        begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        begin.record()
+        srv.verify(add, parent[:n], drafted[:n], lambda layer: (q[:n], k[:n], v[:n]), lambda out: chosen[:n])
+        end.record()
+        return begin, end
+
+    if a.draft:
+        verified(np.zeros(R, np.int64))                      # untimed
     for _ in range(int(todo.max())):
-        marks.append(timed((todo > 0).astype(np.int64)))
-        todo -= todo > 0
+        if not (todo > 0).any():
+            break
+        alive = (todo > 0).astype(np.int64)
+        if a.draft:
+            marks.append(verified(alive * a.draft))
+            kept = np.minimum(srv.drafts.kept.cpu().numpy(), np.maximum(todo, 0))
+            made += int(kept.sum())
+            todo -= kept
+        else:
+            marks.append(timed(alive))
+            todo -= todo > 0
         over = todo == 0
         if over.any():
             srv.finish(torch.from_numpy(over).cuda())
             todo[over] = -1
     torch.cuda.synchronize()
     ms = np.array([b.elapsed_time(e) for b, e in marks])
+    if a.draft:
+        print(f"drafts: {made} tokens in {len(ms)} steps of up to {R} trees of {a.draft}")
     print(f"decode: {len(ms)} steps, median {1e3 * np.median(ms):.0f} us a step, {1e3 * np.median(ms) / a.layers:.0f} us a "
           f"layer; {int(srv.blocks.n_free.item())} of {n_blocks} blocks free at the end")
 
