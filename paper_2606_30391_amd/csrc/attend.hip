@@ -29,6 +29,9 @@
 //   joined by k_tiles_join.
 //   8,192 tokens, 32 heads over 8 of 128: 550 GFLOP in 558 us (985 TFLOP/s; a large library product 1,189), matrix cores
 //   41% of the cycles, VALU issue 39%.  9,012 tokens of 16 heads of 64: 170 us, 27% and 52%: half the products an exponential.
+// k_drafts  drafted tokens: a request's row tile (64 or 128 rows: all its nodes, in most cases) against tiles of 64 keys as in k_tiles,
+//   but all requests' tiles form one line that is cut into pieces of equal cost, as in k_rows, since lengths differ and
+//   a node's row sees every cached key.  Which nodes a row sees is a word of 64 bits, looked at only in the last tiles.
 // k_plan    running sums of the requests' units and tiles, for many requests.
 #include <hip/hip_runtime.h>
 
@@ -87,7 +90,6 @@ struct AttArgs {
   void *out;
   int64_t out_token, out_head;
   float *lse;
-  const unsigned long long *seen;    // drafts: [T] which of its request's new tokens a row sees, else NULL
   const uint8_t *k, *v;
   const float *ks, *vs;
   const long long *plan;             // [2][R + 1] running sums of units and of tiles, or NULL
@@ -95,6 +97,7 @@ struct AttArgs {
   struct Cut *cuts;                  // [workers]
   int4 *joins;                       // what k_tiles_join needs: (groups, splits), then for each row tile the request's
                                      // first token, the tile's first row, the request's rows
+  const unsigned long long *seen;    // k_drafts: [T] which of its request's new tokens a row sees
 };
 
 // What k_rows_join needs of the row tile that begins a join at a piece's start; n = 0: none.
@@ -275,15 +278,13 @@ __device__ __forceinline__ float add_(float x, float y) { return x + y; }
 struct Span {
   int from, count;
   __device__ __forceinline__ bool has(int key) const { return (unsigned)(key - from) < (unsigned)count; }
-  __device__ __forceinline__ bool any() const { return count > 0; }
-  // The same keys counted from `base` on; none unless `there`.
-  __device__ __forceinline__ Span at(int base, bool there) const { return Span{from - base, there ? count : 0}; }
+  // The same keys counted from `base` on.
+  __device__ __forceinline__ Span at(int base) const { return Span{from - base, count}; }
 };
 __device__ __forceinline__ Span span(const AttArgs &a, int pos) {
   const int from = a.window > 0 ? max(pos - a.window + 1, 0) : 0;
   return Span{from, max(pos - from + 1, 0)};
 }
-
 // Some of 64 keys.
 struct Bits {
   unsigned long long word;
@@ -295,49 +296,33 @@ struct TreeSpan {
   unsigned long long word;
   __device__ __forceinline__ bool any() const { return from < nodes || word != 0; }
   // Which of the 64 keys from `base` on.
-  __device__ __forceinline__ Bits at(int base, bool there) const {
+  __device__ __forceinline__ Bits at(int base) const {
     const int lo = min(max(from - base, 0), kNodes), s = nodes - base, hi = min(max(s, 0), kNodes);
     unsigned long long m = hi > lo ? ~0ull >> (kNodes - hi + lo) << lo : 0ull;
     m |= s <= -kNodes || s >= kNodes ? 0ull : s >= 0 ? word << s : word >> -s;
-    return Bits{there ? m : 0ull};
+    return Bits{m};
   }
-  __device__ __forceinline__ bool has(int key) const { return at(key, true).has(0); }
 };
-
+// One that lies in LDS: it is looked at in few tiles, and registers are short.
+struct TreeRow {
+  const TreeSpan *span;
+  __device__ __forceinline__ Bits at(int base) const { return span->at(base); }
+};
 template <bool TREE> struct Seen { typedef Span type; };
-template <> struct Seen<true> { typedef TreeSpan type; };
+template <> struct Seen<true> { typedef TreeRow type; };
 
-// What token t of the request's new ones sees (nothing unless `in`).
-template <bool TREE>
-__device__ __forceinline__ typename Seen<TREE>::type sees_of(const AttArgs &a, const Request &q, int t, bool in) {
+// What node t of a request sees (nothing unless `in`): the keys before the nodes, and nodes by its word.
+__device__ __forceinline__ TreeSpan tree_span(const AttArgs &a, const Request &q, int t, bool in) {
   const int before = q.length - q.n;
-  if constexpr (!TREE) {
-    return span(a, in ? before + t : -1);
-  } else {
-    if (q.n > kNodes) {
-      const Span s = span(a, in ? before + t : -1);
-      return TreeSpan{s.from, s.from + s.count, 0ull};
-    }
-    unsigned long long word = in ? a.seen[q.first + t] : 0ull;
-    word &= ~0ull >> (kNodes - q.n);                   // (a request with rows has at least one)
-    const int pos = before + max(__builtin_popcountll(word) - 1, 0);
-    const int from = a.window > 0 ? max(pos - a.window + 1, 0) : 0;
-    if (a.window > 0)                                  // the nearest of its path, the node itself included
-      for (int n = __builtin_popcountll(word); n > a.window; --n) word &= word - 1;
-    if (before < 0) word = before > -kNodes ? word >> -before << -before : 0ull;
-    return TreeSpan{from, in ? before : 0, word};
-  }
+  unsigned long long word = in ? a.seen[q.first + t] : 0ull;
+  word &= ~0ull >> (kNodes - q.n);                     // (a request with rows has at least one)
+  const int pos = before + max(__builtin_popcountll(word) - 1, 0), from = a.window > 0 ? max(pos - a.window + 1, 0) : 0;
+  if (a.window > 0)                                    // the nearest of its path, the node itself included
+    for (int n = __builtin_popcountll(word); n > a.window; --n) word &= word - 1;
+  if (before < 0) word = before > -kNodes ? word >> -before << -before : 0ull;
+  return TreeSpan{from, in ? before : 0, word};
 }
-// Bounds of the positions up to which the rows of tokens t0 .. t1 see their keys.
-struct Reach {
-  int lo, hi;
-};
-template <bool TREE>
-__device__ __forceinline__ Reach reach(const Request &q, int t0, int t1) {
-  const int before = q.length - q.n;
-  if (TREE && q.n <= kNodes) return Reach{before - 1, q.length - 1};
-  return Reach{before + t0, before + t1};
-}
+
 // Keeps a rare branch a branch: without it the compiler computes the masks of every step.
 __device__ __forceinline__ void rarely() { asm volatile(""); }
 
@@ -408,7 +393,7 @@ struct RowsStep {
   bool ok;
 };
 
-template <typename T, int D, int NT, bool TREE = false>
+template <typename T, int D, int NT>
 struct Rows {
   static constexpr int kRows = 16 * NT, kSteps = D / 32, kPitch = D + 4;
 
@@ -452,7 +437,7 @@ struct Rows {
     typename Vec8<T>::type q[NT][kSteps];
     f4 o[NT][D / 16];
     float m[NT], l[NT];
-    typename Seen<TREE>::type sees[NT];
+    Span sees[NT];
   };
 
   static __device__ __forceinline__ void step(const AttArgs &a, const Request &rq, int base, int pos_min, int pos_max,
@@ -485,7 +470,7 @@ struct Rows {
         for (int i = 0; i < 4; ++i) x[nt][u][i] = fmaf(x[nt][u][i], c, shift);
       if (masked) {
         rarely();
-        const auto sees = st.sees[nt].at(base + 16 * g, s.ok);
+        const Span sees{st.sees[nt].from - base - 16 * g, s.ok ? st.sees[nt].count : 0};
 #pragma unroll
         for (int u = 0; u < 4; ++u)
 #pragma unroll
@@ -545,9 +530,9 @@ struct Rows {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
               h8 sees;
-              const auto seen = st.sees[nt].at(base + 16 * g + 8 * i, s.ok);
 #pragma unroll
-              for (int j = 0; j < 8; ++j) sees[j] = seen.has(j) ? (f16)1.f : (f16)0.f;
+              for (int j = 0; j < 8; ++j)
+                sees[j] = s.ok && st.sees[nt].has(base + 16 * g + 8 * i + j) ? (f16)1.f : (f16)0.f;
               hits = mfma16(decode8<f16>(nan[2 * i] & kOnes, nan[2 * i + 1] & kOnes), sees, hits);
             }
 #pragma unroll
@@ -571,13 +556,13 @@ struct Rows {
   static __device__ __forceinline__ void scan_keys(const AttArgs &a, int r, const Request &rq, int h, int tile, int k0,
                                                    int k1, int stride, State &st) {
     const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-    const int rows = rq.n * a.G, row0 = tile * kRows;
-    const Reach to = reach<TREE>(rq, row0 / a.G, (min(row0 + kRows, rows) - 1) / a.G);
+    const int rows = rq.n * a.G, row0 = tile * kRows, before = rq.length - rq.n;
+    const int pos_min = before + row0 / a.G, pos_max = before + (min(row0 + kRows, rows) - 1) / a.G;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const int i = row0 + nt * 16 + c, t = i / a.G;
       const bool in = i < rows;
-      st.sees[nt] = sees_of<TREE>(a, rq, t, in);
+      st.sees[nt] = span(a, in ? before + t : -1);
       st.m[nt] = kNegInf();
       st.l[nt] = 0.f;
 #pragma unroll
@@ -601,7 +586,7 @@ struct Rows {
       RowsStep<D> s;
       load(a, ids, h, (u0 + u) * kUnit, s);
       ids = blocks(a, table, (u0 + u + stride) * kUnit);
-      step(a, rq, (u0 + u) * kUnit, to.lo, to.hi, s, st);
+      step(a, rq, (u0 + u) * kUnit, pos_min, pos_max, s, st);
     }
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) st.l[nt] = across32(across16(st.l[nt], add_), add_);
@@ -687,9 +672,9 @@ __device__ __forceinline__ int pieces(const AttArgs &a, long long all) {
 __device__ __forceinline__ long long piece_start(long long all, int w, int n) { return all * w / n; }
 
 // A workgroup for each row tile and key head, its waves over the keys in turn: few keys, one launch.
-template <typename T, int D, int NT, bool TREE>
+template <typename T, int D, int NT>
 __global__ void __launch_bounds__(kBlock, (D <= 128 && NT <= 2) ? 2 : 1) k_rows_whole(AttArgs a) {
-  typedef Rows<T, D, NT, TREE> K;
+  typedef Rows<T, D, NT> K;
   __shared__ typename K::Shared sh;
   const int tile = blockIdx.x % a.tiles_each, rest = blockIdx.x / a.tiles_each, h = rest % a.H, r = rest / a.H;
   const Request rq = request(a, r);
@@ -699,9 +684,9 @@ __global__ void __launch_bounds__(kBlock, (D <= 128 && NT <= 2) ? 2 : 1) k_rows_
 }
 
 // A wave a piece.
-template <typename T, int D, int NT, bool TREE>
+template <typename T, int D, int NT>
 __global__ void __launch_bounds__(64, waves_of(D, NT)) k_rows(AttArgs a) {
-  typedef Rows<T, D, NT, TREE> K;
+  typedef Rows<T, D, NT> K;
   __shared__ long long list_[kListed + 1];
   const long long *list = a.plan;
   if (!list) {
@@ -833,23 +818,23 @@ struct Stage {
   bool ok;
 
   // keys to the first threads, values to the last, so that all have some where there are fewer pieces than threads
-  static __device__ __forceinline__ int key_item(int i) { return threadIdx.x + i * kThreads; }
-  static __device__ __forceinline__ int value_item(int i) { return kThreads - 1 - threadIdx.x + i * kThreads; }
+  static __device__ __forceinline__ int key_item(int i, int thread = threadIdx.x) { return thread + i * kThreads; }
+  static __device__ __forceinline__ int value_item(int i, int thread = threadIdx.x) { return kThreads - 1 - thread + i * kThreads; }
   static __device__ __forceinline__ bool has(int item) { return kItems % kThreads == 0 || item < kItems; }
   static __device__ __forceinline__ int key_of(int item) { return item / (D / 16); }
   static __device__ __forceinline__ int key_of_value(int item) { return (item & 3) * 16; }
 
-  __device__ __forceinline__ void begin(const AttArgs &a, int h) {
+  __device__ __forceinline__ void begin(const AttArgs &a, int h, int thread) {
     const int bt = 1 << a.shift;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int x = key_item(i), y = has(value_item(i)) ? value_item(i) : 0;
+      const int x = key_item(i, thread), y = has(value_item(i, thread)) ? value_item(i, thread) : 0;
       k[i] = a.k + (size_t)h * bt * D + (key_of(x) & (bt - 1)) * D + x % (D / 16) * 16;
       v[i] = a.v + (size_t)h * bt * D + (size_t)(y >> 2) * bt + (key_of_value(y) & (bt - 1));
       at_k[i] = (min(key_of(x), kUnit - 1) >> a.shift) * 4;
       at_v[i] = (key_of_value(y) >> a.shift) * 4;
     }
-    at_s = ((threadIdx.x & 3) * 16 >> a.shift) * 4;
+    at_s = ((thread & 3) * 16 >> a.shift) * 4;
   }
 
   // A tile begins at a multiple of 64 keys, so a key's column is the tile's first one and its own part: offsets of less
@@ -969,45 +954,47 @@ struct Stage {
   }
 };
 
-// 32 query rows of a wave: columns of the products.
-template <typename T, int D, bool TREE>
+// 32 query rows of a wave: columns of the products.  It takes both halves of a tile's keys, or (NG = 1) half `half` alone.
+template <typename T, int D, bool TREE = false, int NG = 2>
 struct TileRows {
   typedef typename Vec8<T>::type Vec;
 
   Vec q[D / 16];
   f16v o[D / 32];
-  f16v x[2];                         // logits of a tile, 32 keys each
-  h8 w[2][2];                        // its weights
+  f16v x[NG];                        // logits of a tile, 32 keys each
+  h8 w[NG][2];                       // its weights
   float ref, l;                      // the reference (0 where no key was seen)
   unsigned sums_kept;                // sums of kLeastSum and so many more leave it; 0 where no key was seen
   typename Seen<TREE>::type sees;
+  int half;
+  __device__ __forceinline__ int group(int g) const { return NG == 2 ? g : half; }
 
   // x = K Q': two chains of products side by side, each operand read from LDS a step before it is used
   __device__ __forceinline__ void products(const KeyTile<T, D> &b) {
     const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5;
     // row c of a first product is key 16 (c / 4 % 2) + 4 (c / 8) + c % 4 of its 32
     const int key_row = ((c >> 2) & 1) * 16 + (c >> 3) * 4 + (c & 3);
-    const auto keys = [&](int g, int i) { return *reinterpret_cast<const Vec *>(&b.k[g * 32 + key_row][i * 16 + h * 8]); };
+    const auto keys = [&](int g, int i) { return *reinterpret_cast<const Vec *>(&b.k[group(g) * 32 + key_row][i * 16 + h * 8]); };
 #pragma unroll
-    for (int g = 0; g < 2; ++g)
+    for (int g = 0; g < NG; ++g)
 #pragma unroll
       for (int i = 0; i < 16; ++i) x[g][i] = 0.f;
-    Vec kf[2][2];
+    Vec kf[2][NG];
 #pragma unroll
-    for (int g = 0; g < 2; ++g) kf[0][g] = keys(g, 0);
+    for (int g = 0; g < NG; ++g) kf[0][g] = keys(g, 0);
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) {
       if (i + 1 < D / 16)
 #pragma unroll
-        for (int g = 0; g < 2; ++g) kf[(i + 1) & 1][g] = keys(g, i + 1);
+        for (int g = 0; g < NG; ++g) kf[(i + 1) & 1][g] = keys(g, i + 1);
 #pragma unroll
-      for (int g = 0; g < 2; ++g) x[g] = mfma32(kf[i & 1][g], q[i], x[g]);
+      for (int g = 0; g < NG; ++g) x[g] = mfma32(kf[i & 1][g], q[i], x[g]);
     }
-    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 2 * NG, 0);
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) {
-      __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
-      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, NG, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, NG, 0);
     }
   }
 
@@ -1015,16 +1002,16 @@ struct TileRows {
   __device__ __forceinline__ void logits(const KeyTile<T, D> &b, int base, bool masked) {
     const int h = (threadIdx.x & 63) >> 5;
 #pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      const float cc = b.c[g * 2 + h], shift = b.lv[g * 2 + h] - ref;
+    for (int g = 0; g < NG; ++g) {
+      const float cc = b.c[group(g) * 2 + h], shift = b.lv[group(g) * 2 + h] - ref;
 #pragma unroll
       for (int i = 0; i < 16; ++i) x[g][i] = fmaf(x[g][i], cc, shift);
     }
     if (masked) {
       rarely();
-      const auto s = sees.at(base + h * 16, true);
+      const auto s = sees.at(base + h * 16 + (NG == 2 ? 0 : half * 32));
 #pragma unroll
-      for (int g = 0; g < 2; ++g)
+      for (int g = 0; g < NG; ++g)
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[g][i] = s.has(g * 32 + i) ? x[g][i] : kNegInf();
     }
@@ -1062,12 +1049,12 @@ struct TileRows {
       sums_kept = up ? kSums : sums_kept;
       l *= f;
 #pragma unroll
-      for (int y = g; y < 2; ++y) x[y] -= top;
+      for (int y = g; y < NG; ++y) x[y] -= top;
 #pragma unroll
       for (int t = 0; t < D / 32; ++t) o[t] *= f;
       sum = powers<g>();
     }
-    l = fmaf(sum, b.iv[g * 2 + ((threadIdx.x & 63) >> 5)], l);
+    l = fmaf(sum, b.iv[group(g) * 2 + ((threadIdx.x & 63) >> 5)], l);
   }
 
   // A NaN among the values goes to the rows that see it; `look` as for Stage::clean_values
@@ -1081,8 +1068,13 @@ struct TileRows {
       for (int i = 0; i < W; ++i) nans |= b.nans[i];
       if (__any(nans)) {
         unsigned long long seen = 0;
+        if constexpr (TREE) {
+          seen = sees.at(base).word;
+        } else {
 #pragma unroll 1
-        for (int key = 0; key < kUnit; ++key) seen |= (unsigned long long)sees.has(base + key) << key;
+          for (int key = 0; key < kUnit; ++key) seen |= (unsigned long long)sees.has(base + key) << key;
+        }
+        if (NG == 1) seen &= 0xffffffffull << (half * 32);
 #pragma unroll
         for (int t = 0; t < D / 32; ++t)
 #pragma unroll
@@ -1105,7 +1097,7 @@ struct TileRows {
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
-      for (int t = 0; t < kT; ++t) vf[j][t] = values(2 * g + j, t);
+      for (int t = 0; t < kT; ++t) vf[j][t] = values(2 * group(g) + j, t);
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -1144,7 +1136,7 @@ struct TileWork {
   }
 };
 
-template <int D, int ROWS, bool TREE>
+template <int D, int ROWS>
 __device__ __forceinline__ TileWork tile_work(const AttArgs &a, long long *list_) {
   TileWork k{};
   const long long *list = a.plan ? a.plan + a.R + 1 : nullptr;
@@ -1170,9 +1162,9 @@ __device__ __forceinline__ TileWork tile_work(const AttArgs &a, long long *list_
   k.rq = request(a, k.r);
   k.rows = k.rq.n * a.G;
   k.row0 = (k.at - (int)same(list[k.r])) * ROWS;
-  const Reach to = reach<TREE>(k.rq, k.row0 / a.G, (min(k.row0 + ROWS, k.rows) - 1) / a.G);
-  k.pos_lo = to.lo;
-  k.pos_hi = to.hi;
+  const int before = k.rq.length - k.rq.n;
+  k.pos_lo = before + k.row0 / a.G;
+  k.pos_hi = before + (min(k.row0 + ROWS, k.rows) - 1) / a.G;
   if (k.splits > 1 && k.part == 0 && k.h == 0 && threadIdx.x == 0)
     a.joins[1 + k.at] = make_int4(k.rq.first, k.row0, k.rows, 0);
   const int u = a.window > 0 ? max(k.pos_lo - a.window + 1, 0) / kUnit : 0;
@@ -1183,23 +1175,22 @@ __device__ __forceinline__ TileWork tile_work(const AttArgs &a, long long *list_
 }
 
 // One wave's rows: where they stand, their queries, and where their results go.
-template <typename T, int D, int ROWS, bool TREE>
+template <typename T, int D, int ROWS>
 struct TileWave {
   int i, t, pos_min, pos_max;
   bool in, live;
 
-  __device__ __forceinline__ void begin(const AttArgs &a, const TileWork &k, TileRows<T, D, TREE> &st) {
-    const int lane = threadIdx.x & 63, wave0 = k.row0 + same((int)threadIdx.x >> 6) * 32;
+  __device__ __forceinline__ void begin(const AttArgs &a, const TileWork &k, TileRows<T, D> &st) {
+    const int lane = threadIdx.x & 63, wave0 = k.row0 + same((int)threadIdx.x >> 6) * 32, before = k.rq.length - k.rq.n;
     i = wave0 + (lane & 31);
     t = i / a.G;
     in = i < k.rows;
     live = wave0 < k.rows;
-    const Reach to = reach<TREE>(k.rq, wave0 / a.G, (min(wave0 + 32, k.rows) - 1) / a.G);
-    pos_min = to.lo;
-    pos_max = to.hi;
-    st.sees = sees_of<TREE>(a, k.rq, t, in);
+    pos_min = before + wave0 / a.G;
+    pos_max = before + (min(wave0 + 32, k.rows) - 1) / a.G;
+    st.sees = span(a, in ? before + t : -1);
     st.ref = st.l = 0.f;
-    st.sums_kept = st.sees.any() ? 0u : ~0u;
+    st.sums_kept = st.sees.count > 0 ? 0u : ~0u;
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
@@ -1220,7 +1211,7 @@ struct TileWave {
   __device__ __forceinline__ bool masked(const AttArgs &a, int base) const {
     return base + kUnit - 1 > pos_min || (a.window > 0 && base <= pos_max - a.window);
   }
-  __device__ __forceinline__ void end(const AttArgs &a, const TileWork &k, TileRows<T, D, TREE> &st) const {
+  __device__ __forceinline__ void end(const AttArgs &a, const TileWork &k, TileRows<T, D> &st) const {
     const int half = (threadIdx.x & 63) >> 5;
     st.l = across32(st.l, add_);
     const float m = st.sums_kept == kSums ? st.ref : kNegInf();
@@ -1257,16 +1248,16 @@ __device__ __forceinline__ void lds_barrier() {
 }
 
 // Each tile is staged while the one before is worked on.
-template <typename T, int D, int W, bool TREE>
+template <typename T, int D, int W>
 __global__ void __launch_bounds__(64 * W, D <= 64 && W == 4 ? 3 : D <= 128 ? 2 : 1) k_tiles(AttArgs a) {
   constexpr int ROWS = 32 * W;
   __shared__ KeyTile<T, D> keys[2];
   __shared__ ValueTile<D, W> values[2];
   __shared__ long long list_[kListed + 1];
-  const TileWork k = tile_work<D, ROWS, TREE>(a, list_);
+  const TileWork k = tile_work<D, ROWS>(a, list_);
   if (k.none) return;
-  TileRows<T, D, TREE> st;
-  TileWave<T, D, ROWS, TREE> wave;
+  TileRows<T, D> st;
+  TileWave<T, D, ROWS> wave;
   wave.begin(a, k, st);
   const int32_t *table = a.table + (size_t)k.r * a.MB;
   Stage<T, D, W> g;
@@ -1285,7 +1276,7 @@ __global__ void __launch_bounds__(64 * W, D <= 64 && W == 4 ? 3 : D <= 128 ? 2 :
     g.put_values(values[u & 1]);
   };
   if (k.begin < k.end) {
-    g.begin(a, k.h);
+    g.begin(a, k.h, threadIdx.x);
     blocks(k.begin);
     load(k.begin);
     blocks(k.begin + 1);
@@ -1329,6 +1320,266 @@ __global__ void __launch_bounds__(kBlock) k_tiles_join(AttArgs a) {
   }
 }
 
+// ------------------------------------------------------------------ k_drafts
+
+// What a row tile costs beside its units of keys, in units: the queries, the words and the first tile's way from memory.
+constexpr int kTileCost = 3;
+// Workgroups of a compute unit, and of the chip at once.
+constexpr int groups_each(int D, int KS) { return D <= 64 && KS == 2 ? 3 : D <= 128 ? 2 : 1; }
+constexpr int groups_of(int D, int KS) { return 256 * groups_each(D, KS); }
+// Halves that a tile's keys are dealt to waves in: 64 rows leave two waves for each 32 of them.
+constexpr int rows_of(int KS) { return 128 / KS; }
+
+template <int ROWS>
+__device__ __forceinline__ long long costs_of(const AttArgs &a, int r) {
+  const Request q = request(a, r);
+  return q.n > 0 && q.n <= kNodes ? (long long)(units(a, q) + kTileCost) * cdiv(q.n * a.G, ROWS) * a.H : 0;
+}
+
+template <int ROWS>
+__global__ void __launch_bounds__(1024) k_drafts_plan(AttArgs a, long long *plan) {
+  __shared__ long long lds[16];
+  long long u0 = 0, whole;
+  for (int r0 = 0; r0 < a.R; r0 += 1024) {
+    const int r = r0 + threadIdx.x;
+    const long long u = scan<1024>(r < a.R ? costs_of<ROWS>(a, r) : 0, lds, &whole) + u0;
+    u0 += whole;
+    if (r < a.R) plan[r] = u;
+  }
+  if (threadIdx.x == 0) plan[a.R] = u0;
+}
+
+__device__ __forceinline__ int draft_pieces(const AttArgs &a, long long all) {
+  return (int)min((long long)a.workers, max(all / (kTileCost + 2), 1ll));
+}
+
+// One wave's 32 rows (and half of the keys, where KS = 2) of a row tile.
+template <typename T, int D, int KS>
+struct DraftTile {
+  static constexpr int kRows = rows_of(KS);
+  typedef TileRows<T, D, true, 2 / KS> State;
+
+  struct Work {
+    Request rq;
+    int h, row0, rows;               // key head; first row of the tile; rows of the request
+    int u0, u1;                      // units of keys
+    int part;                        // where the result goes, < 0: it is the rows' own
+  };
+
+  static __device__ __forceinline__ int wave(int thread) { return same(thread >> 6); }
+  static __device__ __forceinline__ int side(int thread) { return wave(thread) / KS; }          // which 32 rows
+  static __device__ __forceinline__ int row(const Work &k, int thread) { return k.row0 + side(thread) * 32 + (thread & 31); }
+
+  static __device__ __forceinline__ void begin(const AttArgs &a, const Work &k, int thread, TreeSpan *spans, State &st) {
+    const int lane = thread & 63, i = row(k, thread), t = i / a.G;
+    const bool in = i < k.rows;
+    st.half = wave(thread) % KS;
+    const TreeSpan sees = tree_span(a, k.rq, t, in);
+    TreeSpan *own = spans + side(thread) * 32 + (lane & 31);
+    st.sees.span = own;
+    if (lane < 32) *own = sees;                        // (the waves of two halves write the same)
+    st.ref = st.l = 0.f;
+    st.sums_kept = sees.any() ? 0u : ~0u;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int y = 0; y < 16; ++y) st.o[d][y] = 0.f;
+    const T *q = static_cast<const T *>(a.q) + (int64_t)(k.rq.first + (in ? t : 0)) * a.q_token +
+                 (int64_t)(k.h * a.G + (in ? i - t * a.G : 0)) * a.q_head;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+      u4 raw = *reinterpret_cast<const u4 *>(q + s * 16 + (lane >> 5) * 8);
+      if (!in) raw = u4{0u, 0u, 0u, 0u};
+      st.q[s] = __builtin_bit_cast(typename Vec8<T>::type, raw);
+    }
+  }
+
+  // The result of the wave's rows, all keys of the piece in it.
+  static __device__ __forceinline__ void end(const AttArgs &a, const Work &k, int thread, const State &st, float m, float l) {
+    const int half = (thread & 63) >> 5, i = row(k, thread), t = i / a.G;
+    if (i >= k.rows) return;
+    if (k.part >= 0) {
+      const size_t p = (size_t)k.part * kRows + i - k.row0;
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+          *reinterpret_cast<f4 *>(a.part_o + p * D + d * 32 + y * 8 + half * 4) =
+              f4{st.o[d][y * 4], st.o[d][y * 4 + 1], st.o[d][y * 4 + 2], st.o[d][y * 4 + 3]};
+      if (half == 0) {
+        a.part_ml[p * 2] = m;
+        a.part_ml[p * 2 + 1] = l;
+      }
+      return;
+    }
+    const int head = k.h * a.G + i - t * a.G;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int y = 0; y < 4; ++y)
+        Rows<T, D, 1>::finish(a, k.rq.first + t, head, d * 32 + y * 8 + half * 4, m, l,
+                              f4{st.o[d][y * 4], st.o[d][y * 4 + 1], st.o[d][y * 4 + 2], st.o[d][y * 4 + 3]});
+  }
+};
+
+// The second half's results of two waves' rows, which the first half's waves take: a lane's own values, register by register.
+template <int D>
+struct Halves {
+  float o[2][D / 2][64], m[2][64], l[2][64];
+};
+
+template <typename T, int D, int KS>
+__global__ void __launch_bounds__(kBlock, groups_each(D, KS)) k_drafts(AttArgs a) {
+  typedef DraftTile<T, D, KS> K;
+  constexpr int kRows = K::kRows;
+  __shared__ KeyTile<T, D> keys[2];
+  __shared__ union { ValueTile<D, kWaves> tile[2]; Halves<D> halves; } values;
+  __shared__ TreeSpan spans[kRows];
+  // 0.  What is read through it is read anew for each row tile: kept in registers, the arguments and indexes that only a tile's
+  // begin and end need push out what the keys are worked on with (18 registers of 128 dims)
+  __shared__ int nought;
+  if (threadIdx.x == 0) nought = 0;
+  lds_barrier();
+  __shared__ long long list_[kListed + 1];
+  const long long *list = a.plan;
+  if (!list) {
+    list_sums(a, [&](int r) { return costs_of<kRows>(a, r); }, list_);
+    list = list_;
+  }
+  const long long all = same(list[a.R]);
+  const int n = draft_pieces(a, all), w = blockIdx.x;
+  Cut cut{};
+  if (w < n) {
+    long long u = piece_start(all, w, n);
+    const long long start = u, end = piece_start(all, w + 1, n);
+    for (int place = 2 * w; u < end; ++place) {
+      const AttArgs &b = (&a)[same(nought)];
+      const int r = find(list, b.R, u);
+      const Request rq = request(b, r);
+      const long long begin = same(list[r]);
+      const int each = units(b, rq), cost = each + kTileCost, at = (int)((u - begin) / cost), tiles = cdiv(rq.n * b.G, kRows);
+      const long long tile0 = begin + (long long)at * cost;
+      const int off = (int)(u - tile0), stop = (int)min((long long)cost, off + (end - u));
+      const int k0 = max(off - kTileCost, 0), k1 = max(stop - kTileCost, 0);
+      typename K::Work k;
+      k.rq = rq;
+      k.h = at / tiles;
+      k.row0 = at % tiles * kRows;
+      k.rows = rq.n * b.G;
+      const int first = first_unit(b, rq);
+      k.u0 = first + k0;
+      k.u1 = first + k1;
+      k.part = k0 == 0 && k1 == each ? -1 : min(place, 2 * w + 1);
+      if (u == start && k0 > 0) {
+        // this piece's start cuts the tile: the first such cut is where the tile's pieces are joined
+        const long long prior = piece_start(all, w - 1, n);
+        if (prior <= tile0 + kTileCost) {
+          const int last = (int)(((tile0 + cost) * n - 1) / all);      // piece of the tile's last unit
+          cut = Cut{last - w + 2, prior < tile0 ? 1 : 0, k.row0, k.rows, rq.first, k.h * b.G, {0, 0}};
+        }
+      }
+      u += stop - off;
+      if (k0 >= k1) continue;                          // only what a tile costs beside its keys: the next piece has it
+
+      const int thread = threadIdx.x + nought;
+      typename K::State st;
+      K::begin(b, k, thread, spans, st);
+      const int before = rq.length - rq.n, live = k.row0 + K::side(thread) * 32 < k.rows;
+      // some row does not see all of the unit
+      const auto look = [&](int unit) {
+        return unit * kUnit + kUnit > before || (a.window > 0 && unit * kUnit < rq.length - a.window);
+      };
+      const int32_t *table = b.table + (size_t)r * b.MB;
+      Stage<T, D, kWaves> g;
+      const auto blocks = [&](int u) { g.blocks(a, table, u * kUnit); };
+      const auto load = [&](int u) {
+        g.load_keys(a, k.h, u * kUnit);
+        g.load_values(a, u * kUnit);
+      };
+      const auto store = [&](int u) {
+        g.put_keys(keys[u & 1]);
+        g.put_scales(a, keys[u & 1]);
+        if (look(u)) {
+          rarely();
+          g.clean_values(rq.length - u * kUnit, values.tile[u & 1]);
+        }
+        g.put_values(values.tile[u & 1]);
+      };
+      g.begin(b, k.h, thread);
+      blocks(k.u0);
+      load(k.u0);
+      blocks(k.u0 + 1);
+      store(k.u0);
+      lds_barrier();
+      for (int u = k.u0; u < k.u1; ++u) {
+        const int base = u * kUnit;
+        if (u + 1 < k.u1) {
+          load(u + 1);
+          blocks(u + 2);
+        }
+        if (live) {
+          st.products(keys[u & 1]);
+          st.logits(keys[u & 1], base, look(u));
+          st.nans(values.tile[u & 1], base, look(u));
+          st.template weights<0>(keys[u & 1]);
+          st.template sums<0>(values.tile[u & 1]);
+          if constexpr (KS == 1) {
+            st.template weights<1>(keys[u & 1]);
+            st.template sums<1>(values.tile[u & 1]);
+          }
+        }
+        if (u + 1 < k.u1) store(u + 1);
+        lds_barrier();
+      }
+      float l = across32(st.l, add_), m = st.sums_kept == kSums ? st.ref : kNegInf();
+      const AttArgs &e = (&a)[same(nought)];
+      const int last = threadIdx.x + nought;
+      if constexpr (KS == 2) {
+        const int lane = last & 63, side = K::side(last);
+        Halves<D> &other = values.halves;
+        if (live && st.half == 1) {
+#pragma unroll
+          for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+            for (int y = 0; y < 16; ++y) other.o[side][d * 16 + y][lane] = st.o[d][y];
+          other.m[side][lane] = m;
+          other.l[side][lane] = l;
+        }
+        lds_barrier();
+        if (live && st.half == 0) {
+          const float m1 = other.m[side][lane], M = fmaxf(m, m1), f0 = weight(m, M), f1 = weight(m1, M);
+          l = fmaf(other.l[side][lane], f1, l * f0);
+          m = M;
+#pragma unroll
+          for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+            for (int y = 0; y < 16; ++y) st.o[d][y] = fmaf(other.o[side][d * 16 + y][lane], f1, st.o[d][y] * f0);
+          K::end(e, k, last, st, m, l);
+        }
+        lds_barrier();                                 // the values' place is free again
+      } else {
+        if (live) K::end(e, k, last, st, m, l);
+      }
+    }
+  }
+  if (threadIdx.x == 0) a.cuts[w] = cut;
+}
+
+// A wave a row of the tile that the cut at piece blockIdx.x + 1 leaves, in turn.
+template <typename T, int D, int KS>
+__global__ void __launch_bounds__(kBlock) k_drafts_join(AttArgs a) {
+  constexpr int kRows = rows_of(KS);
+  const int w = blockIdx.x + 1;
+  const Cut cut = a.cuts[w];
+  if (cut.n == 0) return;
+  for (int row = blockIdx.y * kWaves + (threadIdx.x >> 6); row < kRows; row += gridDim.y * kWaves) {
+    const int i = cut.row0 + row, t = i / a.G;
+    if (i >= cut.rows) return;
+    join_row<T, D>(a, (size_t)(2 * (w - 1) + cut.second) * kRows + row, (size_t)(2 * w) * kRows + row, 2 * kRows, cut.n,
+                   cut.first + t, cut.head + i - t * a.G);
+  }
+}
+
 // ------------------------------------------------------------------ host
 
 struct Shape {
@@ -1341,15 +1592,16 @@ struct Shape {
   int splits_most;                   // and of the parts of one's keys
   long long tile_groups, join_groups;   // workgroups of k_tiles, of k_tiles_join
   int join_rows;                     // rows of a row tile that are mostly in use: the join's waves
+  int halves;                        // drafts: k_drafts' KS, else 0
   size_t plan, cuts, joins, part_ml, part_o, bytes;
 };
 
 size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Row tiles that k_rows keeps in registers, nothing spilled to memory.
-constexpr int row_tiles_most(int D, bool tree) { return tree && D > 64 ? 1 : D <= 96 ? 4 : D <= 128 ? 2 : 1; }
+constexpr int row_tiles_most(int D) { return D <= 96 ? 4 : D <= 128 ? 2 : 1; }
 
-festina_status shape_of(const festina_kv_cache *c, const festina_attention *t, bool tree, Shape *s) {
+festina_status shape_of(const festina_kv_cache *c, const festina_attention *t, bool drafts, Shape *s) {
   const festina_status bad = check_cache(c);
   if (bad != FESTINA_OK) return bad;
   if (!t || t->n_requests < 0 || t->max_blocks < 1 || t->n_tokens < 0 || t->n_heads < 1 || t->max_new < 1 || t->window < 0)
@@ -1361,14 +1613,20 @@ festina_status shape_of(const festina_kv_cache *c, const festina_attention *t, b
     return FESTINA_ERR_UNSUPPORTED;
   const int G = t->n_heads / c->n_kv_heads, H = c->n_kv_heads, D = c->head_dim;
   const long long most = (long long)t->max_new * G;                   // rows of one request and key head
-  const int nt_most = row_tiles_most(D, tree);
+  const int nt_most = row_tiles_most(D);
   *s = Shape{};
-  s->tiles = most > 16 * nt_most && t->max_new > 1;
+  s->tiles = drafts ? t->max_new > kNodes : most > 16 * nt_most && t->max_new > 1;
   const long long rows = s->tiles ? G : most;                         // with prompts about: the single tokens' rows
   s->nt = rows <= 16 ? 1 : min(rows <= 32 ? 2 : 4, nt_most);
   s->join_rows = (int)min(rows, 16ll * s->nt);
   if (s->tiles && G > 16 * nt_most) s->nt = 0;
   s->rows_max = s->tiles ? 16 * s->nt : INT_MAX;
+  if (drafts) {                                        // k_drafts has the trees, k_tiles the runs
+    s->halves = D > 128 || min(most, (long long)kNodes * G) <= rows_of(2) ? 2 : 1;      // (128 rows of 256 dims do not fit the registers)
+    s->join_rows = (int)min(most, (long long)rows_of(s->halves));
+    s->nt = 0;
+    s->rows_max = kNodes * G;
+  }
   const long long keys = (long long)t->max_blocks * c->block_tokens;
   s->tiles_each = (int)((rows + 16 * s->nt - 1) / max(16 * s->nt, 1));
   s->cut = keys > 2 * kWaves * kUnit;
@@ -1376,6 +1634,10 @@ festina_status shape_of(const festina_kv_cache *c, const festina_attention *t, b
     return FESTINA_ERR_UNSUPPORTED;
   size_t parts = 0;
   if (s->nt && s->cut) parts = (size_t)2 * workers_of(D, s->nt) * 16 * s->nt;
+  if (drafts) {
+    parts = (size_t)2 * groups_of(D, s->halves) * rows_of(s->halves);
+    if ((long long)kNodes * G * H > INT_MAX / kNodes) return FESTINA_ERR_UNSUPPORTED;
+  }
   if (s->tiles) {
     // 256 rows a workgroup stage each tile half as often for a row, where registers allow and enough workgroups are
     // left: a prompt of 8,192 tokens (32 heads over 8 of 128 dims) 641 us against 662 with 128; 9,012 tokens of 16
@@ -1401,51 +1663,60 @@ festina_status shape_of(const festina_kv_cache *c, const festina_attention *t, b
   }
   s->plan = 0;
   s->cuts = up((size_t)2 * (t->n_requests + 1) * 8);
-  s->joins = s->cuts + up((size_t)workers_of(D, max(s->nt, 1)) * sizeof(Cut));
+  s->joins = s->cuts + up((size_t)(drafts ? groups_of(D, s->halves) : workers_of(D, max(s->nt, 1))) * sizeof(Cut));
   s->part_ml = s->joins + up((kGroups + 1) * sizeof(int4));
   s->part_o = s->part_ml + up(parts * 8);
   s->bytes = s->part_o + up(parts * D * 4);
   return FESTINA_OK;
 }
 
-template <typename T, int D, int NT, bool TREE>
+template <typename T, int D, int NT>
 void run_rows(AttArgs a, const Shape &s, hipStream_t st) {
   a.workers = workers_of(D, NT);
   if (!s.cut) {
-    k_rows_whole<T, D, NT, TREE><<<(unsigned)(a.R * a.H * s.tiles_each), kBlock, 0, st>>>(a);
+    k_rows_whole<T, D, NT><<<(unsigned)(a.R * a.H * s.tiles_each), kBlock, 0, st>>>(a);
     return;
   }
-  k_rows<T, D, NT, TREE><<<a.workers, 64, 0, st>>>(a);
+  k_rows<T, D, NT><<<a.workers, 64, 0, st>>>(a);
   k_rows_join<T, D, NT><<<dim3(a.workers - 1, (s.join_rows + kWaves - 1) / kWaves), kBlock, 0, st>>>(a);
 }
 
-template <typename T, int D, bool TREE>
-void run_kernels(AttArgs a, const Shape &s, long long *plan, hipStream_t st) {
+template <typename T, int D, int KS>
+void run_drafts(AttArgs a, const Shape &s, long long *plan, hipStream_t st) {
+  if (a.R > kListed) {
+    k_drafts_plan<rows_of(KS)><<<1, 1024, 0, st>>>(a, plan);
+    a.plan = plan;
+  }
+  a.workers = groups_of(D, KS);
+  k_drafts<T, D, KS><<<a.workers, kBlock, 0, st>>>(a);
+  k_drafts_join<T, D, KS><<<dim3(a.workers - 1, (s.join_rows + 2 * kWaves - 1) / (2 * kWaves)), kBlock, 0, st>>>(a);
+}
+
+template <typename T, int D>
+void run(AttArgs a, const Shape &s, long long *plan, hipStream_t st) {
+  if constexpr (D <= 128)
+    if (s.halves == 1) run_drafts<T, D, 1>(a, s, plan, st);
+  if (s.halves == 2) run_drafts<T, D, 2>(a, s, plan, st);
+  if (s.halves && !s.tiles) return;
   if (a.R > kListed) {
     if (s.nt == 1) k_plan<16><<<1, 1024, 0, st>>>(a, plan);
     else if (s.nt == 2) k_plan<32><<<1, 1024, 0, st>>>(a, plan);
     else k_plan<64><<<1, 1024, 0, st>>>(a, plan);
     a.plan = plan;
   }
-  if (s.nt == 1) run_rows<T, D, 1, TREE>(a, s, st);
-  if constexpr (row_tiles_most(D, TREE) >= 2)
-    if (s.nt == 2) run_rows<T, D, 2, TREE>(a, s, st);
-  if constexpr (row_tiles_most(D, TREE) >= 4)
-    if (s.nt == 4) run_rows<T, D, 4, TREE>(a, s, st);
+  if (s.nt == 1) run_rows<T, D, 1>(a, s, st);
+  if constexpr (row_tiles_most(D) >= 2)
+    if (s.nt == 2) run_rows<T, D, 2>(a, s, st);
+  if constexpr (row_tiles_most(D) >= 4)
+    if (s.nt == 4) run_rows<T, D, 4>(a, s, st);
   if (s.tiles) {
     const unsigned grid = (unsigned)s.tile_groups;
     if constexpr (D == 96 || D == 128)
-      if (s.tile_rows == 256) k_tiles<T, D, 8, TREE><<<grid, 512, 0, st>>>(a);
-    if (s.tile_rows == 128) k_tiles<T, D, 4, TREE><<<grid, kBlock, 0, st>>>(a);
+      if (s.tile_rows == 256) k_tiles<T, D, 8><<<grid, 512, 0, st>>>(a);
+    if (s.tile_rows == 128) k_tiles<T, D, 4><<<grid, kBlock, 0, st>>>(a);
     if (s.splits_most > 1)
       k_tiles_join<T, D><<<(unsigned)s.join_groups, kBlock, 0, st>>>(a);
   }
-}
-
-template <typename T, int D>
-void run(const AttArgs &a, const Shape &s, long long *plan, hipStream_t st) {
-  if (a.seen) run_kernels<T, D, true>(a, s, plan, st);
-  else run_kernels<T, D, false>(a, s, plan, st);
 }
 
 template <typename T>
