@@ -66,6 +66,7 @@ constexpr int waves_of(int D, int NT) { return D > 128 || NT > 2 ? 1 : 2; }
 constexpr int workers_of(int D, int NT) { return 1024 * waves_of(D, NT); }
 constexpr int kGroups = 512;         // workgroups of k_tiles that fill the chip: two a compute unit
 constexpr int kJoins = 2048;         // and of its join: eight
+constexpr int kWaveRequests = 64;    // requests whose running sums a wave forms in its registers
 constexpr int kNodes = 64;           // nodes of a draft tree: a request with more new tokens is a run
 constexpr int kListed = 512;         // requests whose running sums a workgroup forms by itself
 constexpr int kMaxRequests = 1 << 20;
@@ -98,6 +99,7 @@ struct AttArgs {
   int4 *joins;                       // what k_tiles_join needs: (groups, splits), then for each row tile the request's
                                      // first token, the tile's first row, the request's rows
   const unsigned long long *seen;    // k_drafts: [T] which of its request's new tokens a row sees
+  int32_t cuts_most;                 // a bound of the row tiles
 };
 
 // What k_rows_join needs of the row tile that begins a join at a piece's start; n = 0: none.
@@ -112,6 +114,14 @@ struct Cut {
 struct Request {
   int first, n, length;
 };
+
+// What k_drafts_join needs of a row tile in several parts; n = 0: it is whole.
+struct DraftCut {
+  int32_t n, p0, p1, step;           // parts; where the first and the second lie, and how far the next ones are apart
+  int32_t row0, rows;                // as above
+  int32_t first, head;
+};
+static_assert(sizeof(DraftCut) == sizeof(Cut), "they share their place");
 
 __device__ __forceinline__ Request request(const AttArgs &a, int r) {
   Request q;
@@ -311,10 +321,9 @@ struct TreeRow {
 template <bool TREE> struct Seen { typedef Span type; };
 template <> struct Seen<true> { typedef TreeRow type; };
 
-// What node t of a request sees (nothing unless `in`): the keys before the nodes, and nodes by its word.
-__device__ __forceinline__ TreeSpan tree_span(const AttArgs &a, const Request &q, int t, bool in) {
+// What a node of a request sees (nothing unless `in`): the keys before the nodes, and nodes by its word.
+__device__ __forceinline__ TreeSpan tree_span(const AttArgs &a, const Request &q, unsigned long long word, bool in) {
   const int before = q.length - q.n;
-  unsigned long long word = in ? a.seen[q.first + t] : 0ull;
   word &= ~0ull >> (kNodes - q.n);                     // (a request with rows has at least one)
   const int pos = before + max(__builtin_popcountll(word) - 1, 0), from = a.window > 0 ? max(pos - a.window + 1, 0) : 0;
   if (a.window > 0)                                    // the nearest of its path, the node itself included
@@ -816,19 +825,21 @@ struct Stage {
   u4 raw_k[kLoads], raw_v[kLoads];
   float ks, vs;
   bool ok;
+  int thread;                                        // the thread's index
 
   // keys to the first threads, values to the last, so that all have some where there are fewer pieces than threads
-  static __device__ __forceinline__ int key_item(int i, int thread = threadIdx.x) { return thread + i * kThreads; }
-  static __device__ __forceinline__ int value_item(int i, int thread = threadIdx.x) { return kThreads - 1 - thread + i * kThreads; }
+  __device__ __forceinline__ int key_item(int i) const { return thread + i * kThreads; }
+  __device__ __forceinline__ int value_item(int i) const { return kThreads - 1 - thread + i * kThreads; }
   static __device__ __forceinline__ bool has(int item) { return kItems % kThreads == 0 || item < kItems; }
   static __device__ __forceinline__ int key_of(int item) { return item / (D / 16); }
   static __device__ __forceinline__ int key_of_value(int item) { return (item & 3) * 16; }
 
-  __device__ __forceinline__ void begin(const AttArgs &a, int h, int thread) {
+  __device__ __forceinline__ void begin(const AttArgs &a, int h, int index) {
+    thread = index;
     const int bt = 1 << a.shift;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int x = key_item(i, thread), y = has(value_item(i, thread)) ? value_item(i, thread) : 0;
+      const int x = key_item(i), y = has(value_item(i)) ? value_item(i) : 0;
       k[i] = a.k + (size_t)h * bt * D + (key_of(x) & (bt - 1)) * D + x % (D / 16) * 16;
       v[i] = a.v + (size_t)h * bt * D + (size_t)(y >> 2) * bt + (key_of_value(y) & (bt - 1));
       at_k[i] = (min(key_of(x), kUnit - 1) >> a.shift) * 4;
@@ -873,7 +884,7 @@ struct Stage {
       for (int i = 0; i < kLoads; ++i)
         if ((unsigned)id_k[i] >= (unsigned)a.NB) raw_k[i] = u4{0u, 0u, 0u, 0u};
     }
-    if (threadIdx.x < 64) {
+    if (thread < 64) {
       ok = (unsigned)id_s < (unsigned)a.NB;
       const size_t at = (size_t)(ok ? id_s : 0) * a.H + h;
       ks = a.ks[at];
@@ -909,12 +920,12 @@ struct Stage {
     }
   }
   __device__ __forceinline__ void put_scales(const AttArgs &a, KeyTile<T, D> &b) const {
-    if (threadIdx.x < 4) {
+    if (thread < 4) {
       // a block that is not there: its codes are zeros and its logits -inf
       const float s = fminf(fmaxf(vs, kScaleMin), kScaleMax);
-      b.c[threadIdx.x] = ok ? a.scale * ks : 0.f;
-      b.lv[threadIdx.x] = ok ? log2_(s) : kNegInf();
-      b.iv[threadIdx.x] = ok ? __builtin_amdgcn_rcpf(s) : 0.f;
+      b.c[thread] = ok ? a.scale * ks : 0.f;
+      b.lv[thread] = ok ? log2_(s) : kNegInf();
+      b.iv[thread] = ok ? __builtin_amdgcn_rcpf(s) : 0.f;
     }
   }
 
@@ -939,7 +950,7 @@ struct Stage {
         any |= has(y) ? bits : 0u;
       }
       const int nans = __any(any != 0);
-      if ((threadIdx.x & 63) == 0) b.nans[threadIdx.x >> 6] = nans;
+      if ((thread & 63) == 0) b.nans[thread >> 6] = nans;
     }
   }
   __device__ __forceinline__ void put_values(ValueTile<D, W> &b) const {
@@ -1322,35 +1333,186 @@ __global__ void __launch_bounds__(kBlock) k_tiles_join(AttArgs a) {
 
 // ------------------------------------------------------------------ k_drafts
 
-// What a row tile costs beside its units of keys, in units: the queries, the words and the first tile's way from memory.
-constexpr int kTileCost = 3;
 // Workgroups of a compute unit, and of the chip at once.
 constexpr int groups_each(int D, int KS) { return D <= 64 && KS == 2 ? 3 : D <= 128 ? 2 : 1; }
 constexpr int groups_of(int D, int KS) { return 256 * groups_each(D, KS); }
 // Halves that a tile's keys are dealt to waves in: 64 rows leave two waves for each 32 of them.
 constexpr int rows_of(int KS) { return 128 / KS; }
 
+// How the keys are dealt to the workgroups.  Few units for each (up to kFew): every row tile is cut into equal parts of at most `part`
+// units and a workgroup has one part, so that none waits for the beginning of a second tile.  Many: all tiles' units form
+// one line that is cut into equal pieces (part = 0), which leaves no workgroup behind, whatever the lengths.
+constexpr int kFew = 16;
+
+// Units of a request's tiles, and the tiles, of all key heads.
+struct Tiles {
+  int units, tiles;
+};
 template <int ROWS>
-__device__ __forceinline__ long long costs_of(const AttArgs &a, int r) {
+__device__ __forceinline__ Tiles draft_tiles(const AttArgs &a, int r) {
   const Request q = request(a, r);
-  return q.n > 0 && q.n <= kNodes ? (long long)(units(a, q) + kTileCost) * cdiv(q.n * a.G, ROWS) * a.H : 0;
+  return q.n > 0 && q.n <= kNodes ? Tiles{units(a, q), cdiv(q.n * a.G, ROWS) * a.H} : Tiles{0, 0};
+}
+template <int ROWS>
+__device__ __forceinline__ long long dealt_of(const AttArgs &a, int r, int part) {
+  const Tiles t = draft_tiles<ROWS>(a, r);
+  return (long long)(part ? cdiv(t.units, part) : t.units) * t.tiles;
+}
+// Units of a part, from all units and tiles; `room` is the most parts that there may be (a tile makes at most one more than
+// its share of the units).
+__device__ __forceinline__ int part_of(long long units, long long tiles, int groups, int room) {
+  return units <= (long long)groups * kFew && groups + tiles <= room ? max(cdiv((int)units, groups), 1) : 0;
 }
 
 template <int ROWS>
-__global__ void __launch_bounds__(1024) k_drafts_plan(AttArgs a, long long *plan) {
+__global__ void __launch_bounds__(1024) k_drafts_plan(AttArgs a, long long *plan, int groups, int room) {
   __shared__ long long lds[16];
-  long long u0 = 0, whole;
+  long long units = 0, tiles = 0, whole, u0 = 0;
   for (int r0 = 0; r0 < a.R; r0 += 1024) {
     const int r = r0 + threadIdx.x;
-    const long long u = scan<1024>(r < a.R ? costs_of<ROWS>(a, r) : 0, lds, &whole) + u0;
+    const Tiles t = r < a.R ? draft_tiles<ROWS>(a, r) : Tiles{0, 0};
+    scan<1024>((long long)t.units * t.tiles, lds, &whole);
+    units += whole;
+    scan<1024>(t.tiles, lds, &whole);
+    tiles += whole;
+  }
+  const int part = part_of(units, tiles, groups, room);
+  for (int r0 = 0; r0 < a.R; r0 += 1024) {
+    const int r = r0 + threadIdx.x;
+    const long long u = scan<1024>(r < a.R ? dealt_of<ROWS>(a, r, part) : 0, lds, &whole) + u0;
     u0 += whole;
     if (r < a.R) plan[r] = u;
   }
-  if (threadIdx.x == 0) plan[a.R] = u0;
+  if (threadIdx.x == 0) {
+    plan[a.R] = u0;
+    plan[a.R + 1] = part;
+  }
 }
 
-__device__ __forceinline__ int draft_pieces(const AttArgs &a, long long all) {
-  return (int)min((long long)a.workers, max(all / (kTileCost + 2), 1ll));
+// Quotients that mostly fit 32 bits (a division of 64 takes a hundred instructions).
+__device__ __forceinline__ long long quotient(long long x, int y) {
+  return (unsigned long long)x >> 32 ? x / y : (long long)((unsigned)x / (unsigned)y);
+}
+
+// What the first wave of a workgroup finds for all of them.
+struct DraftWork {
+  long long all, u, end;             // the line's length; where the workgroup's piece or part begins and ends
+  int part, by_tile;                 // by_tile: cuts are told apart by the tile's number, else by the workgroup's
+  // of a part: its tile's request, and where that stands in the line and among the tiles
+  int r, units, tile;
+  Request rq;
+  long long begin;
+  int tiles[kWaveRequests];          // tiles before each request (few requests only)
+};
+
+// Sum of one value a lane.
+template <typename V>
+__device__ __forceinline__ V wave_sum(V x) {
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
+  return x;
+}
+// Sum of the lanes before.
+template <typename V>
+__device__ __forceinline__ V wave_before(V x) {
+  const int lane = threadIdx.x & 63;
+  V s = x;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const V y = __shfl_up(s, d);
+    if (lane >= d) s += y;
+  }
+  return s - x;
+}
+
+// For the first wave of a workgroup: the list of what comes before each request, and the workgroup's own work.
+template <int ROWS>
+__device__ __forceinline__ void deal(const AttArgs &a, int groups, long long *list_, DraftWork *work) {
+  const int lane = threadIdx.x & 63, w = blockIdx.x, room = gridDim.x;
+  const long long *list = a.plan;
+  int part, r = 0, units_ = 0, tile = 0, all_tiles = 0;
+  long long all, begin = 0;
+  Request rq{0, 0, 0};
+  const bool by_tile = a.cuts_most <= groups && a.R <= kWaveRequests;
+  if (a.R <= kWaveRequests) {
+    // a lane a request: everything stays in registers
+    const bool in = lane < a.R;
+    const Request q = in ? request(a, lane) : Request{0, 0, 0};
+    const bool has = in && q.n > 0 && q.n <= kNodes;
+    const int u = has ? units(a, q) : 0, tiles = has ? cdiv(q.n * a.G, ROWS) * a.H : 0;
+    const long long all_units = wave_sum((long long)u * tiles);
+    all_tiles = same(wave_sum(tiles));
+    part = part_of(all_units, all_tiles, groups, room);
+    if (part && all_tiles < groups) {
+      // a second round would double the time: longer parts, as many as the sum is over the chip's workgroups
+      const int U = (int)all_units;
+      for (int i = 0; i < 3; ++i) {
+        const int over = same(wave_sum(cdiv(u, part) * tiles)) - groups;
+        if (over <= 0) break;
+        const int share = U / part - over;
+        part = max(share > 0 ? cdiv(U, share) : 2 * part, part + 1);
+      }
+    }
+    part = same(part);
+    const long long mine = (long long)(part ? cdiv(u, part) : u) * tiles;
+    const int tiles_before = wave_before(tiles);
+    if (part) {
+      const int before = wave_before((int)mine);
+      all = same(__shfl(before + (int)mine, 63));
+      const unsigned long long m = __ballot(mine > 0 && before <= w);
+      if (w < all) {
+        r = 63 - __builtin_clzll(m);
+        rq = Request{__builtin_amdgcn_readlane(q.first, r), __builtin_amdgcn_readlane(q.n, r), __builtin_amdgcn_readlane(q.length, r)};
+        begin = __builtin_amdgcn_readlane(before, r);
+        units_ = __builtin_amdgcn_readlane(u, r);
+        tile = __builtin_amdgcn_readlane(tiles_before, r);
+      }
+    } else {
+      const long long before = wave_before(mine);
+      all = same(__shfl(before + mine, 63));
+      if (in) {
+        list_[lane] = before;
+        work->tiles[lane] = tiles_before;
+      }
+      if (lane == 0) list_[a.R] = all;
+    }
+  } else {
+    if (list) {
+      part = (int)same(list[a.R + 1]);
+    } else {
+      long long units = 0, tiles = 0;
+      for (int r0 = 0; r0 < a.R; r0 += 64) {
+        const Tiles t = r0 + lane < a.R ? draft_tiles<ROWS>(a, r0 + lane) : Tiles{0, 0};
+        units += (long long)t.units * t.tiles;
+        tiles += t.tiles;
+      }
+      part = same(part_of(wave_sum(units), wave_sum(tiles), groups, room));
+      list_sums(a, [&](int r) { return dealt_of<ROWS>(a, r, part); }, list_);
+      list = list_;
+    }
+    all = same(list[a.R]);
+    if (part && w < all) {
+      r = find(list, a.R, w);
+      rq = request(a, r);
+      begin = same(list[r]);
+      units_ = units(a, rq);
+    }
+  }
+  if (lane == 0) {
+    const int n = (int)min(all, (long long)groups);    // pieces
+    work->all = all;
+    work->u = part ? w : w < n ? quotient(all * w, n) : 0;
+    work->end = part ? min(all, w + 1ll) : w < n ? quotient(all * (w + 1), n) : 0;
+    work->part = part;
+    work->by_tile = by_tile;
+    work->r = r;
+    work->units = units_;
+    work->tile = tile;
+    work->rq = rq;
+    work->begin = begin;
+    // tiles that there are not, and pieces that begin no tile that they do not end
+    if (!by_tile || (w >= all_tiles && w < a.cuts_most)) reinterpret_cast<DraftCut *>(a.cuts)[w].n = 0;
+  }
 }
 
 // One wave's 32 rows (and half of the keys, where KS = 2) of a row tile.
@@ -1370,12 +1532,27 @@ struct DraftTile {
   static __device__ __forceinline__ int side(int thread) { return wave(thread) / KS; }          // which 32 rows
   static __device__ __forceinline__ int row(const Work &k, int thread) { return k.row0 + side(thread) * 32 + (thread & 31); }
 
-  static __device__ __forceinline__ void begin(const AttArgs &a, const Work &k, int thread, TreeSpan *spans, State &st) {
+  // The queries, and the row's word.
+  static __device__ __forceinline__ unsigned long long begin(const AttArgs &a, const Work &k, int thread, State &st) {
     const int lane = thread & 63, i = row(k, thread), t = i / a.G;
     const bool in = i < k.rows;
-    st.half = wave(thread) % KS;
-    const TreeSpan sees = tree_span(a, k.rq, t, in);
+    const T *q = static_cast<const T *>(a.q) + (int64_t)(k.rq.first + (in ? t : 0)) * a.q_token +
+                 (int64_t)(k.h * a.G + (in ? i - t * a.G : 0)) * a.q_head;
+    const unsigned long long word = a.seen[k.rq.first + (in ? t : 0)];
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+      u4 raw = *reinterpret_cast<const u4 *>(q + s * 16 + (lane >> 5) * 8);
+      if (!in) raw = u4{0u, 0u, 0u, 0u};
+      st.q[s] = __builtin_bit_cast(typename Vec8<T>::type, raw);
+    }
+    return in ? word : 0ull;
+  }
+  static __device__ __forceinline__ void sees(const AttArgs &a, const Work &k, int thread, unsigned long long word,
+                                              TreeSpan *spans, State &st) {
+    const int lane = thread & 63;
+    const TreeSpan sees = tree_span(a, k.rq, word, row(k, thread) < k.rows);
     TreeSpan *own = spans + side(thread) * 32 + (lane & 31);
+    st.half = wave(thread) % KS;
     st.sees.span = own;
     if (lane < 32) *own = sees;                        // (the waves of two halves write the same)
     st.ref = st.l = 0.f;
@@ -1384,14 +1561,6 @@ struct DraftTile {
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
       for (int y = 0; y < 16; ++y) st.o[d][y] = 0.f;
-    const T *q = static_cast<const T *>(a.q) + (int64_t)(k.rq.first + (in ? t : 0)) * a.q_token +
-                 (int64_t)(k.h * a.G + (in ? i - t * a.G : 0)) * a.q_head;
-#pragma unroll
-    for (int s = 0; s < D / 16; ++s) {
-      u4 raw = *reinterpret_cast<const u4 *>(q + s * 16 + (lane >> 5) * 8);
-      if (!in) raw = u4{0u, 0u, 0u, 0u};
-      st.q[s] = __builtin_bit_cast(typename Vec8<T>::type, raw);
-    }
   }
 
   // The result of the wave's rows, all keys of the piece in it.
@@ -1431,91 +1600,109 @@ struct Halves {
 template <typename T, int D, int KS>
 __global__ void __launch_bounds__(kBlock, groups_each(D, KS)) k_drafts(AttArgs a) {
   typedef DraftTile<T, D, KS> K;
-  constexpr int kRows = K::kRows;
+  // units on their way from memory: two where registers allow
+  constexpr int kRows = K::kRows, kDeep = KS == 2 && D > 64 && D <= 128 ? 2 : 1;
   __shared__ KeyTile<T, D> keys[2];
   __shared__ union { ValueTile<D, kWaves> tile[2]; Halves<D> halves; } values;
   __shared__ TreeSpan spans[kRows];
   // 0.  What is read through it is read anew for each row tile: kept in registers, the arguments and indexes that only a tile's
   // begin and end need push out what the keys are worked on with (18 registers of 128 dims)
   __shared__ int nought;
+  __shared__ DraftWork work;
   if (threadIdx.x == 0) nought = 0;
-  lds_barrier();
   __shared__ long long list_[kListed + 1];
-  const long long *list = a.plan;
-  if (!list) {
-    list_sums(a, [&](int r) { return costs_of<kRows>(a, r); }, list_);
-    list = list_;
-  }
-  const long long all = same(list[a.R]);
-  const int n = draft_pieces(a, all), w = blockIdx.x;
-  Cut cut{};
-  if (w < n) {
-    long long u = piece_start(all, w, n);
-    const long long start = u, end = piece_start(all, w + 1, n);
-    for (int place = 2 * w; u < end; ++place) {
+  const int w = blockIdx.x;
+  if (K::wave(threadIdx.x) == 0) deal<kRows>(a, groups_of(D, KS), list_, &work);
+  lds_barrier();
+  {
+    long long u = same(work.u);
+    for (int place = 0; u < same(work.end); ++place) {
       const AttArgs &b = (&a)[same(nought)];
-      const int r = find(list, b.R, u);
-      const Request rq = request(b, r);
-      const long long begin = same(list[r]);
-      const int each = units(b, rq), cost = each + kTileCost, at = (int)((u - begin) / cost), tiles = cdiv(rq.n * b.G, kRows);
-      const long long tile0 = begin + (long long)at * cost;
-      const int off = (int)(u - tile0), stop = (int)min((long long)cost, off + (end - u));
-      const int k0 = max(off - kTileCost, 0), k1 = max(stop - kTileCost, 0);
+      const int part = same(work.part);
+      const long long *list = b.plan ? b.plan : list_;
+      int r, each;
+      Request rq;
+      long long begin;
+      if (part) {
+        r = same(work.r), each = same(work.units), begin = same(work.begin);
+        rq = Request{same(work.rq.first), same(work.rq.n), same(work.rq.length)};
+      } else {
+        r = find(list, b.R, u);
+        rq = request(b, r);
+        begin = same(list[r]);
+        each = units(b, rq);
+      }
+      const int cuts = part ? cdiv(each, part) : each, tiles = cdiv(rq.n * b.G, kRows);
+      const int at = (int)quotient(u - begin, cuts), off = (int)(u - begin - (long long)at * cuts);
       typename K::Work k;
       k.rq = rq;
       k.h = at / tiles;
       k.row0 = at % tiles * kRows;
       k.rows = rq.n * b.G;
+      int k0 = off, k1 = (int)min((long long)each, off + (same(work.end) - u));
+      if (part) k0 = each * off / cuts, k1 = each * (off + 1) / cuts;   // (at most groups * kFew units in all)
+      const bool whole = k0 == 0 && k1 == each;
+      k.part = whole ? -1 : part ? w : 2 * w + min(place, 1);
+      if (k0 == 0 && threadIdx.x == 0) {
+        // the tile's first part says where the others are
+        DraftCut cut{0, w, w + 1, 1, k.row0, k.rows, rq.first, k.h * b.G};
+        if (part) {
+          cut.n = whole ? 0 : cuts;
+        } else {
+          const long long all = work.all, n = min(all, (long long)groups_of(D, KS));
+          const int last = (int)(((begin + (long long)(at + 1) * each) * n - 1) / all);      // piece of the tile's last unit
+          cut.n = whole ? 0 : last - w + 1;
+          cut.p0 = k.part, cut.p1 = 2 * (w + 1), cut.step = 2;
+        }
+        DraftCut *out = reinterpret_cast<DraftCut *>(b.cuts);
+        const int j = work.by_tile ? (part ? work.tile : work.tiles[r]) + at : w;
+        if (work.by_tile ? j < b.cuts_most : !whole) out[j] = cut;
+      }
+      u += part ? 1 : k1 - k0;
       const int first = first_unit(b, rq);
       k.u0 = first + k0;
       k.u1 = first + k1;
-      k.part = k0 == 0 && k1 == each ? -1 : min(place, 2 * w + 1);
-      if (u == start && k0 > 0) {
-        // this piece's start cuts the tile: the first such cut is where the tile's pieces are joined
-        const long long prior = piece_start(all, w - 1, n);
-        if (prior <= tile0 + kTileCost) {
-          const int last = (int)(((tile0 + cost) * n - 1) / all);      // piece of the tile's last unit
-          cut = Cut{last - w + 2, prior < tile0 ? 1 : 0, k.row0, k.rows, rq.first, k.h * b.G, {0, 0}};
-        }
-      }
-      u += stop - off;
-      if (k0 >= k1) continue;                          // only what a tile costs beside its keys: the next piece has it
 
-      const int thread = threadIdx.x + nought;
+      const int thread = threadIdx.x + nought, before = rq.length - rq.n;
+      const int32_t *table = b.table + (size_t)r * b.MB;
       typename K::State st;
-      K::begin(b, k, thread, spans, st);
-      const int before = rq.length - rq.n, live = k.row0 + K::side(thread) * 32 < k.rows;
       // some row does not see all of the unit
       const auto look = [&](int unit) {
         return unit * kUnit + kUnit > before || (a.window > 0 && unit * kUnit < rq.length - a.window);
       };
-      const int32_t *table = b.table + (size_t)r * b.MB;
-      Stage<T, D, kWaves> g;
-      const auto blocks = [&](int u) { g.blocks(a, table, u * kUnit); };
-      const auto load = [&](int u) {
-        g.load_keys(a, k.h, u * kUnit);
-        g.load_values(a, u * kUnit);
+      Stage<T, D, kWaves> g[kDeep];                    // what is on its way: the units behind the one that is worked on
+      const auto load = [&](Stage<T, D, kWaves> &s, int u) {
+        s.load_keys(a, k.h, u * kUnit);
+        s.load_values(a, u * kUnit);
       };
-      const auto store = [&](int u) {
-        g.put_keys(keys[u & 1]);
-        g.put_scales(a, keys[u & 1]);
+      const auto store = [&](Stage<T, D, kWaves> &s, int u) {
+        s.put_keys(keys[u & 1]);
+        s.put_scales(a, keys[u & 1]);
         if (look(u)) {
           rarely();
-          g.clean_values(rq.length - u * kUnit, values.tile[u & 1]);
+          s.clean_values(rq.length - u * kUnit, values.tile[u & 1]);
         }
-        g.put_values(values.tile[u & 1]);
+        s.put_values(values.tile[u & 1]);
       };
-      g.begin(b, k.h, thread);
-      blocks(k.u0);
-      load(k.u0);
-      blocks(k.u0 + 1);
-      store(k.u0);
+#pragma unroll
+      for (int i = 0; i < kDeep; ++i) {
+        g[i].begin(b, k.h, thread);
+        g[i].blocks(b, table, (k.u0 + i) * kUnit);
+      }
+      const unsigned long long word = K::begin(b, k, thread, st);
+#pragma unroll
+      for (int i = 0; i < kDeep; ++i)
+        if (i == 0 || k.u0 + i < k.u1) load(g[i], k.u0 + i);
+      g[0].blocks(a, table, (k.u0 + kDeep) * kUnit);
+      K::sees(b, k, thread, word, spans, st);
+      const bool live = k.row0 + K::side(thread) * 32 < k.rows;
+      store(g[0], k.u0);
       lds_barrier();
-      for (int u = k.u0; u < k.u1; ++u) {
+      const auto step = [&](int u, Stage<T, D, kWaves> &next, Stage<T, D, kWaves> &free) {
         const int base = u * kUnit;
-        if (u + 1 < k.u1) {
-          load(u + 1);
-          blocks(u + 2);
+        if (u + kDeep < k.u1) {
+          load(free, u + kDeep);
+          (kDeep == 2 ? next : free).blocks(a, table, (u + kDeep + 1) * kUnit);
         }
         if (live) {
           st.products(keys[u & 1]);
@@ -1528,8 +1715,13 @@ __global__ void __launch_bounds__(kBlock, groups_each(D, KS)) k_drafts(AttArgs a
             st.template sums<1>(values.tile[u & 1]);
           }
         }
-        if (u + 1 < k.u1) store(u + 1);
+        if (u + 1 < k.u1) store(next, u + 1);
         lds_barrier();
+      };
+      for (int u = k.u0; u < k.u1; u += kDeep) {
+        step(u, g[kDeep - 1], g[0]);
+        if constexpr (kDeep == 2)
+          if (u + 1 < k.u1) step(u + 1, g[0], g[1]);
       }
       float l = across32(st.l, add_), m = st.sums_kept == kSums ? st.ref : kNegInf();
       const AttArgs &e = (&a)[same(nought)];
@@ -1562,22 +1754,17 @@ __global__ void __launch_bounds__(kBlock, groups_each(D, KS)) k_drafts(AttArgs a
       }
     }
   }
-  if (threadIdx.x == 0) a.cuts[w] = cut;
 }
 
-// A wave a row of the tile that the cut at piece blockIdx.x + 1 leaves, in turn.
+// A wave a row of a tile that lies in parts.
 template <typename T, int D, int KS>
 __global__ void __launch_bounds__(kBlock) k_drafts_join(AttArgs a) {
   constexpr int kRows = rows_of(KS);
-  const int w = blockIdx.x + 1;
-  const Cut cut = a.cuts[w];
-  if (cut.n == 0) return;
-  for (int row = blockIdx.y * kWaves + (threadIdx.x >> 6); row < kRows; row += gridDim.y * kWaves) {
-    const int i = cut.row0 + row, t = i / a.G;
-    if (i >= cut.rows) return;
-    join_row<T, D>(a, (size_t)(2 * (w - 1) + cut.second) * kRows + row, (size_t)(2 * w) * kRows + row, 2 * kRows, cut.n,
-                   cut.first + t, cut.head + i - t * a.G);
-  }
+  const DraftCut cut = reinterpret_cast<const DraftCut *>(a.cuts)[blockIdx.x];
+  const int row = blockIdx.y * kWaves + (threadIdx.x >> 6), i = cut.row0 + row, t = i / a.G;
+  if (cut.n == 0 || row >= kRows || i >= cut.rows) return;
+  join_row<T, D>(a, (size_t)cut.p0 * kRows + row, (size_t)cut.p1 * kRows + row, cut.step * kRows, cut.n, cut.first + t,
+                 cut.head + i - t * a.G);
 }
 
 // ------------------------------------------------------------------ host
@@ -1593,6 +1780,7 @@ struct Shape {
   long long tile_groups, join_groups;   // workgroups of k_tiles, of k_tiles_join
   int join_rows;                     // rows of a row tile that are mostly in use: the join's waves
   int halves;                        // drafts: k_drafts' KS, else 0
+  int draft_groups, draft_tiles;     // its workgroups, and a bound of the row tiles
   size_t plan, cuts, joins, part_ml, part_o, bytes;
 };
 
@@ -1635,8 +1823,14 @@ festina_status shape_of(const festina_kv_cache *c, const festina_attention *t, b
   size_t parts = 0;
   if (s->nt && s->cut) parts = (size_t)2 * workers_of(D, s->nt) * 16 * s->nt;
   if (drafts) {
-    parts = (size_t)2 * groups_of(D, s->halves) * rows_of(s->halves);
-    if ((long long)kNodes * G * H > INT_MAX / kNodes) return FESTINA_ERR_UNSUPPORTED;
+    // one for each part of a step of few keys: at most a tile more each than the chip's workgroups
+    const int groups = groups_of(D, s->halves);
+    const int rows = rows_of(s->halves), some = min(t->n_requests, t->n_tokens);
+    const long long each = (min((long long)kNodes * G, most) + rows - 1) / rows;
+    const long long tiles = min((long long)t->n_tokens * G / rows + some, some * each) * H;
+    s->draft_tiles = (int)min(tiles, (long long)INT_MAX);
+    s->draft_groups = groups + (int)min(tiles, 2ll * groups);
+    parts = (size_t)max(2 * groups, s->draft_groups) * rows_of(s->halves);
   }
   if (s->tiles) {
     // 256 rows a workgroup stage each tile half as often for a row, where registers allow and enough workgroups are
@@ -1663,7 +1857,7 @@ festina_status shape_of(const festina_kv_cache *c, const festina_attention *t, b
   }
   s->plan = 0;
   s->cuts = up((size_t)2 * (t->n_requests + 1) * 8);
-  s->joins = s->cuts + up((size_t)(drafts ? groups_of(D, s->halves) : workers_of(D, max(s->nt, 1))) * sizeof(Cut));
+  s->joins = s->cuts + up((size_t)(drafts ? s->draft_groups : workers_of(D, max(s->nt, 1))) * sizeof(Cut));
   s->part_ml = s->joins + up((kGroups + 1) * sizeof(int4));
   s->part_o = s->part_ml + up(parts * 8);
   s->bytes = s->part_o + up(parts * D * 4);
@@ -1684,12 +1878,12 @@ void run_rows(AttArgs a, const Shape &s, hipStream_t st) {
 template <typename T, int D, int KS>
 void run_drafts(AttArgs a, const Shape &s, long long *plan, hipStream_t st) {
   if (a.R > kListed) {
-    k_drafts_plan<rows_of(KS)><<<1, 1024, 0, st>>>(a, plan);
+    k_drafts_plan<rows_of(KS)><<<1, 1024, 0, st>>>(a, plan, groups_of(D, KS), s.draft_groups);
     a.plan = plan;
   }
-  a.workers = groups_of(D, KS);
-  k_drafts<T, D, KS><<<a.workers, kBlock, 0, st>>>(a);
-  k_drafts_join<T, D, KS><<<dim3(a.workers - 1, (s.join_rows + 2 * kWaves - 1) / (2 * kWaves)), kBlock, 0, st>>>(a);
+  k_drafts<T, D, KS><<<s.draft_groups, kBlock, 0, st>>>(a);
+  const bool by_tile = s.draft_tiles <= groups_of(D, KS) && a.R <= kWaveRequests;      // as deal() has it
+  k_drafts_join<T, D, KS><<<dim3(by_tile ? s.draft_tiles : s.draft_groups, (s.join_rows + kWaves - 1) / kWaves), kBlock, 0, st>>>(a);
 }
 
 template <typename T, int D>
@@ -1759,6 +1953,7 @@ festina_status attend(const festina_kv_cache *cache, const festina_attention *at
   a.tiles_each = s.tiles_each;
   a.tiles_most = (int)s.tiles_most;
   a.splits_most = s.splits_most;
+  a.cuts_most = s.draft_tiles;
   a.tile_rows = s.tile_rows;
   a.scale = att->scale * 1.44269504088896341f;
   a.table = att->block_table;
