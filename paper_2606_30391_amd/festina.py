@@ -708,15 +708,35 @@ def _used_on(stream, *tensors):
             t.record_stream(stream)
 
 
-def _here(stream, *tensors):
-    """Refuse tensors of another device than the one that the call runs on: the current one, which a torch stream's has to be."""
-    import torch
-    now = torch.cuda.current_device()
-    at = now if stream is None or isinstance(stream, int) else stream.device_index
-    for t in tensors:
-        if t is not None and (t.device.index != now or at != now):
-            raise ValueError(f"tensors, stream and current device have to be one device (tensor on {t.device}, "
-                             f"stream on {at}, current {now})")
+class _Here:
+    """Where calls run, in few attribute reads: the kernels of these calls take about as long as their host work."""
+
+    def __init__(self):
+        import torch
+        # (torch's own names, without which it takes the public way)
+        self.device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        self.raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        self.int32 = torch.int32
+
+    def stream(self, stream, now):
+        """The handle of `stream` (None: the current one of device `now`), which has to be a stream of that device."""
+        if stream is None:
+            return self.raw(now) if self.raw is not None else _stream_handle(None)
+        if not isinstance(stream, int) and stream.device_index != now:
+            raise ValueError(f"stream: one of device {stream.device_index}, not of the current device {now}")
+        return _stream_handle(stream)
+
+    def ints(self, t, name, n, now):
+        """The address of a contiguous int32 tensor of n entries on device `now`."""
+        if t.dtype is not self.int32 or t.get_device() != now or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
+            _check(t, name, (self.int32,), (n,))
+            _on_device(t, name, now)
+        return t.data_ptr()
+
+
+def _on_device(t, name, now):
+    if t.get_device() != now:
+        raise ValueError(f"{name}: on device {t.get_device()}, not on the current device {now}")
 
 
 class _Workspaces:
@@ -775,7 +795,7 @@ class DeviceBlocks:
         self.first, self.slot, self.length, self.n_free_out = i32(R + 1), i32(max(self.max_tokens, 0)), i32(R), i32(1)
         self.served = torch.empty(R, dtype=torch.uint8, device=device)
         self.ws_bytes = festina_blocks_workspace_bytes(R, self.max_tokens)
-        self._ws = _Workspaces()
+        self._ws, self._here = _Workspaces(), _Here()
         self._structs()
 
     def _structs(self):
@@ -802,11 +822,16 @@ class DeviceBlocks:
     def trim(self, keep, stream=None):
         """Give back the blocks behind the first keep[r] (int32, device) tokens of every request: free_ids, length (keep),
         n_free_out."""
-        import torch
-        _check(keep, "keep", (torch.int32,), self.held.shape)
-        _here(stream, keep, self.held)
+        here = self._here
+        now = here.device()
+        at = here.ints(keep, "keep", self.held.numel(), now)
+        if self.table.get_device() != now:
+            _on_device(self.table, "table", now)
+        here.stream(stream, now)
         held, ws, handle = self._ws.get(self.ws_bytes, stream, self.table.device)
-        festina_trim_blocks(self.req, keep, self.out, ws, self.ws_bytes, handle)
+        st = lib().festina_trim_blocks(C.byref(self.req), at, C.byref(self.out), ws, self.ws_bytes, handle)
+        if st != FESTINA_OK:
+            raise FestinaError(st, "festina_trim_blocks")
         if stream is not None:
             _used_on(stream, keep, *self._tensors())
 
@@ -843,7 +868,7 @@ class DeviceCache:
         self._types = {**self._halves, torch.float32: FESTINA_F32}
         self._int32, self._f32, self._rows, self._scale = (torch.int32,), torch.float32, (h, d), d ** -0.5
         self._empty, self._attend, self._cache_ref = torch.empty, lib().festina_attend, C.byref(self.cache)
-        self._attend_drafts, self._int64 = lib().festina_attend_drafts, (torch.int64,)
+        self._attend_drafts, self._int64, self._here = lib().festina_attend_drafts, (torch.int64,), _Here()
         self._graded = torch.is_grad_enabled
 
     @classmethod
@@ -928,47 +953,72 @@ class DeviceCache:
                                 table.data_ptr(), length.data_ptr(), first.data_ptr(), q.data_ptr(), qt, qh,
                                 out.data_ptr(), ot, oh, lse.data_ptr())
         if seen is not None:
-            _check(seen, "seen", self._int64, (T,))
-            _here(stream, q, seen)
-        sizes = (R, columns, T, heads, max_new) if seen is None else (R, columns, T, heads, max_new, 1)
+            return self._over_drafts(att, (R, columns, T, heads, max_new, 1), seen, q, table, length, first, out, lse, stream)
+        sizes = (R, columns, T, heads, max_new)
         n = self._ws_bytes.get(sizes)
         if n is None:
             if len(self._ws_bytes) > 1024:
                 self._ws_bytes.clear()
-            n = (festina_attend_workspace_bytes if seen is None else festina_attend_drafts_workspace_bytes)(self.cache, att)
+            n = festina_attend_workspace_bytes(self.cache, att)
             if n:                                            # 0: refused below, for something that may not be a size
                 self._ws_bytes[sizes] = n
         held, ws, handle = self._ws.get(n, stream, q.device)
-        if seen is None:
-            st = self._attend(self._cache_ref, C.byref(att), ws, n, handle)
-        else:
-            st = self._attend_drafts(self._cache_ref, C.byref(att), seen.data_ptr(), ws, n, handle)
+        st = self._attend(self._cache_ref, C.byref(att), ws, n, handle)
         if st != FESTINA_OK:
-            raise FestinaError(st, "festina_attend" if seen is None else "festina_attend_drafts")
+            raise FestinaError(st, "festina_attend")
         if stream is not None:
-            _used_on(stream, q, table, length, first, out, lse, self.k, self.v, self.k_scale, self.v_scale,
-                     *(() if seen is None else (seen,)))
+            _used_on(stream, q, table, length, first, out, lse, self.k, self.v, self.k_scale, self.v_scale)
+        return out, lse
+
+    def _over_drafts(self, att, sizes, seen, q, table, length, first, out, lse, stream):
+        """The rest of attend() where new tokens are drafts."""
+        now = q.get_device()
+        if seen.dtype is not self._int64[0] or seen.get_device() != now or seen.dim() != 1 or seen.numel() != att.n_tokens or \
+                not seen.is_contiguous():
+            _check(seen, "seen", self._int64, (att.n_tokens,))
+        here = self._here
+        if here.device() != now or seen.get_device() != now or self.k.get_device() != now:
+            raise ValueError("q, seen, cache: on the current device")
+        here.stream(stream, now)
+        n = self._ws_bytes.get(sizes)
+        if n is None:
+            if len(self._ws_bytes) > 1024:
+                self._ws_bytes.clear()
+            n = festina_attend_drafts_workspace_bytes(self.cache, att)
+            if n:
+                self._ws_bytes[sizes] = n
+        held, ws, handle = self._ws.get(n, stream, q.device)
+        st = self._attend_drafts(self._cache_ref, C.byref(att), seen.data_ptr(), ws, n, handle)
+        if st != FESTINA_OK:
+            raise FestinaError(st, "festina_attend_drafts")
+        if stream is not None:
+            _used_on(stream, q, table, length, first, seen, out, lse, self.k, self.v, self.k_scale, self.v_scale)
         return out, lse
 
     def keep(self, table, length, first, path, kept, also=(), stream=None):
         """Move the kept tokens of a step together, here and in the caches `also` (the other layers', of the same sizes): table,
         length (new tokens included) and first are the step's, path [tokens] and kept [requests] (int32) as from
         DeviceDrafts.accept."""
-        _check(table, "table", self._int32, table.shape)
-        if table.dim() != 2:
-            raise ValueError("table: a contiguous tensor of two dimensions is needed")
+        here = self._here
+        now = here.device()
+        if table.dim() != 2 or table.dtype is not here.int32 or table.get_device() != now or not table.is_contiguous():
+            _check(table, "table", self._int32, table.shape)
+            raise ValueError(f"table: a contiguous tensor of two dimensions on the current device {now} is needed")
         R, columns = table.shape
-        _check(length, "length", self._int32, (R,))
-        _check(first, "first", self._int32, (R + 1,))
-        _check(kept, "kept", self._int32, (R,))
-        _check(path, "path", self._int32, (path.numel(),))
+        T = path.numel()
+        q = festina_kept(R, columns, T, table.data_ptr(), here.ints(length, "length", R, now),
+                         here.ints(first, "first", R + 1, now), here.ints(path, "path", T, now),
+                         here.ints(kept, "kept", R, now))
         caches = (self, *also)
+        for c in caches:
+            if c.k.get_device() != now:
+                _on_device(c.k, "cache", now)
         if len({c.k.data_ptr() for c in caches}) != len(caches):
             raise ValueError("also: each cache once (its tokens would be moved twice)")
-        _here(stream, table, length, first, path, kept, *(c.k for c in caches))
-        layers = (festina_kv_cache * len(caches))(*(c.cache for c in caches))
-        festina_keep_tokens(layers, len(caches), festina_kept(R, columns, path.numel(), _ptr(table), _ptr(length),
-                                                              _ptr(first), _ptr(path), _ptr(kept)), stream)
+        st = lib().festina_keep_tokens((festina_kv_cache * len(caches))(*[c.cache for c in caches]), len(caches), C.byref(q),
+                                       here.stream(stream, now))
+        if st != FESTINA_OK:
+            raise FestinaError(st, "festina_keep_tokens")
         if stream is not None:
             _used_on(stream, table, length, first, path, kept, *(x for c in caches for x in (c.k, c.v, c.k_scale, c.v_scale)))
 
@@ -1001,18 +1051,23 @@ class DeviceDrafts:
         self.position, self.path = i32(self.max_tokens), i32(self.max_tokens)
         self.kept, self.next, self.length = (i32(self.n_requests) for _ in range(3))
         self.accepted = festina_accepted(_ptr(self.path), _ptr(self.kept), _ptr(self.next), _ptr(self.length))
-        self._int32 = (torch.int32,)
+        self._here, self._plan, self._accept = _Here(), lib().festina_plan_drafts, lib().festina_accept_drafts
 
-    def _drafts(self, first, length, stream):
-        _check(first, "first", self._int32, (self.n_requests + 1,))
-        _check(length, "length", self._int32, (self.n_requests,))
-        _here(stream, first, length, self.seen)
-        return festina_drafts(self.n_requests, self.max_tokens, first.data_ptr(), length.data_ptr(),
+    def _drafts(self, first, length, now):
+        if self.kept.get_device() != now:
+            _on_device(self.kept, "the drafts", now)
+        here = self._here
+        return festina_drafts(self.n_requests, self.max_tokens, here.ints(first, "first", self.n_requests + 1, now),
+                              here.ints(length, "length", self.n_requests, now),
                               None if self.parent is None else self.parent.data_ptr())
 
     def plan(self, first, length, stream=None):
         """What the nodes see and where they stand; first and length are the step's (DeviceBlocks)."""
-        festina_plan_drafts(self._drafts(first, length, stream), self.seen, self.position, stream)
+        now = self._here.device()
+        st = self._plan(C.byref(self._drafts(first, length, now)), self.seen.data_ptr(), self.position.data_ptr(),
+                        self._here.stream(stream, now))
+        if st != FESTINA_OK:
+            raise FestinaError(st, "festina_plan_drafts")
         if stream is not None:
             _used_on(stream, first, length, *self._tensors())
 
@@ -1020,8 +1075,12 @@ class DeviceDrafts:
         """The nodes that the model's choice [max_tokens] (int32: the token chosen behind each) accepts."""
         if self.token is None:
             raise ValueError("token: the drafted tokens are needed")
-        _check(choice, "choice", self._int32, (self.max_tokens,))
-        festina_accept_drafts(self._drafts(first, length, stream), self.token, choice, self.accepted, stream)
+        now = self._here.device()
+        st = self._accept(C.byref(self._drafts(first, length, now)), self.token.data_ptr(),
+                          self._here.ints(choice, "choice", self.max_tokens, now), C.byref(self.accepted),
+                          self._here.stream(stream, now))
+        if st != FESTINA_OK:
+            raise FestinaError(st, "festina_accept_drafts")
         if stream is not None:
             _used_on(stream, first, length, choice, *self._tensors())
 
@@ -1049,45 +1108,69 @@ class DeviceRotary:
         self.rotary = festina_rotary(self.head_dim, 2 * len(turn), 1 if interleaved else 0, float(eps), _ptr(self.turn),
                                      *(_ptr(w) for w in self.weights))
         self._types = {torch.bfloat16: FESTINA_BF16, torch.float16: FESTINA_F16, torch.float32: FESTINA_F32}
-        self._int32, self._empty, self._graded = (torch.int32,), torch.empty, torch.is_grad_enabled
+        self._here, self._empty, self._graded = _Here(), torch.empty, torch.is_grad_enabled
         self._rotate, self._ref = lib().festina_rotate_heads, C.byref(self.rotary)
 
     def apply(self, q, k, position, q_out=None, k_out=None, stream=None):
         """(q_out, k_out): queries and keys [tokens][heads][head_dim] of one type (any strides but the last) at the int32
         positions [tokens].  Outputs are made where not given, and may be q and k themselves.  For serving: inputs that ask
         for a gradient are refused."""
-        T, D, device = q.shape[0], self.head_dim, q.device
+        here, D, dtype = self._here, self.head_dim, q.dtype
+        now, kind = here.device(), self._types.get(dtype)
         if stream is not None and (q_out is None or k_out is None):
-            with _on(stream, device):
-                return self.apply(q, k, position, self._empty(q.shape, dtype=q.dtype, device=device) if q_out is None else q_out,
-                                  self._empty(k.shape, dtype=k.dtype, device=device) if k_out is None else k_out, stream)
+            with _on(stream, q.device):
+                return self.apply(q, k, position, self._empty(q.shape, dtype=dtype, device=q.device) if q_out is None else q_out,
+                                  self._empty(k.shape, dtype=k.dtype, device=k.device) if k_out is None else k_out, stream)
+        if q.dim() != 3 or k.dim() != 3:
+            raise ValueError("q and k: [tokens][heads][dim]")
+        T, heads, qd = q.shape
+        tokens, kv_heads, kd = k.shape
+        qt, qh, qs = q.stride()
+        kt, kh, ks = k.stride()
+        if kind is None or k.dtype is not dtype or q.get_device() != now or k.get_device() != now or tokens != T or qd != D or \
+                kd != D or (qs != 1 and q.numel()) or (ks != 1 and k.numel()):
+            _check(q, "q", self._types)
+            _check(k, "k", (dtype,))
+            _on_device(q, "q", now)
+            _on_device(k, "k", now)
+            raise ValueError(f"q and k: [{T}][heads][{D}] with their last axis contiguous")
+        if (q.requires_grad or k.requires_grad) and self._graded():
+            raise ValueError("q, k: no gradient passes through (call under torch.no_grad())")
         if q_out is None:
-            q_out = self._empty(q.shape, dtype=q.dtype, device=device)
+            q_out = self._empty((T, heads, D), dtype=dtype, device=q.device)
+            ot, oh = heads * D, D
+        else:
+            ot, oh = self._given(q_out, "q_out", q, now)
         if k_out is None:
-            k_out = self._empty(k.shape, dtype=k.dtype, device=device)
-        for name, x, like in (("q", q, q), ("k", k, k), ("q_out", q_out, q), ("k_out", k_out, k)):
-            if not x.is_cuda or x.dtype not in self._types or x.dtype is not q.dtype:
-                _check(x, name, self._types if name == "q" else (q.dtype,))
-            if x.dim() != 3 or x.shape[0] != T or x.shape[2] != D or x.shape != like.shape or (x.stride(2) != 1 and x.numel()):
-                raise ValueError(f"{name}: [{T}][heads][{D}] with its last axis contiguous")
-            if x.requires_grad and self._graded():
-                raise ValueError(f"{name}: no gradient passes through (call under torch.no_grad())")
-        for name, x, y in (("q", q, q_out), ("k", k, k_out)):
-            if x.data_ptr() == y.data_ptr() and x.stride() != y.stride() and x.numel():
-                raise ValueError(f"{name}_out: {name}'s own memory with its strides, or other memory")
-            if x.numel() and any(s == 0 and n > 1 for s, n in zip(y.stride(), y.shape)):
-                raise ValueError(f"{name}_out: an element of its own for each of {name}")
-        _check(position, "position", self._int32, (T,))
-        _here(stream, q, k, q_out, k_out, position, self.turn)
-        (qt, qh, _), (kt, kh, _), (ot, oh, _), (pt, ph, _) = q.stride(), k.stride(), q_out.stride(), k_out.stride()
-        heads = festina_heads(T, q.shape[1], k.shape[1], self._types[q.dtype], position.data_ptr(), q.data_ptr(),
-                              k.data_ptr(), qt, qh, kt, kh, q_out.data_ptr(), k_out.data_ptr(), ot, oh, pt, ph)
-        st = self._rotate(self._ref, C.byref(heads), _stream_handle(stream))
+            k_out = self._empty((T, kv_heads, D), dtype=dtype, device=q.device)
+            pt, ph = kv_heads * D, D
+        else:
+            pt, ph = self._given(k_out, "k_out", k, now)
+        if self.turn.get_device() != now:
+            _on_device(self.turn, "the rotary", now)
+        st = self._rotate(self._ref, C.byref(festina_heads(
+            T, heads, kv_heads, kind, here.ints(position, "position", T, now), q.data_ptr(), k.data_ptr(), qt, qh, kt, kh,
+            q_out.data_ptr(), k_out.data_ptr(), ot, oh, pt, ph)), here.stream(stream, now))
         if st != FESTINA_OK:
             raise FestinaError(st, "festina_rotate_heads")
         if stream is not None:
             _used_on(stream, q, k, position, q_out, k_out, self.turn, *(w for w in self.weights if w is not None))
         return q_out, k_out
+
+    def _given(self, y, name, x, now):
+        """Strides of an output that the caller brings for x."""
+        _check(y, name, (x.dtype,))
+        _on_device(y, name, now)
+        if y.shape != x.shape or (y.stride(2) != 1 and y.numel()):
+            raise ValueError(f"{name}: the shape {tuple(x.shape)} with its last axis contiguous")
+        if y.requires_grad and self._graded():
+            raise ValueError(f"{name}: no gradient passes through (call under torch.no_grad())")
+        if y.numel():
+            if x.data_ptr() == y.data_ptr() and x.stride() != y.stride():
+                raise ValueError(f"{name}: the input's own memory with its strides, or other memory")
+            if any(s == 0 and n > 1 for s, n in zip(y.stride(), y.shape)):
+                raise ValueError(f"{name}: an element of its own for each of the input")
+        return y.stride()[:2]
 
 
 def _turn(radians: float) -> int:
