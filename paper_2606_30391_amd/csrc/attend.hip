@@ -62,8 +62,9 @@ constexpr int kWaves = 4;
 constexpr int kBlock = 64 * kWaves;
 // Waves of k_rows on a SIMD, and the pieces that it cuts the keys into: one for each wave of 256 compute units.  (Three
 // waves of 128 dims and one row tile, 168 registers each, were slower: 64 requests up to 32,768 tokens 473 us against 440.)
-constexpr int waves_of(int D, int NT) { return D > 128 || NT > 2 ? 1 : 2; }
-constexpr int workers_of(int D, int NT) { return 1024 * waves_of(D, NT); }
+// (32 rows of a tree of 128 dims would lack ten registers for two waves.)
+constexpr int waves_of(int D, int NT, bool tree) { return D > 128 || NT > 2 || (tree && D == 128 && NT == 2) ? 1 : 2; }
+constexpr int workers_of(int D, int NT, bool tree) { return 1024 * waves_of(D, NT, tree); }
 constexpr int kGroups = 512;         // workgroups of k_tiles that fill the chip: two a compute unit
 constexpr int kJoins = 2048;         // and of its join: eight
 constexpr int kWaveRequests = 64;    // requests whose running sums a wave forms in its registers
@@ -332,6 +333,9 @@ __device__ __forceinline__ TreeSpan tree_span(const AttArgs &a, const Request &q
   return TreeSpan{from, in ? before : 0, word};
 }
 
+// What this wave wrote to LDS is there for it.
+__device__ __forceinline__ void lds_wave() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
+
 // Keeps a rare branch a branch: without it the compiler computes the masks of every step.
 __device__ __forceinline__ void rarely() { asm volatile(""); }
 
@@ -402,7 +406,7 @@ struct RowsStep {
   bool ok;
 };
 
-template <typename T, int D, int NT>
+template <typename T, int D, int NT, bool TREE = false>
 struct Rows {
   static constexpr int kRows = 16 * NT, kSteps = D / 32, kPitch = D + 4;
 
@@ -446,7 +450,7 @@ struct Rows {
     typename Vec8<T>::type q[NT][kSteps];
     f4 o[NT][D / 16];
     float m[NT], l[NT];
-    Span sees[NT];
+    typename Seen<TREE>::type sees[NT];
   };
 
   static __device__ __forceinline__ void step(const AttArgs &a, const Request &rq, int base, int pos_min, int pos_max,
@@ -479,11 +483,21 @@ struct Rows {
         for (int i = 0; i < 4; ++i) x[nt][u][i] = fmaf(x[nt][u][i], c, shift);
       if (masked) {
         rarely();
-        const Span sees{st.sees[nt].from - base - 16 * g, s.ok ? st.sees[nt].count : 0};
+        if constexpr (TREE) {
+          lds_wave();                                  // (read here, not kept over the steps)
+          const Bits sees = st.sees[nt].at(base + 16 * g);
+          const unsigned seen = s.ok ? (unsigned)sees.word : 0u;
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
+          for (int u = 0; u < 4; ++u)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[nt][u][i] = sees.has(4 * u + i) ? x[nt][u][i] : kNegInf();
+            for (int i = 0; i < 4; ++i) x[nt][u][i] = seen >> (4 * u + i) & 1 ? x[nt][u][i] : kNegInf();
+        } else {
+          const Span sees{st.sees[nt].from - base - 16 * g, s.ok ? st.sees[nt].count : 0};
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[nt][u][i] = sees.has(4 * u + i) ? x[nt][u][i] : kNegInf();
+        }
       }
       float top = x[nt][0][0];
 #pragma unroll
@@ -539,9 +553,16 @@ struct Rows {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
               h8 sees;
+              if constexpr (TREE) {
+                lds_wave();
+                const unsigned seen = s.ok ? (unsigned)st.sees[nt].at(base + 16 * g + 8 * i).word : 0u;
 #pragma unroll
-              for (int j = 0; j < 8; ++j)
-                sees[j] = s.ok && st.sees[nt].has(base + 16 * g + 8 * i + j) ? (f16)1.f : (f16)0.f;
+                for (int j = 0; j < 8; ++j) sees[j] = seen >> j & 1 ? (f16)1.f : (f16)0.f;
+              } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                  sees[j] = s.ok && st.sees[nt].has(base + 16 * g + 8 * i + j) ? (f16)1.f : (f16)0.f;
+              }
               hits = mfma16(decode8<f16>(nan[2 * i] & kOnes, nan[2 * i + 1] & kOnes), sees, hits);
             }
 #pragma unroll
@@ -562,16 +583,29 @@ struct Rows {
   }
 
   // Rows `tile` of request r and key head h: every `stride`th of its units from k0 to k1.
+  // (`spans`: in LDS, kRows of them; the waves of a workgroup write the same.)
   static __device__ __forceinline__ void scan_keys(const AttArgs &a, int r, const Request &rq, int h, int tile, int k0,
-                                                   int k1, int stride, State &st) {
+                                                   int k1, int stride, TreeSpan *spans, State &st) {
     const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
     const int rows = rq.n * a.G, row0 = tile * kRows, before = rq.length - rq.n;
-    const int pos_min = before + row0 / a.G, pos_max = before + (min(row0 + kRows, rows) - 1) / a.G;
+    if constexpr (TREE) {                              // (a lane a row, before anything is held in registers)
+      const int i = row0 + lane, t = i / a.G;
+      const bool in = lane < kRows && i < rows;
+      const TreeSpan sees = tree_span(a, rq, in ? a.seen[rq.first + t] : 0ull, in);
+      if (lane < kRows) spans[lane] = sees;
+      lds_wave();
+    }
+    const int pos_min = TREE ? before - 1 : before + row0 / a.G;
+    const int pos_max = TREE ? rq.length - 1 : before + (min(row0 + kRows, rows) - 1) / a.G;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const int i = row0 + nt * 16 + c, t = i / a.G;
       const bool in = i < rows;
-      st.sees[nt] = span(a, in ? before + t : -1);
+      if constexpr (TREE) {
+        st.sees[nt].span = spans + nt * 16 + c;
+      } else {
+        st.sees[nt] = span(a, in ? before + t : -1);
+      }
       st.m[nt] = kNegInf();
       st.l[nt] = 0.f;
 #pragma unroll
@@ -603,10 +637,10 @@ struct Rows {
 
   // One wave's keys alone: the rows themselves (part < 0), or the piece's result at its place.
   static __device__ __forceinline__ void piece(const AttArgs &a, int r, const Request &rq, int h, int tile, int k0, int k1,
-                                               int part) {
+                                               int part, TreeSpan *spans) {
     const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
     State st;
-    scan_keys(a, r, rq, h, tile, k0, k1, 1, st);
+    scan_keys(a, r, rq, h, tile, k0, k1, 1, spans, st);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const int i = tile * kRows + nt * 16 + c;
@@ -628,11 +662,12 @@ struct Rows {
   }
 
   // A workgroup's keys: its waves' parts of each row joined in LDS.
-  static __device__ __forceinline__ void whole(const AttArgs &a, int r, const Request &rq, int h, int tile, Shared &sh) {
+  static __device__ __forceinline__ void whole(const AttArgs &a, int r, const Request &rq, int h, int tile, TreeSpan *spans,
+                                               Shared &sh) {
     const int lane = threadIdx.x & 63, wave = same((int)threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
     const int rows = rq.n * a.G, row0 = tile * kRows;
     State st;
-    scan_keys(a, r, rq, h, tile, wave, units(a, rq), kWaves, st);
+    scan_keys(a, r, rq, h, tile, wave, units(a, rq), kWaves, spans, st);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       if (g == 0) {
@@ -681,22 +716,24 @@ __device__ __forceinline__ int pieces(const AttArgs &a, long long all) {
 __device__ __forceinline__ long long piece_start(long long all, int w, int n) { return all * w / n; }
 
 // A workgroup for each row tile and key head, its waves over the keys in turn: few keys, one launch.
-template <typename T, int D, int NT>
-__global__ void __launch_bounds__(kBlock, (D <= 128 && NT <= 2) ? 2 : 1) k_rows_whole(AttArgs a) {
-  typedef Rows<T, D, NT> K;
+template <typename T, int D, int NT, bool TREE>
+__global__ void __launch_bounds__(kBlock, waves_of(D, NT, TREE)) k_rows_whole(AttArgs a) {
+  typedef Rows<T, D, NT, TREE> K;
   __shared__ typename K::Shared sh;
+  __shared__ TreeSpan spans[TREE ? K::kRows : 1];
   const int tile = blockIdx.x % a.tiles_each, rest = blockIdx.x / a.tiles_each, h = rest % a.H, r = rest / a.H;
   const Request rq = request(a, r);
   const int rows = rq.n * a.G;
   if (rows > a.rows_max || tile * K::kRows >= rows) return;
-  K::whole(a, r, rq, h, tile, sh);
+  K::whole(a, r, rq, h, tile, spans, sh);
 }
 
 // A wave a piece.
-template <typename T, int D, int NT>
-__global__ void __launch_bounds__(64, waves_of(D, NT)) k_rows(AttArgs a) {
-  typedef Rows<T, D, NT> K;
+template <typename T, int D, int NT, bool TREE>
+__global__ void __launch_bounds__(64, waves_of(D, NT, TREE)) k_rows(AttArgs a) {
+  typedef Rows<T, D, NT, TREE> K;
   __shared__ long long list_[kListed + 1];
+  __shared__ TreeSpan spans[TREE ? K::kRows : 1];
   const long long *list = a.plan;
   if (!list) {
     list_sums(a, [&](int r) { return units_of<K::kRows>(a, r); }, list_);
@@ -724,7 +761,7 @@ __global__ void __launch_bounds__(64, waves_of(D, NT)) k_rows(AttArgs a) {
           cut = Cut{last - w + 2, prior < tile0 ? 1 : 0, tile * K::kRows, rq.n * a.G, rq.first, h * a.G, {0, 0}};
         }
       }
-      K::piece(a, r, rq, h, tile, k0, k1, k0 == 0 && k1 == each ? -1 : min(place, 2 * w + 1));
+      K::piece(a, r, rq, h, tile, k0, k1, k0 == 0 && k1 == each ? -1 : min(place, 2 * w + 1), spans);
       u += k1 - k0;
     }
   }
@@ -1340,9 +1377,11 @@ constexpr int groups_of(int D, int KS) { return 256 * groups_each(D, KS); }
 constexpr int rows_of(int KS) { return 128 / KS; }
 
 // How the keys are dealt to the workgroups.  Few units for each (up to kFew): every row tile is cut into equal parts of at most `part`
-// units and a workgroup has one part, so that none waits for the beginning of a second tile.  Many: all tiles' units form
-// one line that is cut into equal pieces (part = 0), which leaves no workgroup behind, whatever the lengths.
-constexpr int kFew = 16;
+// units and a workgroup has one part, so that none waits for the beginning of a second tile.  Many: all tiles form
+// one line that is cut into pieces of equal cost (part = 0), which leaves no workgroup behind, whatever the lengths; a tile costs its
+// units and kTileCost more for its beginning, a few round trips to memory (32 requests of 512 to 16,384 tokens, trees of 8:
+// 182 us without it).
+constexpr int kFew = 16, kTileCost = 4;
 
 // Units of a request's tiles, and the tiles, of all key heads.
 struct Tiles {
@@ -1356,7 +1395,7 @@ __device__ __forceinline__ Tiles draft_tiles(const AttArgs &a, int r) {
 template <int ROWS>
 __device__ __forceinline__ long long dealt_of(const AttArgs &a, int r, int part) {
   const Tiles t = draft_tiles<ROWS>(a, r);
-  return (long long)(part ? cdiv(t.units, part) : t.units) * t.tiles;
+  return (long long)(part ? cdiv(t.units, part) : t.units + kTileCost) * t.tiles;
 }
 // Units of a part, from all units and tiles; `room` is the most parts that there may be (a tile makes at most one more than
 // its share of the units).
@@ -1440,12 +1479,14 @@ __device__ __forceinline__ void deal(const AttArgs &a, int groups, long long *li
     const Request q = in ? request(a, lane) : Request{0, 0, 0};
     const bool has = in && q.n > 0 && q.n <= kNodes;
     const int u = has ? units(a, q) : 0, tiles = has ? cdiv(q.n * a.G, ROWS) * a.H : 0;
-    const long long all_units = wave_sum((long long)u * tiles);
-    all_tiles = same(wave_sum(tiles));
-    part = part_of(all_units, all_tiles, groups, room);
+    // (a request's units count up to 2^20 here: more than the most that parts are made of)
+    const int U = same(wave_sum((int)min((long long)u * tiles, 1ll << 20))), tiles_before = wave_before(tiles);
+    all_tiles = same(__shfl(tiles_before + tiles, 63));
+    part = part_of(U, all_tiles, groups, room);
     if (part && all_tiles < groups) {
-      // a second round would double the time: longer parts, as many as the sum is over the chip's workgroups
-      const int U = (int)all_units;
+      // a second round would double the time: parts so long that there are no more than the chip's workgroups (a tile's
+      // last part is half a part on average)
+      part = cdiv(U, groups - all_tiles / 2);
       for (int i = 0; i < 3; ++i) {
         const int over = same(wave_sum(cdiv(u, part) * tiles)) - groups;
         if (over <= 0) break;
@@ -1453,9 +1494,7 @@ __device__ __forceinline__ void deal(const AttArgs &a, int groups, long long *li
         part = max(share > 0 ? cdiv(U, share) : 2 * part, part + 1);
       }
     }
-    part = same(part);
-    const long long mine = (long long)(part ? cdiv(u, part) : u) * tiles;
-    const int tiles_before = wave_before(tiles);
+    const long long mine = (long long)(part ? cdiv(u, part) : u + kTileCost) * tiles;
     if (part) {
       const int before = wave_before((int)mine);
       all = same(__shfl(before + (int)mine, 63));
@@ -1632,25 +1671,28 @@ __global__ void __launch_bounds__(kBlock, groups_each(D, KS)) k_drafts(AttArgs a
         begin = same(list[r]);
         each = units(b, rq);
       }
-      const int cuts = part ? cdiv(each, part) : each, tiles = cdiv(rq.n * b.G, kRows);
-      const int at = (int)quotient(u - begin, cuts), off = (int)(u - begin - (long long)at * cuts);
+      const int cost = part ? cdiv(each, part) : each + kTileCost, tiles = cdiv(rq.n * b.G, kRows);
+      const int at = (int)quotient(u - begin, cost), off = (int)(u - begin - (long long)at * cost);
       typename K::Work k;
       k.rq = rq;
       k.h = at / tiles;
       k.row0 = at % tiles * kRows;
       k.rows = rq.n * b.G;
-      int k0 = off, k1 = (int)min((long long)each, off + (same(work.end) - u));
-      if (part) k0 = each * off / cuts, k1 = each * (off + 1) / cuts;   // (at most groups * kFew units in all)
+      const int stop = part ? off + 1 : (int)min((long long)cost, off + (same(work.end) - u));
+      int k0 = max(off - kTileCost, 0), k1 = max(stop - kTileCost, 0);
+      if (part) k0 = each * off / cost, k1 = each * stop / cost;        // (at most groups * kFew units in all)
+      u += stop - off;
+      if (k0 >= k1) continue;                          // no more than a tile's beginning: the next piece has it
       const bool whole = k0 == 0 && k1 == each;
       k.part = whole ? -1 : part ? w : 2 * w + min(place, 1);
       if (k0 == 0 && threadIdx.x == 0) {
         // the tile's first part says where the others are
         DraftCut cut{0, w, w + 1, 1, k.row0, k.rows, rq.first, k.h * b.G};
         if (part) {
-          cut.n = whole ? 0 : cuts;
+          cut.n = whole ? 0 : cost;
         } else {
           const long long all = work.all, n = min(all, (long long)groups_of(D, KS));
-          const int last = (int)(((begin + (long long)(at + 1) * each) * n - 1) / all);      // piece of the tile's last unit
+          const int last = (int)(((begin + (long long)(at + 1) * cost) * n - 1) / all);      // piece of the tile's last unit
           cut.n = whole ? 0 : last - w + 1;
           cut.p0 = k.part, cut.p1 = 2 * (w + 1), cut.step = 2;
         }
@@ -1658,7 +1700,6 @@ __global__ void __launch_bounds__(kBlock, groups_each(D, KS)) k_drafts(AttArgs a
         const int j = work.by_tile ? (part ? work.tile : work.tiles[r]) + at : w;
         if (work.by_tile ? j < b.cuts_most : !whole) out[j] = cut;
       }
-      u += part ? 1 : k1 - k0;
       const int first = first_unit(b, rq);
       k.u0 = first + k0;
       k.u1 = first + k1;
@@ -1803,26 +1844,30 @@ festina_status shape_of(const festina_kv_cache *c, const festina_attention *t, b
   const long long most = (long long)t->max_new * G;                   // rows of one request and key head
   const int nt_most = row_tiles_most(D);
   *s = Shape{};
-  s->tiles = drafts ? t->max_new > kNodes : most > 16 * nt_most && t->max_new > 1;
+  const long long keys = (long long)t->max_blocks * c->block_tokens;
+  s->cut = keys > 2 * kWaves * kUnit;
+  // Trees of up to 16 rows are k_rows', and up to 32 of tables that one launch does (one request of 403 tokens, trees of 8: 12.1 us
+  // and one launch, 12.7 and two); the others k_drafts' (32 rows of 128 dims, us by k_rows and by k_drafts: 32 requests of the
+  // fleet's lengths 35 and 30, of 512 to 16,384 tokens 160 and 147; 16 rows: 27 and 28, 124 and 143).
+  const bool trees = drafts && most > 16 && (s->cut || most > 16 * min(nt_most, 2));
+  s->tiles = trees ? t->max_new > kNodes : most > 16 * nt_most && t->max_new > 1;
   const long long rows = s->tiles ? G : most;                         // with prompts about: the single tokens' rows
   s->nt = rows <= 16 ? 1 : min(rows <= 32 ? 2 : 4, nt_most);
   s->join_rows = (int)min(rows, 16ll * s->nt);
   if (s->tiles && G > 16 * nt_most) s->nt = 0;
   s->rows_max = s->tiles ? 16 * s->nt : INT_MAX;
-  if (drafts) {                                        // k_drafts has the trees, k_tiles the runs
+  if (trees) {                                         // k_drafts has the trees, k_tiles the runs
     s->halves = D > 128 || min(most, (long long)kNodes * G) <= rows_of(2) ? 2 : 1;      // (128 rows of 256 dims do not fit the registers)
     s->join_rows = (int)min(most, (long long)rows_of(s->halves));
     s->nt = 0;
     s->rows_max = kNodes * G;
   }
-  const long long keys = (long long)t->max_blocks * c->block_tokens;
   s->tiles_each = (int)((rows + 16 * s->nt - 1) / max(16 * s->nt, 1));
-  s->cut = keys > 2 * kWaves * kUnit;
   if (s->nt && !s->cut && (long long)t->n_requests * H * s->tiles_each > kThreadsMost / kBlock)
     return FESTINA_ERR_UNSUPPORTED;
   size_t parts = 0;
-  if (s->nt && s->cut) parts = (size_t)2 * workers_of(D, s->nt) * 16 * s->nt;
-  if (drafts) {
+  if (s->nt && s->cut) parts = (size_t)2 * workers_of(D, s->nt, drafts) * 16 * s->nt;
+  if (trees) {
     // one for each part of a step of few keys: at most a tile more each than the chip's workgroups
     const int groups = groups_of(D, s->halves);
     const int rows = rows_of(s->halves), some = min(t->n_requests, t->n_tokens);
@@ -1857,22 +1902,24 @@ festina_status shape_of(const festina_kv_cache *c, const festina_attention *t, b
   }
   s->plan = 0;
   s->cuts = up((size_t)2 * (t->n_requests + 1) * 8);
-  s->joins = s->cuts + up((size_t)(drafts ? s->draft_groups : workers_of(D, max(s->nt, 1))) * sizeof(Cut));
+  s->joins = s->cuts + up((size_t)(trees ? s->draft_groups : workers_of(D, max(s->nt, 1), drafts)) * sizeof(Cut));
   s->part_ml = s->joins + up((kGroups + 1) * sizeof(int4));
   s->part_o = s->part_ml + up(parts * 8);
   s->bytes = s->part_o + up(parts * D * 4);
   return FESTINA_OK;
 }
 
-template <typename T, int D, int NT>
+template <typename T, int D, int NT, bool TREE>
 void run_rows(AttArgs a, const Shape &s, hipStream_t st) {
-  a.workers = workers_of(D, NT);
+  a.workers = workers_of(D, NT, TREE);
   if (!s.cut) {
-    k_rows_whole<T, D, NT><<<(unsigned)(a.R * a.H * s.tiles_each), kBlock, 0, st>>>(a);
+    k_rows_whole<T, D, NT, TREE><<<(unsigned)(a.R * a.H * s.tiles_each), kBlock, 0, st>>>(a);
     return;
   }
-  k_rows<T, D, NT><<<a.workers, 64, 0, st>>>(a);
-  k_rows_join<T, D, NT><<<dim3(a.workers - 1, (s.join_rows + kWaves - 1) / kWaves), kBlock, 0, st>>>(a);
+  if constexpr (!TREE || NT == 1) {                    // (more rows of trees come here uncut only)
+    k_rows<T, D, NT, TREE><<<a.workers, 64, 0, st>>>(a);
+    k_rows_join<T, D, NT><<<dim3(a.workers - 1, (s.join_rows + kWaves - 1) / kWaves), kBlock, 0, st>>>(a);
+  }
 }
 
 template <typename T, int D, int KS>
@@ -1898,11 +1945,12 @@ void run(AttArgs a, const Shape &s, long long *plan, hipStream_t st) {
     else k_plan<64><<<1, 1024, 0, st>>>(a, plan);
     a.plan = plan;
   }
-  if (s.nt == 1) run_rows<T, D, 1>(a, s, st);
+  const bool tree = a.seen && s.nt;
+  if (s.nt == 1) tree ? run_rows<T, D, 1, true>(a, s, st) : run_rows<T, D, 1, false>(a, s, st);
   if constexpr (row_tiles_most(D) >= 2)
-    if (s.nt == 2) run_rows<T, D, 2>(a, s, st);
+    if (s.nt == 2) tree ? run_rows<T, D, 2, true>(a, s, st) : run_rows<T, D, 2, false>(a, s, st);
   if constexpr (row_tiles_most(D) >= 4)
-    if (s.nt == 4) run_rows<T, D, 4>(a, s, st);
+    if (s.nt == 4) run_rows<T, D, 4, false>(a, s, st);
   if (s.tiles) {
     const unsigned grid = (unsigned)s.tile_groups;
     if constexpr (D == 96 || D == 128)
