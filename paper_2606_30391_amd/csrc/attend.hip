@@ -1380,8 +1380,9 @@ constexpr int rows_of(int KS) { return 128 / KS; }
 // units and a workgroup has one part, so that none waits for the beginning of a second tile.  Many: all tiles form
 // one line that is cut into pieces of equal cost (part = 0), which leaves no workgroup behind, whatever the lengths; a tile costs its
 // units and kTileCost more for its beginning, a few round trips to memory (32 requests of 512 to 16,384 tokens, trees of 8:
-// 182 us without it).
-constexpr int kFew = 16, kTileCost = 4;
+// 182 us without it, 148 with).  64 requests of the fleet's lengths, 10 units a workgroup: in parts 50 us, in pieces 44; 32 requests, 5
+// units: 35 and 39.
+constexpr int kFew = 8, kTileCost = 4;
 
 // Units of a request's tiles, and the tiles, of all key heads.
 struct Tiles {
@@ -1639,8 +1640,7 @@ struct Halves {
 template <typename T, int D, int KS>
 __global__ void __launch_bounds__(kBlock, groups_each(D, KS)) k_drafts(AttArgs a) {
   typedef DraftTile<T, D, KS> K;
-  // units on their way from memory: two where registers allow
-  constexpr int kRows = K::kRows, kDeep = KS == 2 && D > 64 && D <= 128 ? 2 : 1;
+  constexpr int kRows = K::kRows;
   __shared__ KeyTile<T, D> keys[2];
   __shared__ union { ValueTile<D, kWaves> tile[2]; Halves<D> halves; } values;
   __shared__ TreeSpan spans[kRows];
@@ -1711,40 +1711,33 @@ __global__ void __launch_bounds__(kBlock, groups_each(D, KS)) k_drafts(AttArgs a
       const auto look = [&](int unit) {
         return unit * kUnit + kUnit > before || (a.window > 0 && unit * kUnit < rq.length - a.window);
       };
-      Stage<T, D, kWaves> g[kDeep];                    // what is on its way: the units behind the one that is worked on
-      const auto load = [&](Stage<T, D, kWaves> &s, int u) {
-        s.load_keys(a, k.h, u * kUnit);
-        s.load_values(a, u * kUnit);
+      // the unit behind the one that is worked on is on its way (two of them, in registers, were no faster)
+      Stage<T, D, kWaves> g;
+      const auto load = [&](int u) {
+        g.load_keys(a, k.h, u * kUnit);
+        g.load_values(a, u * kUnit);
+        g.blocks(a, table, (u + 1) * kUnit);
       };
-      const auto store = [&](Stage<T, D, kWaves> &s, int u) {
-        s.put_keys(keys[u & 1]);
-        s.put_scales(a, keys[u & 1]);
+      const auto store = [&](int u) {
+        g.put_keys(keys[u & 1]);
+        g.put_scales(a, keys[u & 1]);
         if (look(u)) {
           rarely();
-          s.clean_values(rq.length - u * kUnit, values.tile[u & 1]);
+          g.clean_values(rq.length - u * kUnit, values.tile[u & 1]);
         }
-        s.put_values(values.tile[u & 1]);
+        g.put_values(values.tile[u & 1]);
       };
-#pragma unroll
-      for (int i = 0; i < kDeep; ++i) {
-        g[i].begin(b, k.h, thread);
-        g[i].blocks(b, table, (k.u0 + i) * kUnit);
-      }
+      g.begin(b, k.h, thread);
+      g.blocks(b, table, k.u0 * kUnit);
       const unsigned long long word = K::begin(b, k, thread, st);
-#pragma unroll
-      for (int i = 0; i < kDeep; ++i)
-        if (i == 0 || k.u0 + i < k.u1) load(g[i], k.u0 + i);
-      g[0].blocks(a, table, (k.u0 + kDeep) * kUnit);
+      load(k.u0);
       K::sees(b, k, thread, word, spans, st);
       const bool live = k.row0 + K::side(thread) * 32 < k.rows;
-      store(g[0], k.u0);
+      store(k.u0);
       lds_barrier();
-      const auto step = [&](int u, Stage<T, D, kWaves> &next, Stage<T, D, kWaves> &free) {
+      for (int u = k.u0; u < k.u1; ++u) {
         const int base = u * kUnit;
-        if (u + kDeep < k.u1) {
-          load(free, u + kDeep);
-          (kDeep == 2 ? next : free).blocks(a, table, (u + kDeep + 1) * kUnit);
-        }
+        if (u + 1 < k.u1) load(u + 1);
         if (live) {
           st.products(keys[u & 1]);
           st.logits(keys[u & 1], base, look(u));
@@ -1756,13 +1749,8 @@ __global__ void __launch_bounds__(kBlock, groups_each(D, KS)) k_drafts(AttArgs a
             st.template sums<1>(values.tile[u & 1]);
           }
         }
-        if (u + 1 < k.u1) store(next, u + 1);
+        if (u + 1 < k.u1) store(u + 1);
         lds_barrier();
-      };
-      for (int u = k.u0; u < k.u1; u += kDeep) {
-        step(u, g[kDeep - 1], g[0]);
-        if constexpr (kDeep == 2)
-          if (u + 1 < k.u1) step(u + 1, g[0], g[1]);
       }
       float l = across32(st.l, add_), m = st.sums_kept == kSums ? st.ref : kNegInf();
       const AttArgs &e = (&a)[same(nought)];

@@ -9,8 +9,8 @@
 // k_accept_drafts  from node 0 on, the first child whose token the model chose there: one comparison of all
 //   nodes with their parents' choices, then a ballot a node of the path.
 // k_keep_tokens    a wave for a request, key head, layer, and keys or values.  Kept token i comes from path[i] >= i, in ascending
-//   order, so that a token's new slot never lies behind the slots still to be read: kMoved tokens at a time are read, then
-//   written.  A block's scale afterwards is the largest among the blocks that its tokens came from; scales are
+//   order, so that a token's new slot never lies behind the slots still to be read: some tokens at a time are read, then
+//   written.  The first codes are on their way together with the scales, whose largest each block waits for.  A block's scale afterwards is the largest among the blocks that its tokens came from; scales are
 //   powers of two, so codes are multiplied exactly and rounded once (only where they become subnormal).
 //
 // All three are bound by latency: a launch and a chain of three to six dependent reads.
@@ -117,18 +117,21 @@ __global__ void __launch_bounds__(64 * kWaves) k_accept_drafts(DraftArgs a) {
 
 // ------------------------------------------------------------------ the accepted tokens' keys and values
 
-constexpr int kLayers = 64;          // caches of a launch (their addresses are arguments)
+// Caches of a launch: their addresses are arguments, which take a while to hand over where there are many.
+constexpr int kFewLayers = 8, kLayers = 64;
 
 struct Layer {
   uint8_t *codes[2];
   float *scale[2];
 };
+template <int LAYERS>
 struct KeepArgs {
-  int32_t R, MB, T, H, D, shift, NB;
+  int32_t R, MB, T, H, shift, NB;
   const int32_t *table, *length, *first, *path, *kept;
-  Layer layer[kLayers];
+  Layer layer[LAYERS];
 };
 
+typedef unsigned u4 __attribute__((ext_vector_type(4)));
 typedef float f2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ unsigned recode4(unsigned c, float ratio) {
@@ -141,113 +144,154 @@ __device__ __forceinline__ unsigned recode4(unsigned c, float ratio) {
 // Everything read so far has arrived: what is written next may lie where it was.
 __device__ __forceinline__ void all_read() { __builtin_amdgcn_s_waitcnt(0); }
 
-__global__ void __launch_bounds__(64) k_keep_tokens(KeepArgs a) {
-  __shared__ unsigned most[kNodes / 16 + 1];           // the new scale of each block from the first changed one on
-  __shared__ int block_[kNodes / 16 + 1];
-  __shared__ int2 from_[kNodes];                       // of each moved token: slot where it was,
-  __shared__ int2 to_[kNodes];                         //   slot where it goes, and the factor of its codes
+template <int LAYERS, int D>
+__global__ void __launch_bounds__(64) k_keep_tokens(KeepArgs<LAYERS> a) {
+  constexpr int kBlocks = kNodes / 16 + 1;             // that 64 tokens lie in
+  __shared__ unsigned most[kBlocks];                   // the new scale of each block from the first changed one on
+  __shared__ int2 from_[kNodes], to_[kNodes];          // of each moved token: block and slot where it was, and where it goes
+  __shared__ float factor_[kNodes];                    // of its codes
   const int lane = threadIdx.x, which = blockIdx.y & 1, bt = 1 << a.shift;
   const Layer &layer = a.layer[blockIdx.y >> 1];
   const int h = blockIdx.x % a.H, r = blockIdx.x / a.H;
+  const int length = a.length[r], some = a.kept[r];
   const int2 q = tokens_of(a.first, a.T, r);
-  const int before = same(a.length[r]) - q.y, kept = min(same(a.kept[r]), q.y);
+  const int before = same(length) - q.y, kept = min(same(some), q.y);
   if (q.y > kNodes || kept < 1 || before < 0 || before + q.y > a.MB << a.shift) return;
+  const int c_base = before >> a.shift, cols = ((before + q.y - 1) >> a.shift) - c_base + 1;    // the new tokens' columns
+  const int at_col = lane < cols ? a.table[(size_t)r * a.MB + c_base + lane] : 0;
   const int mine = lane < kept ? a.path[q.x + lane] : INT_MAX;
   const int prior = __shfl_up(mine, 1);
-  // ascending and of its own tokens, which makes path[i] >= i
-  if (__any(lane < kept && ((unsigned)mine >= (unsigned)q.y || (lane > 0 && prior >= mine)))) return;
+  // ascending and of its own tokens, which makes path[i] >= i; and blocks that there are
+  const bool bad = lane < kept && ((unsigned)mine >= (unsigned)q.y || (lane > 0 && prior >= mine));
   const unsigned long long moves = __ballot(lane < kept && mine != lane);
-  if (moves == 0) return;
-  const int m = __builtin_ctzll(moves), c0 = (before + m) >> a.shift;   // first token that moves, and its column
-  const int c1 = (before + q.y - 1) >> a.shift;        // the request's last column
-  const int32_t *table = a.table + (size_t)r * a.MB;
-  const int at_col = lane <= c1 - (before >> a.shift) ? table[(before >> a.shift) + lane] : 0;
-  if (__any((unsigned)at_col >= (unsigned)a.NB)) return;
-  const int c_base = before >> a.shift;
+  if (__any(bad || (unsigned)at_col >= (unsigned)a.NB) || moves == 0) return;
+  const int m = __builtin_ctzll(moves), n = kept - m;  // the first token that moves, and how many
+  const int c0 = (before + m) >> a.shift, stay = (before + m) & (bt - 1);
   uint8_t *codes = layer.codes[which];
   float *scales = layer.scale[which];
-  if (lane < kNodes / 16 + 1) {
-    most[lane] = 0u;
-    block_[lane] = 0;
-  }
-  __syncthreads();
-  const int to = before + lane, since = before + min(mine, q.y - 1);
+  const size_t head = (size_t)D << a.shift;          // codes of a block and head
+  const auto block_of = [&](int b) { return codes + ((size_t)b * a.H + h) * head; };
+  const int last = before + q.y - 1, to = min(before + lane, last), since = before + min(mine, q.y - 1);
   const bool moved = lane >= m && lane < kept;
-  const int b_to = __shfl(at_col, (min(to, before + q.y - 1) >> a.shift) - c_base), b_from = __shfl(at_col, (since >> a.shift) - c_base);
+  const int b_to = __shfl(at_col, (to >> a.shift) - c_base), b_from = __shfl(at_col, (since >> a.shift) - c_base);
+  const int b_first = __shfl(at_col, c0 - c_base);
+  if (moved) {
+    from_[lane - m] = make_int2(b_from, since & (bt - 1));
+    to_[lane - m] = make_int2(b_to, to & (bt - 1));
+  }
+  if (lane < kBlocks) most[lane] = 0u;
+  __syncthreads();
+
+  // keys: 16 codes of a token a lane and load; values: one, whose neighbours are other rows'
+  constexpr int kKeys = 4, kValues = 16;
+  const int groups = D / 16, keys = n * groups, values = n * D;
+  u4 k[kKeys];
+  unsigned v[kValues];
+  const auto key_at = [&](int i, const int2 *place) {
+    const int t = i / groups;
+    return reinterpret_cast<u4 *>(block_of(place[t].x) + (size_t)place[t].y * D + (i - t * groups) * 16);
+  };
+  const auto value_at = [&](int i, const int2 *place) {
+    const int t = i / D;
+    return block_of(place[t].x) + (size_t)(i - t * D) * bt + place[t].y;
+  };
+  const auto read_keys = [&](int i0) {
+#pragma unroll
+    for (int y = 0; y < kKeys; ++y)
+      if (i0 + y * 64 + lane < keys) k[y] = *key_at(i0 + y * 64 + lane, from_);
+  };
+  const auto read_values = [&](int i0) {
+#pragma unroll
+    for (int y = 0; y < kValues; ++y)
+      if (i0 + y * 64 + lane < values) v[y] = *value_at(i0 + y * 64 + lane, from_);
+  };
+  if (which == 0) read_keys(0);
+  else read_values(0);
   const float s_from = moved ? scales[(size_t)b_from * a.H + h] : 0.f;
-  // tokens of the first changed block that stay where they are
-  const int b_first = __shfl(at_col, c0 - c_base), stay = (before + m) & (bt - 1);
-  const float s_stay = stay ? scales[(size_t)b_first * a.H + h] : 0.f;
+  const float s_stay = stay ? scales[(size_t)b_first * a.H + h] : 0.f;     // tokens of the first changed block that stay
   if (moved) atomicMax(&most[(to >> a.shift) - c0], __float_as_uint(s_from));
   if (lane == 0 && stay) atomicMax(&most[0], __float_as_uint(s_stay));
+  all_read();
   __syncthreads();
-  const int n = kept - m;
   const float s_first = __uint_as_float(most[0]);
   if (moved) {
     const float s_to = __uint_as_float(most[(to >> a.shift) - c0]);
-    from_[lane - m] = make_int2(b_from, since & (bt - 1));
-    to_[lane - m] = make_int2((b_to << a.shift) | (to & (bt - 1)), (int)__float_as_uint(s_to > 0.f ? s_from / s_to : 1.f));
+    factor_[lane - m] = s_to > 0.f ? s_from / s_to : 1.f;
     if (lane == m || (to & (bt - 1)) == 0) scales[(size_t)b_to * a.H + h] = s_to;
   }
-  all_read();
   __syncthreads();
-  const size_t head = (size_t)a.D << a.shift;          // codes of a block and head
-  const auto block_of = [&](int b) { return codes + ((size_t)b * a.H + h) * head; };
-  if (stay && s_first > s_stay) {
+  if (stay && s_first > s_stay) {                      // the tokens that stay, anew, before others come beside them
     const float ratio = s_stay / s_first;
     uint8_t *c = block_of(b_first);
     if (which == 0) {
-      for (int i = lane; i < stay * a.D / 4; i += 64) {
+      for (int i = lane; i < stay * D / 4; i += 64) {
         unsigned *p = reinterpret_cast<unsigned *>(c) + i;
         *p = recode4(*p, ratio);
       }
     } else {
       const int words = (stay + 3) / 4;
-      for (int i = lane; i < a.D * words; i += 64) {
+      for (int i = lane; i < D * words; i += 64) {
         const int d = i / words, o = (i - d * words) * 4;
         uint8_t *p = c + (size_t)d * bt + o;
-        const unsigned w = *reinterpret_cast<const unsigned *>(p), x = recode4(w, ratio), mask = o + 4 <= stay ? ~0u : (1u << (8 * (stay - o))) - 1;
+        const unsigned w = *reinterpret_cast<const unsigned *>(p), x = recode4(w, ratio);
+        const unsigned mask = o + 4 <= stay ? ~0u : (1u << (8 * (stay - o))) - 1;
         *reinterpret_cast<unsigned *>(p) = (x & mask) | (w & ~mask);
       }
     }
     all_read();
-    __syncthreads();
   }
-  constexpr int kMoved = 8;
   if (which == 0) {
-    const int words = a.D / 4, all = n * words;        // a lane a word of four codes
-    for (int i0 = 0; i0 < all; i0 += 64 * kMoved) {
-      unsigned w[kMoved];
-#pragma unroll
-      for (int k = 0; k < kMoved; ++k) {
-        const int i = i0 + k * 64 + lane, t = i / words;
-        if (i < all) w[k] = *reinterpret_cast<const unsigned *>(block_of(from_[t].x) + (size_t)from_[t].y * a.D + (i - t * words) * 4);
+    for (int i0 = 0; i0 < keys; i0 += 64 * kKeys) {
+      if (i0 > 0) {
+        read_keys(i0);
+        all_read();
       }
-      all_read();
 #pragma unroll
-      for (int k = 0; k < kMoved; ++k) {
-        const int i = i0 + k * 64 + lane, t = i / words;
-        if (i < all)
-          *reinterpret_cast<unsigned *>(block_of(to_[t].x >> a.shift) + (size_t)(to_[t].x & (bt - 1)) * a.D + (i - t * words) * 4) =
-              recode4(w[k], __uint_as_float((unsigned)to_[t].y));
+      for (int y = 0; y < kKeys; ++y) {
+        const int i = i0 + y * 64 + lane;
+        if (i >= keys) continue;
+        const float f = factor_[i / groups];
+        *key_at(i, to_) = u4{recode4(k[y][0], f), recode4(k[y][1], f), recode4(k[y][2], f), recode4(k[y][3], f)};
       }
       all_read();
     }
   } else {
-    for (int d = lane; d < a.D; d += 64) {             // a lane a row
-      for (int t0 = 0; t0 < n; t0 += kMoved) {
-        unsigned w[kMoved];
-#pragma unroll
-        for (int k = 0; k < kMoved; ++k)
-          if (t0 + k < n) w[k] = block_of(from_[t0 + k].x)[(size_t)d * bt + from_[t0 + k].y];
+    for (int i0 = 0; i0 < values; i0 += 64 * kValues) {
+      if (i0 > 0) {
+        read_values(i0);
         all_read();
-#pragma unroll
-        for (int k = 0; k < kMoved; ++k)
-          if (t0 + k < n)
-            block_of(to_[t0 + k].x >> a.shift)[(size_t)d * bt + (to_[t0 + k].x & (bt - 1))] =
-                (uint8_t)recode4(w[k], __uint_as_float((unsigned)to_[t0 + k].y));
       }
+#pragma unroll
+      for (int y = 0; y < kValues; ++y) {
+        const int i = i0 + y * 64 + lane;
+        if (i < values) *value_at(i, to_) = (uint8_t)recode4(v[y], factor_[i / D]);
+      }
+      all_read();
     }
+  }
+}
+
+template <int LAYERS>
+void keep(const festina_kv_cache *caches, int n, const festina_kept &kept, hipStream_t st) {
+  KeepArgs<LAYERS> a;
+  a.R = kept.n_requests;
+  a.MB = kept.max_blocks;
+  a.T = kept.n_tokens;
+  a.H = caches[0].n_kv_heads;
+  a.shift = __builtin_ctz((unsigned)caches[0].block_tokens);
+  a.NB = caches[0].n_blocks;
+  a.table = kept.block_table;
+  a.length = kept.length;
+  a.first = kept.first;
+  a.path = kept.path;
+  a.kept = kept.kept;
+  for (int i = 0; i < n; ++i) a.layer[i] = Layer{{caches[i].k, caches[i].v}, {caches[i].k_scale, caches[i].v_scale}};
+  const dim3 grid((unsigned)((long long)a.R * a.H), (unsigned)(2 * n));
+  switch (caches[0].head_dim) {
+    case 64: k_keep_tokens<LAYERS, 64><<<grid, 64, 0, st>>>(a); break;
+    case 96: k_keep_tokens<LAYERS, 96><<<grid, 64, 0, st>>>(a); break;
+    case 128: k_keep_tokens<LAYERS, 128><<<grid, 64, 0, st>>>(a); break;
+    default: k_keep_tokens<LAYERS, 256><<<grid, 64, 0, st>>>(a); break;
   }
 }
 
@@ -318,29 +362,12 @@ extern "C" festina_status festina_keep_tokens(const festina_kv_cache *caches, in
   if (n_caches == 0 || kept->n_requests == 0 || kept->n_tokens == 0) return FESTINA_OK;
   if ((long long)kept->max_blocks * caches[0].block_tokens > INT_MAX) return FESTINA_ERR_UNSUPPORTED;
   if (!kept->block_table || !kept->length || !kept->first || !kept->path || !kept->kept) return FESTINA_ERR_INVALID;
-  KeepArgs a;
-  a.R = kept->n_requests;
-  a.MB = kept->max_blocks;
-  a.T = kept->n_tokens;
-  a.H = caches[0].n_kv_heads;
-  a.D = caches[0].head_dim;
-  a.shift = __builtin_ctz((unsigned)caches[0].block_tokens);
-  a.NB = caches[0].n_blocks;
-  a.table = kept->block_table;
-  a.length = kept->length;
-  a.first = kept->first;
-  a.path = kept->path;
-  a.kept = kept->kept;
-  const long long groups = (long long)a.R * a.H;
-  if (groups > UINT_MAX / 64) return FESTINA_ERR_UNSUPPORTED;    // threads along one axis of a grid
+  if ((long long)kept->n_requests * caches[0].n_kv_heads > UINT_MAX / 64) return FESTINA_ERR_UNSUPPORTED;      // threads along one axis of a grid
   hipStream_t st = static_cast<hipStream_t>(stream);
-  for (int i0 = 0; i0 < n_caches; i0 += kLayers) {
-    const int n = n_caches - i0 < kLayers ? n_caches - i0 : kLayers;
-    for (int i = 0; i < n; ++i) {
-      const festina_kv_cache &c = caches[i0 + i];
-      a.layer[i] = Layer{{c.k, c.v}, {c.k_scale, c.v_scale}};
-    }
-    k_keep_tokens<<<dim3((unsigned)groups, (unsigned)(2 * n)), 64, 0, st>>>(a);
+  for (int i = 0; i < n_caches; i += kLayers) {
+    const int n = n_caches - i < kLayers ? n_caches - i : kLayers;
+    if (n <= kFewLayers) keep<kFewLayers>(caches + i, n, *kept, st);
+    else keep<kLayers>(caches + i, n, *kept, st);
   }
   return hipGetLastError() == hipSuccess ? FESTINA_OK : FESTINA_ERR_DEVICE;
 }
