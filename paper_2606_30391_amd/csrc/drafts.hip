@@ -183,7 +183,7 @@ __global__ void __launch_bounds__(64) k_keep_tokens(KeepArgs<LAYERS> a) {
   __syncthreads();
 
   // keys: 16 codes of a token a lane and load; values: one, whose neighbours are other rows'
-  constexpr int kKeys = 4, kValues = 16;
+  constexpr int kKeys = 4, kValues = 8;
   const int groups = D / 16, keys = n * groups, values = n * D;
   u4 k[kKeys];
   unsigned v[kValues];

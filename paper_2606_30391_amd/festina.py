@@ -307,7 +307,7 @@ def lib():
         L.festina_attend_drafts.argtypes = [P(festina_kv_cache), P(festina_attention), C.c_void_p, C.c_void_p, C.c_size_t,
                                             C.c_void_p]
         L.festina_attend_drafts.restype = C.c_int
-        L.festina_keep_tokens.argtypes = [P(festina_kv_cache), C.c_int32, P(festina_kept), C.c_void_p]
+        L.festina_keep_tokens.argtypes = [C.c_void_p, C.c_int32, P(festina_kept), C.c_void_p]
         L.festina_keep_tokens.restype = C.c_int
         L.festina_rotate_heads.argtypes = [P(festina_rotary), P(festina_heads), C.c_void_p]
         L.festina_rotate_heads.restype = C.c_int
@@ -795,7 +795,7 @@ class DeviceBlocks:
         self.first, self.slot, self.length, self.n_free_out = i32(R + 1), i32(max(self.max_tokens, 0)), i32(R), i32(1)
         self.served = torch.empty(R, dtype=torch.uint8, device=device)
         self.ws_bytes = festina_blocks_workspace_bytes(R, self.max_tokens)
-        self._ws, self._here = _Workspaces(), _Here()
+        self._ws, self._here, self._trim = _Workspaces(), _Here(), lib().festina_trim_blocks
         self._structs()
 
     def _structs(self):
@@ -827,9 +827,10 @@ class DeviceBlocks:
         at = here.ints(keep, "keep", self.held.numel(), now)
         if self.table.get_device() != now:
             _on_device(self.table, "table", now)
-        here.stream(stream, now)
+        if stream is not None:
+            here.stream(stream, now)
         held, ws, handle = self._ws.get(self.ws_bytes, stream, self.table.device)
-        st = lib().festina_trim_blocks(C.byref(self.req), at, C.byref(self.out), ws, self.ws_bytes, handle)
+        st = self._trim(C.byref(self.req), at, C.byref(self.out), ws, self.ws_bytes, handle)
         if st != FESTINA_OK:
             raise FestinaError(st, "festina_trim_blocks")
         if stream is not None:
@@ -869,6 +870,7 @@ class DeviceCache:
         self._int32, self._f32, self._rows, self._scale = (torch.int32,), torch.float32, (h, d), d ** -0.5
         self._empty, self._attend, self._cache_ref = torch.empty, lib().festina_attend, C.byref(self.cache)
         self._attend_drafts, self._int64, self._here = lib().festina_attend_drafts, (torch.int64,), _Here()
+        self._keep, self._struct, self._device = lib().festina_keep_tokens, bytes(self.cache), k.get_device()
         self._graded = torch.is_grad_enabled
 
     @classmethod
@@ -979,7 +981,8 @@ class DeviceCache:
         here = self._here
         if here.device() != now or seen.get_device() != now or self.k.get_device() != now:
             raise ValueError("q, seen, cache: on the current device")
-        here.stream(stream, now)
+        if stream is not None:
+            here.stream(stream, now)
         n = self._ws_bytes.get(sizes)
         if n is None:
             if len(self._ws_bytes) > 1024:
@@ -1010,13 +1013,13 @@ class DeviceCache:
                          here.ints(first, "first", R + 1, now), here.ints(path, "path", T, now),
                          here.ints(kept, "kept", R, now))
         caches = (self, *also)
+        structs = [c._struct for c in caches]
         for c in caches:
-            if c.k.get_device() != now:
+            if c._device != now:
                 _on_device(c.k, "cache", now)
-        if len({c.k.data_ptr() for c in caches}) != len(caches):
+        if len(set(structs)) != len(structs):
             raise ValueError("also: each cache once (its tokens would be moved twice)")
-        st = lib().festina_keep_tokens((festina_kv_cache * len(caches))(*[c.cache for c in caches]), len(caches), C.byref(q),
-                                       here.stream(stream, now))
+        st = self._keep(b"".join(structs), len(structs), C.byref(q), here.stream(stream, now))
         if st != FESTINA_OK:
             raise FestinaError(st, "festina_keep_tokens")
         if stream is not None:
