@@ -751,7 +751,7 @@ typedef struct festina_rotary {
 } festina_rotary;
 
 typedef struct festina_heads {
-  int32_t n_tokens;                  /* T >= 0 */
+  int32_t n_tokens;                  /* T >= 0, below 2^26 */
   int32_t n_heads, n_kv_heads;       /* heads of q and of k, >= 0 and at most 65,536 */
   int32_t dtype;                     /* FESTINA_BF16, FESTINA_F16 or FESTINA_F32: q, k and the outputs */
   const int32_t *position;           /* [T], any value */

@@ -237,7 +237,9 @@ extern "C" festina_status festina_rotate_heads(const festina_rotary *rotary, con
   const int groups = (a.heads[0] + each - 1) / each + (a.heads[1] + each - 1) / each;
   // few tokens: the heads of each over several waves, so that none makes two round trips to memory
   a.parts = a.T <= 2048 ? groups : 1;
-  const dim3 grid((unsigned)(((long long)a.T + kWaves - 1) / kWaves), (unsigned)a.parts);
+  const long long blocks = ((long long)a.T + kWaves - 1) / kWaves;
+  if (blocks > UINT_MAX / (64 * kWaves)) return FESTINA_ERR_UNSUPPORTED;   // threads along one axis of a grid
+  const dim3 grid((unsigned)blocks, (unsigned)a.parts);
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (heads->dtype == FESTINA_BF16) launch<FESTINA_BF16>(a, D, grid, st);
   else if (heads->dtype == FESTINA_F16) launch<FESTINA_F16>(a, D, grid, st);

@@ -42,6 +42,12 @@ def attend(tmp_path_factory):
     return _build("attend", "attend_drafts", tmp_path_factory.mktemp("attend_drafts"), *OF_64_AND_128)
 
 
+@pytest.fixture(scope="module")
+def attend_in_pieces(tmp_path_factory):
+    """As for very many keys: all tiles on one line that is cut into equal pieces."""
+    return _build("attend", "attend_drafts", tmp_path_factory.mktemp("attend_in_pieces"), *OF_64_AND_128, ("kFew = 8,", "kFew = 0,"))
+
+
 @pytest.mark.parametrize("odd", [0, 1])
 @pytest.mark.parametrize("args", ["40 8 64 2 16 2 1", "30 64 64 1 16 1 2", "25 64 128 2 32 1 3", "20 33 96 2 64 2 4",
                                   "12 64 256 1 256 1 5", "30 5 64 3 128 1 6"])
@@ -57,15 +63,26 @@ def test_norm_and_rotation(rotate, args):
     _check(rotate, args)
 
 
-@pytest.mark.parametrize("args", [
-    "128 2 4 64 bf16 0 0 0 3 1 300:8 17:3 64:1 0:0 9:9",                # short tables: one launch, or tiles
-    "128 1 4 32 f16 0 0 0 0 1 700:16 1:1 65:5 600:64",                  # tiles of the keys, trees across units
-    "64 1 4 16 bf16 0 0 0 0 1 520:13 130:64 1:1 40:40",                 # four row tiles, cut
+TREES = [
+    "128 2 4 64 bf16 0 0 0 3 1 300:8 17:3 64:1 0:0 9:9",                # short tables: one launch
+    "128 1 4 32 f16 0 0 0 0 1 700:16 1:1 65:5 600:64",                  # 128 rows a tile, trees across units
+    "128 1 4 32 bf16 0 0 0 0 1 700:16 1:1 65:5 600:12",                 # 64 rows, their keys in halves
+    "128 2 4 64 bf16 0 0 0 0 1 900:4 17:3 64:1 0:0 600:4",              # up to 16 rows, cut
+    "64 1 4 16 bf16 0 0 0 0 1 520:13 130:64 1:1 40:40",
     "64 2 2 128 f16 100 0 0 0 1 700:30 130:1 0:1 513:64",               # windows, a row without keys
     "64 1 1 32 bf16 5 0 0 0 2 700:40 30:30 64:64 3:2",                  # windows shorter than the paths
     "64 1 2 16 bf16 0 300 70 0 1 30:1x20 0:0x15 1300:70 7:1x5 900:31",  # trees beside a run
     "64 1 2 16 f16 0 80 0 0 1 30:1x520 1000:40",                        # more requests than a workgroup sums
+    "64 1 2 16 bf16 0 0 0 0 1 30:1x60 200:33 0:0x9 400:20",             # more than a wave has lanes
     "64 1 4 32 bf16 0 0 0 2 3 600:20 300:64 20:30",                     # words that are no trees; fewer held than new
-    "128 1 1 64 f16 33 0 0 0 3 300:64 64:64 700:16", "128 1 8 16 bf16 0 0 0 0 2 520:4 9:2 1:1"])
+    "128 1 1 64 f16 33 0 0 0 3 300:64 64:64 700:16", "128 1 8 16 bf16 0 0 0 0 2 520:4 9:2 1:1"]
+
+
+@pytest.mark.parametrize("args", TREES)
 def test_attention_over_trees(attend, args):
     _check(attend, args)
+
+
+@pytest.mark.parametrize("args", TREES[1:])
+def test_attention_over_trees_in_pieces(attend_in_pieces, args):
+    _check(attend_in_pieces, args)

@@ -135,7 +135,7 @@ def test_rotation(lib):  # noqa: F811
     for k in (dict(n_tokens=-1), dict(n_heads=-1), dict(dtype=7), dict(position=None), dict(q=None), dict(k_out=None),
               dict(q_token_stride=-8), dict(k_out_head_stride=-1), dict(q=FAKE + 1)):
         assert call(**k) == INVALID, k
-    assert call(n_heads=70000) == UNSUPPORTED
+    assert call(n_heads=70000) == UNSUPPORTED and call(n_tokens=2 ** 31 - 1) == UNSUPPORTED
     assert call(n_tokens=0, position=None) == OK and call(n_heads=0, n_kv_heads=0) == OK
     assert call(n_heads=0, q=None, q_out=None) == DEVICE
     assert lib.festina_rotate_heads(None, None, None) == INVALID

@@ -220,3 +220,86 @@ def test_queries_out_of_a_projection_streams_and_graphs():
     for bad in (seen[:-1], seen.int(), seen.cpu(), seen[::2]):
         with pytest.raises((ValueError, TypeError, RuntimeError)):
             cache.attend(c.q, table, length, first, 33, seen=bad)
+
+
+def _against_64_bits(dim, H, G, bt, dtype, lengths, new, window=0, seed=0):
+    """Many or long requests: the same definition on the device in 64 bits, request by request."""
+    from paper_2606_30391_amd import festina
+    rng = np.random.default_rng(seed)
+    g = torch.Generator("cuda").manual_seed(seed)
+    R, T, cols = len(lengths), int(sum(new)), [-(-x // bt) for x in lengths]
+    n = sum(cols) + 1
+    randn = lambda *s: torch.randn(s, generator=g, device="cuda")
+    k, v = (randn(n, H, *s).mul_(112).clamp_(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8) for s in ((bt, dim), (dim, bt)))
+    ks, vs = (torch.exp2(torch.randint(lo, hi, (n, H), generator=g, device="cuda").float()) for lo, hi in ((-8, -5), (-10, -3)))
+    ids = torch.randperm(n, generator=g, device="cuda").int()
+    table = torch.full((R, max(cols)), -1, dtype=torch.int32, device="cuda")
+    first, at = np.concatenate([[0], np.cumsum(new)]), 0
+    words, sees = [], []
+    for r, c in enumerate(cols):
+        table[r, :c] = ids[at:at + c]
+        at += c
+        lines = D.paths(D.tree(rng, new[r], 3), new[r]) if new[r] <= 64 else []
+        words += [sum(1 << x for x in line) for line in lines] or [0] * new[r]
+        sees.append(lines)
+    i32 = lambda x: torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")
+    q = randn(T, H * G, dim).to(TYPES[dtype][0])
+    seen = torch.tensor([w - 2 ** 64 if w >= 2 ** 63 else w for w in words], dtype=torch.int64, device="cuda")
+    out, lse = festina.DeviceCache(k, v, ks, vs).attend(q, table, i32(lengths), i32(first), max(new), window=window, seen=seen)
+    worst = []
+    f64 = lambda x: x.view(torch.float8_e4m3fn).double()
+    for r in range(R):
+        a, L, m = int(first[r]), lengths[r], new[r]
+        before, mine = L - m, table[r, :cols[r]].long()
+        mask = torch.zeros((m, L), dtype=torch.bool, device="cuda")
+        j = torch.arange(L, device="cuda")
+        for i in range(m):
+            line = sees[r][i] if m <= 64 else list(range(i + 1))
+            mask[i, :before] = True
+            mask[i, before + torch.tensor(line, device="cuda")] = True
+            if window:
+                far = j <= before + len(line) - 1 - window
+                mask[i] &= ~(far & (j < before))
+        if m > 64 and window:
+            mask &= j > before + torch.arange(m, device="cuda")[:, None] - window
+        for h in range(H):
+            K_ = (f64(k[mine, h]) * ks[mine, h].double()[:, None, None]).reshape(-1, dim)[:L]
+            V_ = (f64(v[mine, h]) * vs[mine, h].double()[:, None, None]).transpose(1, 2).reshape(-1, dim)[:L]
+            sc = vs[mine, h].double().repeat_interleave(bt)[:L]
+            Q = q[a:a + m, h * G:(h + 1) * G].double().reshape(m * G, dim)
+            x = (Q @ K_.T * dim ** -0.5).masked_fill(~mask.repeat_interleave(G, 0), -torch.inf)
+            w = torch.softmax(x, 1)
+            want = w @ V_
+            keys = mask.sum(1).repeat_interleave(G).double()
+            logit = (Q.abs() @ K_.T.abs()).amax(1) * dim ** -0.5
+            vmax = ((V_ / sc[:, None]).abs().amax(0) * sc.max())[None].expand_as(want)
+            to, tl = K.attend_bounds(want.cpu().numpy(), torch.logsumexp(x, 1).cpu().numpy(),
+                                     ((w @ V_.abs()).cpu().numpy(), vmax.cpu().numpy(), logit.cpu().numpy(), keys.cpu().numpy()),
+                                     dim, TYPES[dtype][1])
+            o = out[a:a + m, h * G:(h + 1) * G].double().reshape(m * G, dim)
+            l = lse[a:a + m, h * G:(h + 1) * G].double().reshape(-1)
+            worst.append(float(((o - want).abs().cpu() / torch.from_numpy(to)).max()))
+            worst.append(float(((l - torch.logsumexp(x, 1)).abs().cpu() / torch.from_numpy(tl)).max()))
+    print(f"[gpu] of the bound at most {max(worst):.3f}", flush=True)
+    assert max(worst) <= 1
+
+
+@pytest.mark.parametrize("dim,H,G,bt,dtype,longest,new,window", [
+    (128, 2, 4, 64, "bf16", 2500, 9, 0), (64, 1, 2, 16, "f16", 900, 40, 0), (96, 1, 8, 32, "bf16", 700, 5, 300)])
+@pytest.mark.parametrize("R", [70, 530])
+def test_many_requests(R, dim, H, G, bt, dtype, longest, new, window):
+    """More requests than a wave has lanes, and than a workgroup sums; few and many units of keys for each workgroup."""
+    rng = np.random.default_rng(R)
+    lengths = [int(x) for x in rng.integers(1, longest if R == 70 else longest // 4, R)]
+    count = [min(x, 1 + int(rng.integers(0, new))) for x in lengths]
+    count[3] = min(lengths[3], new)
+    print(f"[gpu] {R} requests, dim {dim}", flush=True)
+    _against_64_bits(dim, H, G, bt, dtype, lengths, count, window, R)
+
+
+@pytest.mark.parametrize("dim,H,G,bt,dtype,new", [(128, 4, 4, 64, "bf16", 16), (128, 4, 4, 128, "f16", 33), (64, 8, 2, 32, "bf16", 24),
+                                                  (64, 6, 4, 64, "f16", 64), (96, 4, 4, 64, "bf16", 12), (256, 4, 2, 64, "bf16", 12)])
+def test_long_requests_in_pieces(dim, H, G, bt, dtype, new):
+    """So many keys that the workgroups take pieces of all tiles' line, short requests among the long ones."""
+    lengths = [40000, 70, 25000, 130, 33333, 64, 21000, 16001]
+    _against_64_bits(dim, H, G, bt, dtype, lengths, [new, 3, new, new, 1, min(new, 64), new // 2, new], 0, dim)
