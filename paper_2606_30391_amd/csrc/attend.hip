@@ -29,9 +29,13 @@
 //   joined by k_tiles_join.
 //   8,192 tokens, 32 heads over 8 of 128: 550 GFLOP in 558 us (985 TFLOP/s; a large library product 1,189), matrix cores
 //   41% of the cycles, VALU issue 39%.  9,012 tokens of 16 heads of 64: 170 us, 27% and 52%: half the products an exponential.
-// k_drafts  drafted tokens: a request's row tile (64 or 128 rows: all its nodes, in most cases) against tiles of 64 keys as in k_tiles,
-//   but all requests' tiles form one line that is cut into pieces of equal cost, as in k_rows, since lengths differ and
-//   a node's row sees every cached key.  Which nodes a row sees is a word of 64 bits, looked at only in the last tiles.
+// k_drafts  drafted tokens, more than 16 rows of a request (k_rows has fewer, k_rows_whole short tables): row tiles of 64 or 128 rows
+//   against tiles of 64 keys as in k_tiles, but the keys are dealt to the workgroups as in k_rows, since lengths differ and a
+//   node's row sees every cached key: few of them in parts of one row tile, many in equal pieces of all tiles' line.  Which
+//   nodes a row sees is a word of 64 bits, looked at only in the last tiles; 64 rows leave two waves for each 32 of them, which
+//   take half of a tile's keys each.  Bound by latency where keys are few (32 requests of the fleet's lengths, trees of 16, 52 MB: 26 us
+//   and 7 to join the parts) and by the matrix cores and exponentials where they are many (64 requests up to 32,768 tokens, trees of
+//   32, 550 GFLOP over 2.2 GB: 715 us and 40, 730 TFLOP/s).
 // k_plan    running sums of the requests' units and tiles, for many requests.
 #include <hip/hip_runtime.h>
 
@@ -62,9 +66,8 @@ constexpr int kWaves = 4;
 constexpr int kBlock = 64 * kWaves;
 // Waves of k_rows on a SIMD, and the pieces that it cuts the keys into: one for each wave of 256 compute units.  (Three
 // waves of 128 dims and one row tile, 168 registers each, were slower: 64 requests up to 32,768 tokens 473 us against 440.)
-// (32 rows of a tree of 128 dims would lack ten registers for two waves.)
-constexpr int waves_of(int D, int NT, bool tree) { return D > 128 || NT > 2 || (tree && D == 128 && NT == 2) ? 1 : 2; }
-constexpr int workers_of(int D, int NT, bool tree) { return 1024 * waves_of(D, NT, tree); }
+constexpr int waves_of(int D, int NT) { return D > 128 || NT > 2 ? 1 : 2; }
+constexpr int workers_of(int D, int NT) { return 1024 * waves_of(D, NT); }
 constexpr int kGroups = 512;         // workgroups of k_tiles that fill the chip: two a compute unit
 constexpr int kJoins = 2048;         // and of its join: eight
 constexpr int kWaveRequests = 64;    // requests whose running sums a wave forms in its registers
@@ -325,7 +328,7 @@ template <> struct Seen<true> { typedef TreeRow type; };
 // What a node of a request sees (nothing unless `in`): the keys before the nodes, and nodes by its word.
 __device__ __forceinline__ TreeSpan tree_span(const AttArgs &a, const Request &q, unsigned long long word, bool in) {
   const int before = q.length - q.n;
-  word &= ~0ull >> (kNodes - q.n);                     // (a request with rows has at least one)
+  word &= ~0ull >> (kNodes - min(q.n, kNodes));        // (a request with rows has at least one)
   const int pos = before + max(__builtin_popcountll(word) - 1, 0), from = a.window > 0 ? max(pos - a.window + 1, 0) : 0;
   if (a.window > 0)                                    // the nearest of its path, the node itself included
     for (int n = __builtin_popcountll(word); n > a.window; --n) word &= word - 1;
@@ -717,7 +720,7 @@ __device__ __forceinline__ long long piece_start(long long all, int w, int n) { 
 
 // A workgroup for each row tile and key head, its waves over the keys in turn: few keys, one launch.
 template <typename T, int D, int NT, bool TREE>
-__global__ void __launch_bounds__(kBlock, waves_of(D, NT, TREE)) k_rows_whole(AttArgs a) {
+__global__ void __launch_bounds__(kBlock, waves_of(D, NT)) k_rows_whole(AttArgs a) {
   typedef Rows<T, D, NT, TREE> K;
   __shared__ typename K::Shared sh;
   __shared__ TreeSpan spans[TREE ? K::kRows : 1];
@@ -730,7 +733,7 @@ __global__ void __launch_bounds__(kBlock, waves_of(D, NT, TREE)) k_rows_whole(At
 
 // A wave a piece.
 template <typename T, int D, int NT, bool TREE>
-__global__ void __launch_bounds__(64, waves_of(D, NT, TREE)) k_rows(AttArgs a) {
+__global__ void __launch_bounds__(64, waves_of(D, NT)) k_rows(AttArgs a) {
   typedef Rows<T, D, NT, TREE> K;
   __shared__ long long list_[kListed + 1];
   __shared__ TreeSpan spans[TREE ? K::kRows : 1];
@@ -1834,13 +1837,15 @@ festina_status shape_of(const festina_kv_cache *c, const festina_attention *t, b
   *s = Shape{};
   const long long keys = (long long)t->max_blocks * c->block_tokens;
   s->cut = keys > 2 * kWaves * kUnit;
-  // Trees of up to 16 rows are k_rows', and up to 32 of tables that one launch does (one request of 403 tokens, trees of 8: 12.1 us
-  // and one launch, 12.7 and two); the others k_drafts' (32 rows of 128 dims, us by k_rows and by k_drafts: 32 requests of the
-  // fleet's lengths 35 and 30, of 512 to 16,384 tokens 160 and 147; 16 rows: 27 and 28, 124 and 143).
-  const bool trees = drafts && most > 16 && (s->cut || most > 16 * min(nt_most, 2));
-  s->tiles = trees ? t->max_new > kNodes : most > 16 * nt_most && t->max_new > 1;
+  // Trees of up to 16 rows are k_rows', as single tokens are (us by k_rows and by k_drafts, 32 requests of 128 dims, 16 rows: of the
+  // fleet's lengths 27 and 28, of 512 to 16,384 tokens 124 and 143; 32 rows, for which it would read the cache twice: 35 and 30, 196
+  // and 148), and so are those of up to kWholeRows rows, in tiles of 16, of tables that one launch does (up to 510 tokens, one
+  // request, 32 rows: 7 and 12; 32 requests, 64 rows: 23 and 30, 128 rows: 34 and 40; 64 requests, 128 rows: 61 and 57).
+  constexpr int kWholeRows = 128;
+  const bool trees = drafts && (most > (s->cut ? 16 : kWholeRows) || t->max_new > kNodes);     // (runs are k_tiles' there)
+  s->tiles = drafts ? trees && t->max_new > kNodes : most > 16 * nt_most && t->max_new > 1;
   const long long rows = s->tiles ? G : most;                         // with prompts about: the single tokens' rows
-  s->nt = rows <= 16 ? 1 : min(rows <= 32 ? 2 : 4, nt_most);
+  s->nt = rows <= 16 || drafts ? 1 : min(rows <= 32 ? 2 : 4, nt_most);
   s->join_rows = (int)min(rows, 16ll * s->nt);
   if (s->tiles && G > 16 * nt_most) s->nt = 0;
   s->rows_max = s->tiles ? 16 * s->nt : INT_MAX;
@@ -1854,7 +1859,7 @@ festina_status shape_of(const festina_kv_cache *c, const festina_attention *t, b
   if (s->nt && !s->cut && (long long)t->n_requests * H * s->tiles_each > kThreadsMost / kBlock)
     return FESTINA_ERR_UNSUPPORTED;
   size_t parts = 0;
-  if (s->nt && s->cut) parts = (size_t)2 * workers_of(D, s->nt, drafts) * 16 * s->nt;
+  if (s->nt && s->cut) parts = (size_t)2 * workers_of(D, s->nt) * 16 * s->nt;
   if (trees) {
     // one for each part of a step of few keys: at most a tile more each than the chip's workgroups
     const int groups = groups_of(D, s->halves);
@@ -1890,7 +1895,7 @@ festina_status shape_of(const festina_kv_cache *c, const festina_attention *t, b
   }
   s->plan = 0;
   s->cuts = up((size_t)2 * (t->n_requests + 1) * 8);
-  s->joins = s->cuts + up((size_t)(trees ? s->draft_groups : workers_of(D, max(s->nt, 1), drafts)) * sizeof(Cut));
+  s->joins = s->cuts + up((size_t)(trees ? s->draft_groups : workers_of(D, max(s->nt, 1))) * sizeof(Cut));
   s->part_ml = s->joins + up((kGroups + 1) * sizeof(int4));
   s->part_o = s->part_ml + up(parts * 8);
   s->bytes = s->part_o + up(parts * D * 4);
@@ -1899,15 +1904,13 @@ festina_status shape_of(const festina_kv_cache *c, const festina_attention *t, b
 
 template <typename T, int D, int NT, bool TREE>
 void run_rows(AttArgs a, const Shape &s, hipStream_t st) {
-  a.workers = workers_of(D, NT, TREE);
+  a.workers = workers_of(D, NT);
   if (!s.cut) {
     k_rows_whole<T, D, NT, TREE><<<(unsigned)(a.R * a.H * s.tiles_each), kBlock, 0, st>>>(a);
     return;
   }
-  if constexpr (!TREE || NT == 1) {                    // (more rows of trees come here uncut only)
-    k_rows<T, D, NT, TREE><<<a.workers, 64, 0, st>>>(a);
-    k_rows_join<T, D, NT><<<dim3(a.workers - 1, (s.join_rows + kWaves - 1) / kWaves), kBlock, 0, st>>>(a);
-  }
+  k_rows<T, D, NT, TREE><<<a.workers, 64, 0, st>>>(a);
+  k_rows_join<T, D, NT><<<dim3(a.workers - 1, (s.join_rows + kWaves - 1) / kWaves), kBlock, 0, st>>>(a);
 }
 
 template <typename T, int D, int KS>
@@ -1936,7 +1939,7 @@ void run(AttArgs a, const Shape &s, long long *plan, hipStream_t st) {
   const bool tree = a.seen && s.nt;
   if (s.nt == 1) tree ? run_rows<T, D, 1, true>(a, s, st) : run_rows<T, D, 1, false>(a, s, st);
   if constexpr (row_tiles_most(D) >= 2)
-    if (s.nt == 2) tree ? run_rows<T, D, 2, true>(a, s, st) : run_rows<T, D, 2, false>(a, s, st);
+    if (s.nt == 2) run_rows<T, D, 2, false>(a, s, st);
   if constexpr (row_tiles_most(D) >= 4)
     if (s.nt == 4) run_rows<T, D, 4, false>(a, s, st);
   if (s.tiles) {

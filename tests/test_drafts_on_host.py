@@ -69,6 +69,8 @@ TREES = [
     "128 1 4 32 bf16 0 0 0 0 1 700:16 1:1 65:5 600:12",                 # 64 rows, their keys in halves
     "128 2 4 64 bf16 0 0 0 0 1 900:4 17:3 64:1 0:0 600:4",              # up to 16 rows, cut
     "64 1 4 16 bf16 0 0 0 0 1 520:13 130:64 1:1 40:40",
+    "64 1 1 16 f16 0 0 0 0 1 100:90 300:31 64:64",                      # a run in a short table
+    "128 1 4 64 bf16 0 0 0 0 1 500:32 77:20 30:30",                     # eight row tiles of one launch
     "64 2 2 128 f16 100 0 0 0 1 700:30 130:1 0:1 513:64",               # windows, a row without keys
     "64 1 1 32 bf16 5 0 0 0 2 700:40 30:30 64:64 3:2",                  # windows shorter than the paths
     "64 1 2 16 bf16 0 300 70 0 1 30:1x20 0:0x15 1300:70 7:1x5 900:31",  # trees beside a run

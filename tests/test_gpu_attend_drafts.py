@@ -93,6 +93,8 @@ SHAPES = [  # requests, dim, kv heads, group, block, type
     ([(2000, 64), (100, 1), (130, 2)], 64, 7, 2, 32, "f16"), ([(900, 5)] * 12, 96, 2, 1, 64, "bf16"),
     ([(1500, 70), (900, 31), (64, 64), (12, 2)], 64, 2, 2, 16, "bf16"),                # beside a run
     ([(1500, 170), (900, 31), (64, 64), (12, 2)], 128, 1, 4, 64, "f16"),
+    ([(100, 90), (300, 31), (64, 64), (12, 2)], 64, 2, 1, 64, "bf16"), ([(65, 65), (300, 64)], 128, 1, 1, 16, "f16"),   # and in a short table
+    ([(500, 32), (77, 20), (64, 30), (512, 32)], 128, 1, 4, 64, "bf16"), ([(500, 8), (77, 3)], 256, 1, 16, 64, "f16"),     # eight row tiles of one launch
     ([(9, 2), (65, 1)] * 300, 64, 1, 2, 16, "bf16")]                                   # more than a workgroup sums
 
 
