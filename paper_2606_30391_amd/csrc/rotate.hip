@@ -10,7 +10,7 @@
 // A wave takes a token: a lane makes a cosine and a sine or two, which all heads share through LDS, then each lane holds
 // 16 elements of a head, eight of either half (or pairs of neighbours), so that no element crosses lanes, only the sum
 // of squares does; neighbouring lanes hold neighbouring 16 bytes.  Bound by the bytes it moves: 41,100 tokens of 32 and 8 heads of
-// 128 in bfloat16, 842 MB in 150 us, 5.6 TB/s (a large copy: 4.9); on a step of 256 tokens by latency: 5.5 us.
+// 128 in bfloat16, 842 MB in 150 us, 5.6 TB/s (a large copy: 4.9); on a step of 256 tokens by latency: 4.9 us.
 // (Stores that mark the outputs as not to be kept: 142 us, and float32 heads 77 us against 57.)
 #include <hip/hip_runtime.h>
 
