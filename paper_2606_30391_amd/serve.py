@@ -64,13 +64,19 @@ class Server:
         request after request (device int32; festina_drafts).  qkv as for step(); choose(outputs of the layers) returns the
         tokens [tokens] (device int32) that the model chooses behind the nodes.  Returns the layers' outputs; drafts.next [requests]
         is the token behind each request's accepted ones, drafts.kept their number, drafts.path which they were."""
+        import torch
         b, d = self.blocks, self.drafts
+        each, int32 = (int(np.sum(add)),), (torch.int32,)    # (copies would repeat what is shorter)
+        festina._check(parent, "parent", int32, each)
+        festina._check(token, "token", int32, each)
         tokens = self._begin(add)
         d.parent[:tokens].copy_(parent)
         d.token[:tokens].copy_(token)
         d.plan(b.first, b.length)
         out = self._layers(tokens, int(np.max(add, initial=1)), qkv, window, rotary, d)
-        self.choice[:tokens].copy_(choose(out))
+        choice = choose(out)
+        festina._check(choice, "choose()", int32, each)
+        self.choice[:tokens].copy_(choice)
         d.accept(b.first, b.length, self.choice)
         if self.caches:
             self.caches[0].keep(b.table, b.length, b.first, d.path, d.kept, also=self.caches[1:])

@@ -92,3 +92,20 @@ def test_the_command_verifies_drafts(capsys, draft):
     assert "drafts:" in said and "decode:" in said
     free = said.split("us a layer; ")[1].split(" blocks free")[0].split(" of ")
     assert free[0] == free[1]                                # every block came back
+
+
+def test_trees_and_choices_of_other_sizes_than_the_step_are_refused():
+    from paper_2606_30391_amd.serve import Server
+    srv = Server(2, CONTEXT, BLOCKS, TOKENS, 1, H, DIM, BT)
+    data = [torch.randn((5, h, DIM), device="cuda").bfloat16() for h in (H * G, H, H)]
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    parent, token, choice = i32(-1, 0, 0, -1, 0), i32(7, 8, 9, 7, 8), i32(9, 0, 5, 1, 1)
+    step = lambda p, t, c: srv.verify([3, 2], p, t, lambda layer: data, lambda out: c)
+    for change in ((i32(-1), token, choice), (parent, i32(7), choice), (parent, token, i32(9)), (parent[:4], token, choice),
+                   (parent, token[None], choice), (parent, token, choice.cpu()), (parent.long(), token, choice)):
+        with pytest.raises(ValueError):
+            step(*change)
+        assert srv.blocks.held.tolist() == [0, 0] and srv.blocks.n_free.tolist() == [BLOCKS]
+    step(parent, token, choice)                              # none of them left anything behind
+    assert srv.drafts.kept.tolist() == [2, 1] and srv.drafts.next.tolist() == [5, 1]
+    assert srv.blocks.held.tolist() == [2, 1] and srv.blocks.n_free.tolist() == [BLOCKS - 2]
