@@ -736,7 +736,7 @@ class _Here:
 
 def _on_device(t, name, now):
     if t.get_device() != now:
-        raise ValueError(f"{name}: on device {t.get_device()}, not on the current device {now}")
+        raise ValueError(f"{name}: on device {t.get_device()}, not on device {now} (that of the call)")
 
 
 class _Workspaces:
@@ -1051,6 +1051,9 @@ class DeviceDrafts:
         self.parent, self.token = parent, token
         i32 = lambda n: torch.empty(n, dtype=torch.int32, device=device)
         self.seen = torch.empty(self.max_tokens, dtype=torch.int64, device=device)
+        for name, t in (("parent", parent), ("token", token)):
+            if t is not None:
+                _on_device(t, name, self.seen.get_device())
         self.position, self.path = i32(self.max_tokens), i32(self.max_tokens)
         self.kept, self.next, self.length = (i32(self.n_requests) for _ in range(3))
         self.accepted = festina_accepted(_ptr(self.path), _ptr(self.kept), _ptr(self.next), _ptr(self.length))
@@ -1094,7 +1097,7 @@ class DeviceDrafts:
 
 class DeviceRotary:
     """Norm and rotation of queries and keys (festina_rotary): freq, radians per position of each rotated pair (host numbers,
-    at most head_dim / 2), weights of the heads' norms or None, and whether pairs are neighbours (interleaved) or half of the
+    at most head_dim / 2), weights of the heads' norms or None (copied), and whether pairs are neighbours (interleaved) or half of the
     rotated elements apart.  What a model's layers share of these is kept once and may be used by all."""
 
     def __init__(self, freq, head_dim: int, q_weight=None, k_weight=None, eps: float = 1e-6, interleaved: bool = False,

@@ -283,3 +283,10 @@ def test_tensors_that_do_not_fit_are_refused():
                 lambda: festina.DeviceDrafts(i32([-1]), None, 1).accept(i32([0, 1]), i32([1]), i32([1]))):
         with pytest.raises((ValueError, TypeError, RuntimeError)):
             bad()
+
+
+def test_trees_on_another_device_than_the_results_are_refused():
+    from paper_2606_30391_amd import festina
+    for trees in ((i32([-1, 0]), None), (None, i32([1, 2]))):
+        with pytest.raises(ValueError, match="on device 0, not on device -1"):
+            festina.DeviceDrafts(*trees, 1, device="cpu")
