@@ -1487,9 +1487,9 @@ __device__ __forceinline__ void deal(const AttArgs &a, int groups, long long *li
     const int U = same(wave_sum((int)min((long long)u * tiles, 1ll << 20))), tiles_before = wave_before(tiles);
     all_tiles = same(__shfl(tiles_before + tiles, 63));
     part = part_of(U, all_tiles, groups, room);
-    if (part && all_tiles < groups) {
+    if (part && all_tiles > 0 && all_tiles < groups) {
       // a second round would double the time: parts so long that there are no more than the chip's workgroups (a tile's
-      // last part is half a part on average)
+      // last part is half a part on average; runs alone, or no new tokens, have no tiles)
       part = cdiv(U, groups - all_tiles / 2);
       for (int i = 0; i < 3; ++i) {
         const int over = same(wave_sum(cdiv(u, part) * tiles)) - groups;

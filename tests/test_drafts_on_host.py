@@ -88,3 +88,20 @@ def test_attention_over_trees(attend, args):
 @pytest.mark.parametrize("args", TREES[1:])
 def test_attention_over_trees_in_pieces(attend_in_pieces, args):
     _check(attend_in_pieces, args)
+
+
+NO_TREES = [
+    "64 1 1 16 f16 0 0 0 0 1 300:90",                                   # a run alone
+    "128 1 4 32 bf16 40 0 0 2 1 700:70 900:65",                         # runs alone, rows of no request
+    "64 2 1 16 bf16 0 0 80 3 1 300:0 40:0",                             # no request has new tokens
+    "64 1 2 16 bf16 0 300 70 5 1 30:0x20 600:0"]
+
+
+@pytest.mark.parametrize("args", NO_TREES)
+def test_steps_without_trees(attend, args):
+    _check(attend, args)
+
+
+@pytest.mark.parametrize("args", NO_TREES)
+def test_steps_without_trees_in_pieces(attend_in_pieces, args):
+    _check(attend_in_pieces, args)

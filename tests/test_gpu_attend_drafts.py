@@ -305,3 +305,13 @@ def test_long_requests_in_pieces(dim, H, G, bt, dtype, new):
     """So many keys that the workgroups take pieces of all tiles' line, short requests among the long ones."""
     lengths = [40000, 70, 25000, 130, 33333, 64, 21000, 16001]
     _against_64_bits(dim, H, G, bt, dtype, lengths, [new, 3, new, new, 1, min(new, 64), new // 2, new], 0, dim)
+
+
+@pytest.mark.parametrize("requests,dim,G,max_new", [
+    ([(300, 90)], 64, 1, None), ([(700, 70), (900, 65)], 128, 4, None), ([(300, 0), (40, 0)], 64, 1, 80),
+    ([(30, 0)] * 20 + [(600, 0)], 96, 2, 70)])
+def test_steps_without_trees(requests, dim, G, max_new):
+    c = Case(np.random.default_rng(8), requests, dim, 2, G, 16, "bf16", extra=4)
+    print(f"[gpu] dim {dim} group {G} requests {requests[:3]}", flush=True)
+    for window in (0, 50):
+        c.check(c.run(window, max_new), window)
