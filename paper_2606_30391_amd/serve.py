@@ -55,7 +55,8 @@ class Server:
         step's tokens, request after request; tokens is sum(add).  blocks.served says afterwards whose tokens were
         in the step: where blocks or step_tokens run out, those of the requests from there on are not, and their
         rows of the output hold nothing.  rotary (a DeviceRotary) is applied to the queries and keys at their positions."""
-        out = self._layers(self._begin(add), int(np.max(add, initial=1)), qkv, window, rotary)
+        add = np.ascontiguousarray(add, np.int32)
+        out = self._layers(self._begin(add), int(add.max(initial=1)), qkv, window, rotary)
         self.blocks.advance()
         return out
 
@@ -65,15 +66,15 @@ class Server:
         tokens [tokens] (device int32) that the model chooses behind the nodes.  Returns the layers' outputs; drafts.next [requests]
         is the token behind each request's accepted ones, drafts.kept their number, drafts.path which they were."""
         import torch
-        b, d = self.blocks, self.drafts
-        each, int32 = (int(np.sum(add)),), (torch.int32,)    # (copies would repeat what is shorter)
+        b, d, add = self.blocks, self.drafts, np.ascontiguousarray(add, np.int32)
+        each, int32 = (int(add.sum()),), (torch.int32,)      # (copies would repeat what is shorter)
         festina._check(parent, "parent", int32, each)
         festina._check(token, "token", int32, each)
         tokens = self._begin(add)
         d.parent[:tokens].copy_(parent)
         d.token[:tokens].copy_(token)
         d.plan(b.first, b.length)
-        out = self._layers(tokens, int(np.max(add, initial=1)), qkv, window, rotary, d)
+        out = self._layers(tokens, int(add.max(initial=1)), qkv, window, rotary, d)
         choice = choose(out)
         festina._check(choice, "choose()", int32, each)
         self.choice[:tokens].copy_(choice)
@@ -86,9 +87,8 @@ class Server:
         return out
 
     def _begin(self, add):
-        """Blocks and slots of a step; the number of its tokens."""
+        """Blocks and slots of a step with add (an int32 array) new tokens; how many they are."""
         import torch
-        add = np.ascontiguousarray(add, np.int32)
         tokens, b = int(add.sum()), self.blocks
         if add.shape != tuple(b.add.shape) or add.min(initial=0) < 0 or tokens > b.max_tokens:
             raise ValueError(f"add: {b.add.shape[0]} counts, none negative, of at most {b.max_tokens} tokens in all")

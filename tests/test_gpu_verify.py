@@ -109,3 +109,15 @@ def test_trees_and_choices_of_other_sizes_than_the_step_are_refused():
     step(parent, token, choice)                              # none of them left anything behind
     assert srv.drafts.kept.tolist() == [2, 1] and srv.drafts.next.tolist() == [5, 1]
     assert srv.blocks.held.tolist() == [2, 1] and srv.blocks.n_free.tolist() == [BLOCKS - 2]
+
+
+def test_counts_as_a_tensor_on_the_host():
+    from paper_2606_30391_amd.serve import Server
+    srv = Server(2, CONTEXT, BLOCKS, TOKENS, 1, H, DIM, BT)
+    data = [torch.randn((5, h, DIM), device="cuda").bfloat16() for h in (H * G, H, H)]
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    add = torch.tensor([3, 2])
+    srv.step(add, lambda layer: data)
+    assert srv.blocks.held.tolist() == [3, 2]
+    srv.verify(add, i32(-1, 0, 0, -1, 0), i32(7, 8, 9, 7, 8), lambda layer: data, lambda out: i32(9, 0, 5, 1, 1))
+    assert srv.blocks.held.tolist() == [5, 3] and srv.drafts.kept.tolist() == [2, 1]
