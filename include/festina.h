@@ -671,7 +671,9 @@ festina_status festina_attend(const festina_kv_cache *cache, const festina_atten
  * The calls of a step: festina_plan_drafts once; in each layer festina_rotate_heads, festina_store_kv and
  * festina_attend_drafts; then festina_accept_drafts with the tokens that the model chose, festina_keep_tokens for
  * all layers, and festina_trim_blocks.  A request with more than 64 new tokens is a run (a prompt beside the trees):
- * each of its tokens follows the one before, and all are kept. */
+ * each of its tokens follows the one before, and all are kept.  Up to 64 known tokens (the rest of a prompt) are a tree as any
+ * others: they are kept, whatever the model chooses, where each one's parent is the one before it and the caller writes the
+ * next one's token over the model's choice at each but the last. */
 typedef struct festina_drafts {
   int32_t n_requests;                /* R >= 0, at most 2^20 */
   int32_t n_tokens;                  /* T >= 0 entries of the token arrays below */

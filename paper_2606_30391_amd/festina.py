@@ -1032,7 +1032,11 @@ class DeviceDrafts:
     the most that a step may have.
 
     plan() makes seen [tokens] (int64: bit j for node j; DeviceCache.attend) and position [tokens] (int32: DeviceRotary),
-    accept() path [tokens], kept [n_requests], next [n_requests] and length [n_requests].  stream= as for DeviceBlocks."""
+    accept() path [tokens], kept [n_requests], next [n_requests] and length [n_requests].  stream= as for DeviceBlocks.
+
+    A request's new tokens are guesses but for node 0, and those that the model did not choose are not accepted.  The rest of
+    a prompt stays where its tokens are a chain and choice holds each next one's token in the model's place (Server.verify's
+    known does so); more than 64 new tokens are a run, kept whole, whose parents are not read."""
 
     def __init__(self, parent, token, n_requests: int, max_tokens=None, device=None):
         import torch

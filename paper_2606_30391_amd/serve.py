@@ -25,6 +25,7 @@ import numpy as np
 from . import festina, workloads
 
 UNIT = 2048                # most prompt tokens of one request in a step (the sweep workload's prefill unit)
+NODES = 64                 # most tokens of a draft tree (festina_drafts): more of one request are a run
 
 
 class Server:
@@ -60,24 +61,36 @@ class Server:
         self.blocks.advance()
         return out
 
-    def verify(self, add, parent, token, qkv, choose, window: int = 0, rotary=None):
+    def verify(self, add, parent, token, qkv, choose, window: int = 0, rotary=None, known=None):
         """One step of drafted tokens: add[r] nodes of request r's tree (host integers; 0: none), parent and token [tokens] theirs,
         request after request (device int32; festina_drafts).  qkv as for step(); choose(outputs of the layers) returns the
         tokens [tokens] (device int32) that the model chooses behind the nodes.  Returns the layers' outputs; drafts.next [requests]
-        is the token behind each request's accepted ones, drafts.kept their number, drafts.path which they were."""
+        is the token behind each request's accepted ones, drafts.kept their number, drafts.path which they were.
+
+        known[r] (host integers, of which 0 is as 1) says how many of request r's tokens are no guesses, such as the rest of a prompt: from
+        the first on they follow one another, whatever parent says, and all are kept, whatever the model chooses; the tree goes on
+        behind the last of them.  Without it the first alone is known, and what the model would not have chosen leaves the cache.
+        More than 64 new tokens of a request are no tree but a run, all of them known: parent is not read for them."""
         import torch
         b, d, add = self.blocks, self.drafts, np.ascontiguousarray(add, np.int32)
+        chain = None if known is None else self._chain(add, known)
         each, int32 = (int(add.sum()),), (torch.int32,)      # (copies would repeat what is shorter)
         festina._check(parent, "parent", int32, each)
         festina._check(token, "token", int32, each)
         tokens = self._begin(add)
         d.parent[:tokens].copy_(parent)
         d.token[:tokens].copy_(token)
+        if chain is not None:
+            at, then, node = self._indexes(chain)
+            d.parent.index_copy_(0, then, node.int())
         d.plan(b.first, b.length)
         out = self._layers(tokens, int(add.max(initial=1)), qkv, window, rotary, d)
         choice = choose(out)
         festina._check(choice, "choose()", int32, each)
         self.choice[:tokens].copy_(choice)
+        if chain is not None:
+            # the first child with the chosen token is the next known one
+            self.choice.index_copy_(0, at, d.token.index_select(0, then))
         d.accept(b.first, b.length, self.choice)
         if self.caches:
             self.caches[0].keep(b.table, b.length, b.first, d.path, d.kept, also=self.caches[1:])
@@ -85,6 +98,25 @@ class Server:
         b.trim(d.length)
         b.advance()
         return out
+
+    @staticmethod
+    def _chain(add, known):
+        """Known tokens that another known one follows: their index in the step, that one's, and their index in their request."""
+        known = np.ascontiguousarray(known, np.int64)
+        if add.ndim != 1 or known.shape != add.shape or (known < 0).any() or (known > add).any() or ((add > NODES) & (known < add)).any():
+            raise ValueError(f"known: a count for each request, of at most its new tokens; all of more than {NODES}")
+        n = np.where(add > NODES, 0, np.maximum(known - 1, 0))
+        if not n.any():
+            return None
+        node = np.concatenate([np.arange(x) for x in n])
+        at = np.repeat(np.cumsum(add, dtype=np.int64) - add, n) + node
+        return np.stack([at, at + 1, node])
+
+    def _indexes(self, chain):
+        import torch
+        host = torch.empty(chain.shape, dtype=torch.int64, pin_memory=True)      # as in _begin()
+        host.numpy()[:] = chain
+        return host.to(self.choice.device, non_blocking=True).unbind(0)
 
     def _begin(self, add):
         """Blocks and slots of a step with add (an int32 array) new tokens; how many they are."""
