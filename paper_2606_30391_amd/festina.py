@@ -11,6 +11,7 @@ module raises.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 
 import numpy as np
@@ -1123,14 +1124,18 @@ class DeviceRotary:
 
     def apply(self, q, k, position, q_out=None, k_out=None, stream=None):
         """(q_out, k_out): queries and keys [tokens][heads][head_dim] of one type (any strides but the last) at the int32
-        positions [tokens].  Outputs are made where not given, and may be q and k themselves.  For serving: inputs that ask
-        for a gradient are refused."""
+        positions [tokens].  Outputs are made where not given, and may be q and k themselves, else they share no memory with either
+        nor with each other.  For serving: inputs that ask for a gradient are refused."""
+        return self._apply(q, k, position, q_out, k_out, stream, q_out, k_out)
+
+    def _apply(self, q, k, position, q_out, k_out, stream, q_given, k_given):
         here, D, dtype = self._here, self.head_dim, q.dtype
         now, kind = here.device(), self._types.get(dtype)
         if stream is not None and (q_out is None or k_out is None):
             with _on(stream, q.device):
-                return self.apply(q, k, position, self._empty(q.shape, dtype=dtype, device=q.device) if q_out is None else q_out,
-                                  self._empty(k.shape, dtype=k.dtype, device=k.device) if k_out is None else k_out, stream)
+                return self._apply(q, k, position, self._empty(q.shape, dtype=dtype, device=q.device) if q_out is None else q_out,
+                                   self._empty(k.shape, dtype=k.dtype, device=k.device) if k_out is None else k_out, stream,
+                                   q_given, k_given)
         if q.dim() != 3 or k.dim() != 3:
             raise ValueError("q and k: [tokens][heads][dim]")
         T, heads, qd = q.shape
@@ -1146,16 +1151,18 @@ class DeviceRotary:
             raise ValueError(f"q and k: [{T}][heads][{D}] with their last axis contiguous")
         if (q.requires_grad or k.requires_grad) and self._graded():
             raise ValueError("q, k: no gradient passes through (call under torch.no_grad())")
+        if q_given is not None or k_given is not None:
+            self._given(q, k, q_given, k_given, now)
         if q_out is None:
             q_out = self._empty((T, heads, D), dtype=dtype, device=q.device)
             ot, oh = heads * D, D
         else:
-            ot, oh = self._given(q_out, "q_out", q, now)
+            ot, oh, _ = q_out.stride()
         if k_out is None:
             k_out = self._empty((T, kv_heads, D), dtype=dtype, device=q.device)
             pt, ph = kv_heads * D, D
         else:
-            pt, ph = self._given(k_out, "k_out", k, now)
+            pt, ph, _ = k_out.stride()
         if self.turn.get_device() != now:
             _on_device(self.turn, "the rotary", now)
         st = self._rotate(self._ref, C.byref(festina_heads(
@@ -1167,20 +1174,81 @@ class DeviceRotary:
             _used_on(stream, q, k, position, q_out, k_out, self.turn, *(w for w in self.weights if w is not None))
         return q_out, k_out
 
-    def _given(self, y, name, x, now):
-        """Strides of an output that the caller brings for x."""
-        _check(y, name, (x.dtype,))
-        _on_device(y, name, now)
-        if y.shape != x.shape or (y.stride(2) != 1 and y.numel()):
-            raise ValueError(f"{name}: the shape {tuple(x.shape)} with its last axis contiguous")
-        if y.requires_grad and self._graded():
-            raise ValueError(f"{name}: no gradient passes through (call under torch.no_grad())")
-        if y.numel():
-            if x.data_ptr() == y.data_ptr() and x.stride() != y.stride():
-                raise ValueError(f"{name}: the input's own memory with its strides, or other memory")
-            if any(s == 0 and n > 1 for s, n in zip(y.stride(), y.shape)):
+    def _given(self, q, k, q_out, k_out, now):
+        """Outputs that the caller brings: a token's heads are several waves' work, so what one writes no other may read or write."""
+        D = self.head_dim
+        x, y = _place(q, D), _place(k, D)
+        places = []
+        for out, name, t, own, other in ((q_out, "q_out", q, x, y), (k_out, "k_out", k, y, x)):
+            if out is None:
+                continue
+            at = own
+            if out is not t:
+                if out.dtype is not t.dtype or out.get_device() != now:
+                    _check(out, name, (t.dtype,))
+                    _on_device(out, name, now)
+                if out.shape != t.shape or (out.stride(2) != 1 and out.numel()):
+                    raise ValueError(f"{name}: the shape {tuple(t.shape)} with its last axis contiguous")
+                if out.requires_grad and self._graded():
+                    raise ValueError(f"{name}: no gradient passes through (call under torch.no_grad())")
+                at = _place(out, D)
+                if at != own and at[1] > own[0] and own[1] > at[0] and _meet(at, own, D):
+                    raise ValueError(f"{name}: the input's own memory with its strides, or other memory")
+            if not _once(at, D):
                 raise ValueError(f"{name}: an element of its own for each of the input")
-        return y.stride()[:2]
+            if at[1] > other[0] and other[1] > at[0] and _meet(at, other, D):
+                raise ValueError(f"{name}: shares memory with the other input")
+            places.append(at)
+            if q_out is q and k_out is k:                    # in place: all has been looked at
+                if not _once(y, D):
+                    raise ValueError("k_out: an element of its own for each of the input")
+                return
+        if len(places) == 2 and _meet(*places, D):
+            raise ValueError("q_out and k_out: share memory")
+
+
+def _place(t, D):
+    """Where a tensor [tokens][heads][D] lies, in elements: its begin and end, sizes, and strides (0 where they do not count)."""
+    (T, H, _), (s, p, _) = t.shape, t.stride()
+    if T <= 1:
+        s = 0
+    if H <= 1:
+        p = 0
+    a = t.data_ptr() // t.element_size()
+    return a, a + (T - 1) * s + (H - 1) * p + D, T, H, s, p
+
+
+def _starts(x):
+    a, _, T, H, s, p = x
+    return np.sort((a + np.arange(T, dtype=np.int64)[:, None] * s + np.arange(H, dtype=np.int64) * p).ravel())
+
+
+def _meet(x, y, D) -> bool:
+    """Whether two tensors [tokens][heads][D] of one type with contiguous last axes (their _place) share an element."""
+    (a, a_end, T, H, s, p), (b, b_end, U, K, r, q) = x, y
+    if a_end <= b or b_end <= a or not (T * H and U * K and D):
+        return False
+    if s == r and s:                                         # side by side in each token
+        width, other, d = (H - 1) * p + D, (K - 1) * q + D, (b - a) % s
+        if width <= d and d + other <= s:
+            return False
+    step = math.gcd(s, p, r, q)                              # or in each head
+    if step and D <= (b - a) % step <= step - D:
+        return False
+    starts, at = _starts(y), _starts(x)
+    return bool((np.searchsorted(starts, at - D, "right") < np.searchsorted(starts, at + D, "left")).any())
+
+
+def _once(x, D) -> bool:
+    """Whether such a tensor has each of its elements at a place of its own."""
+    _, _, T, H, s, p = x
+    if not (T * H and D):
+        return True
+    (inner, n), (outer, m) = ((s, T), (p, H)) if (T > 1 and s <= p) or H <= 1 else ((p, H), (s, T))
+    if (n <= 1 or inner >= D) and (m <= 1 or outer >= (n - 1) * inner + D):
+        return True
+    starts = _starts(x)
+    return bool((starts[1:] - starts[:-1] >= D).all())
 
 
 def _turn(radians: float) -> int:

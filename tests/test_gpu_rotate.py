@@ -146,3 +146,43 @@ def test_graph_stream_and_no_tokens():
     assert all(torch.equal(x, y) for x, y in zip(got, want))
     none = r.apply(q[:0], k[:0], p[:0])
     assert none[0].shape == (0, 6, 128)
+
+
+def test_outputs_that_share_memory_are_refused():
+    from paper_2606_30391_amd import festina
+    r = festina.DeviceRotary(_freq(32), 64)
+    p = torch.arange(6, dtype=torch.int32, device="cuda")
+    buf = torch.randn((6, 12, 64), device="cuda").bfloat16()
+    was = buf.clone()
+    q, k = buf[:, 1:9], buf[:, 10:12]
+    fresh = torch.zeros((6, 8, 64), dtype=torch.bfloat16, device="cuda")
+    for name, out in (("a head further", dict(q_out=buf[:, 0:8])), ("over the keys", dict(q_out=buf[:, 3:11])),
+                      ("over the queries", dict(k_out=buf[:, 7:9])), ("each other", dict(q_out=fresh, k_out=fresh[:, :2])),
+                      ("in place beside its input's", dict(q_out=q, k_out=q[:, 6:])),
+                      ("half a head further", dict(q_out=buf.flatten(1)[:, 32:32 + 512].unflatten(1, (8, 64)))),
+                      ("itself", dict(q_out=torch.zeros(9000, dtype=torch.bfloat16, device="cuda").as_strided((6, 8, 64), (512, 32, 1)))),
+                      ("itself in another token", dict(k_out=torch.zeros(9000, dtype=torch.bfloat16, device="cuda").as_strided((6, 2, 64), (64, 64, 1))))):
+        print(f"[gpu] {name}", flush=True)
+        with pytest.raises(ValueError):
+            r.apply(q, k, p, **out)
+    assert torch.equal(buf, was)
+
+
+def test_outputs_beside_their_inputs():
+    from paper_2606_30391_amd import festina
+    r = festina.DeviceRotary(_freq(32), 64, torch.ones(64), torch.ones(64))
+    for T in (1, 6):
+        p = torch.arange(T, dtype=torch.int32, device="cuda") + 5
+        q, k = (torch.randn((T, h, 64), device="cuda").bfloat16() for h in (4, 2))
+        want = r.apply(q, k, p)
+        pairs = torch.zeros((T, 6, 2, 64), dtype=torch.bfloat16, device="cuda")      # a head's output behind its input
+        pairs[:, :4, 0], pairs[:, 4:, 0] = q, k
+        print(f"[gpu] {T} tokens", flush=True)
+        r.apply(pairs[:, :4, 0], pairs[:, 4:, 0], p, pairs[:, :4, 1], pairs[:, 4:, 1])
+        assert torch.equal(pairs[:, :4, 1], want[0]) and torch.equal(pairs[:, 4:, 1], want[1])
+        assert torch.equal(pairs[:, :4, 0], q) and torch.equal(pairs[:, 4:, 0], k)
+        packed = torch.cat([q, k, torch.zeros_like(q), torch.zeros_like(k)], 1)      # all four of a token side by side
+        r.apply(packed[:, :4], packed[:, 4:6], p, packed[:, 6:10], packed[:, 10:])
+        assert torch.equal(packed[:, 6:], torch.cat(want, 1)) and torch.equal(packed[:, :6], torch.cat([q, k], 1))
+        r.apply(packed[:, :4], packed[:, 4:6], p, packed[:, :4], packed[:, 4:6])     # and in place
+        assert torch.equal(packed[:, :6], torch.cat(want, 1))
