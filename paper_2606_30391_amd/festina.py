@@ -709,6 +709,20 @@ def _used_on(stream, *tensors):
             t.record_stream(stream)
 
 
+def _dual_levels():
+    """What has _current_level, of forward-mode differentiation: -1 where there is none (torch's own name; without it every
+    call looks)."""
+    import types
+    from torch.autograd import forward_ad
+    return forward_ad if hasattr(forward_ad, "_current_level") else types.SimpleNamespace(_current_level=0)
+
+
+def _tangents(*tensors) -> bool:
+    """Whether one of them has a forward-mode tangent."""
+    from torch.autograd import forward_ad
+    return any(forward_ad.unpack_dual(t).tangent is not None for t in tensors)
+
+
 class _Here:
     """Where calls run, in few attribute reads: the kernels of these calls take about as long as their host work."""
 
@@ -872,7 +886,7 @@ class DeviceCache:
         self._empty, self._attend, self._cache_ref = torch.empty, lib().festina_attend, C.byref(self.cache)
         self._attend_drafts, self._int64, self._here = lib().festina_attend_drafts, (torch.int64,), _Here()
         self._keep, self._struct, self._device = lib().festina_keep_tokens, bytes(self.cache), k.get_device()
-        self._graded = torch.is_grad_enabled
+        self._graded, self._dual = torch.is_grad_enabled, _dual_levels()
 
     @classmethod
     def empty(cls, n_blocks: int, block_tokens: int, n_kv_heads: int, head_dim: int, device="cuda", scratch_of=None):
@@ -905,7 +919,7 @@ class DeviceCache:
         [requests][columns], length [requests] (new tokens included) and first [requests+1] are a step's
         (DeviceBlocks); max_new bounds the new tokens of one request.  out and lse are made where not given.  seen
         [tokens] (int64, DeviceDrafts.plan) says which of its request's new tokens each sees, where they are drafts.  For
-        serving: queries that ask for a gradient are refused."""
+        serving: queries that ask for a gradient or carry a tangent are refused."""
         # every check by itself: _check() where one fails names what is wrong (a decode step's kernels take about as
         # long as this function's host work, so it keeps to a few attribute reads a tensor)
         dim = self._rows[1]
@@ -914,8 +928,8 @@ class DeviceCache:
         i32 = self._int32[0]
         if kind is None or not q.is_cuda:
             _check(q, "q", self._halves)
-        if q.requires_grad and self._graded():
-            raise ValueError("q: no gradient passes through a cache in 8 bits (call under torch.no_grad())")
+        if (q.requires_grad and self._graded()) or (self._dual._current_level >= 0 and _tangents(q)):
+            raise ValueError("q: no gradient passes through a cache in 8 bits (call under torch.no_grad(), without tangents)")
         if q.dim() != 3 or q.shape[2] != dim or (q.stride(2) != 1 and q.numel()):
             raise ValueError(f"q: [tokens][heads][{dim}] with its last axis contiguous")
         if table.dtype is not i32 or not table.is_cuda:
@@ -1119,13 +1133,13 @@ class DeviceRotary:
         self.rotary = festina_rotary(self.head_dim, 2 * len(turn), 1 if interleaved else 0, float(eps), _ptr(self.turn),
                                      *(_ptr(w) for w in self.weights))
         self._types = {torch.bfloat16: FESTINA_BF16, torch.float16: FESTINA_F16, torch.float32: FESTINA_F32}
-        self._here, self._empty, self._graded = _Here(), torch.empty, torch.is_grad_enabled
+        self._here, self._empty, self._graded, self._dual = _Here(), torch.empty, torch.is_grad_enabled, _dual_levels()
         self._rotate, self._ref = lib().festina_rotate_heads, C.byref(self.rotary)
 
     def apply(self, q, k, position, q_out=None, k_out=None, stream=None):
         """(q_out, k_out): queries and keys [tokens][heads][head_dim] of one type (any strides but the last) at the int32
         positions [tokens].  Outputs are made where not given, and may be q and k themselves, else they share no memory with either
-        nor with each other.  For serving: inputs that ask for a gradient are refused."""
+        nor with each other.  For serving: inputs that ask for a gradient or carry a tangent are refused."""
         return self._apply(q, k, position, q_out, k_out, stream, q_out, k_out)
 
     def _apply(self, q, k, position, q_out, k_out, stream, q_given, k_given):
@@ -1149,8 +1163,8 @@ class DeviceRotary:
             _on_device(q, "q", now)
             _on_device(k, "k", now)
             raise ValueError(f"q and k: [{T}][heads][{D}] with their last axis contiguous")
-        if (q.requires_grad or k.requires_grad) and self._graded():
-            raise ValueError("q, k: no gradient passes through (call under torch.no_grad())")
+        if ((q.requires_grad or k.requires_grad) and self._graded()) or (self._dual._current_level >= 0 and _tangents(q, k)):
+            raise ValueError("q, k: no gradient passes through (call under torch.no_grad(), without tangents)")
         if q_given is not None or k_given is not None:
             self._given(q, k, q_given, k_given, now)
         if q_out is None:
@@ -1189,8 +1203,8 @@ class DeviceRotary:
                     _on_device(out, name, now)
                 if out.shape != t.shape or (out.stride(2) != 1 and out.numel()):
                     raise ValueError(f"{name}: the shape {tuple(t.shape)} with its last axis contiguous")
-                if out.requires_grad and self._graded():
-                    raise ValueError(f"{name}: no gradient passes through (call under torch.no_grad())")
+                if (out.requires_grad and self._graded()) or (self._dual._current_level >= 0 and _tangents(out)):
+                    raise ValueError(f"{name}: no gradient passes through (call under torch.no_grad(), without tangents)")
                 at = _place(out, D)
                 if at != own and at[1] > own[0] and own[1] > at[0] and _meet(at, own, D):
                     raise ValueError(f"{name}: the input's own memory with its strides, or other memory")
