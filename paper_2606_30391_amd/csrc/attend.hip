@@ -1987,7 +1987,7 @@ festina_status attend(const festina_kv_cache *cache, const festina_attention *at
   a.G = a.Hq / a.H;
   a.shift = __builtin_ctz((unsigned)cache->block_tokens);
   a.NB = cache->n_blocks;
-  a.window = att->window;
+  a.window = min(att->window, INT_MAX / 2);            // no key is further away, and a row's position less this stays in 32 bits
   a.rows_max = s.rows_max;
   a.tiles_each = s.tiles_each;
   a.tiles_most = (int)s.tiles_most;

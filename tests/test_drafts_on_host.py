@@ -105,3 +105,14 @@ def test_steps_without_trees(attend, args):
 @pytest.mark.parametrize("args", NO_TREES)
 def test_steps_without_trees_in_pieces(attend_in_pieces, args):
     _check(attend_in_pieces, args)
+
+
+FAR_WINDOWS = [
+    "64 1 4 32 bf16 2147483647 0 0 2 3 600:20 300:64 20:30",            # windows past all positions, fewer held than new
+    "128 1 1 64 f16 2147483647 0 0 0 1 40:64 700:16 2:9", "64 1 1 16 f16 1073741824 0 0 0 1 100:40 600:33 7:20",
+    "64 1 2 16 bf16 2147483600 0 0 0 1 900:4 3:6 1:1"]
+
+
+@pytest.mark.parametrize("args", FAR_WINDOWS)
+def test_windows_past_all_positions(attend, args):
+    _check(attend, args)

@@ -315,3 +315,17 @@ def test_steps_without_trees(requests, dim, G, max_new):
     print(f"[gpu] dim {dim} group {G} requests {requests[:3]}", flush=True)
     for window in (0, 50):
         c.check(c.run(window, max_new), window)
+
+
+@pytest.mark.parametrize("requests,dim,G", [([(300, 20), (40, 33), (600, 64)], 64, 4), ([(200, 4), (70, 9), (0, 2)], 128, 1),
+                                            ([(700, 70), (90, 80), (300, 12)], 64, 2)])
+def test_windows_past_all_positions_with_fewer_held_than_new(requests, dim, G):
+    c = Case(np.random.default_rng(9), requests, dim, 2, G, 16, "bf16")
+    c.length[1] = c.new[1] * 2 // 3
+    print(f"[gpu] dim {dim} group {G} {requests}", flush=True)
+    for window in (2 ** 31 - 1, 2 ** 31 - 64, 2 ** 40):
+        c.check(c.run(window), window)
+        table, length, first, _ = c.device()
+        far, none = (c.cache().attend(c.q, table, length, first, int(c.new.max()), window=w) for w in (window, 0))
+        n = int(c.first[-1])
+        assert all(torch.equal(x[:n].nan_to_num(9e9), y[:n].nan_to_num(9e9)) for x, y in zip(far, none))
