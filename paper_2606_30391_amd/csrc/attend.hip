@@ -33,9 +33,10 @@
 //   against tiles of 64 keys as in k_tiles, but the keys are dealt to the workgroups as in k_rows, since lengths differ and a
 //   node's row sees every cached key: few of them in parts of one row tile, many in equal pieces of all tiles' line.  Which
 //   nodes a row sees is a word of 64 bits, looked at only in the last tiles; 64 rows leave two waves for each 32 of them, which
-//   take half of a tile's keys each.  Bound by latency where keys are few (32 requests of the fleet's lengths, trees of 16, 52 MB: 26 us
-//   and 7 to join the parts) and by the matrix cores and exponentials where they are many (64 requests up to 32,768 tokens, trees of
-//   32, 550 GFLOP over 2.2 GB: 715 us and 40, 730 TFLOP/s).
+//   take half of a tile's keys each.  Bound by latency: where keys are few by that of a tile's beginning (32 requests of the fleet's
+//   lengths, trees of 16, 51 MB: 27 us and 7.5 to join the parts), where they are many by that of the codes, of which a workgroup has one
+//   unit in flight (64 requests up to 32,768 tokens, trees of 32, 550 GFLOP over 2.2 GB: 723 to 787 us on different cards, 700 to 760
+//   TFLOP/s, and 40 for the join; matrix cores 37% and VALU issue 38% of the cycles; with keys that stay in the caches a fifth less).
 // k_plan    running sums of the requests' units and tiles, for many requests.
 #include <hip/hip_runtime.h>
 
@@ -70,9 +71,11 @@ constexpr int waves_of(int D, int NT) { return D > 128 || NT > 2 ? 1 : 2; }
 constexpr int workers_of(int D, int NT) { return 1024 * waves_of(D, NT); }
 constexpr int kGroups = 512;         // workgroups of k_tiles that fill the chip: two a compute unit
 constexpr int kJoins = 2048;         // and of its join: eight
-constexpr int kWaveRequests = 64;    // requests whose running sums a wave forms in its registers
+constexpr int kWaveRequests = 64;    // requests whose running sums a wave forms in its registers (k_drafts, trees of 16, the fleet's
+                                     // lengths: 64 requests 56.0 us, 65 requests 56.0)
 constexpr int kNodes = 64;           // nodes of a draft tree: a request with more new tokens is a run
-constexpr int kListed = 512;         // requests whose running sums a workgroup forms by itself
+constexpr int kListed = 512;         // requests whose running sums a workgroup forms by itself (likewise 512 requests 270.9 us; 513,
+                                     // for which a launch does, 271.1)
 constexpr int kMaxRequests = 1 << 20;
 constexpr long long kThreadsMost = UINT_MAX;     // along one axis of a grid
 constexpr float kLn2 = 0.6931471805599453f;
@@ -1840,7 +1843,10 @@ festina_status shape_of(const festina_kv_cache *c, const festina_attention *t, b
   // Trees of up to 16 rows are k_rows', as single tokens are (us by k_rows and by k_drafts, 32 requests of 128 dims, 16 rows: of the
   // fleet's lengths 27 and 28, of 512 to 16,384 tokens 124 and 143; 32 rows, for which it would read the cache twice: 35 and 30, 196
   // and 148), and so are those of up to kWholeRows rows, in tiles of 16, of tables that one launch does (up to 510 tokens, one
-  // request, 32 rows: 7 and 12; 32 requests, 64 rows: 23 and 30, 128 rows: 34 and 40; 64 requests, 128 rows: 61 and 57).
+  // request, 32 rows: 7 and 12; 32 requests, 64 rows: 23 and 29, 128 rows: 35 and 40).  Each tile of 16 rows reads its request's
+  // keys anew, so more requests turn it around, the sooner the more rows: 64 requests, 128 rows: 62 and 58; 128 requests, 32 rows:
+  // 37 and 49, 64 rows: 62 and 59, 128 rows: 114 and 79; 512 requests, 32 rows: 131 and 149, 64 rows: 239 and 170, 128 rows: 460 and
+  // 218.  (The rule does not look at the requests.)
   constexpr int kWholeRows = 128;
   const bool trees = drafts && (most > (s->cut ? 16 : kWholeRows) || t->max_new > kNodes);     // (runs are k_tiles' there)
   s->tiles = drafts ? trees && t->max_new > kNodes : most > 16 * nt_most && t->max_new > 1;
@@ -1850,7 +1856,9 @@ festina_status shape_of(const festina_kv_cache *c, const festina_attention *t, b
   if (s->tiles && G > 16 * nt_most) s->nt = 0;
   s->rows_max = s->tiles ? 16 * s->nt : INT_MAX;
   if (trees) {                                         // k_drafts has the trees, k_tiles the runs
-    s->halves = D > 128 || min(most, (long long)kNodes * G) <= rows_of(2) ? 2 : 1;      // (128 rows of 256 dims do not fit the registers)
+    // (128 rows of 256 dims do not fit the registers.  A run in the step sets max_new, and with it the tile of the trees beside it:
+    // 32 requests of the fleet's lengths, one of them with a run of 777, trees of 8: 73 us, single tokens: 71, which take 66 without words)
+    s->halves = D > 128 || min(most, (long long)kNodes * G) <= rows_of(2) ? 2 : 1;
     s->join_rows = (int)min(most, (long long)rows_of(s->halves));
     s->nt = 0;
     s->rows_max = kNodes * G;

@@ -235,7 +235,10 @@ extern "C" festina_status festina_rotate_heads(const festina_rotary *rotary, con
   a.vec = (at & 15) == 0;
   const int each = 64 / (D == 96 ? 8 : D / 16);
   const int groups = (a.heads[0] + each - 1) / each + (a.heads[1] + each - 1) / each;
-  // few tokens: the heads of each over several waves, so that none makes two round trips to memory
+  // few tokens: the heads of each over several waves, so that none makes two round trips to memory; each of them makes the token's
+  // cosines anew.  One wave a token and one a group of heads, us: 32 and 8 heads of 128 in bfloat16, 256 tokens 7.3 and 4.8, 1,024: 8.5
+  // and 8.2, 2,048: 11.6 and 12.9, 4,096: 16.3 and 21.0; 14 and 2 heads of 64 in half, 1,024: 5.5 and 4.9, 2,048: 6.1 and 6.1, 4,096:
+  // 8.3 and 9.5; 16 and 16 heads of 96 in float32, 512: 9.3 and 6.6, 1,024: 10.1 and 10.5, 2,048: 14.2 and 18.9
   a.parts = a.T <= 2048 ? groups : 1;
   const long long blocks = ((long long)a.T + kWaves - 1) / kWaves;
   if (blocks > UINT_MAX / (64 * kWaves)) return FESTINA_ERR_UNSUPPORTED;   // threads along one axis of a grid
